@@ -401,6 +401,43 @@ int mamba2_state_step(float *h_out, const float *h_in, const int32_t *parent_idx
                       const void *z, const float *dt_bias, void *out, int64_t n_out, int64_t n_in,
                       int64_t H, int64_t P, int64_t N, int dt_softplus, mamba_dtype_t io, void *hip_stream);
 
+/*
+ * Gated-delta layer core: the scalar-decay layer above with the delta rule's write (Yang, Kautz & Hatamizadeh, "Gated Delta
+ * Networks: Improving Mamba2 with Delta Rule", 2024), a fixed-size state of the same shape.  Per value head h, with the key head
+ * h / (H / Hk) that it shares with its neighbours:
+ *   delta[t,h] = softplus(dt[t,h] + dt_bias[h])      (dt_softplus = 0: delta = dt + dt_bias)
+ *   a = exp(delta A[h]);   b = sigmoid(beta[t,h])     (beta_sigmoid = 0: b = beta)
+ *   k = k_t / sqrt(sum k_t^2 + eps), q likewise       (qk_norm = 0: as they are)
+ *   S_t[h] = a S_{t-1}[h] (I - b k k^T) + b v_t[h,:] (outer) k
+ *   o_t[h,:] = scale S_t[h] q
+ *   out = o                                           (norm_w NULL)
+ *   out = o / sqrt(mean over the head's P channels of o^2 + eps) norm_w
+ *   out = out silu(z)                                 (when z is given)
+ * Layout (device pointers, 16-byte aligned): q, k (batch, L, Hk, N); v, z, out (batch, L, H, P); dt, beta (batch, L, H) in the I/O
+ * dtype; A, dt_bias float[H]; norm_w float[P] (z, norm_w, dt_bias, h0, h_final nullable); states h0, h_final (batch, H, P, N) float,
+ * as the scalar-decay layer has them (mamba_state_fork copies them with D = H * P).  N and P each 64 or 128; H a multiple of Hk.
+ *
+ * mamba_gated_delta_fwd encodes a sequence, bf16 or float32 I/O.  workspace: device scratch of
+ * mamba_gated_delta_workspace_bytes(batch, L, H, Hk, P, N) bytes (0 for an unsupported shape), caller-owned; nothing in it has to be
+ * kept or cleared between calls.  h_final may be h0 (any other overlap of the two is an error).
+ * mamba_gated_delta_step advances n_out draft branches by one token (q, k (n_out, Hk, N); v, z, out (n_out, H, P); dt, beta
+ * (n_out, H); h_in (n_in, H, P, N), h_out (n_out, H, P, N)); branch j continues from h_in[parent_idx[j]] (device int32[n_out]; NULL:
+ * h_in[j], n_in == n_out, and then h_out may be h_in); an index outside [0, n_in) reads nothing and gives NaN for that branch.
+ * A NaN or an infinity in the inputs of a token reaches the state from there on, as the equations have it, and may reach the outputs
+ * of up to 63 tokens ahead of it.  batch, H, n_out <= 65535; L <= 2^31.
+ */
+size_t mamba_gated_delta_workspace_bytes(int64_t batch, int64_t L, int64_t H, int64_t Hk, int64_t P, int64_t N);
+int mamba_gated_delta_fwd(const void *q, const void *k, const void *v, const void *dt, const float *A, const void *beta,
+                          const void *z, const float *norm_w, const float *dt_bias, const float *h0, void *out, float *h_final,
+                          void *workspace, size_t workspace_bytes, int64_t batch, int64_t L, int64_t H, int64_t Hk, int64_t P,
+                          int64_t N, float scale, float eps, int dt_softplus, int beta_sigmoid, int qk_norm, mamba_dtype_t io,
+                          void *hip_stream);
+int mamba_gated_delta_step(float *h_out, const float *h_in, const int32_t *parent_idx, const void *q, const void *k, const void *v,
+                           const void *dt, const float *A, const void *beta, const void *z, const float *norm_w,
+                           const float *dt_bias, void *out, int64_t n_out, int64_t n_in, int64_t H, int64_t Hk, int64_t P, int64_t N,
+                           float scale, float eps, int dt_softplus, int beta_sigmoid, int qk_norm, mamba_dtype_t io,
+                           void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -85,6 +85,12 @@ def _declare(lib):
     lib.mamba2_ssd_fwd.restype = _int
     lib.mamba2_state_step.argtypes = [_vp] * 12 + [_i64] * 5 + [_int, _int, _vp]
     lib.mamba2_state_step.restype = _int
+    lib.mamba_gated_delta_workspace_bytes.argtypes = [_i64] * 6
+    lib.mamba_gated_delta_workspace_bytes.restype = _sz
+    lib.mamba_gated_delta_fwd.argtypes = [_vp] * 13 + [_sz] + [_i64] * 6 + [ctypes.c_float] * 2 + [_int] * 4 + [_vp]
+    lib.mamba_gated_delta_fwd.restype = _int
+    lib.mamba_gated_delta_step.argtypes = [_vp] * 13 + [_i64] * 6 + [ctypes.c_float] * 2 + [_int] * 4 + [_vp]
+    lib.mamba_gated_delta_step.restype = _int
     lib.mamba_embedding_fwd.argtypes = [_vp, _vp, _vp, _i64, _i64, _i64, _int, _vp]
     lib.mamba_embedding_fwd.restype = _int
     lib.mamba_topk_fwd.argtypes = [_vp, _vp, _vp, _i64, _i64, _int, _int, _vp]
@@ -129,7 +135,8 @@ EXPORTS = ("mamba_status_string", "mamba_conv1d_fwd", "mamba_scan_workspace_byte
            "mamba_scan_fwd", "mamba_scan_fwd_static", "mamba_conv1d_fwd_strided", "mamba_scan_fwd_strided", "mamba_state_step", "mamba_conv_state_step", "mamba_state_fork", "mamba_tree_plan",
            "mamba_tree_parents", "mamba_linear_fwd", "mamba_rmsnorm_fwd", "mamba_block_workspace_bytes",
            "mamba_block_workspace_layout", "mamba_block_fwd", "mamba_block_step", "mamba_embedding_fwd", "mamba_topk_fwd",
-           "mamba2_ssd_workspace_bytes", "mamba2_ssd_fwd", "mamba2_state_step")
+           "mamba2_ssd_workspace_bytes", "mamba2_ssd_fwd", "mamba2_state_step",
+           "mamba_gated_delta_workspace_bytes", "mamba_gated_delta_fwd", "mamba_gated_delta_step")
 
 
 class MambaError(RuntimeError):
@@ -144,6 +151,9 @@ _marshal.bind(MambaError, torch.OutOfMemoryError, *[ctypes.cast(getattr(lib, nam
     "mamba_state_fork", "mamba_linear_fwd", "mamba_rmsnorm_fwd", "mamba_block_workspace_bytes", "mamba_block_fwd",
     "mamba_block_step", "mamba_embedding_fwd", "mamba_topk_fwd", "mamba2_ssd_workspace_bytes", "mamba2_ssd_fwd",
     "mamba2_state_step")])
+_delta = _marshal._delta
+_delta.bind(MambaError, torch.OutOfMemoryError, *[ctypes.cast(getattr(lib, name), _vp).value for name in (
+    "mamba_gated_delta_workspace_bytes", "mamba_gated_delta_fwd", "mamba_gated_delta_step")])
 
 
 def mamba_status_string(status: int) -> str:
@@ -460,3 +470,27 @@ def mamba2_state_step(h_in, x, dt, A, Bm, Cm, Dskip=None, z=None, dt_bias=None, 
     """h_in (n_in,H,P,N) f32; x, z (n_out,H,P); dt (n_out,H); Bm, Cm (n_out,N) -> h_out (n_out,H,P,N), out (n_out,H,P)."""
     return _marshal.ssd_step(h_in, x, dt, A, Bm, Cm, Dskip, z, dt_bias, parent_idx, h_out, out, dt_softplus,
                              _raw(stream))
+
+
+def mamba_gated_delta_workspace_bytes(batch, L, H, Hk, P, N) -> int:
+    return int(lib.mamba_gated_delta_workspace_bytes(batch, L, H, Hk, P, N))
+
+
+def mamba_gated_delta_fwd(q, k, v, dt, A, beta, z=None, norm_w=None, dt_bias=None, h0=None, out=None, h_final=None, workspace=None,
+                          scale=None, eps=1e-6, want_state=True, dt_softplus=True, beta_sigmoid=True, qk_norm=True, stream=None):
+    """Gated-delta layer core over a sequence: q, k (B,L,Hk,N), v, z (B,L,H,P), dt, beta (B,L,H) bf16|f32; A, dt_bias (H), norm_w (P)
+    f32; h0 (B,H,P,N) f32 -> out (B,L,H,P), h_final (B,H,P,N).  scale defaults to N ** -0.5."""
+    if stream is not None and workspace is None:
+        need = mamba_gated_delta_workspace_bytes(*v.shape[:3], q.shape[2], v.shape[3], q.shape[3])
+        if need > 0:
+            workspace = _scratch(need, v.device, stream)
+    return _delta.gated_delta_fwd(q, k, v, dt, A, beta, z, norm_w, dt_bias, h0, out, h_final, workspace, want_state,
+                                  scale, eps, dt_softplus, beta_sigmoid, qk_norm, _raw(stream))
+
+
+def mamba_gated_delta_step(h_in, q, k, v, dt, A, beta, z=None, norm_w=None, dt_bias=None, parent_idx=None, h_out=None, out=None,
+                           scale=None, eps=1e-6, dt_softplus=True, beta_sigmoid=True, qk_norm=True, stream=None):
+    """One token for n_out draft branches: h_in (n_in,H,P,N) f32; q, k (n_out,Hk,N), v, z (n_out,H,P), dt, beta (n_out,H); parent_idx
+    int32[n_out] -> h_out (n_out,H,P,N), out (n_out,H,P).  Without parent_idx h_out may be h_in."""
+    return _delta.gated_delta_step(h_in, q, k, v, dt, A, beta, z, norm_w, dt_bias, parent_idx, h_out, out,
+                                   scale, eps, dt_softplus, beta_sigmoid, qk_norm, _raw(stream))

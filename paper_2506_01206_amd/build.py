@@ -13,7 +13,8 @@ CSRC = os.path.join(HERE, "csrc")
 OBJDIR = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libmamba_hip.so")
 MARSHAL = os.path.join(HERE, "_marshal.so")
-SOURCES = ["api.cpp", "sd_tree_search.cpp", "conv1d.hip", "scan.hip", "scan_direct.hip", "scan_lanes.hip", "strided.hip", "step.hip", "fork.hip", "linear.hip", "draft_in.hip", "xdt.hip", "norm.hip", "vocab.hip", "ssd.hip"]
+SOURCES = ["api.cpp", "sd_tree_search.cpp", "conv1d.hip", "scan.hip", "scan_direct.hip", "scan_lanes.hip", "strided.hip", "step.hip", "fork.hip", "linear.hip", "draft_in.hip", "xdt.hip", "norm.hip", "vocab.hip", "ssd.hip", "delta.hip"]
+MARSHAL_SOURCES = ["marshal.cpp", "marshal_delta.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # packed-fp32 VALU instructions are switched off for every device function.  The first 14 dwords of a kernel's arguments, up to
 # the first aggregate, come in registers instead of through a scalar load (a trip to the cache that every address waits for).
@@ -47,7 +48,7 @@ def marshal_command(out: str, compiler: str, flags=("-O2", "-Wall")) -> list:
              "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI]
             + ["-isystem" + d for d in (os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"),
                                         sysconfig.get_paths()["include"], os.path.join(os.path.dirname(os.path.dirname(HIPCC)), "include"))]
-            + [os.path.join(CSRC, "marshal.cpp"), "-o", out, "-L" + os.path.join(root, "lib")]
+            + [os.path.join(CSRC, src) for src in MARSHAL_SOURCES] + ["-o", out, "-L" + os.path.join(root, "lib")]
             + ["-l" + n for n in ("torch_python", "torch_cpu", "torch", "c10", "c10_hip")])
 
 

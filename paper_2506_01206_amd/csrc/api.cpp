@@ -881,6 +881,100 @@ int mamba2_state_step(float *h_out, const float *h_in, const int32_t *parent_idx
     return (int)launch_ssd_step(a, static_cast<hipStream_t>(hip_stream));
 }
 
+namespace {
+bool delta_shape_ok(int64_t H, int64_t Hk, int64_t P, int64_t N)
+{
+    return (P == 64 || P == 128) && (N == 64 || N == 128) && (H == 0 || (Hk > 0 && H % Hk == 0));
+}
+struct DeltaBytes {
+    int64_t key, value, head, state_in, state_out;   // a q or k, a v or out, a dt or beta tensor; the states
+};
+bool delta_bytes(int64_t rows, int64_t n_in, int64_t L, int64_t H, int64_t Hk, int64_t P, int64_t N, int e, DeltaBytes *b)
+{
+    int64_t hp, hn, t;
+    return mul_ok(H, P, &hp) && mul_ok(Hk, N, &hn) && size3(rows, L, hn, e, &b->key) && size3(rows, L, hp, e, &b->value) &&
+           size3(rows, L, H, e, &b->head) && size3(n_in, hp, N, 4, &b->state_in) && size3(rows, hp, N, 4, &b->state_out) &&
+           size3(rows, L / 64 + 2, H, 1, &t) && size3(t, 64, 1024, 1, &t);
+}
+// what both entry points refuse: pointers, alignment, and outputs over inputs
+int delta_pointers(const DeltaArgs &a, const DeltaBytes &b)
+{
+    if (!a.q || !a.k || !a.v || !a.dt || !a.A || !a.beta || !a.out) return MAMBA_ERR_NULL_POINTER;
+    for (const void *p : {a.q, a.k, a.v, a.dt, a.beta, a.z, (const void *)a.A, (const void *)a.norm_w, (const void *)a.dt_bias,
+                          (const void *)a.h_in, (const void *)a.h_out, (const void *)a.parent, (const void *)a.out, (const void *)a.ws})
+        if (!aligned16(p)) return MAMBA_ERR_MISALIGNED;
+    const struct { const void *p; int64_t n; } in[] = {{a.q, b.key}, {a.k, b.key}, {a.v, b.value}, {a.z, b.value}, {a.dt, b.head},
+                                                       {a.beta, b.head}, {a.A, a.H * 4}, {a.dt_bias, a.H * 4},
+                                                       {a.norm_w, (int64_t)a.P * 4}, {a.parent, a.rows * 4}};
+    for (const auto &i : in)
+        if (overlap(a.out, b.value, i.p, i.n) || overlap(a.h_out, b.state_out, i.p, i.n)) return MAMBA_ERR_ALIAS;
+    if (overlap(a.out, b.value, a.h_in, b.state_in) || overlap(a.out, b.value, a.h_out, b.state_out)) return MAMBA_ERR_ALIAS;
+    if (!(a.h_out == a.h_in && !a.parent) && overlap(a.h_out, b.state_out, a.h_in, b.state_in)) return MAMBA_ERR_ALIAS;
+    return MAMBA_OK;
+}
+}  // namespace
+
+size_t mamba_gated_delta_workspace_bytes(int64_t batch, int64_t L, int64_t H, int64_t Hk, int64_t P, int64_t N)
+{
+    DeltaBytes b;
+    if (batch <= 0 || L <= 0 || H <= 0 || !delta_shape_ok(H, Hk, P, N) || !delta_bytes(batch, batch, L, H, Hk, P, N, 4, &b)) return 0;
+    return gated_delta_workspace_bytes(batch, L, H, Hk, P, N);
+}
+
+int mamba_gated_delta_fwd(const void *q, const void *k, const void *v, const void *dt, const float *A, const void *beta, const void *z,
+                          const float *norm_w, const float *dt_bias, const float *h0, void *out, float *h_final, void *workspace,
+                          size_t workspace_bytes, int64_t batch, int64_t L, int64_t H, int64_t Hk, int64_t P, int64_t N, float scale,
+                          float eps, int dt_softplus, int beta_sigmoid, int qk_norm, mamba_dtype_t io, void *hip_stream)
+{
+    const int e = io_size(io);
+    if (e == 0) return MAMBA_ERR_UNSUPPORTED;
+    if (batch < 0 || L < 0 || H < 0 || Hk < 0 || P < 0 || N < 0) return MAMBA_ERR_BAD_SHAPE;
+    DeltaBytes b;
+    if (!delta_bytes(batch, batch, L, H, Hk, P, N, e, &b)) return MAMBA_ERR_BAD_SHAPE;
+    if (!delta_shape_ok(H, Hk, P, N) || batch > kMaxGridYZ || H > kMaxGridYZ || L > ((int64_t)1 << 31)) return MAMBA_ERR_UNSUPPORTED;
+    if (batch == 0 || H == 0) return MAMBA_OK;
+    if (L == 0) {
+        if (!h_final || h_final == h0) return MAMBA_OK;
+        if (!aligned16(h_final) || !aligned16(h0)) return MAMBA_ERR_MISALIGNED;
+        if (overlap(h_final, b.state_out, h0, b.state_in)) return MAMBA_ERR_ALIAS;
+        return (int)launch_copy_state(h0, h_final, batch * H * P * N, static_cast<hipStream_t>(hip_stream));
+    }
+    const DeltaArgs a{h_final, h0, nullptr, q, k, v, dt, beta, z, A, norm_w, dt_bias, out, static_cast<float *>(workspace),
+                      batch, batch, L, H, Hk, (int)P, (int)N, (int)io, scale, eps, dt_softplus, beta_sigmoid, qk_norm};
+    if (const int st = delta_pointers(a, b)) return st;
+    const size_t need = gated_delta_workspace_bytes(batch, L, H, Hk, P, N);
+    if (need > 0) {
+        if (!workspace || workspace_bytes < need) return MAMBA_ERR_WORKSPACE;
+        const struct { const void *p; int64_t n; } all[] = {{q, b.key}, {k, b.key}, {v, b.value}, {z, b.value}, {dt, b.head}, {beta, b.head},
+                                                            {A, H * 4}, {dt_bias, H * 4}, {norm_w, P * 4}, {h0, b.state_in},
+                                                            {h_final, b.state_out}, {out, b.value}};
+        for (const auto &i : all)
+            if (overlap(workspace, (int64_t)need, i.p, i.n)) return MAMBA_ERR_ALIAS;
+    }
+    return (int)launch_gated_delta(a, static_cast<hipStream_t>(hip_stream));
+}
+
+int mamba_gated_delta_step(float *h_out, const float *h_in, const int32_t *parent_idx, const void *q, const void *k, const void *v,
+                           const void *dt, const float *A, const void *beta, const void *z, const float *norm_w, const float *dt_bias,
+                           void *out, int64_t n_out, int64_t n_in, int64_t H, int64_t Hk, int64_t P, int64_t N, float scale, float eps,
+                           int dt_softplus, int beta_sigmoid, int qk_norm, mamba_dtype_t io, void *hip_stream)
+{
+    const int e = io_size(io);
+    if (e == 0) return MAMBA_ERR_UNSUPPORTED;
+    if (n_out < 0 || n_in < 0 || H < 0 || Hk < 0 || P < 0 || N < 0) return MAMBA_ERR_BAD_SHAPE;
+    DeltaBytes b;
+    if (!delta_bytes(n_out, n_in, 1, H, Hk, P, N, e, &b)) return MAMBA_ERR_BAD_SHAPE;
+    if (!parent_idx && n_in != n_out) return MAMBA_ERR_BAD_SHAPE;
+    if (n_out > 0 && n_in == 0) return MAMBA_ERR_BAD_SHAPE;
+    if (!delta_shape_ok(H, Hk, P, N) || n_out > kMaxGridYZ || H > kMaxGridYZ) return MAMBA_ERR_UNSUPPORTED;
+    if (n_out == 0 || H == 0) return MAMBA_OK;
+    if (!h_out || !h_in) return MAMBA_ERR_NULL_POINTER;
+    const DeltaArgs a{h_out, h_in, parent_idx, q, k, v, dt, beta, z, A, norm_w, dt_bias, out, nullptr,
+                      n_out, n_in, 1, H, Hk, (int)P, (int)N, (int)io, scale, eps, dt_softplus, beta_sigmoid, qk_norm};
+    if (const int st = delta_pointers(a, b)) return st;
+    return (int)launch_gated_delta_step(a, static_cast<hipStream_t>(hip_stream));
+}
+
 int mamba_tree_plan(const int32_t *tree, int gamma, int64_t n_layers, int64_t D, int64_t N, int K,
                     mamba_dtype_t conv_dtype, mamba_tree_plan_t *plan)
 {

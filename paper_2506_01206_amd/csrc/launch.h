@@ -113,6 +113,25 @@ struct SsdStepArgs {
 };
 hipError_t launch_ssd_step(const SsdStepArgs &a, hipStream_t stream);
 
+// Gated-delta layer core.  q, k: (rows, L, Hk, N); v, z, out: (rows, L, H, P); dt, beta: (rows, L, H); A, dt_bias: (H); norm_w: (P);
+// states (rows, H, P, N) fp32.  N, P in {64, 128}.
+struct DeltaArgs {
+    float *h_out;            // or nullptr
+    const float *h_in;       // or nullptr: zeros
+    const int32_t *parent;   // step: row of h_in each row continues from, or nullptr
+    const void *q, *k, *v, *dt, *beta, *z;
+    const float *A, *norm_w, *dt_bias;
+    void *out;
+    float *ws;
+    int64_t rows, n_in, L, H, Hk;
+    int P, N, io;
+    float scale, eps;
+    int dt_softplus, beta_sigmoid, qk_norm;
+};
+size_t gated_delta_workspace_bytes(int64_t batch, int64_t L, int64_t H, int64_t Hk, int64_t P, int64_t N);
+hipError_t launch_gated_delta(const DeltaArgs &a, hipStream_t stream);
+hipError_t launch_gated_delta_step(const DeltaArgs &a, hipStream_t stream);
+
 // The states of a step as one kernel argument: the compiler brings arguments in registers only up to the first aggregate, so that
 // a kernel whose first argument this is fetches them all as it goes (who gains by that is in build.py).
 struct StepStates {
