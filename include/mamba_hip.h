@@ -438,6 +438,57 @@ int mamba_gated_delta_step(float *h_out, const float *h_in, const int32_t *paren
                            float scale, float eps, int dt_softplus, int beta_sigmoid, int qk_norm, mamba_dtype_t io,
                            void *hip_stream);
 
+/*
+ * Children under the rules that the verifier decodes by: a drafted token that its penalties or its grammar would not let through is
+ * never accepted (Sec. 4.1: every node of the draft tree proposes the tokens that become its children).
+ *
+ * mamba_token_counts: occurrences of every token in each of n_seq sequences, tokens (n_seq, L) device int32 (numbers outside [0,V),
+ *   such as the -1 of a padded row, are skipped), into counts (n_seq, V) device int32.  An entry's lower 31 bits are the
+ *   occurrences in the generated text, bit 31 says that the token stands in the prompt: with prompt = 0 the call adds
+ *   occurrences, with prompt = 1 it sets that bit.  accumulate = 0: counts are written from scratch, else what they hold is kept
+ *   and added to.  V <= 2^25.
+ * mamba_logits_constrain_fwd: out[m,v] from logits[m,v], (M,V) bf16 or float32 both, out may be logits itself:
+ *   c = generated occurrences of v in the row's sequence, and in the row's path
+ *   x = x > 0 ? x / repetition : x * repetition      where c > 0 or v stands in the prompt
+ *   x = (x - frequency c) - presence                 where c > 0
+ *   x = x + bias[v]
+ *   x = -inf                                         where the row's mask does not allow v
+ *   in float32, every operation rounded to nearest; rounded once more at the store.
+ * mamba_topk_constrained_fwd: the k tokens of every row with the largest x, as mamba_topk_fwd ranks them (largest first, ties to the
+ *   lower index, NaN as -inf) among those that the mask allows; idx -1, val -inf where no token is left.  With path_out ((M k,
+ *   path_len + 1) device int32) row m k + j gets the path of row m with that child behind it: the order in which a draft tree keeps its
+ *   children, so that path_out is the next position's path.  1 <= k <= 8.  workspace: device scratch of
+ *   mamba_topk_constrained_workspace_bytes(M, V, k) bytes (0: none needed).
+ *
+ * mamba_constraints_t (a HOST struct of device pointers; NULL leaves a rule out):
+ *   penalties (n_seq, 3) float: repetition (> 0), presence, frequency of each sequence; NULL: none, counts and path are not read
+ *   counts (n_seq, V) as above; path (M, path_len): the tokens that lead to the row, counted as generated (outside [0,V): skipped)
+ *   seq_idx (M): the row's sequence; NULL: sequence 0 where n_seq is 1, row m's own where it is M
+ *   bias (V) float, the same for all rows
+ *   mask (n_masks, ceil(V / 32)): bit v % 32 of word v / 32 set where v is allowed; mask_idx (M): the row's mask, -1 for none; NULL: as seq_idx
+ * A row whose seq_idx or mask_idx is out of range reads nothing out of bounds: NaN in all of out, no token left in the choice.
+ * M (V / 8192 rounded up) <= 2^31 - 1, V <= 2^25, path_len <= 4096.
+ */
+typedef struct {
+    const int32_t *counts;
+    const float *penalties;
+    const int32_t *seq_idx;
+    const int32_t *path;
+    const float *bias;
+    const int32_t *mask;
+    const int32_t *mask_idx;
+    int64_t n_seq, n_masks, path_len;
+} mamba_constraints_t;
+
+int mamba_token_counts(const int32_t *tokens, int32_t *counts, int64_t n_seq, int64_t L, int64_t V, int accumulate, int prompt,
+                       void *hip_stream);
+int mamba_logits_constrain_fwd(const void *logits, const mamba_constraints_t *c, void *out, int64_t M, int64_t V, mamba_dtype_t io,
+                               void *hip_stream);
+size_t mamba_topk_constrained_workspace_bytes(int64_t M, int64_t V, int k);
+int mamba_topk_constrained_fwd(const void *logits, const mamba_constraints_t *c, int32_t *idx, float *val, int32_t *path_out,
+                               void *workspace, size_t workspace_bytes, int64_t M, int64_t V, int k, mamba_dtype_t io,
+                               void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

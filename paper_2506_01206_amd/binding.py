@@ -68,6 +68,12 @@ class BlockParams(ctypes.Structure):
                 ("out_proj_w", ctypes.c_void_p)]
 
 
+class Constraints(ctypes.Structure):
+    """mamba_constraints_t of include/mamba_hip.h."""
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("counts", "penalties", "seq_idx", "path", "bias", "mask", "mask_idx")]
+                + [(n, ctypes.c_int64) for n in ("n_seq", "n_masks", "path_len")])
+
+
 def _declare(lib):
     """Attach the C signatures of include/mamba_hip.h to a loaded library."""
     _bpp = ctypes.POINTER(BlockParams)
@@ -91,6 +97,15 @@ def _declare(lib):
     lib.mamba_gated_delta_fwd.restype = _int
     lib.mamba_gated_delta_step.argtypes = [_vp] * 13 + [_i64] * 6 + [ctypes.c_float] * 2 + [_int] * 4 + [_vp]
     lib.mamba_gated_delta_step.restype = _int
+    _cp = ctypes.POINTER(Constraints)
+    lib.mamba_token_counts.argtypes = [_vp] * 2 + [_i64] * 3 + [_int] * 2 + [_vp]
+    lib.mamba_token_counts.restype = _int
+    lib.mamba_logits_constrain_fwd.argtypes = [_vp, _cp, _vp, _i64, _i64, _int, _vp]
+    lib.mamba_logits_constrain_fwd.restype = _int
+    lib.mamba_topk_constrained_workspace_bytes.argtypes = [_i64, _i64, _int]
+    lib.mamba_topk_constrained_workspace_bytes.restype = _sz
+    lib.mamba_topk_constrained_fwd.argtypes = [_vp, _cp] + [_vp] * 4 + [_sz, _i64, _i64, _int, _int, _vp]
+    lib.mamba_topk_constrained_fwd.restype = _int
     lib.mamba_embedding_fwd.argtypes = [_vp, _vp, _vp, _i64, _i64, _i64, _int, _vp]
     lib.mamba_embedding_fwd.restype = _int
     lib.mamba_topk_fwd.argtypes = [_vp, _vp, _vp, _i64, _i64, _int, _int, _vp]
@@ -136,7 +151,8 @@ EXPORTS = ("mamba_status_string", "mamba_conv1d_fwd", "mamba_scan_workspace_byte
            "mamba_tree_parents", "mamba_linear_fwd", "mamba_rmsnorm_fwd", "mamba_block_workspace_bytes",
            "mamba_block_workspace_layout", "mamba_block_fwd", "mamba_block_step", "mamba_embedding_fwd", "mamba_topk_fwd",
            "mamba2_ssd_workspace_bytes", "mamba2_ssd_fwd", "mamba2_state_step",
-           "mamba_gated_delta_workspace_bytes", "mamba_gated_delta_fwd", "mamba_gated_delta_step")
+           "mamba_gated_delta_workspace_bytes", "mamba_gated_delta_fwd", "mamba_gated_delta_step",
+           "mamba_token_counts", "mamba_logits_constrain_fwd", "mamba_topk_constrained_workspace_bytes", "mamba_topk_constrained_fwd")
 
 
 class MambaError(RuntimeError):
@@ -153,7 +169,8 @@ _marshal.bind(MambaError, torch.OutOfMemoryError, *[ctypes.cast(getattr(lib, nam
     "mamba2_state_step")])
 _delta = _marshal._delta
 _delta.bind(MambaError, torch.OutOfMemoryError, *[ctypes.cast(getattr(lib, name), _vp).value for name in (
-    "mamba_gated_delta_workspace_bytes", "mamba_gated_delta_fwd", "mamba_gated_delta_step")])
+    "mamba_gated_delta_workspace_bytes", "mamba_gated_delta_fwd", "mamba_gated_delta_step", "mamba_token_counts",
+    "mamba_logits_constrain_fwd", "mamba_topk_constrained_workspace_bytes", "mamba_topk_constrained_fwd")])
 
 
 def mamba_status_string(status: int) -> str:
@@ -494,3 +511,32 @@ def mamba_gated_delta_step(h_in, q, k, v, dt, A, beta, z=None, norm_w=None, dt_b
     int32[n_out] -> h_out (n_out,H,P,N), out (n_out,H,P).  Without parent_idx h_out may be h_in."""
     return _delta.gated_delta_step(h_in, q, k, v, dt, A, beta, z, norm_w, dt_bias, parent_idx, h_out, out,
                                    scale, eps, dt_softplus, beta_sigmoid, qk_norm, _raw(stream))
+
+
+def mamba_token_counts(tokens, V, counts=None, prompt=False, stream=None):
+    """tokens int32 (S,L), what is outside [0,V) skipped -> counts int32 (S,V): occurrences, or with prompt=True bit 31 where a token
+    occurs.  counts given: added to, in place."""
+    return _delta.token_counts(tokens, V, counts, prompt, _raw(stream))
+
+
+def mamba_logits_constrain_fwd(logits, counts=None, penalties=None, seq_idx=None, path=None, bias=None, mask=None, mask_idx=None, out=None,
+                               stream=None):
+    """logits (M,V) bf16|f32 under penalties (S,3) f32 (repetition, presence, frequency) by counts int32 (S,V) and path int32 (M,T), bias
+    (V) f32 and mask int32 (R, ceil(V/32)); seq_idx, mask_idx int32 (M).  out may be logits."""
+    return _delta.logits_constrain_fwd(logits, counts, penalties, seq_idx, path, bias, mask, mask_idx, out, _raw(stream))
+
+
+def mamba_topk_constrained_workspace_bytes(M, V, k) -> int:
+    return int(lib.mamba_topk_constrained_workspace_bytes(M, V, k))
+
+
+def mamba_topk_constrained_fwd(logits, k, counts=None, penalties=None, seq_idx=None, path=None, bias=None, mask=None, mask_idx=None, idx=None,
+                               val=None, path_out=None, want_path=False, workspace=None, stream=None):
+    """The k best allowed tokens of every row of the constrained logits -> idx int32 (M,k), val f32 (M,k), path_out int32 (M k, T+1) or
+    None: row m k + j the path of row m with its child j behind it."""
+    if stream is not None and workspace is None:
+        need = mamba_topk_constrained_workspace_bytes(*logits.shape, k)
+        if need > 0:
+            workspace = _scratch(need, logits.device, stream)
+    return _delta.topk_constrained_fwd(logits, k, counts, penalties, seq_idx, path, bias, mask, mask_idx, idx, val, path_out, want_path,
+                                       workspace, _raw(stream))

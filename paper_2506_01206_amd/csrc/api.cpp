@@ -11,6 +11,7 @@ namespace {
 using namespace mamba;
 
 constexpr int64_t kMaxGridYZ = 65535;
+constexpr int64_t kMaxVocabulary = (int64_t)1 << 25;
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
@@ -973,6 +974,105 @@ int mamba_gated_delta_step(float *h_out, const float *h_in, const int32_t *paren
                       n_out, n_in, 1, H, Hk, (int)P, (int)N, (int)io, scale, eps, dt_softplus, beta_sigmoid, qk_norm};
     if (const int st = delta_pointers(a, b)) return st;
     return (int)launch_gated_delta_step(a, static_cast<hipStream_t>(hip_stream));
+}
+
+int mamba_token_counts(const int32_t *tokens, int32_t *counts, int64_t n_seq, int64_t L, int64_t V, int accumulate, int prompt,
+                       void *hip_stream)
+{
+    int64_t tb, cb;
+    if (!size3(n_seq, L, 1, 4, &tb) || !size3(n_seq, V, 1, 4, &cb)) return MAMBA_ERR_BAD_SHAPE;
+    if (V > kMaxVocabulary || L > 0x7fffffff || (V > 0 && !token_counts_grid_ok(n_seq, V))) return MAMBA_ERR_UNSUPPORTED;
+    if (n_seq == 0 || V == 0 || (L == 0 && accumulate)) return MAMBA_OK;
+    if ((!tokens && L > 0) || !counts) return MAMBA_ERR_NULL_POINTER;
+    if (!aligned16(tokens) || !aligned16(counts)) return MAMBA_ERR_MISALIGNED;
+    if (overlap(tokens, tb, counts, cb)) return MAMBA_ERR_ALIAS;
+    return (int)launch_token_counts(tokens, counts, n_seq, L, V, accumulate, prompt, static_cast<hipStream_t>(hip_stream));
+}
+
+namespace {
+
+// Rules checked for a call on M rows; in: what they read, for the checks of the outputs.
+struct Span {
+    const void *p;
+    int64_t n;
+};
+int constraints_checked(const mamba_constraints_t *c, int64_t M, int64_t V, ConstrainArgs *a, Span (&in)[7])
+{
+    if (!c) return MAMBA_ERR_NULL_POINTER;
+    if (c->n_seq < 0 || c->n_masks < 0 || c->path_len < 0) return MAMBA_ERR_BAD_SHAPE;
+    if (c->path_len > 4096) return MAMBA_ERR_UNSUPPORTED;
+    int64_t counts, penalties, path, mask;
+    if (!size3(c->n_seq, V, 1, 4, &counts) || !size3(c->n_seq, 3, 1, 4, &penalties) || !size3(M, c->path_len, 1, 4, &path) ||
+        !size3(c->n_masks, (V + 31) / 32, 1, 4, &mask))
+        return MAMBA_ERR_BAD_SHAPE;
+    // a rule of sequences or masks has some, and without an index they are one for all rows or one a row
+    if ((c->counts || c->penalties) && (c->n_seq == 0 || (!c->seq_idx && c->n_seq != 1 && c->n_seq != M))) return MAMBA_ERR_BAD_SHAPE;
+    if (c->mask && (c->n_masks == 0 || (!c->mask_idx && c->n_masks != 1 && c->n_masks != M))) return MAMBA_ERR_BAD_SHAPE;
+    if (c->path_len > 0 && !c->path) return MAMBA_ERR_NULL_POINTER;
+    const Span spans[7] = {{c->counts, counts}, {c->penalties, penalties}, {c->seq_idx, M * 4}, {c->path, path}, {c->bias, V * 4}, {c->mask, mask}, {c->mask_idx, M * 4}};
+    for (int i = 0; i < 7; ++i) {
+        if (!aligned16(spans[i].p)) return MAMBA_ERR_MISALIGNED;
+        in[i] = spans[i];
+    }
+    *a = ConstrainArgs{c->counts, c->penalties, c->seq_idx, c->path_len > 0 ? c->path : nullptr, c->bias, c->mask, c->mask_idx,
+                       c->n_seq, c->n_masks, c->path_len, V};
+    return MAMBA_OK;
+}
+
+}  // namespace
+
+int mamba_logits_constrain_fwd(const void *logits, const mamba_constraints_t *c, void *out, int64_t M, int64_t V, mamba_dtype_t io,
+                               void *hip_stream)
+{
+    const int e = io_size(io);
+    if (e == 0) return MAMBA_ERR_UNSUPPORTED;
+    int64_t lb;
+    if (!size3(M, V, 1, e, &lb)) return MAMBA_ERR_BAD_SHAPE;
+    if (V > kMaxVocabulary || !constrain_grid_ok(M, V)) return MAMBA_ERR_UNSUPPORTED;
+    ConstrainArgs a;
+    Span in[7];
+    if (const int st = constraints_checked(c, M, V, &a, in)) return st;
+    if (M == 0 || V == 0) return MAMBA_OK;
+    if (!logits || !out) return MAMBA_ERR_NULL_POINTER;
+    if (!aligned16(logits) || !aligned16(out)) return MAMBA_ERR_MISALIGNED;
+    if (out != logits && overlap(out, lb, logits, lb)) return MAMBA_ERR_ALIAS;
+    for (const Span &s : in)
+        if (overlap(out, lb, s.p, s.n)) return MAMBA_ERR_ALIAS;
+    return (int)launch_constrain(logits, out, a, M, (int)io, static_cast<hipStream_t>(hip_stream));
+}
+
+size_t mamba_topk_constrained_workspace_bytes(int64_t M, int64_t V, int k)
+{
+    if (M <= 0 || V <= 0 || k < 1 || k > 8 || V > kMaxVocabulary || !constrain_grid_ok(M, V)) return 0;
+    return children_workspace_bytes(M, V, k);
+}
+
+int mamba_topk_constrained_fwd(const void *logits, const mamba_constraints_t *c, int32_t *idx, float *val, int32_t *path_out,
+                               void *workspace, size_t workspace_bytes, int64_t M, int64_t V, int k, mamba_dtype_t io, void *hip_stream)
+{
+    const int e = io_size(io);
+    if (e == 0) return MAMBA_ERR_UNSUPPORTED;
+    int64_t lb;
+    if (!size3(M, V, 1, e, &lb)) return MAMBA_ERR_BAD_SHAPE;
+    if (k < 1 || k > 8 || V > kMaxVocabulary || !constrain_grid_ok(M, V)) return MAMBA_ERR_UNSUPPORTED;
+    ConstrainArgs a;
+    Span in[7];
+    if (const int st = constraints_checked(c, M, V, &a, in)) return st;
+    if (M == 0) return MAMBA_OK;
+    if (V == 0) return MAMBA_ERR_BAD_SHAPE;
+    if (!logits || !idx || !val) return MAMBA_ERR_NULL_POINTER;
+    if (!aligned16(logits) || !aligned16(idx) || !aligned16(val) || !aligned16(path_out) || !aligned16(workspace)) return MAMBA_ERR_MISALIGNED;
+    const size_t need = children_workspace_bytes(M, V, k);
+    if (need > 0 && (!workspace || workspace_bytes < need)) return MAMBA_ERR_WORKSPACE;
+    const Span out[4] = {{idx, M * k * 4}, {val, M * k * 4}, {path_out, M * k * (a.path_len + 1) * 4}, {need > 0 ? workspace : nullptr, (int64_t)need}};
+    for (int i = 0; i < 4; ++i) {
+        if (overlap(out[i].p, out[i].n, logits, lb)) return MAMBA_ERR_ALIAS;
+        for (const Span &s : in)
+            if (overlap(out[i].p, out[i].n, s.p, s.n)) return MAMBA_ERR_ALIAS;
+        for (int j = 0; j < i; ++j)
+            if (overlap(out[i].p, out[i].n, out[j].p, out[j].n)) return MAMBA_ERR_ALIAS;
+    }
+    return (int)launch_children(logits, idx, val, path_out, workspace, a, M, k, (int)io, static_cast<hipStream_t>(hip_stream));
 }
 
 int mamba_tree_plan(const int32_t *tree, int gamma, int64_t n_layers, int64_t D, int64_t N, int K,

@@ -1,0 +1,400 @@
+// Logits under the rules that a verifier decodes by (penalties for repeated tokens, biases, grammar masks), and the children that a
+// draft tree's branches propose under them (Sec. 4.1: a drafted token that the verifier's rules forbid is never accepted).
+//
+//   c = occurrences of v in the generated text of the row's sequence and in the row's own path through the tree
+//   x = x > 0 ? x / repetition : x * repetition      where c > 0 or v stands in the prompt
+//   x = (x - frequency c) - presence                 where c > 0
+//   x = x + bias[v]
+//   not allowed by the row's mask: -inf, and no candidate
+//
+// Every operation is one float32 operation, rounded: which of two tokens is ahead does not depend on how the compiler contracts.
+#include "device_math.h"
+#include "launch.h"
+
+namespace mamba {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kTurns = 4;                                            // vectors of 8 tokens to a lane
+constexpr int kSlice = kThreads * kTurns * 8;                        // tokens to a workgroup
+constexpr int32_t kNoKey = INT32_MIN;                                // below every key
+
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));      // rows of V elements start anywhere
+typedef int32_t i32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+
+__device__ __forceinline__ void load8(const float *p, float *x)
+{
+    const f32x4_any a = *reinterpret_cast<const f32x4_any *>(p), b = *reinterpret_cast<const f32x4_any *>(p + 4);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = a[i], x[4 + i] = b[i];
+}
+__device__ __forceinline__ void load8(const bf16_t *p, float *x)
+{
+    const u32x4_any a = *reinterpret_cast<const u32x4_any *>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[2 * i] = bf16_lo(a[i]), x[2 * i + 1] = bf16_hi(a[i]);
+}
+__device__ __forceinline__ void load8(const int32_t *p, int32_t *x)
+{
+    const i32x4_any a = *reinterpret_cast<const i32x4_any *>(p), b = *reinterpret_cast<const i32x4_any *>(p + 4);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = a[i], x[4 + i] = b[i];
+}
+__device__ __forceinline__ void store8(float *p, const float *x)
+{
+    f32x4_any a, b;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) a[i] = x[i], b[i] = x[4 + i];
+    *reinterpret_cast<f32x4_any *>(p) = a;
+    *reinterpret_cast<f32x4_any *>(p + 4) = b;
+}
+__device__ __forceinline__ void store8(bf16_t *p, const float *x)
+{
+    u32x4_any a;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) a[i] = f32x2_to_bf16x2(x[2 * i], x[2 * i + 1]);
+    *reinterpret_cast<u32x4_any *>(p) = a;
+}
+
+// What holds for one row of logits.
+struct RowRules {
+    bool known;                                                      // its indices are in range
+    float repetition, presence, frequency;
+    const int32_t *counts, *path;
+    const uint8_t *mask;
+};
+__device__ __forceinline__ RowRules rules_of(const ConstrainArgs &c, int64_t m)
+{
+    RowRules r;
+    const int64_t s = c.seq_idx ? c.seq_idx[m] : c.n_seq == 1 ? 0 : m;
+    const int64_t g = !c.mask ? -1 : c.mask_idx ? c.mask_idx[m] : c.n_masks == 1 ? 0 : m;
+    r.known = (!(c.counts || c.penalties) || (s >= 0 && s < c.n_seq)) && g >= -1 && g < c.n_masks;
+    const int64_t s_safe = r.known ? s : 0;
+    r.repetition = 1.0f, r.presence = r.frequency = 0.0f;
+    if (c.penalties) r.repetition = c.penalties[3 * s_safe], r.presence = c.penalties[3 * s_safe + 1], r.frequency = c.penalties[3 * s_safe + 2];
+    r.counts = c.counts && c.penalties ? c.counts + s_safe * c.V : nullptr;
+    r.path = c.penalties ? c.path ? c.path + m * c.path_len : nullptr : nullptr;
+    r.mask = r.known && g >= 0 ? reinterpret_cast<const uint8_t *>(c.mask + g * ((c.V + 31) / 32)) : nullptr;
+    return r;
+}
+
+// The 8 tokens from v on, of a row that has as many behind v: what is fetched for them ...
+struct Fetched {
+    float x[8], bias[8];
+    int32_t counts[8];
+    uint32_t mask;
+};
+template <typename T>
+__device__ __forceinline__ void fetch8(const ConstrainArgs &c, const RowRules &r, const T *row, int64_t v, Fetched &f)
+{
+    load8(row + v, f.x);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f.bias[i] = 0.0f, f.counts[i] = 0;
+    if (c.bias) load8(c.bias + v, f.bias);
+    if (r.counts) load8(r.counts + v, f.counts);
+    f.mask = 0xff;
+    if (r.mask) {
+        const int64_t at = v >> 3, last = (c.V + 31) / 32 * 4 - 1;   // (v is no multiple of 8 in a row's last vector)
+        f.mask = (r.mask[at] | (uint32_t)r.mask[at < last ? at + 1 : last] << 8) >> (v & 7);
+    }
+}
+// ... and what becomes of one
+__device__ __forceinline__ float adjusted(const RowRules &r, float x, int32_t count, int32_t on_path, float bias, bool has_bias)
+{
+#pragma clang fp contract(off)
+    const int32_t times = (count & 0x7fffffff) + on_path;
+    if (count < 0 || times > 0) {
+        x = x > 0.0f ? x / r.repetition : x * r.repetition;
+        if (times > 0) {
+            const float f = r.frequency * (float)times;
+            x = x - f;
+            x = x - r.presence;
+        }
+    }
+    return has_bias ? x + bias : x;
+}
+// occurrences of the 8 tokens from v on in the row's path (few branches have one here: the caller asks `near` ahead)
+__device__ __forceinline__ bool path_near(const RowRules &r, int64_t T, int64_t v)
+{
+    bool near = false;
+    for (int64_t t = 0; t < T; ++t) near |= (uint64_t)((int64_t)r.path[t] - v) < 8;
+    return near;
+}
+__device__ __forceinline__ void path_counts(const RowRules &r, int64_t T, int64_t v, int32_t *times)
+{
+    for (int64_t t = 0; t < T; ++t) {
+        const int64_t d = (int64_t)r.path[t] - v;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) times[i] += d == i;
+    }
+}
+template <typename T>
+__device__ __forceinline__ void adjust8(const ConstrainArgs &c, const RowRules &r, int64_t v, Fetched &f)
+{
+    int32_t on_path[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (r.path && path_near(r, c.path_len, v)) path_counts(r, c.path_len, v, on_path);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f.x[i] = adjusted(r, f.x[i], f.counts[i], on_path[i], f.bias[i], c.bias != nullptr);
+}
+// one token of a row shorter than a vector
+template <typename T>
+__device__ __forceinline__ float adjust1(const ConstrainArgs &c, const RowRules &r, const T *row, int64_t v, bool *allowed)
+{
+    int32_t on_path = 0;
+    if (r.path)
+        for (int64_t t = 0; t < c.path_len; ++t) on_path += r.path[t] == v;
+    *allowed = !r.mask || (r.mask[v >> 3] >> (v & 7) & 1);
+    return adjusted(r, ld_io(row, v), r.counts ? r.counts[v] : 0, on_path, c.bias ? c.bias[v] : 0.0f, c.bias != nullptr);
+}
+
+// grid: (rows x slices); out may be logits (a thread reads what it writes)
+template <typename T>
+__global__ void __launch_bounds__(kThreads) constrain_kernel(const T *logits, T *out, ConstrainArgs c, int64_t slices)
+{
+    const int64_t m = blockIdx.x / slices, v0 = (blockIdx.x - m * slices) * kSlice + threadIdx.x * 8;
+    const RowRules r = rules_of(c, m);
+    const T *row = logits + m * c.V;
+    T *to = out + m * c.V;
+    const float nan = __int_as_float(0x7fc00000);
+    Fetched f[kTurns];
+#pragma unroll
+    for (int u = 0; u < kTurns; ++u) {
+        const int64_t v = v0 + u * kThreads * 8;
+        if (v + 8 <= c.V) fetch8(c, r, row, v, f[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < kTurns; ++u) {
+        const int64_t v = v0 + u * kThreads * 8;
+        if (v + 8 <= c.V) {
+            adjust8<T>(c, r, v, f[u]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[u].x[i] = !r.known ? nan : (f[u].mask >> i & 1) ? f[u].x[i] : -INFINITY;
+            store8(to + v, f[u].x);
+        } else {
+            for (int64_t w = v; w < c.V; ++w) {                      // (fewer than 8 tokens at the end of a row)
+                bool allowed;
+                const float x = adjust1(c, r, row, w, &allowed);
+                st_io(to, w, !r.known ? nan : allowed ? x : -INFINITY);
+            }
+        }
+    }
+}
+
+template <int CTRL> __device__ __forceinline__ int32_t lane_max(int32_t v)
+{
+    return max(v, __builtin_amdgcn_update_dpp(v, v, CTRL, 0xf, 0xf, false));
+}
+// largest of the 64 lanes: quad_perm [1,0,3,2], [2,3,0,1], row_half_mirror, row_mirror, row_bcast:15, row_bcast:31
+__device__ __forceinline__ int32_t wave_max(int32_t v)
+{
+    v = lane_max<0x140>(lane_max<0x141>(lane_max<0x4e>(lane_max<0xb1>(v))));
+    return __builtin_amdgcn_readlane(lane_max<0x143>(lane_max<0x142>(v)), 63);
+}
+// Keys order as signed integers like the values (NaN as -inf, -0 as +0).
+__device__ __forceinline__ int32_t key_of(float x)
+{
+    const float v = x != x ? -INFINITY : x + 0.0f;
+    const int32_t b = __float_as_int(v);
+    return b ^ ((b >> 31) & 0x7fffffff);
+}
+__device__ __forceinline__ float value_of(int32_t key) { return __int_as_float(key ^ ((key >> 31) & 0x7fffffff)); }
+
+// child n of row m, by a whole wavefront: token, value, and the path that leads to it
+__device__ __forceinline__ void write_child(const ConstrainArgs &c, int64_t m, int n, int k, int32_t key, int32_t token, int32_t *idx, float *val,
+                                            int32_t *path_out, int lane)
+{
+    const bool some = key != kNoKey;
+    const int64_t at = m * k + n;
+    if (lane == 0) {
+        idx[at] = some ? token : -1;
+        val[at] = some ? value_of(key) : -INFINITY;
+    }
+    if (path_out)
+        for (int64_t t = lane; t <= c.path_len; t += 64)
+            path_out[at * (c.path_len + 1) + t] = t < c.path_len ? c.path[m * c.path_len + t] : some ? token : -1;
+}
+
+// The k best of one slice of one row.  A lane keeps its 32 tokens' keys in registers and offers the best; the workgroup's best is
+// found k times, and only the wavefront that owned it looks through its registers again.
+// grid: (rows x slices); with one slice the result is the row's, with more the slices' go to `part` and merge_kernel takes over
+template <typename T>
+__global__ void __launch_bounds__(kThreads)
+children_kernel(const T *__restrict__ logits, int32_t *__restrict__ idx, float *__restrict__ val, int32_t *__restrict__ path_out,
+                int2 *__restrict__ part, ConstrainArgs c, int64_t slices, int k)
+{
+    const int64_t m = blockIdx.x / slices, slice = blockIdx.x - m * slices;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int64_t v0 = slice * kSlice + tid * 8;
+    const RowRules r = rules_of(c, m);
+    const T *row = logits + m * c.V;
+    int32_t key[kTurns][8];
+    Fetched f[kTurns];
+    const bool vectors = c.V >= 8;
+    // A row's last vector starts 8 tokens ahead of the row's end, and what the vector before it has is left out.
+    auto start = [&](int u) { return min(v0 + u * kThreads * 8, c.V - 8); };
+#pragma unroll
+    for (int u = 0; u < kTurns; ++u)
+        if (vectors && v0 + u * kThreads * 8 < c.V) fetch8(c, r, row, start(u), f[u]);
+    int32_t best = kNoKey, best_at = -1;                             // first of the lane's largest
+#pragma unroll
+    for (int u = 0; u < kTurns; ++u) {
+        const int64_t v = v0 + u * kThreads * 8;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) key[u][i] = kNoKey;
+        if (!r.known || v >= c.V) continue;
+        if (vectors) {
+            const int64_t s = start(u);
+            adjust8<T>(c, r, s, f[u]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (s + i >= v && (f[u].mask >> i & 1)) key[u][i] = key_of(f[u].x[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < c.V) {
+                    bool allowed;
+                    const float x = adjust1(c, r, row, i, &allowed);
+                    if (allowed) key[u][i] = key_of(x);
+                }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (key[u][i] > best) best = key[u][i], best_at = u * 8 + i;
+    }
+    // a token's number in the row from its place in the lane
+    auto token_of = [&](int at) { return (int32_t)((vectors ? start(at >> 3) : v0) + (at & 7)); };
+    int32_t best_token = token_of(max(best_at, 0));
+    __shared__ int2 heads[2][kThreads / 64];
+    for (int n = 0; n < k; ++n) {
+        const int32_t wk = wave_max(best), wt = wave_max(best == wk ? ~best_token : INT32_MIN);
+        if (lane == 0) heads[n & 1][wave] = make_int2(wk, wt);       // (the other half may still be being read)
+        __syncthreads();
+        int32_t win = kNoKey, not_token = INT32_MIN;
+#pragma unroll
+        for (int w = 0; w < kThreads / 64; ++w) {
+            const int2 h = heads[n & 1][w];
+            if (h.x > win || (h.x == win && h.y > not_token)) win = h.x, not_token = h.y;
+        }
+        const int32_t token = ~not_token;
+        if (wave == 0) {
+            if (slices == 1) write_child(c, m, n, k, win, token, idx, val, path_out, lane);
+            else if (lane == 0) part[(m * slices + slice) * k + n] = make_int2(win, token);
+        }
+        if (win != kNoKey && best == win && best_token == token) {   // the owner's next: the best behind the one that was taken
+            best = kNoKey, best_at = -1;
+#pragma unroll
+            for (int u = 0; u < kTurns; ++u) {
+                const int32_t first = token_of(u * 8);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int32_t q = key[u][i];
+                    if ((q < win || (q == win && first + i > token)) && q > best) best = q, best_at = u * 8 + i;
+                }
+            }
+            best_token = token_of(max(best_at, 0));
+        }
+    }
+}
+
+// The k best of a row's slices: one wavefront, which goes through the slices' candidates (k each, most often fewer than 64 in all)
+// for the best one behind the one taken last.
+__global__ void __launch_bounds__(64)
+merge_kernel(const int2 *__restrict__ part, int32_t *__restrict__ idx, float *__restrict__ val, int32_t *__restrict__ path_out, ConstrainArgs c,
+             int64_t slices, int k)
+{
+    const int64_t m = blockIdx.x, n_part = slices * k;
+    const int lane = threadIdx.x;
+    part += m * n_part;
+    const int2 first = lane < n_part ? part[lane] : make_int2(kNoKey, 0);
+    int32_t win = INT32_MAX, token = -1;
+    for (int n = 0; n < k; ++n) {
+        int32_t best = kNoKey, best_token = INT32_MAX;
+        auto offer = [&](int2 p) {
+            if ((p.x < win || (p.x == win && p.y > token)) && (p.x > best || (p.x == best && p.y < best_token))) best = p.x, best_token = p.y;
+        };
+        offer(first);
+        for (int64_t e = lane + 64; e < n_part; e += 64) offer(part[e]);
+        win = wave_max(best);
+        token = ~wave_max(best == win ? ~best_token : INT32_MIN);
+        write_child(c, m, n, k, win, token, idx, val, path_out, lane);
+        if (win == kNoKey) token = INT32_MAX;                        // nothing is left: no entry is behind this
+    }
+}
+
+// Occurrences of every token in its sequence.  A workgroup has a range of the vocabulary and counts in LDS, over all of the
+// sequence's tokens (numbers outside the vocabulary, such as the -1 of a padded row, are in no range), and writes its range whole:
+// no clearing beforehand, and integer sums, whatever their order.
+constexpr int kCountThreads = 1024, kCountRange = 8192;
+__global__ void __launch_bounds__(kCountThreads)
+token_counts_kernel(const int32_t *__restrict__ tokens, int32_t *__restrict__ counts, int64_t L, int64_t V, int64_t ranges, int accumulate, int prompt)
+{
+    __shared__ int32_t n[kCountRange];
+    const int64_t s = blockIdx.x / ranges, v0 = (blockIdx.x - s * ranges) * kCountRange;
+    const int len = (int)min((int64_t)kCountRange, V - v0);
+    for (int i = threadIdx.x; i < len; i += kCountThreads) n[i] = 0;
+    __syncthreads();
+    constexpr int kAhead = 4;
+    for (int64_t t0 = threadIdx.x; t0 < L; t0 += kCountThreads * kAhead) {
+        int64_t v[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) v[i] = t0 + i * kCountThreads < L ? (int64_t)tokens[s * L + t0 + i * kCountThreads] - v0 : -1;
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+            if (v[i] >= 0 && v[i] < len) atomicAdd(&n[v[i]], 1);
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < len; i += kCountThreads) {
+        const uint32_t old = accumulate ? (uint32_t)counts[s * V + v0 + i] : 0u, more = (uint32_t)n[i];
+        counts[s * V + v0 + i] = (int32_t)(prompt ? old | (more ? 0x80000000u : 0u) : (old & 0x80000000u) | ((old + more) & 0x7fffffffu));
+    }
+}
+
+int64_t slices_of(int64_t V) { return (V + kSlice - 1) / kSlice; }
+
+}  // namespace
+
+bool constrain_grid_ok(int64_t M, int64_t V) { return M <= 0x7fffffff / (slices_of(V) > 0 ? slices_of(V) : 1); }
+bool token_counts_grid_ok(int64_t n_seq, int64_t V) { return n_seq <= 0x7fffffff / ((V + kCountRange - 1) / kCountRange); }
+
+size_t children_workspace_bytes(int64_t M, int64_t V, int k)
+{
+    const int64_t slices = slices_of(V);
+    return slices > 1 ? (size_t)(M * slices * k) * sizeof(int2) : 0;
+}
+
+hipError_t launch_constrain(const void *logits, void *out, const ConstrainArgs &c, int64_t M, int io, hipStream_t stream)
+{
+    const int64_t slices = slices_of(c.V);
+    const unsigned grid = (unsigned)(M * slices);
+    if (io == kIoBf16) constrain_kernel<<<grid, kThreads, 0, stream>>>(static_cast<const bf16_t *>(logits), static_cast<bf16_t *>(out), c, slices);
+    else constrain_kernel<<<grid, kThreads, 0, stream>>>(static_cast<const float *>(logits), static_cast<float *>(out), c, slices);
+    return hipGetLastError();
+}
+
+hipError_t launch_children(const void *logits, int32_t *idx, float *val, int32_t *path_out, void *ws, const ConstrainArgs &c, int64_t M, int k, int io,
+                           hipStream_t stream)
+{
+    const int64_t slices = slices_of(c.V);
+    const unsigned grid = (unsigned)(M * slices);
+    int2 *part = static_cast<int2 *>(ws);
+    if (io == kIoBf16)
+        children_kernel<<<grid, kThreads, 0, stream>>>(static_cast<const bf16_t *>(logits), idx, val, path_out, part, c, slices, k);
+    else
+        children_kernel<<<grid, kThreads, 0, stream>>>(static_cast<const float *>(logits), idx, val, path_out, part, c, slices, k);
+    if (slices > 1) {
+        if (hipError_t e = hipGetLastError()) return e;
+        merge_kernel<<<(unsigned)M, 64, 0, stream>>>(part, idx, val, path_out, c, slices, k);
+    }
+    return hipGetLastError();
+}
+
+hipError_t launch_token_counts(const int32_t *tokens, int32_t *counts, int64_t n_seq, int64_t L, int64_t V, int accumulate, int prompt,
+                               hipStream_t stream)
+{
+    const int64_t ranges = (V + kCountRange - 1) / kCountRange;
+    token_counts_kernel<<<(unsigned)(n_seq * ranges), kCountThreads, 0, stream>>>(tokens, counts, L, V, ranges, accumulate, prompt);
+    return hipGetLastError();
+}
+
+}  // namespace mamba

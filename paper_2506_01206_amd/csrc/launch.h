@@ -240,4 +240,22 @@ hipError_t launch_embedding(const int32_t *tokens, const void *table, void *out,
                             hipStream_t stream);
 hipError_t launch_topk(const void *logits, int32_t *idx, float *val, int64_t M, int64_t V, int k, hipStream_t stream);
 
+// Rules that a row of logits (M, V) goes through; the members of mamba_constraints_t, and V.
+struct ConstrainArgs {
+    const int32_t *counts;
+    const float *penalties;
+    const int32_t *seq_idx, *path;
+    const float *bias;
+    const int32_t *mask, *mask_idx;
+    int64_t n_seq, n_masks, path_len, V;
+};
+bool constrain_grid_ok(int64_t M, int64_t V);
+bool token_counts_grid_ok(int64_t n_seq, int64_t V);
+size_t children_workspace_bytes(int64_t M, int64_t V, int k);
+hipError_t launch_constrain(const void *logits, void *out, const ConstrainArgs &c, int64_t M, int io, hipStream_t stream);
+hipError_t launch_children(const void *logits, int32_t *idx, float *val, int32_t *path_out, void *ws, const ConstrainArgs &c, int64_t M, int k, int io,
+                           hipStream_t stream);
+hipError_t launch_token_counts(const int32_t *tokens, int32_t *counts, int64_t n_seq, int64_t L, int64_t V, int accumulate, int prompt,
+                               hipStream_t stream);
+
 }  // namespace mamba

@@ -5,7 +5,8 @@ blocks, a final RMSNorm and the LM head.  It encodes the prefix once and then dr
 (N_1..N_gamma) as batch generation (Sec. 4.1): at position i every live branch proposes N_i children,
 the children copy their parent's states and all B_i = N_1 * ... * N_i branches advance together.
 Here the N_i children of a node are its N_i most probable next tokens (greedy candidates instead of
-samples, so that runs are reproducible).  States live in one cache per distinct batch size
+samples, so that runs are reproducible), under penalties, biases and masks where the verifier decodes by
+some (``constrain``).  States live in one cache per distinct batch size
 (``mamba_tree_plan``); every draft position has fixed shapes, allocates nothing and never touches
 the host, so a whole draft round is captured once per tree in a HIP graph and replayed.
 
@@ -34,12 +35,55 @@ class MambaDrafter:
         self.root_ssm = torch.empty((self.nl, 1, self.D, self.N), dtype=torch.float32, device=self.dev)
         self.root_logits = torch.empty((1, self.V), dtype=torch.bfloat16, device=self.dev)
         self._trees = {}
+        self._rules = None
+
+    # ------------------------------------------------------------------ rules that the verifier decodes by
+    def constrain(self, repetition=1.0, presence=0.0, frequency=0.0, bias=None, mask=None):
+        """Draft under the rules that the verifier decodes by: penalties for repeated tokens, bias (V) f32 on the logits, mask int32
+        (ceil(V/32)) or (positions, ceil(V/32)) with a set bit where a token is allowed (the last row holds for deeper positions).  The
+        next ``prefill`` takes its tokens as the prompt, ``observe`` adds what was generated since; tokens on the way from the root of
+        the tree count as generated.  A branch that may take fewer tokens than the tree has children there gets token -1 for the
+        others, whose own descendants are of no use.  Calling it again changes the rules in place (captured rounds follow); None for
+        ``repetition`` drops them."""
+        if repetition is None:
+            self._rules = None
+            return
+        if not repetition > 0:
+            raise ValueError("repetition must be above zero, got %r" % (repetition,))
+        words = (self.V + 31) // 32
+        if self._rules is None:
+            full = lambda *shape: torch.full(shape, -1, dtype=torch.int32, device=self.dev)
+            self._rules = dict(counts=torch.zeros((1, self.V), dtype=torch.int32, device=self.dev),
+                               penalties=torch.empty((1, 3), dtype=torch.float32, device=self.dev),
+                               bias=torch.empty((self.V,), dtype=torch.float32, device=self.dev),
+                               masks=[full(1, words) for _ in range(m.MAMBA_MAX_DEPTH)])
+            for bufs in self._trees.values():
+                bufs["constrained_graph"] = None         # (of buffers that were dropped)
+        r = self._rules
+        mask = None if mask is None else mask.reshape(-1, mask.shape[-1])
+        if bias is not None and tuple(bias.shape) != (self.V,):
+            raise ValueError("bias must have shape %s, got %s" % ((self.V,), tuple(bias.shape)))
+        if mask is not None and (mask.dtype != torch.int32 or mask.shape[1] != words or not 1 <= mask.shape[0] <= m.MAMBA_MAX_DEPTH):
+            raise ValueError("mask must be int32 with %d words a row and 1 to %d rows" % (words, m.MAMBA_MAX_DEPTH))
+        r["penalties"].copy_(torch.tensor([[repetition, presence, frequency]], dtype=torch.float32))
+        r["bias"].zero_() if bias is None else r["bias"].copy_(bias)
+        for i, row in enumerate(r["masks"]):
+            row.fill_(-1) if mask is None else row[0].copy_(mask[min(i, mask.shape[0] - 1)])
+
+    def observe(self, tokens):
+        """Tokens (int32[n]) that were generated behind the prompt: what was accepted, not what was drafted."""
+        if self._rules is None:
+            raise RuntimeError("observe() is for a drafter under rules: call constrain() first")
+        m.mamba_token_counts(tokens.view(1, -1), self.V, counts=self._rules["counts"])
 
     # ------------------------------------------------------------------ prefix encoding
     def prefill(self, tokens):
         """Encode a prefix (int32[L]); returns the logits of the next token (1, V) and keeps the
         per-layer states of the prefix as the root of later draft trees."""
         L = tokens.shape[0]
+        if self._rules is not None:
+            self._rules["counts"].zero_()
+            m.mamba_token_counts(tokens.view(1, -1), self.V, counts=self._rules["counts"], prompt=True)
         hid = m.mamba_embedding_fwd(tokens, self.embedding).view(1, L, self.dm)
         ws = torch.empty(max(m.mamba_block_workspace_bytes(self.blocks[0], 1, L), 16), dtype=torch.uint8, device=self.dev)
         for l, blk in enumerate(self.blocks):
@@ -56,14 +100,15 @@ class MambaDrafter:
             return self._trees[tree]
         from .tree import TreeDraftCache
         c = TreeDraftCache(tree, self.nl, self.D, self.N, self.K, torch.bfloat16, self.dev)
-        bufs = dict(cache=c, tree=tree, graph=None, pos=[None])
+        bufs = dict(cache=c, tree=tree, graph=None, constrained_graph=None, pos=[None])
         for i in range(1, c.gamma + 1):
             b_i, b_prev, n_i = c.batch[i], c.batch[i - 1], tree[i - 1]
             mk = lambda shape, dt: torch.empty(shape, dtype=dt, device=self.dev)
             bufs["pos"].append(dict(
                 cand=mk((b_prev, n_i), torch.int32), cand_val=mk((b_prev, n_i), torch.float32),
                 hid=mk((b_i, self.dm), torch.bfloat16), normed=mk((b_i, self.dm), torch.bfloat16),
-                logits=mk((b_i, self.V), torch.bfloat16),
+                logits=mk((b_i, self.V), torch.bfloat16), path=mk((b_i, i), torch.int32),
+                part=mk((max(m.mamba_topk_constrained_workspace_bytes(b_prev, self.V, n_i), 16),), torch.uint8),
                 ws=mk((max(m.mamba_block_workspace_bytes(self.blocks[0], b_i, 1), 16),), torch.uint8)))
         self._trees[tree] = bufs
         return bufs
@@ -75,7 +120,13 @@ class MambaDrafter:
             p, n_i = bufs["pos"][i], tree[i - 1]
             # the N_i most probable tokens of every branch become its children: child j of branch b sits
             # in row b * N_i + j, which is the order parent[row] = row // N_i assumes
-            m.mamba_topk_fwd(logits, n_i, idx=p["cand"], val=p["cand_val"])
+            if self._rules is None:
+                m.mamba_topk_fwd(logits, n_i, idx=p["cand"], val=p["cand_val"])
+            else:
+                r = self._rules
+                m.mamba_topk_constrained_fwd(logits, n_i, counts=r["counts"], penalties=r["penalties"], bias=r["bias"], mask=r["masks"][i - 1],
+                                             path=bufs["pos"][i - 1]["path"] if i > 1 else None, idx=p["cand"], val=p["cand_val"],
+                                             path_out=p["path"], workspace=p["part"])
             m.mamba_embedding_fwd(p["cand"].view(-1), self.embedding, out=p["hid"])
             src, dst = c.cache_index(i - 1), c.cache_index(i)
             for l, blk in enumerate(self.blocks):
@@ -92,10 +143,11 @@ class MambaDrafter:
         bufs = self._buffers(tree)
         c = bufs["cache"]
         c.set_root(self.root_conv, self.root_ssm)
+        kind = "graph" if self._rules is None else "constrained_graph"
         if not use_graph:
             self._round(bufs)
         else:
-            if bufs["graph"] is None:
+            if bufs[kind] is None:
                 self._round(bufs)                        # loads every kernel before the capture
                 c.set_root(self.root_conv, self.root_ssm)
                 g = torch.cuda.CUDAGraph()
@@ -105,7 +157,7 @@ class MambaDrafter:
                     with torch.cuda.graph(g, stream=side):
                         self._round(bufs)
                 torch.cuda.current_stream().wait_stream(side)
-                bufs["graph"] = g
-            bufs["graph"].replay()
+                bufs[kind] = g
+            bufs[kind].replay()
         tokens = [bufs["pos"][i]["cand"].view(-1) for i in range(1, c.gamma + 1)]
         return tokens, bufs["pos"][c.gamma]["logits"]
