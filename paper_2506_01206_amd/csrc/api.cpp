@@ -887,6 +887,7 @@ bool delta_shape_ok(int64_t H, int64_t Hk, int64_t P, int64_t N)
 {
     return (P == 64 || P == 128) && (N == 64 || N == 128) && (H == 0 || (Hk > 0 && H % Hk == 0));
 }
+constexpr int64_t kMaxDeltaHeads = (int64_t)1 << 27;                 // batch x H: eight workgroups to a head in one grid dimension
 struct DeltaBytes {
     int64_t key, value, head, state_in, state_out;   // a q or k, a v or out, a dt or beta tensor; the states
 };
@@ -932,7 +933,8 @@ int mamba_gated_delta_fwd(const void *q, const void *k, const void *v, const voi
     if (batch < 0 || L < 0 || H < 0 || Hk < 0 || P < 0 || N < 0) return MAMBA_ERR_BAD_SHAPE;
     DeltaBytes b;
     if (!delta_bytes(batch, batch, L, H, Hk, P, N, e, &b)) return MAMBA_ERR_BAD_SHAPE;
-    if (!delta_shape_ok(H, Hk, P, N) || batch > kMaxGridYZ || H > kMaxGridYZ || L > ((int64_t)1 << 31)) return MAMBA_ERR_UNSUPPORTED;
+    if (!delta_shape_ok(H, Hk, P, N) || batch > kMaxGridYZ || H > kMaxGridYZ || batch * H > kMaxDeltaHeads || L > ((int64_t)1 << 31))
+        return MAMBA_ERR_UNSUPPORTED;
     if (batch == 0 || H == 0) return MAMBA_OK;
     if (L == 0) {
         if (!h_final || h_final == h0) return MAMBA_OK;

@@ -258,8 +258,12 @@ def test_fwd_keys_that_lean_to_one_side_and_extreme_decays(m, alike, A, beta):
     c["beta"] = storage(W(c["beta"]) + beta, synth.BF16)
     out, hf = m.mamba_gated_delta_fwd(**device(c))
     ro, rh = oracle_scan(c)
-    assert_close(values(to_host(out)), ro, TOL_BF16, "out")
-    assert_close(to_host(hf), rh, TOL_F32, "final state")
+    # A state that never forgets keeps the error of every token's write, each up to 2^-18 of its size as a factor and 2^-18 as a left-out
+    # product, and keys that are alike make them lean to one side: 200 * 2^-17 = 1.5e-3 of a write (which is no larger than the state's
+    # own elements here), where elsewhere only the last chunk or two count.
+    forgets = A <= -16.0
+    assert_close(values(to_host(out)), ro, TOL_BF16 if forgets else TOL_BF16 + 200 * 2.0 ** -17, "out")
+    assert_close(to_host(hf), rh, TOL_F32 if forgets else 200 * 2.0 ** -17, "final state")
 
 
 @pytest.mark.gpu
