@@ -153,14 +153,15 @@ template <typename T, int N, int P> hipError_t recurrent(const DeltaArgs &a, hip
 // ---------------------------------------------------------------------------------------------------
 // A context in chunks of 64 tokens on the matrix cores.  With G_t the running sum of delta A inside a chunk and S the state at its
 // start, the writes u_t = b_t (v_t - a_t S_{t-1} k_t) of a chunk solve a triangular system,
-//   T[t,s] = b_t exp(G_t - G_s) k_t . k_s  (s < t),   X = (I + T)^-1 diag(b),   U = X (V - diag(exp G) K S^T)
-//   O = diag(exp G) Q S^T + M U,   M[t,s] = exp(G_t - G_s) q_t . k_s  (s <= t)
-//   S <- exp(G_end) S + sum_s exp(G_end - G_s) u_s k_s^T
-// X and M do not depend on the state: delta_prepare_kernel forms them for all chunks at once.  What is left goes chunk after chunk, but
-// every row of S (a value channel) by itself: delta_walk_kernel gives a workgroup 16 PT channels of a head.
+//   T[t,s] = b_t exp(G_t - G_s) k_t . k_s  (s < t),   X = (I + T)^-1 diag(b),   R = V - diag(exp G) K S^T,   U = X R
+//   M[t,s] = exp(G_t - G_s) q_t . k_s  (s <= t),      O = diag(exp G) Q S^T + (M X) R
+//   S <- exp(G_end) S + sum_s (exp(G_end - G_s) u_s) k_s^T
+// X and M X do not depend on the state: delta_prepare_kernel forms them for all chunks at once.  What is left goes chunk after chunk,
+// but every row of S (a value channel) by itself: delta_walk_kernel gives a workgroup 16 channels of a head.
 // The lengths of q and k are float32 factors of rows and columns, so that k and q enter the products as they were given, exact in
-// bfloat16.  Of two factors that are both computed (X, R, U, M, S) each is carried as two bfloat16 terms, the rounded value and
-// the remainder, and a product takes three of the four: the states are float32 results, and single terms are off by 2^-9.
+// bfloat16.  A computed factor (X, R, U, S) is carried as three bfloat16 terms, which hold all of a float32 (8 bits each, cut off, not
+// rounded, so that what is left is exact), and of the products of two such all but the three smallest are formed: the states are float32
+// results, and two terms were off by 3e-6 of them.  The outputs are rounded to bfloat16 and take two terms of S, R and M X.
 // The triangular systems are solved, not expanded: powers of T grow like binomials where keys lean to one side, the inverse does not.
 // Fragments of v_mfma_f32_16x16x32_bf16: lane l has row (or column) l % 16 and eight consecutive k from 8 (l / 16); of the result
 // column l % 16, rows 4 (l / 16) .. + 3.  What the preparation leaves for the walk is stored in that order, a kilobyte a fragment.
@@ -171,23 +172,39 @@ constexpr int kC = 64;                                            // tokens of a
 constexpr int kTiles = 6;                                         // 16 x 32 fragments of a lower triangle: 1, 1, 2, 2 to a row of tiles
 constexpr int kFrag = 512;                                        // bf16 of a fragment
 constexpr int kTri = kTiles * kFrag;
-constexpr int kScalars = 256;                                     // floats: factors of k S, of q S, of the write to the state (64 each), decay
-constexpr int kChunkHalves = 4 * kTri + 2 * kScalars;             // 16-bit words of a chunk and head: X and M in two terms each, scalars
+constexpr int kScalars = 256;                                     // floats, four to a token: its factors of k S and of q S, the chunk's decay
+// 16-bit words of a chunk and head: X times the decay to the end (three terms), M X (two), scalars
+constexpr int kAtMX = 3 * kTri, kAtScalars = 5 * kTri, kChunkHalves = 5 * kTri + 2 * kScalars;
 __device__ __forceinline__ int tile_at(int t_tile, int k_step) { return (t_tile < 2 ? t_tile : 2 * t_tile - 2) + k_step; }
 
 __device__ __forceinline__ bf16x8 as_frag(uint4 q) { return __builtin_bit_cast(bf16x8, q); }
+__device__ __forceinline__ bf16x8 as_frag(uint2 a, uint2 b) { return as_frag(make_uint4(a.x, a.y, b.x, b.y)); }
 __device__ __forceinline__ bf16x8 lds_frag(const uint16_t *p) { return as_frag(*reinterpret_cast<const uint4 *>(p)); }
 __device__ __forceinline__ f32x4_t mma(bf16x8 a, bf16x8 b, f32x4_t c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ f32x4_t mma(float a, float b, f32x4_t c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
 
-// four values -> their bf16 roundings and the bf16 of what the roundings dropped
-__device__ __forceinline__ void split4(f32x4_t v, uint16_t *top, uint16_t *rem)
+// the upper halves of four values, in order, and what they leave of them
+__device__ __forceinline__ uint2 take_top(f32x4_t &v)
 {
-    const uint32_t t01 = f32x2_to_bf16x2(v[0], v[1]), t23 = f32x2_to_bf16x2(v[2], v[3]);
-    *reinterpret_cast<uint2 *>(top) = make_uint2(t01, t23);
-    *reinterpret_cast<uint2 *>(rem) = make_uint2(f32x2_to_bf16x2(v[0] - bf16_lo(t01), v[1] - bf16_hi(t01)),
-                                                 f32x2_to_bf16x2(v[2] - bf16_lo(t23), v[3] - bf16_hi(t23)));
+    const uint32_t a = __float_as_uint(v[0]), b = __float_as_uint(v[1]), c = __float_as_uint(v[2]), d = __float_as_uint(v[3]);
+    const uint2 top = make_uint2(__builtin_amdgcn_perm(b, a, 0x07060302), __builtin_amdgcn_perm(d, c, 0x07060302));
+    v[0] -= __uint_as_float(a & 0xffff0000u), v[1] -= __uint_as_float(b & 0xffff0000u);
+    v[2] -= __uint_as_float(c & 0xffff0000u), v[3] -= __uint_as_float(d & 0xffff0000u);
+    return top;
 }
+// four values as three bfloat16 terms
+struct Terms {
+    uint2 hi, mid, lo;
+};
+__device__ __forceinline__ Terms terms_of(f32x4_t v)
+{
+    Terms t;
+    t.hi = take_top(v);
+    t.mid = take_top(v);
+    t.lo = take_top(v);
+    return t;
+}
+__device__ __forceinline__ void put(uint16_t *p, uint2 v) { *reinterpret_cast<uint2 *>(p) = v; }
 
 // Workgroup barrier for what is exchanged through LDS; global loads and stores in flight stay there.
 __device__ __forceinline__ void lds_barrier()
@@ -197,17 +214,28 @@ __device__ __forceinline__ void lds_barrier()
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
+// 16-bit words of a chunk and key head: K^T, K and Q as fragments
+template <int N> constexpr int kKeyHalves = 3 * N * kC;
+// The state that row `row` of tile `tile` of 16 stands for: with 128 states pairs of tiles take turns of four, so that a lane's four of
+// both are eight adjacent ones, as a fragment of K has them.
+template <int N> __device__ __forceinline__ int state_of(int tile, int row)
+{
+    return N == 64 ? tile * 16 + row : (tile >> 1) * 32 + (row >> 2) * 8 + (tile & 1) * 4 + (row & 3);
+}
+
 // grid: (chunks, H, batch)
 template <int N>
 __global__ void __launch_bounds__(kThreads)
 delta_prepare_kernel(const bf16_t *__restrict__ q, const bf16_t *__restrict__ k, const bf16_t *__restrict__ dt, const bf16_t *__restrict__ beta,
-                     const float *__restrict__ A, const float *__restrict__ dt_bias, uint16_t *__restrict__ ws, uint16_t *__restrict__ kt,
+                     const float *__restrict__ A, const float *__restrict__ dt_bias, uint16_t *__restrict__ ws, uint16_t *__restrict__ frags,
                      int64_t L, int64_t H, int64_t group, DeltaOptions o)
 {
     constexpr int kRow = N + 8, kSys = kC + 4;
-    __shared__ __attribute__((aligned(16))) uint16_t ks[kC * kRow], qs[kC * kRow];
-    __shared__ __attribute__((aligned(16))) float sys[kC * kSys], inv[kC * kSys];
+    __shared__ __attribute__((aligned(16))) uint16_t ks[kC * kRow];
+    __shared__ __attribute__((aligned(16))) float sys[kC * kSys], inv[kC * kSys], mq[kC * kSys];   // T; (I + T)^-1; first q, then M
     __shared__ __attribute__((aligned(16))) float rk[kC], rq[kC], G[kC], bt[kC];
+    uint16_t *qs = reinterpret_cast<uint16_t *>(mq);
+    static_assert(sizeof(uint16_t) * kC * kRow <= sizeof(mq), "q shares its place with M");
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c16 = lane & 15, g4 = lane >> 4;
     const int64_t chunk = blockIdx.x, n_chunks = gridDim.x, h = blockIdx.y, b = blockIdx.z;
     const int64_t Hk = H / group, hk = h / group, tok0 = chunk * kC;
@@ -267,54 +295,69 @@ delta_prepare_kernel(const bf16_t *__restrict__ q, const bf16_t *__restrict__ k,
 
     // T and M, tile by tile of 16 x 16: lane has token t = l % 16 of the tile and four s.  A wavefront has a row of tiles of T and
     // the row of M as far from the other end: five tiles each.
-    auto tiles = [&](const uint16_t *rows, int t_tile, auto put) {
-        bf16x8 of_t[N / 32];
+    auto tile = [&](const uint16_t *rows, int t_tile, int s_tile) {
+        const int t = t_tile * 16 + c16, s0 = s_tile * 16 + 4 * g4;
+        f32x4_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int i = 0; i < N / 32; ++i) of_t[i] = lds_frag(&rows[(t_tile * 16 + c16) * kRow + i * 32 + g4 * 8]);
-        const int t = t_tile * 16 + c16;
+        for (int i = 0; i < N / 32; ++i)
+            acc = mma(lds_frag(&ks[(s_tile * 16 + c16) * kRow + i * 32 + g4 * 8]), lds_frag(&rows[t * kRow + i * 32 + g4 * 8]), acc);
+        const float4 Gs = *reinterpret_cast<const float4 *>(&G[s0]), rs = *reinterpret_cast<const float4 *>(&rk[s0]);
         const float Gt = G[t];
-        for (int s_tile = 0; s_tile <= (t_tile | 1); ++s_tile) {
-            f32x4_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
-            const int s0 = s_tile * 16 + 4 * g4;
-            if (s_tile <= t_tile) {
-                bf16x8 of_s[N / 32];
-#pragma unroll
-                for (int i = 0; i < N / 32; ++i) of_s[i] = lds_frag(&ks[(s_tile * 16 + c16) * kRow + i * 32 + g4 * 8]);
-#pragma unroll
-                for (int i = 0; i < N / 32; ++i) acc = mma(of_s[i], of_t[i], acc);
-                const float4 Gs = *reinterpret_cast<const float4 *>(&G[s0]), rs = *reinterpret_cast<const float4 *>(&rk[s0]);
-                acc[0] *= exp2_hw(Gt - Gs.x) * rs.x, acc[1] *= exp2_hw(Gt - Gs.y) * rs.y;
-                acc[2] *= exp2_hw(Gt - Gs.z) * rs.z, acc[3] *= exp2_hw(Gt - Gs.w) * rs.w;
-            }
-            put(t, s_tile, s0, acc);
-        }
+        acc[0] *= exp2_hw(Gt - Gs.x) * rs.x, acc[1] *= exp2_hw(Gt - Gs.y) * rs.y;
+        acc[2] *= exp2_hw(Gt - Gs.z) * rs.z, acc[3] *= exp2_hw(Gt - Gs.w) * rs.w;
+        return acc;
     };
-    tiles(ks, wave, [&](int t, int, int s0, f32x4_t v) {
+    for (int s_tile = 0; s_tile <= wave; ++s_tile) {
+        const int t = wave * 16 + c16, s0 = s_tile * 16 + 4 * g4;
+        f32x4_t v = tile(ks, wave, s_tile);
         const float f = bt[t] * rk[t];
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = s0 + i < t ? v[i] * f : 0.0f;
         *reinterpret_cast<f32x4_t *>(&sys[t * kSys + s0]) = v;
-    });
-    tiles(qs, 3 - wave, [&](int t, int s_tile, int s0, f32x4_t v) {
-        const float f = rq[t];
+    }
+    f32x4_t m[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = s0 + i <= t ? v[i] * f : 0.0f;
-        const int at = tile_at(t >> 4, s_tile >> 1) * kFrag + (c16 + 16 * ((s_tile & 1) * 2 + (g4 >> 1))) * 8 + 4 * (g4 & 1);
-        split4(v, ws + 2 * kTri + at, ws + 3 * kTri + at);
-    });
-    // the keys the other way round, for the write to the state: once for the value heads that share them
+    for (int s_tile = 0; s_tile < 4; ++s_tile)
+        if (s_tile <= 3 - wave) {
+            const int t = (3 - wave) * 16 + c16, s0 = s_tile * 16 + 4 * g4;
+            m[s_tile] = tile(qs, 3 - wave, s_tile);
+            const float f = rq[t];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) m[s_tile][i] = s0 + i <= t ? m[s_tile][i] * f : 0.0f;
+        }
+    // keys and queries as the fragments that the walk takes: once for the value heads that share them
     if (h % group == 0) {
-        uint16_t *to = kt + ((b * Hk + hk) * n_chunks + chunk) * (N * kC);
+        uint16_t *to = frags + ((b * Hk + hk) * n_chunks + chunk) * kKeyHalves<N>;
+        // K^T: rows are states, columns tokens
         for (int f = wave; f < N / 8; f += 4) {
-            const int n = (f >> 1) * 16 + c16, s0 = (f & 1) * 32 + g4 * 8;
+            const int n = state_of<N>(f >> 1, c16), s0 = (f & 1) * 32 + g4 * 8;
             uint32_t w[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) w[i] = ks[(s0 + 2 * i) * kRow + n] | (uint32_t)ks[(s0 + 2 * i + 1) * kRow + n] << 16;
             *reinterpret_cast<uint4 *>(to + f * kFrag + lane * 8) = make_uint4(w[0], w[1], w[2], w[3]);
         }
+        // K: rows are tokens, columns the states of the walk's wavefront f / (N / 32); with 64 states two tiles of tokens side by side
+        for (int f = wave; f < N / 8; f += 4) {
+            uint4 piece;
+            if constexpr (N == 128) {
+                piece = *reinterpret_cast<const uint4 *>(&ks[((f & 3) * 16 + c16) * kRow + (f >> 2) * 32 + 8 * g4]);
+            } else {
+                const uint16_t *at = &ks[((f & 1) * 32 + c16) * kRow + (f >> 1) * 16 + 4 * g4];
+                const uint2 lo = *reinterpret_cast<const uint2 *>(at), hi = *reinterpret_cast<const uint2 *>(at + 16 * kRow);
+                piece = make_uint4(lo.x, lo.y, hi.x, hi.y);
+            }
+            *reinterpret_cast<uint4 *>(to + N * kC + f * kFrag + lane * 8) = piece;
+        }
+        // Q: rows are tokens, columns states
+        for (int f = wave; f < N / 8; f += 4)
+            *reinterpret_cast<uint4 *>(to + 2 * N * kC + f * kFrag + lane * 8) =
+                *reinterpret_cast<const uint4 *>(&qs[((f / (N / 32)) * 16 + c16) * kRow + (f % (N / 32)) * 32 + 8 * g4]);
     }
     lds_barrier();
 
+#pragma unroll
+    for (int s_tile = 0; s_tile < 4; ++s_tile)
+        if (s_tile <= 3 - wave) *reinterpret_cast<f32x4_t *>(&mq[((3 - wave) * 16 + c16) * kSys + s_tile * 16 + 4 * g4]) = m[s_tile];
     // (I + T)^-1: the four 16 x 16 blocks on the diagonal by substitution, a column to a lane ...
     {
         const float *d = sys + wave * 16 * kSys + wave * 16;
@@ -369,226 +412,399 @@ delta_prepare_kernel(const bf16_t *__restrict__ q, const bf16_t *__restrict__ k,
         store_block(r, c, acc);
     }
     lds_barrier();
-    // X in two terms, and the factors of rows
+    // X times the decay to the end of the chunk, in three terms
+    const float end = G[kC - 1];
     for (int step = 0; step <= wave >> 1; ++step) {
         const int t = wave * 16 + c16, s0 = step * 32 + g4 * 8, at = tile_at(wave, step) * kFrag + lane * 8;
+        const float f = rk[t] * exp2_hw(end - G[t]);
+        Terms w[2];
 #pragma unroll
-        for (int i = 0; i < 8; i += 4) {
-            f32x4_t v = *reinterpret_cast<const f32x4_t *>(&inv[t * kSys + s0 + i]);
-            const float4 w = *reinterpret_cast<const float4 *>(&bt[s0 + i]);
-            v[0] = s0 + i <= t ? v[0] * w.x : 0.0f, v[1] = s0 + i + 1 <= t ? v[1] * w.y : 0.0f;
-            v[2] = s0 + i + 2 <= t ? v[2] * w.z : 0.0f, v[3] = s0 + i + 3 <= t ? v[3] * w.w : 0.0f;
-            split4(v, ws + at + i, ws + kTri + at + i);
+        for (int i = 0; i < 2; ++i) {
+            f32x4_t v = *reinterpret_cast<const f32x4_t *>(&inv[t * kSys + s0 + 4 * i]);
+            const f32x4_t strength = *reinterpret_cast<const f32x4_t *>(&bt[s0 + 4 * i]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = s0 + 4 * i + j <= t ? v[j] * strength[j] * f : 0.0f;
+            w[i] = terms_of(v);
         }
+        *reinterpret_cast<uint4 *>(ws + at) = make_uint4(w[0].hi.x, w[0].hi.y, w[1].hi.x, w[1].hi.y);
+        *reinterpret_cast<uint4 *>(ws + kTri + at) = make_uint4(w[0].mid.x, w[0].mid.y, w[1].mid.x, w[1].mid.y);
+        *reinterpret_cast<uint4 *>(ws + 2 * kTri + at) = make_uint4(w[0].lo.x, w[0].lo.y, w[1].lo.x, w[1].lo.y);
     }
-    if (wave == 0) {
-        float *f = reinterpret_cast<float *>(ws + 4 * kTri);
-        const float e = exp2_hw(G[lane]), end = G[kC - 1];
-        f[lane] = rk[lane] * e;
-        f[kC + lane] = rq[lane] * e;
-        f[2 * kC + lane] = rk[lane] * exp2_hw(end - G[lane]);
-        if (lane == 0) f[3 * kC] = exp2_hw(end);
+    // M X, five products of blocks to a wavefront; lane has token t and four adjacent s.  (The blocks above the diagonal that a fragment of
+    // 32 columns takes along are zeros.)
+    auto out_block = [&](int row, int col) {
+        f32x4_t acc = zero;
+        for (int mid = col; mid <= row; ++mid) {
+            const f32x4_t a = *reinterpret_cast<const f32x4_t *>(&mq[(row * 16 + c16) * kSys + mid * 16 + 4 * g4]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int j = mid * 16 + 4 * g4 + i, s = col * 16 + c16;
+                acc = mma(s <= j ? inv[j * kSys + s] : 0.0f, a[i], acc);
+            }
+        }
+        const f32x4_t strength = *reinterpret_cast<const f32x4_t *>(&bt[col * 16 + 4 * g4]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[i] = col * 16 + 4 * g4 + i <= row * 16 + c16 ? acc[i] * strength[i] : 0.0f;
+        const int at = kAtMX + tile_at(row, col >> 1) * kFrag + (c16 + 16 * ((col & 1) * 2 + (g4 >> 1))) * 8 + 4 * (g4 & 1);
+        put(ws + at, take_top(acc));
+        put(ws + kTri + at, take_top(acc));
+    };
+    if (wave == 0) out_block(3, 0), out_block(0, 0), out_block(0, 1);
+    else if (wave == 1) out_block(3, 1), out_block(1, 0);
+    else if (wave == 2) out_block(2, 0), out_block(3, 2), out_block(2, 3);
+    else out_block(2, 1), out_block(3, 3), out_block(2, 2), out_block(1, 1);
+    if (wave == 1) {
+        const float e = exp2_hw(G[lane]);
+        reinterpret_cast<float4 *>(ws + kAtScalars)[lane] = make_float4(rk[lane] * e, rq[lane] * e, exp2_hw(end), 0.0f);
     }
 }
 
-// The chunks of one (batch row, head) in order, for 16 PT of its channels, whose rows of S stay in MFMA accumulators (transposed: lane
-// has a channel and four adjacent states).  Four wavefronts; three phases of a chunk, each ending in a barrier:
-//   1  wavefront w has tokens 16 w .. + 15: R = V - diag K S^T and the first half of the outputs, Q S^T
-//   2  U = X R of its tokens
-//   3  the second half of the outputs, M U; and the write to the state, N / 64 tiles of 16 states each
-// All operands but S, R and U come from memory as fragments, requested as soon as the chunk before has used up their registers.
-// grid: 8 channel blocks (heads / 8 rounded up); the blocks of a head, which read the same fragments, are 8 apart: on one XCD
-template <int N, int PT>
-__global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(1, 2)))
-delta_walk_kernel(const bf16_t *q, const bf16_t *k, const bf16_t *v, const bf16_t *z, const uint16_t *ws, const uint16_t *kt, const float *h0,
-                  float *h_final, bf16_t *out, float *raw, int64_t L, int64_t H, int64_t group, int P, int64_t heads, int64_t n_chunks)
-{
-    constexpr int kRowS = N + 8, kRowU = kC + 8, kSteps = N / 32, kNT = N / 64;
-    __shared__ __attribute__((aligned(16))) uint16_t s_hi[16 * PT * kRowS], s_lo[16 * PT * kRowS];          // S as [channel][state]
-    __shared__ __attribute__((aligned(16))) uint16_t r_hi[16 * PT * kRowU], r_lo[16 * PT * kRowU];          // R as [channel][token]
-    __shared__ __attribute__((aligned(16))) uint16_t u_hi[16 * PT * kRowU], u_lo[16 * PT * kRowU];          // U
-    __shared__ __attribute__((aligned(16))) uint16_t w_hi[16 * PT * kRowU], w_lo[16 * PT * kRowU];          // U times the decay to the end
-    const uint32_t blocks = (uint32_t)P / (16 * PT), place = blockIdx.x >> 3;
-    const int64_t hb = (int64_t)(place / blocks) * 8 + (blockIdx.x & 7);
-    if (hb >= heads) return;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c16 = lane & 15, g4 = lane >> 4;
-    const int64_t b = hb / H, h = hb - b * H, Hk = H / group, hk = h / group;
-    const int p0 = (int)(place % blocks) * 16 * PT;
-    const int t_own = wave * 16 + c16;                            // as a row of K and Q, and as the column of outputs
-
-    const uint16_t *own = ws + hb * n_chunks * kChunkHalves;
-    const uint16_t *own_kt = kt + (b * Hk + hk) * n_chunks * (N * kC) + wave * kNT * 2 * kFrag + lane * 8;
-    // What is requested of a chunk; past the last one, the last one's again.
-    uint4 kf[kSteps], qf[kSteps], xh[2], xl[2], mh[2], ml[2], ktf[kNT][2];
-    uint16_t vf[PT][4];
-    float4 k_factor, w_factor;
-    float q_factor, decay;
-    auto token = [&](int64_t chunk, int t) { return b * L + min(chunk * kC + t, L - 1); };
-    auto fetch_1 = [&](int64_t chunk) {
-        chunk = min(chunk, n_chunks - 1);
-        const int64_t at = (token(chunk, t_own) * Hk + hk) * N + g4 * 8;
-#pragma unroll
-        for (int i = 0; i < kSteps; ++i) kf[i] = *reinterpret_cast<const uint4 *>(k + at + i * 32), qf[i] = *reinterpret_cast<const uint4 *>(q + at + i * 32);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const bf16_t *row = v + (token(chunk, wave * 16 + 4 * g4 + i) * H + h) * P + p0 + c16;
-#pragma unroll
-            for (int p = 0; p < PT; ++p) vf[p][i] = row[p * 16];
-        }
-        const float *f = reinterpret_cast<const float *>(own + chunk * kChunkHalves + 4 * kTri);
-        k_factor = *reinterpret_cast<const float4 *>(f + wave * 16 + 4 * g4);
-    };
-    auto fetch_2 = [&](int64_t chunk) {
-        const uint16_t *x = own + min(chunk, n_chunks - 1) * kChunkHalves + lane * 8;
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-            if (i <= wave >> 1) {
-                xh[i] = *reinterpret_cast<const uint4 *>(x + tile_at(wave, i) * kFrag);
-                xl[i] = *reinterpret_cast<const uint4 *>(x + kTri + tile_at(wave, i) * kFrag);
-            }
-        w_factor = *reinterpret_cast<const float4 *>(reinterpret_cast<const float *>(own + min(chunk, n_chunks - 1) * kChunkHalves + 4 * kTri) + 2 * kC + wave * 16 + 4 * g4);
-    };
-    auto fetch_3 = [&](int64_t chunk) {
-        chunk = min(chunk, n_chunks - 1);
-        const uint16_t *x = own + chunk * kChunkHalves + 2 * kTri + lane * 8;
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-            if (i <= wave >> 1) {
-                mh[i] = *reinterpret_cast<const uint4 *>(x + tile_at(wave, i) * kFrag);
-                ml[i] = *reinterpret_cast<const uint4 *>(x + kTri + tile_at(wave, i) * kFrag);
-            }
-#pragma unroll
-        for (int j = 0; j < kNT; ++j)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) ktf[j][i] = *reinterpret_cast<const uint4 *>(own_kt + chunk * (N * kC) + (j * 2 + i) * kFrag);
-        const float *f = reinterpret_cast<const float *>(own + chunk * kChunkHalves + 4 * kTri);
-        q_factor = f[kC + t_own];
-        decay = f[3 * kC];
-    };
-    fetch_1(0);
-    fetch_2(0);
-    fetch_3(0);
-
-    f32x4_t acc[kNT][PT];                                         // [j][p][i]: state 16 (kNT wave + j) + 4 g4 + i of channel p0 + 16 p + c16
-    auto park_state = [&]() {
-#pragma unroll
-        for (int j = 0; j < kNT; ++j)
-#pragma unroll
-            for (int p = 0; p < PT; ++p) {
-                const int at = (p * 16 + c16) * kRowS + (wave * kNT + j) * 16 + 4 * g4;
-                split4(acc[j][p], &s_hi[at], &s_lo[at]);
-            }
-    };
-#pragma unroll
-    for (int j = 0; j < kNT; ++j)
-#pragma unroll
-        for (int p = 0; p < PT; ++p) {
-            acc[j][p] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-            if (h0) acc[j][p] = *reinterpret_cast<const f32x4_t *>(h0 + (hb * P + p0 + p * 16 + c16) * N + (wave * kNT + j) * 16 + 4 * g4);
-        }
-    park_state();
-    lds_barrier();
-
-    for (int64_t chunk = 0; chunk < n_chunks; ++chunk) {
-        f32x4_t o[PT];
-#pragma unroll
-        for (int p = 0; p < PT; ++p) {
-            bf16x8 sh[kSteps], sl[kSteps];
-#pragma unroll
-            for (int i = 0; i < kSteps; ++i) {
-                sh[i] = lds_frag(&s_hi[(p * 16 + c16) * kRowS + i * 32 + g4 * 8]);
-                sl[i] = lds_frag(&s_lo[(p * 16 + c16) * kRowS + i * 32 + g4 * 8]);
-            }
-            f32x4_t r = {0.0f, 0.0f, 0.0f, 0.0f};
-            o[p] = r;
-#pragma unroll
-            for (int i = 0; i < kSteps; ++i) r = mma(as_frag(kf[i]), sh[i], r);
-#pragma unroll
-            for (int i = 0; i < kSteps; ++i) r = mma(as_frag(kf[i]), sl[i], r);
-#pragma unroll
-            for (int i = 0; i < kSteps; ++i) o[p] = mma(sh[i], as_frag(qf[i]), o[p]);
-#pragma unroll
-            for (int i = 0; i < kSteps; ++i) o[p] = mma(sl[i], as_frag(qf[i]), o[p]);
-            r[0] = fmaf(-k_factor.x, r[0], bf16_to_f32(vf[p][0])), r[1] = fmaf(-k_factor.y, r[1], bf16_to_f32(vf[p][1]));
-            r[2] = fmaf(-k_factor.z, r[2], bf16_to_f32(vf[p][2])), r[3] = fmaf(-k_factor.w, r[3], bf16_to_f32(vf[p][3]));
-            const int at = (p * 16 + c16) * kRowU + wave * 16 + 4 * g4;
-            split4(r, &r_hi[at], &r_lo[at]);
-        }
-        fetch_1(chunk + 1);
-        lds_barrier();
-#pragma unroll
-        for (int p = 0; p < PT; ++p) {
-            f32x4_t u = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-                if (i <= wave >> 1) {
-                    const bf16x8 rh = lds_frag(&r_hi[(p * 16 + c16) * kRowU + i * 32 + g4 * 8]), rl = lds_frag(&r_lo[(p * 16 + c16) * kRowU + i * 32 + g4 * 8]);
-                    u = mma(as_frag(xh[i]), rh, u);
-                    u = mma(as_frag(xh[i]), rl, u);
-                    u = mma(as_frag(xl[i]), rh, u);
-                }
-            const int at = (p * 16 + c16) * kRowU + wave * 16 + 4 * g4;
-            split4(u, &u_hi[at], &u_lo[at]);
-            u[0] *= w_factor.x, u[1] *= w_factor.y, u[2] *= w_factor.z, u[3] *= w_factor.w;
-            split4(u, &w_hi[at], &w_lo[at]);
-        }
-        fetch_2(chunk + 1);
-        lds_barrier();
-#pragma unroll
-        for (int p = 0; p < PT; ++p) {
-            bf16x8 wh[2], wl[2];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                wh[i] = lds_frag(&w_hi[(p * 16 + c16) * kRowU + i * 32 + g4 * 8]);
-                wl[i] = lds_frag(&w_lo[(p * 16 + c16) * kRowU + i * 32 + g4 * 8]);
-            }
-#pragma unroll
-            for (int j = 0; j < kNT; ++j) {
-                acc[j][p] *= decay;
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    acc[j][p] = mma(as_frag(ktf[j][i]), wh[i], acc[j][p]);
-                    acc[j][p] = mma(as_frag(ktf[j][i]), wl[i], acc[j][p]);
-                }
-            }
-            o[p] *= q_factor;
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-                if (i <= wave >> 1) {
-                    const bf16x8 uh = lds_frag(&u_hi[(p * 16 + c16) * kRowU + i * 32 + g4 * 8]), ul = lds_frag(&u_lo[(p * 16 + c16) * kRowU + i * 32 + g4 * 8]);
-                    o[p] = mma(uh, as_frag(mh[i]), o[p]);
-                    o[p] = mma(ul, as_frag(mh[i]), o[p]);
-                    o[p] = mma(uh, as_frag(ml[i]), o[p]);
-                }
-        }
-        park_state();
-        fetch_3(chunk + 1);
-        if (chunk * kC + t_own < L) {
-            const int64_t at = ((b * L + chunk * kC + t_own) * H + h) * P + p0 + 4 * g4;
-#pragma unroll
-            for (int p = 0; p < PT; ++p) {
-                if (raw) {
-                    *reinterpret_cast<f32x4_t *>(raw + at + p * 16) = o[p];
-                    continue;
-                }
-                float y[4] = {o[p][0], o[p][1], o[p][2], o[p][3]};
-                if (z) {
-                    float g[4];
-                    load4(z + at + p * 16, g);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) y[i] *= silu_f32(g[i]);
-                }
-                *reinterpret_cast<uint2 *>(out + at + p * 16) = make_uint2(f32x2_to_bf16x2(y[0], y[1]), f32x2_to_bf16x2(y[2], y[3]));
-            }
-        }
-        lds_barrier();
+// The chunks of one (batch row, head) in order, for 16 of its channels.  Two roles of four wavefronts, three barriers to a chunk:
+//   chain    wavefront w keeps the states n of the w-th quarter in MFMA accumulators (lane: a channel, four adjacent states), which are
+//            the right operand of K S^T as they lie there: the contraction over n takes a lane group's states in any order, if K is
+//            read in the same one.  Every wavefront leaves its part of K S^T for all 64 tokens in LDS                        | A
+//            adds up the parts of the 16 tokens 16 w ..: R, three terms                                                   | B
+//            U = X R of those tokens, with their decay to the end                                                         | C
+//            the write to its states
+//   outputs  wavefront w has the tokens 16 w ..: Q S^T after B, (M X) R after C, gate and store, with the next chunk under way in the chain
+// All operands but S, R and U come from memory, requested two chunks ahead into two sets of registers used in turn.
+struct WalkArgs {
+    const bf16_t *v, *z;
+    const uint16_t *ws, *frags;
+    const float *h0;
+    float *h_final;
+    bf16_t *out;
+    float *raw;
+    int64_t L, H, group, heads, n_chunks;
+    int P;
+};
+constexpr int kWalkPlain = 0, kWalkGate = 1, kWalkRaw = 2;        // outputs as they are, gated, or in float32 for the norm
+constexpr int kRowV = kC + 4;
+// What is exchanged lies in LDS as the fragments that will be read, a kilobyte each: whole lines both ways, no bank conflicts.
+template <int N> struct __attribute__((aligned(16))) WalkLds {
+    float part[4 * 4 * 256];                                      // parts of K S^T, [token tile][wavefront][lane][4]
+    uint16_t s_hi[N / 32 * kFrag], s_mid[N / 32 * kFrag];         // S, channels by states
+    uint16_t r_hi[2 * kFrag], r_mid[2 * kFrag], r_lo[2 * kFrag];  // R, channels by tokens
+    uint16_t u_hi[2 * kFrag], u_mid[2 * kFrag], u_lo[2 * kFrag];  // decayed U
+    uint16_t v[2][16 * kRowV];                                    // V, [channel][token], two chunks
+    float factors[2][3][kC];                                      // of the rows of K S^T and of Q S^T; the chunk's decay
+    float o[4][16 * 16];                                          // a wavefront's outputs, [token][channel]
+};
+// Where a workgroup and a lane are.
+template <int N> struct WalkPlace {
+    int lane, wave, c16, g4, p0;
+    int64_t hb, b, h, Hk, hk;
+    const uint16_t *own;                                          // the head's part of the workspace
+    uint32_t value_row;                                           // elements of a token
+    // where the four adjacent k from 16 tile + 4 g4 of row c16 lie in fragments, and where a lane's eight of fragment i
+    __device__ __forceinline__ int in_frags(int tile) const { return (tile >> 1) * kFrag + (c16 + 16 * ((tile & 1) * 2 + (g4 >> 1))) * 8 + 4 * (g4 & 1); }
+    __device__ __forceinline__ int of_lane(int i) const { return i * kFrag + lane * 8; }
+};
+// A request for a later chunk goes out where its registers are free, and stays there: the compiler would move it.
+__device__ __forceinline__ void requested() { __builtin_amdgcn_sched_barrier(0); }
+// An operand of the chunks in order, by running address (an address formed anew from the chunk's number is some 20 scalar instructions
+// of a wavefront that has none to spare); behind the last chunk it stays there.
+template <typename T> struct Cursor {
+    const T *p;
+    int64_t stride;
+    int left;                                                     // chunks behind this one
+    __device__ __forceinline__ void advance()
+    {
+        p += left > 0 ? stride : 0;
+        left -= left > 0;
     }
-    if (!h_final) return;
+};
+
+// TWO: the wavefront's row of tiles has two fragments of 32 columns (wavefronts 2 and 3)
+template <int N, bool TWO> __device__ __forceinline__ void walk_chain(const WalkArgs &a, const WalkPlace<N> &me, WalkLds<N> &lds)
+{
+    constexpr int kNT = N / 64, kX = TWO ? 2 : 1;
+    const f32x4_t zero = {0.0f, 0.0f, 0.0f, 0.0f};
+    const int n_chunks = (int)a.n_chunks;
+    const uint32_t lane8 = (uint32_t)me.lane * 8;
+    // (the state ahead of the operands: what the loop waits for at its head is then never what it has just requested)
+    f32x4_t acc[kNT];                                             // [j][i]: state_of(kNT wave + j, 4 g4 + i) of channel p0 + c16
 #pragma unroll
-    for (int j = 0; j < kNT; ++j)
+    for (int j = 0; j < kNT; ++j) {
+        acc[j] = zero;
+        if (a.h0) acc[j] = *reinterpret_cast<const f32x4_t *>(a.h0 + (me.hb * a.P + me.p0 + me.c16) * N + state_of<N>(me.wave * kNT + j, 4 * me.g4));
+    }
+    struct Operands {
+        uint2 k[4][kNT];
+        uint4 x[3][kX], kt[kNT][2];
+    };
+    const uint16_t *frags = a.frags + (me.b * me.Hk + me.hk) * a.n_chunks * kKeyHalves<N> + me.wave * kNT * 2 * kFrag;
+    Cursor<uint16_t> keys_t{frags, kKeyHalves<N>, n_chunks - 1}, keys{frags + N * kC, kKeyHalves<N>, n_chunks - 1}, xs{me.own, kChunkHalves, n_chunks - 1};
+    auto fetch_k = [&](Operands &f) {
+        if constexpr (kNT == 2) {
 #pragma unroll
-        for (int p = 0; p < PT; ++p)
-            *reinterpret_cast<f32x4_t *>(h_final + (hb * P + p0 + p * 16 + c16) * N + (wave * kNT + j) * 16 + 4 * g4) = acc[j][p];
+            for (int t = 0; t < 4; ++t) {
+                const uint4 both_tiles = *reinterpret_cast<const uint4 *>(keys.p + t * kFrag + lane8);
+                f.k[t][0] = make_uint2(both_tiles.x, both_tiles.y), f.k[t][1] = make_uint2(both_tiles.z, both_tiles.w);
+            }
+        } else {
+#pragma unroll
+            for (int t = 0; t < 4; t += 2) {
+                const uint4 two_rows = *reinterpret_cast<const uint4 *>(keys.p + t / 2 * kFrag + lane8);
+                f.k[t][0] = make_uint2(two_rows.x, two_rows.y), f.k[t + 1][0] = make_uint2(two_rows.z, two_rows.w);
+            }
+        }
+        keys.advance();
+        requested();
+    };
+    auto fetch_x = [&](Operands &f) {
+#pragma unroll
+        for (int n = 0; n < 3; ++n)
+#pragma unroll
+            for (int i = 0; i < kX; ++i) f.x[n][i] = *reinterpret_cast<const uint4 *>(xs.p + n * kTri + tile_at(me.wave, i) * kFrag + lane8);
+        xs.advance();
+        requested();
+    };
+    auto fetch_kt = [&](Operands &f) {
+#pragma unroll
+        for (int j = 0; j < kNT; ++j)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) f.kt[j][i] = *reinterpret_cast<const uint4 *>(keys_t.p + (j * 2 + i) * kFrag + lane8);
+        keys_t.advance();
+        requested();
+    };
+    Operands even, odd;
+    fetch_k(even), fetch_x(even), fetch_kt(even), fetch_k(odd), fetch_x(odd);
+    __builtin_amdgcn_s_setprio(1);                                // the chain's instructions ahead of the other role's
+    const int at = me.in_frags(me.wave);
+    // (requests go out where the wavefront waits for LDS anyway: a request holds its wavefront for some 14 cycles, and 12 of them at once
+    // are a sixth of a chunk)
+    auto step = [&](int parity, Operands &f, Operands &other) __attribute__((always_inline)) {
+        Terms s[kNT];
+#pragma unroll
+        for (int j = 0; j < kNT; ++j) s[j] = terms_of(acc[j]);
+        if constexpr (kNT == 2) {
+            *reinterpret_cast<uint4 *>(&lds.s_hi[me.of_lane(me.wave)]) = make_uint4(s[0].hi.x, s[0].hi.y, s[1].hi.x, s[1].hi.y);
+            *reinterpret_cast<uint4 *>(&lds.s_mid[me.of_lane(me.wave)]) = make_uint4(s[0].mid.x, s[0].mid.y, s[1].mid.x, s[1].mid.y);
+        } else {
+            put(&lds.s_hi[at], s[0].hi);
+            put(&lds.s_mid[at], s[0].mid);
+        }
+        f32x4_t sum[4];
+        if constexpr (kNT == 2) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t) sum[t] = mma(as_frag(f.k[t][0], f.k[t][1]), as_frag(s[0].lo, s[1].lo), zero);
+#pragma unroll
+            for (int t = 0; t < 4; ++t) sum[t] = mma(as_frag(f.k[t][0], f.k[t][1]), as_frag(s[0].mid, s[1].mid), sum[t]);
+#pragma unroll
+            for (int t = 0; t < 4; ++t) sum[t] = mma(as_frag(f.k[t][0], f.k[t][1]), as_frag(s[0].hi, s[1].hi), sum[t]);
+        } else {                                                  // 16 states a wavefront: two terms to a product, the keys twice
+#pragma unroll
+            for (int t = 0; t < 4; ++t) sum[t] = mma(as_frag(f.k[t][0], f.k[t][0]), as_frag(s[0].lo, make_uint2(0, 0)), zero);
+#pragma unroll
+            for (int t = 0; t < 4; ++t) sum[t] = mma(as_frag(f.k[t][0], f.k[t][0]), as_frag(s[0].mid, s[0].hi), sum[t]);
+        }
+#pragma unroll
+        for (int t = 0; t < 4; ++t) *reinterpret_cast<f32x4_t *>(&lds.part[(t * 4 + me.wave) * 256 + me.lane * 4]) = sum[t];
+        lds_barrier();                                            // A
+        f32x4_t r[4];
+#pragma unroll
+        for (int w = 0; w < 4; ++w) r[w] = *reinterpret_cast<const f32x4_t *>(&lds.part[(me.wave * 4 + w) * 256 + me.lane * 4]);
+        const uint2 values = *reinterpret_cast<const uint2 *>(&lds.v[parity][me.c16 * kRowV + me.wave * 16 + 4 * me.g4]);
+        const f32x4_t k_factor = *reinterpret_cast<const f32x4_t *>(&lds.factors[parity][0][me.wave * 16 + 4 * me.g4]);
+        const float decay = lds.factors[parity][2][0];
+        fetch_k(f);
+        r[0] = (r[0] + r[1]) + (r[2] + r[3]);
+        r[0][0] = fmaf(-k_factor[0], r[0][0], bf16_lo(values.x)), r[0][1] = fmaf(-k_factor[1], r[0][1], bf16_hi(values.x));
+        r[0][2] = fmaf(-k_factor[2], r[0][2], bf16_lo(values.y)), r[0][3] = fmaf(-k_factor[3], r[0][3], bf16_hi(values.y));
+        const Terms rt = terms_of(r[0]);
+        put(&lds.r_hi[at], rt.hi);
+        put(&lds.r_mid[at], rt.mid);
+        put(&lds.r_lo[at], rt.lo);
+        lds_barrier();                                            // B
+        bf16x8 rf[3][kX];
+#pragma unroll
+        for (int i = 0; i < kX; ++i) {
+            const int from = me.of_lane(i);
+            rf[0][i] = lds_frag(&lds.r_hi[from]), rf[1][i] = lds_frag(&lds.r_mid[from]), rf[2][i] = lds_frag(&lds.r_lo[from]);
+        }
+        fetch_kt(other);
+        f32x4_t u[2] = {zero, zero};
+#pragma unroll
+        for (int i = 0; i < kX; ++i) {
+            const bf16x8 xh = as_frag(f.x[0][i]), xm = as_frag(f.x[1][i]), xl = as_frag(f.x[2][i]);
+            u[1] = mma(xl, rf[0][i], u[1]);
+            u[0] = mma(xm, rf[0][i], u[0]);
+            u[1] = mma(xh, rf[2][i], u[1]);
+            u[0] = mma(xh, rf[1][i], u[0]);
+            u[1] = mma(xm, rf[1][i], u[1]);
+            u[0] = mma(xh, rf[0][i], u[0]);
+        }
+        const Terms ut = terms_of(u[0] + u[1]);
+        put(&lds.u_hi[at], ut.hi);
+        put(&lds.u_mid[at], ut.mid);
+        put(&lds.u_lo[at], ut.lo);
+#pragma unroll
+        for (int j = 0; j < kNT; ++j) acc[j] *= decay;
+        lds_barrier();                                            // C
+        bf16x8 uf[3][2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int from = me.of_lane(i);
+            uf[0][i] = lds_frag(&lds.u_lo[from]), uf[1][i] = lds_frag(&lds.u_mid[from]), uf[2][i] = lds_frag(&lds.u_hi[from]);
+        }
+        fetch_x(f);
+#pragma unroll
+        for (int n = 0; n < 3; ++n)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < kNT; ++j) acc[j] = mma(as_frag(f.kt[j][i]), uf[n][i], acc[j]);
+    };
+    int left = n_chunks;                                          // (in pairs: the loads in flight are then the same at every turn)
+    for (; left > 1; left -= 2) {
+        step(0, even, odd);
+        step(1, odd, even);
+    }
+    if (left > 0) step(0, even, odd);
+    if (a.h_final)
+#pragma unroll
+        for (int j = 0; j < kNT; ++j)
+            *reinterpret_cast<f32x4_t *>(a.h_final + (me.hb * a.P + me.p0 + me.c16) * N + state_of<N>(me.wave * kNT + j, 4 * me.g4)) = acc[j];
+}
+
+template <int N, int MODE, bool TWO> __device__ __forceinline__ void walk_outputs(const WalkArgs &a, const WalkPlace<N> &me, WalkLds<N> &lds)
+{
+    constexpr int kSteps = N / 32, kX = TWO ? 2 : 1;
+    const f32x4_t zero = {0.0f, 0.0f, 0.0f, 0.0f};
+    const int n_chunks = (int)a.n_chunks;
+    const uint32_t lane8 = (uint32_t)me.lane * 8;
+    // V, the gates and the outputs: token lane / 4 of the wavefront's 16, four channels, so that four adjacent lanes have a row's 32 bytes
+    // (a request costs a cycle for every run of adjacent lanes that reads adjacent bytes: 64 of them as a fragment has its rows).
+    // Behind the end: the last token again.
+    const int t_own = me.wave * 16 + (me.lane >> 2), p_own = 4 * (me.lane & 3);
+    const uint32_t live = (uint32_t)(a.L - (int64_t)(n_chunks - 1) * kC);
+    const uint32_t value_at = (uint32_t)t_own * me.value_row + (uint32_t)p_own, value_last = min((uint32_t)t_own, live - 1) * me.value_row + (uint32_t)p_own;
+    const int64_t first = (me.b * a.L * a.H + me.h) * a.P + me.p0, chunk_values = (int64_t)kC * me.value_row;
+    struct Operands {
+        uint4 q[kSteps], mx[2][kX];
+        uint2 z, v;
+        float factor;                                             // number lane % 4 of token lane / 4
+    };
+    Cursor<uint16_t> queries{a.frags + (me.b * me.Hk + me.hk) * a.n_chunks * kKeyHalves<N> + 2 * N * kC + me.wave * kSteps * kFrag, kKeyHalves<N>, n_chunks - 1};
+    Cursor<bf16_t> values{a.v + first, chunk_values, n_chunks - 1}, gates{MODE == kWalkGate ? a.z + first : nullptr, chunk_values, n_chunks - 1};
+    Cursor<uint16_t> xs{me.own + kAtMX, kChunkHalves, n_chunks - 1};
+    Cursor<float> factors{reinterpret_cast<const float *>(me.own + kAtScalars) + me.wave * 64, kChunkHalves / 2, n_chunks - 1};
+    auto fetch_q = [&](Operands &f) {
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) f.q[i] = *reinterpret_cast<const uint4 *>(queries.p + i * kFrag + lane8);
+        queries.advance();
+        requested();
+    };
+    auto fetch_mx = [&](Operands &f) {
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int i = 0; i < kX; ++i) f.mx[n][i] = *reinterpret_cast<const uint4 *>(xs.p + n * kTri + tile_at(me.wave, i) * kFrag + lane8);
+        xs.advance();
+        requested();
+    };
+    auto fetch_v = [&](Operands &f) {
+        f.v = *reinterpret_cast<const uint2 *>(values.p + (values.left > 0 ? value_at : value_last));
+        f.factor = factors.p[(uint32_t)me.lane];
+        values.advance(), factors.advance();
+        requested();
+    };
+    auto fetch_z = [&](Operands &f) {
+        if constexpr (MODE == kWalkGate) {
+            f.z = *reinterpret_cast<const uint2 *>(gates.p + (gates.left > 0 ? value_at : value_last));
+            gates.advance();
+            requested();
+        }
+    };
+    // V of a chunk, the other way round, and the factors of its rows
+    auto park_v = [&](int parity, const Operands &f) {
+        uint16_t *to = &lds.v[parity][p_own * kRowV + t_own];
+        to[0] = (uint16_t)f.v.x, to[kRowV] = (uint16_t)(f.v.x >> 16), to[2 * kRowV] = (uint16_t)f.v.y, to[3 * kRowV] = (uint16_t)(f.v.y >> 16);
+        if ((me.lane & 3) < 3) lds.factors[parity][me.lane & 3][t_own] = f.factor;
+    };
+    Operands even, odd;
+    fetch_v(even), fetch_v(odd), fetch_q(even), fetch_q(odd), fetch_mx(even), fetch_z(even);
+    park_v(0, even);
+    fetch_v(even);
+    int64_t to = first + value_at;                                // this lane's outputs of the chunk
+    // (what this role requests goes out where the chain has more to do: all of it behind C made the chain wait there)
+    auto step = [&](int parity, bool stores, Operands &f, Operands &other) __attribute__((always_inline)) {
+        lds_barrier();                                            // A
+        park_v(parity ^ 1, other);
+        fetch_v(other);
+        fetch_mx(other);
+        fetch_z(other);
+        lds_barrier();                                            // B (the chain is short between the two, and would wait for this role)
+        f32x4_t o = zero, o2 = zero;
+        const float q_factor = lds.factors[parity][1][me.wave * 16 + me.c16];
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+            const int from = me.of_lane(i);
+            o2 = mma(lds_frag(&lds.s_mid[from]), as_frag(f.q[i]), o2);
+            o = mma(lds_frag(&lds.s_hi[from]), as_frag(f.q[i]), o);
+        }
+        o = (o + o2) * q_factor;
+        lds_barrier();                                            // C
+        fetch_q(f);
+#pragma unroll
+        for (int i = 0; i < kX; ++i) {
+            const int from = me.of_lane(i);
+            const bf16x8 rh = lds_frag(&lds.r_hi[from]), rm = lds_frag(&lds.r_mid[from]);
+            o = mma(rm, as_frag(f.mx[0][i]), o);
+            o = mma(rh, as_frag(f.mx[1][i]), o);
+            o = mma(rh, as_frag(f.mx[0][i]), o);
+        }
+        // a lane has a token's four channels 4 g4 ..: to the order of the rows, within the wavefront
+        *reinterpret_cast<f32x4_t *>(&lds.o[me.wave][me.c16 * 16 + 4 * me.g4]) = o;
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+        o = *reinterpret_cast<const f32x4_t *>(&lds.o[me.wave][me.lane * 4]);
+        if constexpr (MODE == kWalkGate) {
+            o[0] *= silu_f32(bf16_lo(f.z.x)), o[1] *= silu_f32(bf16_hi(f.z.x));
+            o[2] *= silu_f32(bf16_lo(f.z.y)), o[3] *= silu_f32(bf16_hi(f.z.y));
+        }
+        if (stores) {
+            if constexpr (MODE == kWalkRaw) *reinterpret_cast<f32x4_t *>(a.raw + to) = o;
+            else *reinterpret_cast<uint2 *>(a.out + to) = make_uint2(f32x2_to_bf16x2(o[0], o[1]), f32x2_to_bf16x2(o[2], o[3]));
+        }
+        to += chunk_values;
+    };
+    // (the last chunk, which may be short, by itself: at every other turn all lanes store, and the compiler knows what is in flight)
+    int left = n_chunks;
+    for (; left > 2; left -= 2) {
+        step(0, true, even, odd);
+        step(1, true, odd, even);
+    }
+    const bool last = (uint32_t)t_own < live;
+    if (left == 2) {
+        step(0, true, even, odd);
+        step(1, last, odd, even);
+    } else {
+        step(0, last, even, odd);
+    }
+}
+
+// grid: 8 channel blocks (heads / 8 rounded up); the blocks of a head, which read the same fragments, are 8 apart: on one XCD
+template <int N, int MODE>
+__global__ void __launch_bounds__(2 * kThreads) delta_walk_kernel(WalkArgs a)
+{
+    __shared__ WalkLds<N> lds;
+    const uint32_t blocks = (uint32_t)a.P / 16, place = blockIdx.x >> 3;
+    WalkPlace<N> at;
+    at.hb = (int64_t)(place / blocks) * 8 + (blockIdx.x & 7);
+    if (at.hb >= a.heads) return;
+    const int role = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    at.lane = threadIdx.x & 63, at.wave = role & 3, at.c16 = at.lane & 15, at.g4 = at.lane >> 4;
+    at.b = at.hb / a.H, at.h = at.hb - at.b * a.H, at.Hk = a.H / a.group, at.hk = at.h / a.group;
+    at.p0 = (int)(place % blocks) * 16;
+    at.own = a.ws + at.hb * a.n_chunks * kChunkHalves;
+    at.value_row = (uint32_t)(a.H * a.P);
+    if (role < 2) walk_chain<N, false>(a, at, lds);
+    else if (role < 4) walk_chain<N, true>(a, at, lds);
+    else if (role < 6) walk_outputs<N, MODE, false>(a, at, lds);
+    else walk_outputs<N, MODE, true>(a, at, lds);
 }
 
 // The norm over a head's channels, which the walk's workgroups have in parts, and the gate: P / 4 lanes to a (token, head).
@@ -612,29 +828,29 @@ delta_norm_kernel(const float *__restrict__ raw, const bf16_t *__restrict__ z, c
     if (at < n) *reinterpret_cast<uint2 *>(out + at * 4) = make_uint2(f32x2_to_bf16x2(y[0], y[1]), f32x2_to_bf16x2(y[2], y[3]));
 }
 
-// Where the parts of the workspace lie (bytes from its start): fragments of a chunk and value head, transposed keys of a chunk and key
-// head, outputs ahead of their norm.
+// Where the parts of the workspace lie (bytes from its start): what the preparation leaves of a chunk and value head, fragments of a
+// chunk and key head, outputs ahead of their norm.
 struct DeltaPlan {
-    int64_t chunks, kt_at, raw_at, bytes;
+    int64_t chunks, frags_at, raw_at, bytes;
 };
 DeltaPlan delta_plan(int64_t batch, int64_t L, int64_t H, int64_t Hk, int64_t P, int64_t N)
 {
     DeltaPlan p;
     p.chunks = (L + kC - 1) / kC;
-    p.kt_at = batch * H * p.chunks * kChunkHalves * 2;
-    p.raw_at = p.kt_at + batch * Hk * p.chunks * N * kC * 2;
+    p.frags_at = batch * H * p.chunks * kChunkHalves * 2;
+    p.raw_at = p.frags_at + batch * Hk * p.chunks * 3 * N * kC * 2;
     p.bytes = p.raw_at + batch * L * H * P * 4;
     return p;
 }
 
-template <int N, int PT> void walk(const DeltaArgs &a, const DeltaPlan &p, float *raw, hipStream_t stream)
+template <int N, int MODE> void walk(const DeltaArgs &a, const DeltaPlan &p, float *raw, hipStream_t stream)
 {
     const char *ws = reinterpret_cast<const char *>(a.ws);
     const int64_t heads = a.rows * a.H;
-    delta_walk_kernel<N, PT><<<(unsigned)((heads + 7) / 8 * 8 * (a.P / (16 * PT))), kThreads, 0, stream>>>(
-        static_cast<const bf16_t *>(a.q), static_cast<const bf16_t *>(a.k), static_cast<const bf16_t *>(a.v), static_cast<const bf16_t *>(a.z),
-        reinterpret_cast<const uint16_t *>(ws), reinterpret_cast<const uint16_t *>(ws + p.kt_at), a.h_in, a.h_out, static_cast<bf16_t *>(a.out),
-        raw, a.L, a.H, a.H / a.Hk, a.P, heads, p.chunks);
+    delta_walk_kernel<N, MODE><<<(unsigned)((heads + 7) / 8 * 8 * (a.P / 16)), 2 * kThreads, 0, stream>>>(
+        WalkArgs{static_cast<const bf16_t *>(a.v), static_cast<const bf16_t *>(a.z),
+                 reinterpret_cast<const uint16_t *>(ws), reinterpret_cast<const uint16_t *>(ws + p.frags_at), a.h_in, a.h_out,
+                 static_cast<bf16_t *>(a.out), raw, a.L, a.H, a.H / a.Hk, heads, p.chunks, a.P});
 }
 
 template <int N> hipError_t chunked(const DeltaArgs &a, hipStream_t stream)
@@ -643,11 +859,13 @@ template <int N> hipError_t chunked(const DeltaArgs &a, hipStream_t stream)
     char *ws = reinterpret_cast<char *>(a.ws);
     delta_prepare_kernel<N><<<dim3((unsigned)p.chunks, (unsigned)a.H, (unsigned)a.rows), kThreads, 0, stream>>>(
         static_cast<const bf16_t *>(a.q), static_cast<const bf16_t *>(a.k), static_cast<const bf16_t *>(a.dt), static_cast<const bf16_t *>(a.beta),
-        a.A, a.dt_bias, reinterpret_cast<uint16_t *>(ws), reinterpret_cast<uint16_t *>(ws + p.kt_at), a.L, a.H, a.H / a.Hk,
+        a.A, a.dt_bias, reinterpret_cast<uint16_t *>(ws), reinterpret_cast<uint16_t *>(ws + p.frags_at), a.L, a.H, a.H / a.Hk,
         DeltaOptions{a.scale, a.eps, a.dt_softplus, a.beta_sigmoid, a.qk_norm});
     if (hipError_t e = hipGetLastError()) return e;
     float *raw = a.norm_w ? reinterpret_cast<float *>(ws + p.raw_at) : nullptr;
-    walk<N, 2>(a, p, raw, stream);
+    if (raw) walk<N, kWalkRaw>(a, p, raw, stream);
+    else if (a.z) walk<N, kWalkGate>(a, p, raw, stream);
+    else walk<N, kWalkPlain>(a, p, raw, stream);
     if (hipError_t e = hipGetLastError()) return e;
     if (raw) {
         const int64_t n = a.rows * a.L * a.H * a.P / 4;
