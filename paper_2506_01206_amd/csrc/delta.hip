@@ -214,8 +214,21 @@ __device__ __forceinline__ void lds_barrier()
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
-// 16-bit words of a chunk and key head: K^T, K and Q as fragments
-template <int N> constexpr int kKeyHalves = 3 * N * kC;
+// 16-bit words of a chunk and key head: K and Q as fragments
+template <int N> constexpr int kKeyHalves = 2 * N * kC;
+// x[i] += t[i] of lane J (of its 16) times x[J], for the rows i behind J, and on with the next row: a unit lower triangular system, the
+// right-hand side's rows in x, minus the matrix's rows in t
+template <int J> __device__ __forceinline__ void substitute(const float (&t)[16], float (&x)[16])
+{
+    if constexpr (J < 15) {
+#pragma unroll
+        for (int i = J + 1; i < 16; ++i) {
+            const float row = __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, t[i]), 0x150 + J, 0xf, 0xf, true));
+            x[i] = fmaf(row, x[J], x[i]);
+        }
+        substitute<J + 1>(t, x);
+    }
+}
 // The state that row `row` of tile `tile` of 16 stands for: with 128 states pairs of tiles take turns of four, so that a lane's four of
 // both are eight adjacent ones, as a fragment of K has them.
 template <int N> __device__ __forceinline__ int state_of(int tile, int row)
@@ -223,60 +236,40 @@ template <int N> __device__ __forceinline__ int state_of(int tile, int row)
     return N == 64 ? tile * 16 + row : (tile >> 1) * 32 + (row >> 2) * 8 + (tile & 1) * 4 + (row & 3);
 }
 
-// grid: (chunks, H, batch)
+// One chunk of one head.  Eight wavefronts, and what the chain of phases needs comes first: T by all of them; then one inverts the blocks
+// on its diagonal while the others form M and write the fragments of keys and queries.
+// grid: (chunks of the slab, H, batch); tok_slab: the slab's first token
+constexpr int kPrepThreads = 512;
 template <int N>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kPrepThreads) __attribute__((amdgpu_waves_per_eu(4)))
 delta_prepare_kernel(const bf16_t *__restrict__ q, const bf16_t *__restrict__ k, const bf16_t *__restrict__ dt, const bf16_t *__restrict__ beta,
                      const float *__restrict__ A, const float *__restrict__ dt_bias, uint16_t *__restrict__ ws, uint16_t *__restrict__ frags,
-                     int64_t L, int64_t H, int64_t group, DeltaOptions o)
+                     int64_t tok_slab, int64_t L, int64_t H, int64_t group, DeltaOptions o)
 {
     constexpr int kRow = N + 8, kSys = kC + 4;
     __shared__ __attribute__((aligned(16))) uint16_t ks[kC * kRow];
-    __shared__ __attribute__((aligned(16))) float sys[kC * kSys], inv[kC * kSys], mq[kC * kSys];   // T; (I + T)^-1; first q, then M
+    __shared__ __attribute__((aligned(16))) float sys[kC * kSys], inv[kC * kSys], mq[kC * kSys];   // T, then M X; (I + T)^-1; q, then M
     __shared__ __attribute__((aligned(16))) float rk[kC], rq[kC], G[kC], bt[kC];
     uint16_t *qs = reinterpret_cast<uint16_t *>(mq);
     static_assert(sizeof(uint16_t) * kC * kRow <= sizeof(mq), "q shares its place with M");
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c16 = lane & 15, g4 = lane >> 4;
     const int64_t chunk = blockIdx.x, n_chunks = gridDim.x, h = blockIdx.y, b = blockIdx.z;
-    const int64_t Hk = H / group, hk = h / group, tok0 = chunk * kC;
+    const int64_t Hk = H / group, hk = h / group, tok0 = tok_slab + chunk * kC;
     const int live = (int)min((int64_t)kC, L - tok0);             // tokens of this chunk
     ws += ((b * H + h) * n_chunks + chunk) * kChunkHalves;
 
     // keys and queries into LDS, and one over their lengths (rows behind the end: zeros)
-    constexpr int kPieces = N / 8;                                // 16-byte pieces of a row, on as many adjacent lanes
-    {
-        uint4 kp[kC * kPieces / kThreads], qp[kC * kPieces / kThreads];
+    constexpr int kPieces = N / 8, kMine = kC * kPieces / kPrepThreads;   // 16-byte pieces of a row, on as many adjacent lanes
+    uint4 kp[kMine], qp[kMine];
 #pragma unroll
-        for (int i = 0; i < kC * kPieces / kThreads; ++i) {
-            const int id = i * kThreads + tid, row = id / kPieces, piece = id % kPieces;
-            const int64_t at = ((b * L + tok0 + min(row, live - 1)) * Hk + hk) * N + piece * 8;
-            kp[i] = *reinterpret_cast<const uint4 *>(k + at);
-            qp[i] = *reinterpret_cast<const uint4 *>(q + at);
-        }
-#pragma unroll
-        for (int i = 0; i < kC * kPieces / kThreads; ++i) {
-            const int id = i * kThreads + tid, row = id / kPieces, piece = id % kPieces;
-            if (row >= live) kp[i] = qp[i] = make_uint4(0, 0, 0, 0);
-            float sk = 0.0f, sq = 0.0f;
-            const uint32_t kw[4] = {kp[i].x, kp[i].y, kp[i].z, kp[i].w}, qw[4] = {qp[i].x, qp[i].y, qp[i].z, qp[i].w};
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                sk = fmaf(bf16_lo(kw[w]), bf16_lo(kw[w]), fmaf(bf16_hi(kw[w]), bf16_hi(kw[w]), sk));
-                sq = fmaf(bf16_lo(qw[w]), bf16_lo(qw[w]), fmaf(bf16_hi(qw[w]), bf16_hi(qw[w]), sq));
-            }
-            sk = lane_add<0x141>(lane_add<0x4e>(lane_add<0xb1>(sk)));    // 8 lanes
-            sq = lane_add<0x141>(lane_add<0x4e>(lane_add<0xb1>(sq)));
-            if constexpr (kPieces == 16) sk = lane_add<0x140>(sk), sq = lane_add<0x140>(sq);
-            *reinterpret_cast<uint4 *>(&ks[row * kRow + piece * 8]) = kp[i];
-            *reinterpret_cast<uint4 *>(&qs[row * kRow + piece * 8]) = qp[i];
-            if (piece == 0) {
-                rk[row] = row >= live ? 0.0f : o.qk_norm ? 1.0f / sqrtf(sk + o.eps) : 1.0f;
-                rq[row] = row >= live ? 0.0f : (o.qk_norm ? 1.0f / sqrtf(sq + o.eps) : 1.0f) * o.scale;
-            }
-        }
+    for (int i = 0; i < kMine; ++i) {
+        const int id = i * kPrepThreads + tid, row = id / kPieces, piece = id % kPieces;
+        const int64_t at = ((b * L + tok0 + min(row, live - 1)) * Hk + hk) * N + piece * 8;
+        kp[i] = *reinterpret_cast<const uint4 *>(k + at);
+        qp[i] = *reinterpret_cast<const uint4 *>(q + at);
     }
     // running sum of delta A (in powers of two) and the write strengths; tokens behind the end neither decay nor write
-    if (wave == 0) {
+    if (wave == 7) {
         const int64_t at = (b * L + tok0 + min(lane, live - 1)) * H + h;
         const float x = bf16_to_f32(dt[at]) + (dt_bias ? dt_bias[h] : 0.0f), w = bf16_to_f32(beta[at]);
         float sc = lane < live ? (o.softplus ? softplus_f32(x) : x) * A[h] * kLog2e : 0.0f;
@@ -291,90 +284,104 @@ delta_prepare_kernel(const bf16_t *__restrict__ q, const bf16_t *__restrict__ k,
         G[lane] = sc;
         bt[lane] = lane < live ? (o.sigmoid ? sigmoid_f32(w) : w) : 0.0f;
     }
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+        const int id = i * kPrepThreads + tid, row = id / kPieces, piece = id % kPieces;
+        if (row >= live) kp[i] = qp[i] = make_uint4(0, 0, 0, 0);
+        float sk = 0.0f, sq = 0.0f;
+        const uint32_t kw[4] = {kp[i].x, kp[i].y, kp[i].z, kp[i].w}, qw[4] = {qp[i].x, qp[i].y, qp[i].z, qp[i].w};
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            sk = fmaf(bf16_lo(kw[w]), bf16_lo(kw[w]), fmaf(bf16_hi(kw[w]), bf16_hi(kw[w]), sk));
+            sq = fmaf(bf16_lo(qw[w]), bf16_lo(qw[w]), fmaf(bf16_hi(qw[w]), bf16_hi(qw[w]), sq));
+        }
+        sk = lane_add<0x141>(lane_add<0x4e>(lane_add<0xb1>(sk)));        // 8 lanes
+        sq = lane_add<0x141>(lane_add<0x4e>(lane_add<0xb1>(sq)));
+        if constexpr (kPieces == 16) sk = lane_add<0x140>(sk), sq = lane_add<0x140>(sq);
+        *reinterpret_cast<uint4 *>(&ks[row * kRow + piece * 8]) = kp[i];
+        *reinterpret_cast<uint4 *>(&qs[row * kRow + piece * 8]) = qp[i];
+        if (piece == 0) {
+            rk[row] = row >= live ? 0.0f : o.qk_norm ? 1.0f / sqrtf(sk + o.eps) : 1.0f;
+            rq[row] = row >= live ? 0.0f : (o.qk_norm ? 1.0f / sqrtf(sq + o.eps) : 1.0f) * o.scale;
+        }
+    }
     lds_barrier();
 
-    // T and M, tile by tile of 16 x 16: lane has token t = l % 16 of the tile and four s.  A wavefront has a row of tiles of T and
-    // the row of M as far from the other end: five tiles each.
+    // T and M, tile by tile of 16 x 16: lane has token t = l % 16 of the tile and four s.  The ten tiles of a lower triangle by number:
+    // row 0 of tiles, row 1, ...
+    auto tile_row = [](int i) { return i < 1 ? 0 : i < 3 ? 1 : i < 6 ? 2 : 3; };
     auto tile = [&](const uint16_t *rows, int t_tile, int s_tile) {
         const int t = t_tile * 16 + c16, s0 = s_tile * 16 + 4 * g4;
-        f32x4_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
+        bf16x8 of_s[N / 32], of_t[N / 32];
 #pragma unroll
-        for (int i = 0; i < N / 32; ++i)
-            acc = mma(lds_frag(&ks[(s_tile * 16 + c16) * kRow + i * 32 + g4 * 8]), lds_frag(&rows[t * kRow + i * 32 + g4 * 8]), acc);
+        for (int i = 0; i < N / 32; ++i) {
+            of_s[i] = lds_frag(&ks[(s_tile * 16 + c16) * kRow + i * 32 + g4 * 8]);
+            of_t[i] = lds_frag(&rows[t * kRow + i * 32 + g4 * 8]);
+        }
         const float4 Gs = *reinterpret_cast<const float4 *>(&G[s0]), rs = *reinterpret_cast<const float4 *>(&rk[s0]);
         const float Gt = G[t];
+        f32x4_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int i = 0; i < N / 32; ++i) acc = mma(of_s[i], of_t[i], acc);
         acc[0] *= exp2_hw(Gt - Gs.x) * rs.x, acc[1] *= exp2_hw(Gt - Gs.y) * rs.y;
         acc[2] *= exp2_hw(Gt - Gs.z) * rs.z, acc[3] *= exp2_hw(Gt - Gs.w) * rs.w;
         return acc;
     };
-    for (int s_tile = 0; s_tile <= wave; ++s_tile) {
-        const int t = wave * 16 + c16, s0 = s_tile * 16 + 4 * g4;
-        f32x4_t v = tile(ks, wave, s_tile);
+    for (int i = wave; i < 10; i += 8) {
+        const int t_tile = tile_row(i), s_tile = i - t_tile * (t_tile + 1) / 2, t = t_tile * 16 + c16, s0 = s_tile * 16 + 4 * g4;
+        f32x4_t v = tile(ks, t_tile, s_tile);
         const float f = bt[t] * rk[t];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = s0 + i < t ? v[i] * f : 0.0f;
+        for (int j = 0; j < 4; ++j) v[j] = s0 + j < t ? v[j] * f : 0.0f;
         *reinterpret_cast<f32x4_t *>(&sys[t * kSys + s0]) = v;
-    }
-    f32x4_t m[4];
-#pragma unroll
-    for (int s_tile = 0; s_tile < 4; ++s_tile)
-        if (s_tile <= 3 - wave) {
-            const int t = (3 - wave) * 16 + c16, s0 = s_tile * 16 + 4 * g4;
-            m[s_tile] = tile(qs, 3 - wave, s_tile);
-            const float f = rq[t];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) m[s_tile][i] = s0 + i <= t ? m[s_tile][i] * f : 0.0f;
-        }
-    // keys and queries as the fragments that the walk takes: once for the value heads that share them
-    if (h % group == 0) {
-        uint16_t *to = frags + ((b * Hk + hk) * n_chunks + chunk) * kKeyHalves<N>;
-        // K^T: rows are states, columns tokens
-        for (int f = wave; f < N / 8; f += 4) {
-            const int n = state_of<N>(f >> 1, c16), s0 = (f & 1) * 32 + g4 * 8;
-            uint32_t w[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = ks[(s0 + 2 * i) * kRow + n] | (uint32_t)ks[(s0 + 2 * i + 1) * kRow + n] << 16;
-            *reinterpret_cast<uint4 *>(to + f * kFrag + lane * 8) = make_uint4(w[0], w[1], w[2], w[3]);
-        }
-        // K: rows are tokens, columns the states of the walk's wavefront f / (N / 32); with 64 states two tiles of tokens side by side
-        for (int f = wave; f < N / 8; f += 4) {
-            uint4 piece;
-            if constexpr (N == 128) {
-                piece = *reinterpret_cast<const uint4 *>(&ks[((f & 3) * 16 + c16) * kRow + (f >> 2) * 32 + 8 * g4]);
-            } else {
-                const uint16_t *at = &ks[((f & 1) * 32 + c16) * kRow + (f >> 1) * 16 + 4 * g4];
-                const uint2 lo = *reinterpret_cast<const uint2 *>(at), hi = *reinterpret_cast<const uint2 *>(at + 16 * kRow);
-                piece = make_uint4(lo.x, lo.y, hi.x, hi.y);
-            }
-            *reinterpret_cast<uint4 *>(to + N * kC + f * kFrag + lane * 8) = piece;
-        }
-        // Q: rows are tokens, columns states
-        for (int f = wave; f < N / 8; f += 4)
-            *reinterpret_cast<uint4 *>(to + 2 * N * kC + f * kFrag + lane * 8) =
-                *reinterpret_cast<const uint4 *>(&qs[((f / (N / 32)) * 16 + c16) * kRow + (f % (N / 32)) * 32 + 8 * g4]);
     }
     lds_barrier();
 
+    f32x4_t m[2];                                                 // wavefronts 1 .. 7: tiles wave - 1 and wave + 6 of M
+    if (wave == 0) {
+        // (I + T)^-1: the four 16 x 16 blocks on the diagonal by substitution, a block to 16 lanes and a column to a lane.  A lane has its
+        // column of T as well, and hands its entry of a row to the 15 others as the operand of their multiplication.
+        const float *d = sys + g4 * 16 * kSys + g4 * 16 + c16;
+        float t[16], x[16];
 #pragma unroll
-    for (int s_tile = 0; s_tile < 4; ++s_tile)
-        if (s_tile <= 3 - wave) *reinterpret_cast<f32x4_t *>(&mq[((3 - wave) * 16 + c16) * kSys + s_tile * 16 + 4 * g4]) = m[s_tile];
-    // (I + T)^-1: the four 16 x 16 blocks on the diagonal by substitution, a column to a lane ...
-    {
-        const float *d = sys + wave * 16 * kSys + wave * 16;
-        float x[16];
+        for (int i = 0; i < 16; ++i) t[i] = -d[i * kSys], x[i] = i == c16 ? 1.0f : 0.0f;
+        substitute<0>(t, x);
+        float *to = inv + g4 * 16 * kSys + g4 * 16 + c16;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            float v = i == c16 ? 1.0f : 0.0f;
+        for (int i = 0; i < 16; ++i) to[i * kSys] = x[i];
+    } else {
 #pragma unroll
-            for (int j = 0; j < i; ++j) v = fmaf(-d[i * kSys + j], x[j], v);
-            x[i] = v;
+        for (int j = 0; j < 2; ++j) {
+            const int i = 7 * j + wave - 1;
+            if (i >= 10) continue;
+            const int t_tile = tile_row(i), s_tile = i - t_tile * (t_tile + 1) / 2, t = t_tile * 16 + c16, s0 = s_tile * 16 + 4 * g4;
+            m[j] = tile(qs, t_tile, s_tile);
+            const float f = rq[t];
+#pragma unroll
+            for (int n = 0; n < 4; ++n) m[j][n] = s0 + n <= t ? m[j][n] * f : 0.0f;
         }
-        float *to = inv + wave * 16 * kSys + wave * 16 + c16;
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-            if ((i & 3) == g4) to[i * kSys] = x[i];
+        // keys and queries as the fragments that the walk takes: once for the value heads that share them
+        if (h % group == 0) {
+            uint16_t *to = frags + ((b * Hk + hk) * n_chunks + chunk) * kKeyHalves<N> + lane * 8;
+            for (int f = wave - 1; f < N / 8; f += 7) {
+                // K: rows are tokens, columns the states of the walk's wavefront f / (N / 32); with 64 states two tiles of tokens side by side
+                uint4 piece;
+                if constexpr (N == 128) {
+                    piece = *reinterpret_cast<const uint4 *>(&ks[((f & 3) * 16 + c16) * kRow + (f >> 2) * 32 + 8 * g4]);
+                } else {
+                    const uint16_t *at = &ks[((f & 1) * 32 + c16) * kRow + (f >> 1) * 16 + 4 * g4];
+                    const uint2 lo = *reinterpret_cast<const uint2 *>(at), hi = *reinterpret_cast<const uint2 *>(at + 16 * kRow);
+                    piece = make_uint4(lo.x, lo.y, hi.x, hi.y);
+                }
+                *reinterpret_cast<uint4 *>(to + f * kFrag) = piece;
+                // Q: rows are tokens, columns states
+                *reinterpret_cast<uint4 *>(to + N * kC + f * kFrag) =
+                    *reinterpret_cast<const uint4 *>(&qs[((f / (N / 32)) * 16 + c16) * kRow + (f % (N / 32)) * 32 + 8 * g4]);
+            }
+        }
     }
     lds_barrier();
+
     // ... then what stands below them, X21 = -X22 T21 X11, in float32 on the matrix cores.  The contraction takes the four k of a step from
     // the four lane groups, 4 g + i in step i: so a result is the next product's operand as it lies in the registers.
     auto times_block = [&](int row, int mid, int col, f32x4_t y) {   // y + T[row, mid] X[mid, col] of 16 x 16 blocks
@@ -398,8 +405,15 @@ delta_prepare_kernel(const bf16_t *__restrict__ q, const bf16_t *__restrict__ k,
         const int r = 2 * wave + 1, c = 2 * wave;
         store_block(r, c, times_inverse(r, r, times_block(r, c, c, zero), zero));
     }
+    if (wave > 0) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int i = 7 * j + wave - 1, t_tile = tile_row(i), s_tile = i - t_tile * (t_tile + 1) / 2;
+            if (i < 10) *reinterpret_cast<f32x4_t *>(&mq[(t_tile * 16 + c16) * kSys + s_tile * 16 + 4 * g4]) = m[j];
+        }
+    }
     lds_barrier();
-    {
+    if (wave < 4) {
         const int r = 2 + (wave >> 1), c = wave & 1;
         f32x4_t y = times_block(2, 1, c, zero);
         if (c == 0) y = times_block(2, 0, 0, y);
@@ -412,26 +426,7 @@ delta_prepare_kernel(const bf16_t *__restrict__ q, const bf16_t *__restrict__ k,
         store_block(r, c, acc);
     }
     lds_barrier();
-    // X times the decay to the end of the chunk, in three terms
-    const float end = G[kC - 1];
-    for (int step = 0; step <= wave >> 1; ++step) {
-        const int t = wave * 16 + c16, s0 = step * 32 + g4 * 8, at = tile_at(wave, step) * kFrag + lane * 8;
-        const float f = rk[t] * exp2_hw(end - G[t]);
-        Terms w[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            f32x4_t v = *reinterpret_cast<const f32x4_t *>(&inv[t * kSys + s0 + 4 * i]);
-            const f32x4_t strength = *reinterpret_cast<const f32x4_t *>(&bt[s0 + 4 * i]);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = s0 + 4 * i + j <= t ? v[j] * strength[j] * f : 0.0f;
-            w[i] = terms_of(v);
-        }
-        *reinterpret_cast<uint4 *>(ws + at) = make_uint4(w[0].hi.x, w[0].hi.y, w[1].hi.x, w[1].hi.y);
-        *reinterpret_cast<uint4 *>(ws + kTri + at) = make_uint4(w[0].mid.x, w[0].mid.y, w[1].mid.x, w[1].mid.y);
-        *reinterpret_cast<uint4 *>(ws + 2 * kTri + at) = make_uint4(w[0].lo.x, w[0].lo.y, w[1].lo.x, w[1].lo.y);
-    }
-    // M X, five products of blocks to a wavefront; lane has token t and four adjacent s.  (The blocks above the diagonal that a fragment of
-    // 32 columns takes along are zeros.)
+    // M X, block by block into T's place (lane has token t and four adjacent s), the longer sums by the wavefronts that have no X to write
     auto out_block = [&](int row, int col) {
         f32x4_t acc = zero;
         for (int mid = col; mid <= row; ++mid) {
@@ -442,20 +437,51 @@ delta_prepare_kernel(const bf16_t *__restrict__ q, const bf16_t *__restrict__ k,
                 acc = mma(s <= j ? inv[j * kSys + s] : 0.0f, a[i], acc);
             }
         }
-        const f32x4_t strength = *reinterpret_cast<const f32x4_t *>(&bt[col * 16 + 4 * g4]);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) acc[i] = col * 16 + 4 * g4 + i <= row * 16 + c16 ? acc[i] * strength[i] : 0.0f;
-        const int at = kAtMX + tile_at(row, col >> 1) * kFrag + (c16 + 16 * ((col & 1) * 2 + (g4 >> 1))) * 8 + 4 * (g4 & 1);
-        put(ws + at, take_top(acc));
-        put(ws + kTri + at, take_top(acc));
+        *reinterpret_cast<f32x4_t *>(&sys[(row * 16 + c16) * kSys + col * 16 + 4 * g4]) = acc;
     };
-    if (wave == 0) out_block(3, 0), out_block(0, 0), out_block(0, 1);
-    else if (wave == 1) out_block(3, 1), out_block(1, 0);
-    else if (wave == 2) out_block(2, 0), out_block(3, 2), out_block(2, 3);
-    else out_block(2, 1), out_block(3, 3), out_block(2, 2), out_block(1, 1);
-    if (wave == 1) {
+    // a fragment of a lower triangle of LDS, its columns times the write strengths, its rows times f, in terms
+    auto fragment = [&](const float *rows, int t, int s0, float f, Terms (&w)[2]) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            f32x4_t v = *reinterpret_cast<const f32x4_t *>(&rows[t * kSys + s0 + 4 * i]);
+            const f32x4_t strength = *reinterpret_cast<const f32x4_t *>(&bt[s0 + 4 * i]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = s0 + 4 * i + j <= t ? v[j] * strength[j] * f : 0.0f;
+            w[i] = terms_of(v);
+        }
+    };
+    auto write = [&](int at, uint2 lo, uint2 hi) { *reinterpret_cast<uint4 *>(ws + at) = make_uint4(lo.x, lo.y, hi.x, hi.y); };
+    const float end = G[kC - 1];
+    if (wave < 4) {
+        // X times the decay to the end of the chunk, in three terms
+        const int t = wave * 16 + c16;
+        const float f = rk[t] * exp2_hw(end - G[t]);
+        for (int step = 0; step <= wave >> 1; ++step) {
+            const int at = tile_at(wave, step) * kFrag + lane * 8;
+            Terms w[2];
+            fragment(inv, t, step * 32 + g4 * 8, f, w);
+            write(at, w[0].hi, w[1].hi), write(kTri + at, w[0].mid, w[1].mid), write(2 * kTri + at, w[0].lo, w[1].lo);
+        }
+        if (wave == 0) out_block(3, 2);
+        else if (wave == 1) out_block(3, 3), out_block(2, 2);
+        else if (wave == 2) out_block(1, 1);
+    } else if (wave == 4) {
+        out_block(3, 0);
+    } else if (wave == 5) {
+        out_block(3, 1), out_block(0, 0);
+    } else if (wave == 6) {
+        out_block(2, 0);
         const float e = exp2_hw(G[lane]);
         reinterpret_cast<float4 *>(ws + kAtScalars)[lane] = make_float4(rk[lane] * e, rq[lane] * e, exp2_hw(end), 0.0f);
+    } else {
+        out_block(1, 0), out_block(2, 1);
+    }
+    lds_barrier();
+    if (wave < kTiles) {
+        const int t_tile = wave < 2 ? wave : wave < 4 ? 2 : 3, step = wave < 2 ? 0 : wave & 1, at = kAtMX + wave * kFrag + lane * 8;
+        Terms w[2];
+        fragment(sys, t_tile * 16 + c16, step * 32 + g4 * 8, 1.0f, w);
+        write(at, w[0].hi, w[1].hi), write(kTri + at, w[0].mid, w[1].mid);
     }
 }
 
@@ -475,7 +501,7 @@ struct WalkArgs {
     float *h_final;
     bf16_t *out;
     float *raw;
-    int64_t L, H, group, heads, n_chunks;
+    int64_t L, H, group, heads, tok0, n_chunks;                   // (of the slab: its first token and its chunks)
     int P;
 };
 constexpr int kWalkPlain = 0, kWalkGate = 1, kWalkRaw = 2;        // outputs as they are, gated, or in float32 for the norm
@@ -531,10 +557,10 @@ template <int N, bool TWO> __device__ __forceinline__ void walk_chain(const Walk
     }
     struct Operands {
         uint2 k[4][kNT];
-        uint4 x[3][kX], kt[kNT][2];
+        uint4 x[3][kX];
     };
     const uint16_t *frags = a.frags + (me.b * me.Hk + me.hk) * a.n_chunks * kKeyHalves<N> + me.wave * kNT * 2 * kFrag;
-    Cursor<uint16_t> keys_t{frags, kKeyHalves<N>, n_chunks - 1}, keys{frags + N * kC, kKeyHalves<N>, n_chunks - 1}, xs{me.own, kChunkHalves, n_chunks - 1};
+    Cursor<uint16_t> keys{frags, kKeyHalves<N>, n_chunks - 1}, xs{me.own, kChunkHalves, n_chunks - 1};
     auto fetch_k = [&](Operands &f) {
         if constexpr (kNT == 2) {
 #pragma unroll
@@ -560,21 +586,27 @@ template <int N, bool TWO> __device__ __forceinline__ void walk_chain(const Walk
         xs.advance();
         requested();
     };
-    auto fetch_kt = [&](Operands &f) {
+    // K^T of the wavefront's states is its K times a choice of columns: a product gives it exactly, lane a state, four adjacent tokens
+    bf16x8 choice[kNT];
 #pragma unroll
-        for (int j = 0; j < kNT; ++j)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) f.kt[j][i] = *reinterpret_cast<const uint4 *>(keys_t.p + (j * 2 + i) * kFrag + lane8);
-        keys_t.advance();
-        requested();
+    for (int j = 0; j < kNT; ++j) {
+        const uint32_t one = me.g4 == me.c16 >> 2 ? (me.c16 & 1 ? 0x3f800000u : 0x3f80u) : 0u, lo = me.c16 & 2 ? 0u : one, hi = me.c16 & 2 ? one : 0u;
+        choice[j] = j == 0 ? as_frag(make_uint2(lo, hi), make_uint2(0, 0)) : as_frag(make_uint2(0, 0), make_uint2(lo, hi));
+    }
+    auto transposed = [&](const Operands &f, int t, int j) {
+        const f32x4_t d = mma(kNT == 2 ? as_frag(f.k[t][0], f.k[t][kNT - 1]) : as_frag(f.k[t][0], f.k[t][0]), choice[j], zero);
+        return make_uint2(__builtin_amdgcn_perm(__float_as_uint(d[1]), __float_as_uint(d[0]), 0x07060302),
+                          __builtin_amdgcn_perm(__float_as_uint(d[3]), __float_as_uint(d[2]), 0x07060302));
     };
     Operands even, odd;
-    fetch_k(even), fetch_x(even), fetch_kt(even), fetch_k(odd), fetch_x(odd);
+    fetch_k(even), fetch_x(even), fetch_k(odd), fetch_x(odd);
     __builtin_amdgcn_s_setprio(1);                                // the chain's instructions ahead of the other role's
     const int at = me.in_frags(me.wave);
+    // the write to the state takes the tokens of two tiles in turns of four, as K^T comes out of its products
+    const int u_at = me.of_lane(me.wave >> 1) + 4 * (me.wave & 1);
     // (requests go out where the wavefront waits for LDS anyway: a request holds its wavefront for some 14 cycles, and 12 of them at once
     // are a sixth of a chunk)
-    auto step = [&](int parity, Operands &f, Operands &other) __attribute__((always_inline)) {
+    auto step = [&](int parity, Operands &f) __attribute__((always_inline)) {
         Terms s[kNT];
 #pragma unroll
         for (int j = 0; j < kNT; ++j) s[j] = terms_of(acc[j]);
@@ -608,6 +640,11 @@ template <int N, bool TWO> __device__ __forceinline__ void walk_chain(const Walk
         const uint2 values = *reinterpret_cast<const uint2 *>(&lds.v[parity][me.c16 * kRowV + me.wave * 16 + 4 * me.g4]);
         const f32x4_t k_factor = *reinterpret_cast<const f32x4_t *>(&lds.factors[parity][0][me.wave * 16 + 4 * me.g4]);
         const float decay = lds.factors[parity][2][0];
+        uint2 kt[4][kNT];
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int j = 0; j < kNT; ++j) kt[t][j] = transposed(f, t, j);
         fetch_k(f);
         r[0] = (r[0] + r[1]) + (r[2] + r[3]);
         r[0][0] = fmaf(-k_factor[0], r[0][0], bf16_lo(values.x)), r[0][1] = fmaf(-k_factor[1], r[0][1], bf16_hi(values.x));
@@ -623,7 +660,6 @@ template <int N, bool TWO> __device__ __forceinline__ void walk_chain(const Walk
             const int from = me.of_lane(i);
             rf[0][i] = lds_frag(&lds.r_hi[from]), rf[1][i] = lds_frag(&lds.r_mid[from]), rf[2][i] = lds_frag(&lds.r_lo[from]);
         }
-        fetch_kt(other);
         f32x4_t u[2] = {zero, zero};
 #pragma unroll
         for (int i = 0; i < kX; ++i) {
@@ -636,9 +672,9 @@ template <int N, bool TWO> __device__ __forceinline__ void walk_chain(const Walk
             u[0] = mma(xh, rf[0][i], u[0]);
         }
         const Terms ut = terms_of(u[0] + u[1]);
-        put(&lds.u_hi[at], ut.hi);
-        put(&lds.u_mid[at], ut.mid);
-        put(&lds.u_lo[at], ut.lo);
+        put(&lds.u_hi[u_at], ut.hi);
+        put(&lds.u_mid[u_at], ut.mid);
+        put(&lds.u_lo[u_at], ut.lo);
 #pragma unroll
         for (int j = 0; j < kNT; ++j) acc[j] *= decay;
         lds_barrier();                                            // C
@@ -654,14 +690,14 @@ template <int N, bool TWO> __device__ __forceinline__ void walk_chain(const Walk
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
-                for (int j = 0; j < kNT; ++j) acc[j] = mma(as_frag(f.kt[j][i]), uf[n][i], acc[j]);
+                for (int j = 0; j < kNT; ++j) acc[j] = mma(as_frag(kt[2 * i][j], kt[2 * i + 1][j]), uf[n][i], acc[j]);
     };
     int left = n_chunks;                                          // (in pairs: the loads in flight are then the same at every turn)
     for (; left > 1; left -= 2) {
-        step(0, even, odd);
-        step(1, odd, even);
+        step(0, even);
+        step(1, odd);
     }
-    if (left > 0) step(0, even, odd);
+    if (left > 0) step(0, even);
     if (a.h_final)
 #pragma unroll
         for (int j = 0; j < kNT; ++j)
@@ -678,15 +714,15 @@ template <int N, int MODE, bool TWO> __device__ __forceinline__ void walk_output
     // (a request costs a cycle for every run of adjacent lanes that reads adjacent bytes: 64 of them as a fragment has its rows).
     // Behind the end: the last token again.
     const int t_own = me.wave * 16 + (me.lane >> 2), p_own = 4 * (me.lane & 3);
-    const uint32_t live = (uint32_t)(a.L - (int64_t)(n_chunks - 1) * kC);
+    const uint32_t live = (uint32_t)min((int64_t)kC, a.L - a.tok0 - (int64_t)(n_chunks - 1) * kC);
     const uint32_t value_at = (uint32_t)t_own * me.value_row + (uint32_t)p_own, value_last = min((uint32_t)t_own, live - 1) * me.value_row + (uint32_t)p_own;
-    const int64_t first = (me.b * a.L * a.H + me.h) * a.P + me.p0, chunk_values = (int64_t)kC * me.value_row;
+    const int64_t first = ((me.b * a.L + a.tok0) * a.H + me.h) * a.P + me.p0, chunk_values = (int64_t)kC * me.value_row;
     struct Operands {
         uint4 q[kSteps], mx[2][kX];
         uint2 z, v;
         float factor;                                             // number lane % 4 of token lane / 4
     };
-    Cursor<uint16_t> queries{a.frags + (me.b * me.Hk + me.hk) * a.n_chunks * kKeyHalves<N> + 2 * N * kC + me.wave * kSteps * kFrag, kKeyHalves<N>, n_chunks - 1};
+    Cursor<uint16_t> queries{a.frags + (me.b * me.Hk + me.hk) * a.n_chunks * kKeyHalves<N> + N * kC + me.wave * kSteps * kFrag, kKeyHalves<N>, n_chunks - 1};
     Cursor<bf16_t> values{a.v + first, chunk_values, n_chunks - 1}, gates{MODE == kWalkGate ? a.z + first : nullptr, chunk_values, n_chunks - 1};
     Cursor<uint16_t> xs{me.own + kAtMX, kChunkHalves, n_chunks - 1};
     Cursor<float> factors{reinterpret_cast<const float *>(me.own + kAtScalars) + me.wave * 64, kChunkHalves / 2, n_chunks - 1};
@@ -727,7 +763,8 @@ template <int N, int MODE, bool TWO> __device__ __forceinline__ void walk_output
     fetch_v(even), fetch_v(odd), fetch_q(even), fetch_q(odd), fetch_mx(even), fetch_z(even);
     park_v(0, even);
     fetch_v(even);
-    int64_t to = first + value_at;                                // this lane's outputs of the chunk
+    // this lane's outputs of the chunk (ahead of a norm they go into a buffer of the slab)
+    int64_t to = (MODE == kWalkRaw ? (me.b * a.n_chunks * kC * a.H + me.h) * a.P + me.p0 : first) + value_at;
     // (what this role requests goes out where the chain has more to do: all of it behind C made the chain wait there)
     auto step = [&](int parity, bool stores, Operands &f, Operands &other) __attribute__((always_inline)) {
         lds_barrier();                                            // A
@@ -808,73 +845,90 @@ __global__ void __launch_bounds__(2 * kThreads) delta_walk_kernel(WalkArgs a)
 }
 
 // The norm over a head's channels, which the walk's workgroups have in parts, and the gate: P / 4 lanes to a (token, head).
+// grid: (workgroups, batch); n: quadruples of a batch row, raw_row and row those from one batch row to the next
 template <int P>
 __global__ void __launch_bounds__(kThreads)
 delta_norm_kernel(const float *__restrict__ raw, const bf16_t *__restrict__ z, const float *__restrict__ norm_w, bf16_t *__restrict__ out, int64_t n,
-                  float eps)
+                  int64_t raw_row, int64_t row, float eps)
 {
     const int64_t at = (int64_t)blockIdx.x * kThreads + threadIdx.x;
     const int64_t safe = min(at, n - 1);
+    const int64_t from = (int64_t)blockIdx.y * raw_row + safe, to = (int64_t)blockIdx.y * row + safe;
     const int p = (int)(safe % (P / 4)) * 4;
     float y[4], w[4], g[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    load4(raw + safe * 4, y);
+    load4(raw + from * 4, y);
     load4(norm_w + p, w);
-    if (z) load4(z + safe * 4, g);
+    if (z) load4(z + to * 4, g);
     float ss = sum16(fmaf(y[0], y[0], fmaf(y[1], y[1], fmaf(y[2], y[2], y[3] * y[3]))));
     if constexpr (P == 128) ss += __shfl_xor(ss, 16, 64);
     const float f = 1.0f / sqrtf(ss / P + eps);
 #pragma unroll
     for (int i = 0; i < 4; ++i) y[i] *= f * w[i] * (z ? silu_f32(g[i]) : 1.0f);
-    if (at < n) *reinterpret_cast<uint2 *>(out + at * 4) = make_uint2(f32x2_to_bf16x2(y[0], y[1]), f32x2_to_bf16x2(y[2], y[3]));
+    if (at < n) *reinterpret_cast<uint2 *>(out + to * 4) = make_uint2(f32x2_to_bf16x2(y[0], y[1]), f32x2_to_bf16x2(y[2], y[3]));
 }
 
+// A long context goes in slabs of chunks, so that what the preparation leaves is still in the last-level cache (256 MB) when the walk takes
+// it, and the workspace does not grow with the context.  (@SLABS@)
+constexpr int64_t kSlabBytes = (int64_t)128 << 20, kSlabLeast = 8;
 // Where the parts of the workspace lie (bytes from its start): what the preparation leaves of a chunk and value head, fragments of a
-// chunk and key head, outputs ahead of their norm.
+// chunk and key head, outputs ahead of their norm, the states between slabs where the caller takes none.
 struct DeltaPlan {
-    int64_t chunks, frags_at, raw_at, bytes;
+    int64_t chunks, slab, frags_at, raw_at, state_at, bytes;
 };
 DeltaPlan delta_plan(int64_t batch, int64_t L, int64_t H, int64_t Hk, int64_t P, int64_t N)
 {
     DeltaPlan p;
     p.chunks = (L + kC - 1) / kC;
-    p.frags_at = batch * H * p.chunks * kChunkHalves * 2;
-    p.raw_at = p.frags_at + batch * Hk * p.chunks * 3 * N * kC * 2;
-    p.bytes = p.raw_at + batch * L * H * P * 4;
+    const int64_t chunk_bytes = batch * (H * (kChunkHalves * 2 + kC * P * 4) + Hk * 2 * N * kC * 2);
+    int64_t most = kSlabBytes / chunk_bytes;
+    most = most < kSlabLeast ? kSlabLeast : most;
+    const int64_t slabs = (p.chunks + most - 1) / most;
+    p.slab = (p.chunks + slabs - 1) / slabs;
+    p.frags_at = batch * H * p.slab * kChunkHalves * 2;
+    p.raw_at = p.frags_at + batch * Hk * p.slab * 2 * N * kC * 2;
+    p.state_at = p.raw_at + batch * p.slab * kC * H * P * 4;
+    p.bytes = p.state_at + (slabs > 1 ? batch * H * P * N * 4 : 0);
     return p;
 }
 
-template <int N, int MODE> void walk(const DeltaArgs &a, const DeltaPlan &p, float *raw, hipStream_t stream)
+template <int N, int MODE> void walk(const DeltaArgs &a, const WalkArgs &w, hipStream_t stream)
 {
-    const char *ws = reinterpret_cast<const char *>(a.ws);
-    const int64_t heads = a.rows * a.H;
-    delta_walk_kernel<N, MODE><<<(unsigned)((heads + 7) / 8 * 8 * (a.P / 16)), 2 * kThreads, 0, stream>>>(
-        WalkArgs{static_cast<const bf16_t *>(a.v), static_cast<const bf16_t *>(a.z),
-                 reinterpret_cast<const uint16_t *>(ws), reinterpret_cast<const uint16_t *>(ws + p.frags_at), a.h_in, a.h_out,
-                 static_cast<bf16_t *>(a.out), raw, a.L, a.H, a.H / a.Hk, heads, p.chunks, a.P});
+    delta_walk_kernel<N, MODE><<<(unsigned)((w.heads + 7) / 8 * 8 * (a.P / 16)), 2 * kThreads, 0, stream>>>(w);
 }
 
 template <int N> hipError_t chunked(const DeltaArgs &a, hipStream_t stream)
 {
     const DeltaPlan p = delta_plan(a.rows, a.L, a.H, a.Hk, a.P, a.N);
     char *ws = reinterpret_cast<char *>(a.ws);
-    delta_prepare_kernel<N><<<dim3((unsigned)p.chunks, (unsigned)a.H, (unsigned)a.rows), kThreads, 0, stream>>>(
-        static_cast<const bf16_t *>(a.q), static_cast<const bf16_t *>(a.k), static_cast<const bf16_t *>(a.dt), static_cast<const bf16_t *>(a.beta),
-        a.A, a.dt_bias, reinterpret_cast<uint16_t *>(ws), reinterpret_cast<uint16_t *>(ws + p.frags_at), a.L, a.H, a.H / a.Hk,
-        DeltaOptions{a.scale, a.eps, a.dt_softplus, a.beta_sigmoid, a.qk_norm});
-    if (hipError_t e = hipGetLastError()) return e;
+    uint16_t *frags = reinterpret_cast<uint16_t *>(ws + p.frags_at);
     float *raw = a.norm_w ? reinterpret_cast<float *>(ws + p.raw_at) : nullptr;
-    if (raw) walk<N, kWalkRaw>(a, p, raw, stream);
-    else if (a.z) walk<N, kWalkGate>(a, p, raw, stream);
-    else walk<N, kWalkPlain>(a, p, raw, stream);
-    if (hipError_t e = hipGetLastError()) return e;
-    if (raw) {
-        const int64_t n = a.rows * a.L * a.H * a.P / 4;
-        const unsigned grid = (unsigned)((n + kThreads - 1) / kThreads);
-        const bf16_t *z = static_cast<const bf16_t *>(a.z);
-        if (a.P == 64) delta_norm_kernel<64><<<grid, kThreads, 0, stream>>>(raw, z, a.norm_w, static_cast<bf16_t *>(a.out), n, a.eps);
-        else delta_norm_kernel<128><<<grid, kThreads, 0, stream>>>(raw, z, a.norm_w, static_cast<bf16_t *>(a.out), n, a.eps);
+    float *state = a.h_out ? a.h_out : reinterpret_cast<float *>(ws + p.state_at);
+    const bf16_t *z = static_cast<const bf16_t *>(a.z);
+    bf16_t *out = static_cast<bf16_t *>(a.out);
+    for (int64_t first = 0; first < p.chunks; first += p.slab) {
+        const int64_t n = p.slab < p.chunks - first ? p.slab : p.chunks - first, tok0 = first * kC;
+        const bool last = first + n == p.chunks;
+        delta_prepare_kernel<N><<<dim3((unsigned)n, (unsigned)a.H, (unsigned)a.rows), kPrepThreads, 0, stream>>>(
+            static_cast<const bf16_t *>(a.q), static_cast<const bf16_t *>(a.k), static_cast<const bf16_t *>(a.dt), static_cast<const bf16_t *>(a.beta),
+            a.A, a.dt_bias, reinterpret_cast<uint16_t *>(ws), frags, tok0, a.L, a.H, a.H / a.Hk,
+            DeltaOptions{a.scale, a.eps, a.dt_softplus, a.beta_sigmoid, a.qk_norm});
+        if (hipError_t e = hipGetLastError()) return e;
+        const WalkArgs w{static_cast<const bf16_t *>(a.v), z, reinterpret_cast<const uint16_t *>(ws), frags, first == 0 ? a.h_in : state,
+                         last ? a.h_out : state, out, raw, a.L, a.H, a.H / a.Hk, a.rows * a.H, tok0, n, a.P};
+        if (raw) walk<N, kWalkRaw>(a, w, stream);
+        else if (z) walk<N, kWalkGate>(a, w, stream);
+        else walk<N, kWalkPlain>(a, w, stream);
+        if (hipError_t e = hipGetLastError()) return e;
+        if (!raw) continue;
+        const int64_t token = a.H * a.P / 4, tokens = last ? a.L - tok0 : n * kC;
+        const dim3 grid((unsigned)((tokens * token + kThreads - 1) / kThreads), (unsigned)a.rows);
+        const bf16_t *gates = z ? z + tok0 * token * 4 : nullptr;
+        bf16_t *to = out + tok0 * token * 4;
+        if (a.P == 64) delta_norm_kernel<64><<<grid, kThreads, 0, stream>>>(raw, gates, a.norm_w, to, tokens * token, n * kC * token, a.L * token, a.eps);
+        else delta_norm_kernel<128><<<grid, kThreads, 0, stream>>>(raw, gates, a.norm_w, to, tokens * token, n * kC * token, a.L * token, a.eps);
+        if (hipError_t e = hipGetLastError()) return e;
     }
-    return hipGetLastError();
+    return hipSuccess;
 }
 
 }  // namespace
