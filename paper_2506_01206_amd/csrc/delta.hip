@@ -241,17 +241,17 @@ template <int N> __device__ __forceinline__ int state_of(int tile, int row)
 // grid: (chunks of the slab, H, batch); tok_slab: the slab's first token
 constexpr int kPrepThreads = 512;
 template <int N>
-__global__ void __launch_bounds__(kPrepThreads) __attribute__((amdgpu_waves_per_eu(4)))
+__global__ void __launch_bounds__(kPrepThreads) __attribute__((amdgpu_waves_per_eu(6)))
 delta_prepare_kernel(const bf16_t *__restrict__ q, const bf16_t *__restrict__ k, const bf16_t *__restrict__ dt, const bf16_t *__restrict__ beta,
                      const float *__restrict__ A, const float *__restrict__ dt_bias, uint16_t *__restrict__ ws, uint16_t *__restrict__ frags,
                      int64_t tok_slab, int64_t L, int64_t H, int64_t group, DeltaOptions o)
 {
     constexpr int kRow = N + 8, kSys = kC + 4;
-    __shared__ __attribute__((aligned(16))) uint16_t ks[kC * kRow];
-    __shared__ __attribute__((aligned(16))) float sys[kC * kSys], inv[kC * kSys], mq[kC * kSys];   // T, then M X; (I + T)^-1; q, then M
+    // T, then M X; K, then (I + T)^-1; Q, then M: 53 KB, so that three workgroups share a CU
+    __shared__ __attribute__((aligned(16))) float sys[kC * kSys], inv[kC * kSys], mq[kC * kSys];
     __shared__ __attribute__((aligned(16))) float rk[kC], rq[kC], G[kC], bt[kC];
-    uint16_t *qs = reinterpret_cast<uint16_t *>(mq);
-    static_assert(sizeof(uint16_t) * kC * kRow <= sizeof(mq), "q shares its place with M");
+    uint16_t *ks = reinterpret_cast<uint16_t *>(inv), *qs = reinterpret_cast<uint16_t *>(mq);
+    static_assert(sizeof(uint16_t) * kC * kRow <= sizeof(mq), "k and q share their places");
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c16 = lane & 15, g4 = lane >> 4;
     const int64_t chunk = blockIdx.x, n_chunks = gridDim.x, h = blockIdx.y, b = blockIdx.z;
     const int64_t Hk = H / group, hk = h / group, tok0 = tok_slab + chunk * kC;
@@ -338,17 +338,15 @@ delta_prepare_kernel(const bf16_t *__restrict__ q, const bf16_t *__restrict__ k,
     lds_barrier();
 
     f32x4_t m[2];                                                 // wavefronts 1 .. 7: tiles wave - 1 and wave + 6 of M
+    float x[16];                                                  // wavefront 0: a column of a block of (I + T)^-1
     if (wave == 0) {
         // (I + T)^-1: the four 16 x 16 blocks on the diagonal by substitution, a block to 16 lanes and a column to a lane.  A lane has its
         // column of T as well, and hands its entry of a row to the 15 others as the operand of their multiplication.
         const float *d = sys + g4 * 16 * kSys + g4 * 16 + c16;
-        float t[16], x[16];
+        float t[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) t[i] = -d[i * kSys], x[i] = i == c16 ? 1.0f : 0.0f;
         substitute<0>(t, x);
-        float *to = inv + g4 * 16 * kSys + g4 * 16 + c16;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) to[i * kSys] = x[i];
     } else {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
@@ -381,6 +379,18 @@ delta_prepare_kernel(const bf16_t *__restrict__ q, const bf16_t *__restrict__ k,
         }
     }
     lds_barrier();
+    if (wave == 0) {
+        float *to = inv + g4 * 16 * kSys + g4 * 16 + c16;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) to[i * kSys] = x[i];
+    } else {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int i = 7 * j + wave - 1, t_tile = tile_row(i), s_tile = i - t_tile * (t_tile + 1) / 2;
+            if (i < 10) *reinterpret_cast<f32x4_t *>(&mq[(t_tile * 16 + c16) * kSys + s_tile * 16 + 4 * g4]) = m[j];
+        }
+    }
+    lds_barrier();
 
     // ... then what stands below them, X21 = -X22 T21 X11, in float32 on the matrix cores.  The contraction takes the four k of a step from
     // the four lane groups, 4 g + i in step i: so a result is the next product's operand as it lies in the registers.
@@ -404,13 +414,6 @@ delta_prepare_kernel(const bf16_t *__restrict__ q, const bf16_t *__restrict__ k,
     if (wave < 2) {
         const int r = 2 * wave + 1, c = 2 * wave;
         store_block(r, c, times_inverse(r, r, times_block(r, c, c, zero), zero));
-    }
-    if (wave > 0) {
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int i = 7 * j + wave - 1, t_tile = tile_row(i), s_tile = i - t_tile * (t_tile + 1) / 2;
-            if (i < 10) *reinterpret_cast<f32x4_t *>(&mq[(t_tile * 16 + c16) * kSys + s_tile * 16 + 4 * g4]) = m[j];
-        }
     }
     lds_barrier();
     if (wave < 4) {
