@@ -258,15 +258,16 @@ delta_prepare_kernel(const bf16_t *__restrict__ q, const bf16_t *__restrict__ k,
     const int live = (int)min((int64_t)kC, L - tok0);             // tokens of this chunk
     ws += ((b * H + h) * n_chunks + chunk) * kChunkHalves;
 
-    // keys and queries into LDS, and one over their lengths (rows behind the end: zeros)
+    // keys and queries into LDS (rows behind the end: zeros)
     constexpr int kPieces = N / 8, kMine = kC * kPieces / kPrepThreads;   // 16-byte pieces of a row, on as many adjacent lanes
     uint4 kp[kMine], qp[kMine];
+    const int64_t first = ((b * L + tok0) * Hk + hk) * N;
 #pragma unroll
     for (int i = 0; i < kMine; ++i) {
         const int id = i * kPrepThreads + tid, row = id / kPieces, piece = id % kPieces;
-        const int64_t at = ((b * L + tok0 + min(row, live - 1)) * Hk + hk) * N + piece * 8;
-        kp[i] = *reinterpret_cast<const uint4 *>(k + at);
-        qp[i] = *reinterpret_cast<const uint4 *>(q + at);
+        const uint32_t at = (uint32_t)min(row, live - 1) * (uint32_t)(Hk * N) + (uint32_t)(piece * 8);
+        kp[i] = *reinterpret_cast<const uint4 *>(k + first + at);
+        qp[i] = *reinterpret_cast<const uint4 *>(q + first + at);
     }
     // running sum of delta A (in powers of two) and the write strengths; tokens behind the end neither decay nor write
     if (wave == 7) {
@@ -288,22 +289,25 @@ delta_prepare_kernel(const bf16_t *__restrict__ q, const bf16_t *__restrict__ k,
     for (int i = 0; i < kMine; ++i) {
         const int id = i * kPrepThreads + tid, row = id / kPieces, piece = id % kPieces;
         if (row >= live) kp[i] = qp[i] = make_uint4(0, 0, 0, 0);
-        float sk = 0.0f, sq = 0.0f;
-        const uint32_t kw[4] = {kp[i].x, kp[i].y, kp[i].z, kp[i].w}, qw[4] = {qp[i].x, qp[i].y, qp[i].z, qp[i].w};
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            sk = fmaf(bf16_lo(kw[w]), bf16_lo(kw[w]), fmaf(bf16_hi(kw[w]), bf16_hi(kw[w]), sk));
-            sq = fmaf(bf16_lo(qw[w]), bf16_lo(qw[w]), fmaf(bf16_hi(qw[w]), bf16_hi(qw[w]), sq));
-        }
-        sk = lane_add<0x141>(lane_add<0x4e>(lane_add<0xb1>(sk)));        // 8 lanes
-        sq = lane_add<0x141>(lane_add<0x4e>(lane_add<0xb1>(sq)));
-        if constexpr (kPieces == 16) sk = lane_add<0x140>(sk), sq = lane_add<0x140>(sq);
         *reinterpret_cast<uint4 *>(&ks[row * kRow + piece * 8]) = kp[i];
         *reinterpret_cast<uint4 *>(&qs[row * kRow + piece * 8]) = qp[i];
-        if (piece == 0) {
-            rk[row] = row >= live ? 0.0f : o.qk_norm ? 1.0f / sqrtf(sk + o.eps) : 1.0f;
-            rq[row] = row >= live ? 0.0f : (o.qk_norm ? 1.0f / sqrtf(sq + o.eps) : 1.0f) * o.scale;
+    }
+    lds_barrier();
+    // one over the lengths of keys (wavefronts 0 .. 3) and queries: the diagonal of a tile of K K^T or Q Q^T
+    {
+        const int t_tile = wave & 3, t = t_tile * 16 + c16;
+        const uint16_t *rows = wave < 4 ? ks : qs;
+        f32x4_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (o.qk_norm) {
+#pragma unroll
+            for (int i = 0; i < N / 32; ++i) {
+                const bf16x8 f = lds_frag(&rows[t * kRow + i * 32 + g4 * 8]);
+                acc = mma(f, f, acc);
+            }
         }
+        const float square = (c16 & 2) ? (c16 & 1) ? acc[3] : acc[2] : (c16 & 1) ? acc[1] : acc[0];
+        const float inverse = t >= live ? 0.0f : o.qk_norm ? 1.0f / sqrtf(square + o.eps) : 1.0f;
+        if (g4 == c16 >> 2) (wave < 4 ? rk : rq)[t] = wave < 4 ? inverse : inverse * o.scale;
     }
     lds_barrier();
 
