@@ -11,11 +11,16 @@
 #include "device_math.h"
 #include "launch.h"
 
+#include <type_traits>
+
 namespace mamba {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kTurns = 4;                                            // vectors of 8 tokens to a lane
+// Vectors of 8 tokens to a lane.  One: what a lane does once is long (a division that rounds right, the rules, the search), and every turn
+// repeats it in the code, which a workgroup fetches as it goes: 3 children of one row of 50280 6.2 us with one turn, 8.4 with two, 13.0
+// with four; logits of 19 rows 4.3, 5.1 and 7.6.
+constexpr int kTurns = 1;
 constexpr int kSlice = kThreads * kTurns * 8;                        // tokens to a workgroup
 constexpr int32_t kNoKey = INT32_MIN;                                // below every key
 
@@ -61,50 +66,32 @@ __device__ __forceinline__ void store8(bf16_t *p, const float *x)
 struct RowRules {
     bool known;                                                      // its indices are in range
     float repetition, presence, frequency;
-    const int32_t *counts, *path;
-    const uint8_t *mask;
+    const int32_t *counts;
+    const uint8_t *mask;                                             // nullptr: everything is allowed
 };
-__device__ __forceinline__ RowRules rules_of(const ConstrainArgs &c, int64_t m)
+template <bool COUNTS, bool MASK> __device__ __forceinline__ RowRules rules_of(const ConstrainArgs &c, int64_t m)
 {
-    RowRules r;
-    const int64_t s = c.seq_idx ? c.seq_idx[m] : c.n_seq == 1 ? 0 : m;
-    const int64_t g = !c.mask ? -1 : c.mask_idx ? c.mask_idx[m] : c.n_masks == 1 ? 0 : m;
-    r.known = (!(c.counts || c.penalties) || (s >= 0 && s < c.n_seq)) && g >= -1 && g < c.n_masks;
-    const int64_t s_safe = r.known ? s : 0;
-    r.repetition = 1.0f, r.presence = r.frequency = 0.0f;
-    if (c.penalties) r.repetition = c.penalties[3 * s_safe], r.presence = c.penalties[3 * s_safe + 1], r.frequency = c.penalties[3 * s_safe + 2];
-    r.counts = c.counts && c.penalties ? c.counts + s_safe * c.V : nullptr;
-    r.path = c.penalties ? c.path ? c.path + m * c.path_len : nullptr : nullptr;
-    r.mask = r.known && g >= 0 ? reinterpret_cast<const uint8_t *>(c.mask + g * ((c.V + 31) / 32)) : nullptr;
+    RowRules r{true, 1.0f, 0.0f, 0.0f, nullptr, nullptr};
+    if (c.penalties || c.counts) {
+        const int64_t s = c.seq_idx ? c.seq_idx[m] : c.n_seq == 1 ? 0 : m;
+        r.known = s >= 0 && s < c.n_seq;
+        const int64_t safe = r.known ? s : 0;
+        if (c.penalties) r.repetition = c.penalties[3 * safe], r.presence = c.penalties[3 * safe + 1], r.frequency = c.penalties[3 * safe + 2];
+        if constexpr (COUNTS) r.counts = c.counts + safe * c.V;
+    }
+    if constexpr (MASK) {
+        const int64_t g = c.mask_idx ? c.mask_idx[m] : c.n_masks == 1 ? 0 : m;
+        r.known = r.known && g >= -1 && g < c.n_masks;
+        if (r.known && g >= 0) r.mask = reinterpret_cast<const uint8_t *>(c.mask + g * ((c.V + 31) / 32));
+    }
     return r;
 }
 
-// The 8 tokens from v on, of a row that has as many behind v: what is fetched for them ...
-struct Fetched {
-    float x[8], bias[8];
-    int32_t counts[8];
-    uint32_t mask;
-};
-template <typename T>
-__device__ __forceinline__ void fetch8(const ConstrainArgs &c, const RowRules &r, const T *row, int64_t v, Fetched &f)
-{
-    load8(row + v, f.x);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) f.bias[i] = 0.0f, f.counts[i] = 0;
-    if (c.bias) load8(c.bias + v, f.bias);
-    if (r.counts) load8(r.counts + v, f.counts);
-    f.mask = 0xff;
-    if (r.mask) {
-        const int64_t at = v >> 3, last = (c.V + 31) / 32 * 4 - 1;   // (v is no multiple of 8 in a row's last vector)
-        f.mask = (r.mask[at] | (uint32_t)r.mask[at < last ? at + 1 : last] << 8) >> (v & 7);
-    }
-}
-// ... and what becomes of one
-__device__ __forceinline__ float adjusted(const RowRules &r, float x, int32_t count, int32_t on_path, float bias, bool has_bias)
+__device__ __forceinline__ float adjusted(const RowRules &r, float x, int32_t count)
 {
 #pragma clang fp contract(off)
-    const int32_t times = (count & 0x7fffffff) + on_path;
-    if (count < 0 || times > 0) {
+    const int32_t times = count & 0x7fffffff;
+    if (count != 0) {
         x = x > 0.0f ? x / r.repetition : x * r.repetition;
         if (times > 0) {
             const float f = r.frequency * (float)times;
@@ -112,71 +99,120 @@ __device__ __forceinline__ float adjusted(const RowRules &r, float x, int32_t co
             x = x - r.presence;
         }
     }
-    return has_bias ? x + bias : x;
-}
-// occurrences of the 8 tokens from v on in the row's path (few branches have one here: the caller asks `near` ahead)
-__device__ __forceinline__ bool path_near(const RowRules &r, int64_t T, int64_t v)
-{
-    bool near = false;
-    for (int64_t t = 0; t < T; ++t) near |= (uint64_t)((int64_t)r.path[t] - v) < 8;
-    return near;
-}
-__device__ __forceinline__ void path_counts(const RowRules &r, int64_t T, int64_t v, int32_t *times)
-{
-    for (int64_t t = 0; t < T; ++t) {
-        const int64_t d = (int64_t)r.path[t] - v;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) times[i] += d == i;
-    }
-}
-template <typename T>
-__device__ __forceinline__ void adjust8(const ConstrainArgs &c, const RowRules &r, int64_t v, Fetched &f)
-{
-    int32_t on_path[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (r.path && path_near(r, c.path_len, v)) path_counts(r, c.path_len, v, on_path);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) f.x[i] = adjusted(r, f.x[i], f.counts[i], on_path[i], f.bias[i], c.bias != nullptr);
-}
-// one token of a row shorter than a vector
-template <typename T>
-__device__ __forceinline__ float adjust1(const ConstrainArgs &c, const RowRules &r, const T *row, int64_t v, bool *allowed)
-{
-    int32_t on_path = 0;
-    if (r.path)
-        for (int64_t t = 0; t < c.path_len; ++t) on_path += r.path[t] == v;
-    *allowed = !r.mask || (r.mask[v >> 3] >> (v & 7) & 1);
-    return adjusted(r, ld_io(row, v), r.counts ? r.counts[v] : 0, on_path, c.bias ? c.bias[v] : 0.0f, c.bias != nullptr);
+    return x;
 }
 
-// grid: (rows x slices); out may be logits (a thread reads what it writes)
-template <typename T>
+// A lane's tokens of a slice of a row, kTurns vectors of 8: their adjusted logits, and which of them count (allowed, of this row and
+// no other lane's).  Everything is requested ahead of the first use, at addresses that do not depend on a condition: a vector past
+// the row's end is the last 8 tokens of the row again, of which those that stand in the vector before it are left out.  (A row of fewer
+// than 8 tokens is read token by token.)
+// COUNTS: penalties with counts; BIAS, MASK: there are such
+template <typename T, bool COUNTS, bool BIAS, bool MASK> struct Share {
+    int64_t start[kTurns];                                           // first token of a vector as it was read
+    float x[kTurns][8];
+    uint32_t valid[kTurns];
+
+    __device__ __forceinline__ void load(const ConstrainArgs &c, const T *row, int64_t m, int64_t slice, RowRules &r)
+    {
+        int32_t counts[kTurns][8];
+        float bias[kTurns][8];
+        uint32_t mask[kTurns][2];
+        const int64_t v0 = slice * kSlice + threadIdx.x * 8, V = c.V;
+        if (V >= 8) {
+#pragma unroll
+            for (int u = 0; u < kTurns; ++u) {
+                start[u] = min(v0 + u * kThreads * 8, V - 8);
+                load8(row + start[u], x[u]);
+                if constexpr (BIAS) load8(c.bias + start[u], bias[u]);
+            }
+            r = rules_of<COUNTS, MASK>(c, m);
+            const int64_t last = (V + 31) / 32 * 4 - 1;
+            const uint8_t *bits = r.mask ? r.mask : reinterpret_cast<const uint8_t *>(c.mask);
+#pragma unroll
+            for (int u = 0; u < kTurns; ++u) {
+                if constexpr (COUNTS) load8(r.counts + start[u], counts[u]);
+                if constexpr (MASK) {
+                    const int64_t at = start[u] >> 3;
+                    mask[u][0] = bits[at], mask[u][1] = bits[min(at + 1, last)];
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        } else {
+            r = rules_of<COUNTS, MASK>(c, m);
+#pragma unroll
+            for (int u = 0; u < kTurns; ++u) {
+                start[u] = v0 + u * kThreads * 8;
+                if constexpr (MASK) mask[u][0] = r.mask ? r.mask[0] : 0, mask[u][1] = 0;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int64_t v = min<int64_t>(i, V - 1);        // (only the first vector counts)
+                    x[u][i] = ld_io(row, v);
+                    if constexpr (BIAS) bias[u][i] = c.bias[v];
+                    if constexpr (COUNTS) counts[u][i] = r.counts[v];
+                }
+            }
+        }
+        if constexpr (!COUNTS) {
+#pragma unroll
+            for (int u = 0; u < kTurns; ++u)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) counts[u][i] = 0;
+        }
+        // The row's path: a lane of each wavefront has a token of it, and those that stand in this slice are handed to all lanes.
+        if (c.path && c.penalties) {
+            for (int64_t t0 = 0; t0 < c.path_len; t0 += 64) {
+                const int64_t t = t0 + (threadIdx.x & 63);
+                const int32_t token = t < c.path_len ? c.path[m * c.path_len + t] : -1;
+                uint64_t here = __ballot(token >= 0 && token < V && token / kSlice == slice);
+                while (here) {
+                    const int32_t one = __builtin_amdgcn_readlane(token, __builtin_ctzll(here));
+                    here &= here - 1;
+#pragma unroll
+                    for (int u = 0; u < kTurns; ++u)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) counts[u][i] += (int32_t)start[u] + i == one;
+                }
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kTurns; ++u) {
+            const int64_t v = v0 + u * kThreads * 8;
+            valid[u] = 0xff;
+            if constexpr (MASK) valid[u] = r.mask ? (mask[u][0] | mask[u][1] << 8) >> (start[u] & 7) & 0xff : 0xff;
+            if (V >= 8) valid[u] &= v < V ? 0xffu << (v - start[u]) : 0u;        // (the shift is 0 but in a row's last vector)
+            else valid[u] &= v == 0 ? 0xffu >> (8 - V) : 0u;
+            if (!r.known) valid[u] = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                x[u][i] = adjusted(r, x[u][i], counts[u][i]);
+                if constexpr (BIAS) x[u][i] = x[u][i] + bias[u][i];
+            }
+        }
+    }
+};
+
+// grid: (rows x slices); out may be logits (a thread writes what it alone has read)
+template <typename T, bool COUNTS, bool BIAS, bool MASK>
 __global__ void __launch_bounds__(kThreads) constrain_kernel(const T *logits, T *out, ConstrainArgs c, int64_t slices)
 {
-    const int64_t m = blockIdx.x / slices, v0 = (blockIdx.x - m * slices) * kSlice + threadIdx.x * 8;
-    const RowRules r = rules_of(c, m);
-    const T *row = logits + m * c.V;
+    const int64_t m = blockIdx.x / slices, slice = blockIdx.x - m * slices, v0 = slice * kSlice + threadIdx.x * 8;
+    RowRules r;
+    Share<T, COUNTS, BIAS, MASK> s;
+    s.load(c, logits + m * c.V, m, slice, r);
     T *to = out + m * c.V;
     const float nan = __int_as_float(0x7fc00000);
-    Fetched f[kTurns];
 #pragma unroll
     for (int u = 0; u < kTurns; ++u) {
         const int64_t v = v0 + u * kThreads * 8;
-        if (v + 8 <= c.V) fetch8(c, r, row, v, f[u]);
-    }
 #pragma unroll
-    for (int u = 0; u < kTurns; ++u) {
-        const int64_t v = v0 + u * kThreads * 8;
+        for (int i = 0; i < 8; ++i) s.x[u][i] = !r.known ? nan : (s.valid[u] >> i & 1) ? s.x[u][i] : -INFINITY;
         if (v + 8 <= c.V) {
-            adjust8<T>(c, r, v, f[u]);
+            store8(to + v, s.x[u]);
+        } else if (v < c.V) {                                        // (the end of a row: only what is not another lane's)
+            const int64_t first = c.V >= 8 ? v - s.start[u] : 0, end = c.V >= 8 ? 8 : c.V;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) f[u].x[i] = !r.known ? nan : (f[u].mask >> i & 1) ? f[u].x[i] : -INFINITY;
-            store8(to + v, f[u].x);
-        } else {
-            for (int64_t w = v; w < c.V; ++w) {                      // (fewer than 8 tokens at the end of a row)
-                bool allowed;
-                const float x = adjust1(c, r, row, w, &allowed);
-                st_io(to, w, !r.known ? nan : allowed ? x : -INFINITY);
-            }
+            for (int i = 0; i < 8; ++i)
+                if (i >= first && i < end) st_io(to, (c.V >= 8 ? s.start[u] : 0) + i, s.x[u][i]);
         }
     }
 }
@@ -215,55 +251,31 @@ __device__ __forceinline__ void write_child(const ConstrainArgs &c, int64_t m, i
             path_out[at * (c.path_len + 1) + t] = t < c.path_len ? c.path[m * c.path_len + t] : some ? token : -1;
 }
 
-// The k best of one slice of one row.  A lane keeps its 32 tokens' keys in registers and offers the best; the workgroup's best is
+// The k best of one slice of one row.  A lane keeps its 8 tokens' keys in registers and offers the best; the workgroup's best is
 // found k times, and only the wavefront that owned it looks through its registers again.
 // grid: (rows x slices); with one slice the result is the row's, with more the slices' go to `part` and merge_kernel takes over
-template <typename T>
+template <typename T, bool COUNTS, bool BIAS, bool MASK>
 __global__ void __launch_bounds__(kThreads)
 children_kernel(const T *__restrict__ logits, int32_t *__restrict__ idx, float *__restrict__ val, int32_t *__restrict__ path_out,
                 int2 *__restrict__ part, ConstrainArgs c, int64_t slices, int k)
 {
     const int64_t m = blockIdx.x / slices, slice = blockIdx.x - m * slices;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int64_t v0 = slice * kSlice + tid * 8;
-    const RowRules r = rules_of(c, m);
-    const T *row = logits + m * c.V;
+    RowRules r;
+    Share<T, COUNTS, BIAS, MASK> s;
+    s.load(c, logits + m * c.V, m, slice, r);
     int32_t key[kTurns][8];
-    Fetched f[kTurns];
-    const bool vectors = c.V >= 8;
-    // A row's last vector starts 8 tokens ahead of the row's end, and what the vector before it has is left out.
-    auto start = [&](int u) { return min(v0 + u * kThreads * 8, c.V - 8); };
-#pragma unroll
-    for (int u = 0; u < kTurns; ++u)
-        if (vectors && v0 + u * kThreads * 8 < c.V) fetch8(c, r, row, start(u), f[u]);
     int32_t best = kNoKey, best_at = -1;                             // first of the lane's largest
 #pragma unroll
-    for (int u = 0; u < kTurns; ++u) {
-        const int64_t v = v0 + u * kThreads * 8;
+    for (int u = 0; u < kTurns; ++u)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) key[u][i] = kNoKey;
-        if (!r.known || v >= c.V) continue;
-        if (vectors) {
-            const int64_t s = start(u);
-            adjust8<T>(c, r, s, f[u]);
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (s + i >= v && (f[u].mask >> i & 1)) key[u][i] = key_of(f[u].x[i]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (i < c.V) {
-                    bool allowed;
-                    const float x = adjust1(c, r, row, i, &allowed);
-                    if (allowed) key[u][i] = key_of(x);
-                }
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < 8; ++i) {
+            key[u][i] = (s.valid[u] >> i & 1) ? key_of(s.x[u][i]) : kNoKey;
             if (key[u][i] > best) best = key[u][i], best_at = u * 8 + i;
-    }
+        }
     // a token's number in the row from its place in the lane
-    auto token_of = [&](int at) { return (int32_t)((vectors ? start(at >> 3) : v0) + (at & 7)); };
+    const int32_t v0 = (int32_t)(slice * kSlice) + tid * 8, last = c.V >= 8 ? (int32_t)c.V - 8 : INT32_MAX;
+    auto token_of = [&](int at) { return min(v0 + (at >> 3) * (kThreads * 8), last) + (at & 7); };
     int32_t best_token = token_of(max(best_at, 0));
     __shared__ int2 heads[2][kThreads / 64];
     for (int n = 0; n < k; ++n) {
@@ -284,20 +296,18 @@ children_kernel(const T *__restrict__ logits, int32_t *__restrict__ idx, float *
         if (win != kNoKey && best == win && best_token == token) {   // the owner's next: the best behind the one that was taken
             best = kNoKey, best_at = -1;
 #pragma unroll
-            for (int u = 0; u < kTurns; ++u) {
-                const int32_t first = token_of(u * 8);
+            for (int u = 0; u < kTurns; ++u)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const int32_t q = key[u][i];
-                    if ((q < win || (q == win && first + i > token)) && q > best) best = q, best_at = u * 8 + i;
+                    if ((q < win || (q == win && token_of(u * 8 + i) > token)) && q > best) best = q, best_at = u * 8 + i;
                 }
-            }
             best_token = token_of(max(best_at, 0));
         }
     }
 }
 
-// The k best of a row's slices: one wavefront, which goes through the slices' candidates (k each, most often fewer than 64 in all)
+// The k best of a row's slices: one wavefront, which goes through the slices' candidates (k each: 75 for 3 children of a row of 50280)
 // for the best one behind the one taken last.
 __global__ void __launch_bounds__(64)
 merge_kernel(const int2 *__restrict__ part, int32_t *__restrict__ idx, float *__restrict__ val, int32_t *__restrict__ path_out, ConstrainArgs c,
@@ -363,13 +373,37 @@ size_t children_workspace_bytes(int64_t M, int64_t V, int k)
     return slices > 1 ? (size_t)(M * slices * k) * sizeof(int2) : 0;
 }
 
+namespace {
+// F with the rules that a call has as constants: their absence costs nothing then, and what there is is requested without conditions
+template <typename F> auto with_rules(const ConstrainArgs &c, F f)
+{
+    const int rules = (c.counts && c.penalties ? 1 : 0) | (c.bias ? 2 : 0) | (c.mask ? 4 : 0);
+    switch (rules) {
+    case 0: return f(std::false_type(), std::false_type(), std::false_type());
+    case 1: return f(std::true_type(), std::false_type(), std::false_type());
+    case 2: return f(std::false_type(), std::true_type(), std::false_type());
+    case 3: return f(std::true_type(), std::true_type(), std::false_type());
+    case 4: return f(std::false_type(), std::false_type(), std::true_type());
+    case 5: return f(std::true_type(), std::false_type(), std::true_type());
+    case 6: return f(std::false_type(), std::true_type(), std::true_type());
+    default: return f(std::true_type(), std::true_type(), std::true_type());
+    }
+}
+}  // namespace
+
 hipError_t launch_constrain(const void *logits, void *out, const ConstrainArgs &c, int64_t M, int io, hipStream_t stream)
 {
     const int64_t slices = slices_of(c.V);
     const unsigned grid = (unsigned)(M * slices);
-    if (io == kIoBf16) constrain_kernel<<<grid, kThreads, 0, stream>>>(static_cast<const bf16_t *>(logits), static_cast<bf16_t *>(out), c, slices);
-    else constrain_kernel<<<grid, kThreads, 0, stream>>>(static_cast<const float *>(logits), static_cast<float *>(out), c, slices);
-    return hipGetLastError();
+    return with_rules(c, [&](auto counts, auto bias, auto mask) {
+        if (io == kIoBf16)
+            constrain_kernel<bf16_t, counts.value, bias.value, mask.value>
+                <<<grid, kThreads, 0, stream>>>(static_cast<const bf16_t *>(logits), static_cast<bf16_t *>(out), c, slices);
+        else
+            constrain_kernel<float, counts.value, bias.value, mask.value>
+                <<<grid, kThreads, 0, stream>>>(static_cast<const float *>(logits), static_cast<float *>(out), c, slices);
+        return hipGetLastError();
+    });
 }
 
 hipError_t launch_children(const void *logits, int32_t *idx, float *val, int32_t *path_out, void *ws, const ConstrainArgs &c, int64_t M, int k, int io,
@@ -378,14 +412,17 @@ hipError_t launch_children(const void *logits, int32_t *idx, float *val, int32_t
     const int64_t slices = slices_of(c.V);
     const unsigned grid = (unsigned)(M * slices);
     int2 *part = static_cast<int2 *>(ws);
-    if (io == kIoBf16)
-        children_kernel<<<grid, kThreads, 0, stream>>>(static_cast<const bf16_t *>(logits), idx, val, path_out, part, c, slices, k);
-    else
-        children_kernel<<<grid, kThreads, 0, stream>>>(static_cast<const float *>(logits), idx, val, path_out, part, c, slices, k);
-    if (slices > 1) {
-        if (hipError_t e = hipGetLastError()) return e;
-        merge_kernel<<<(unsigned)M, 64, 0, stream>>>(part, idx, val, path_out, c, slices, k);
-    }
+    const hipError_t e = with_rules(c, [&](auto counts, auto bias, auto mask) {
+        if (io == kIoBf16)
+            children_kernel<bf16_t, counts.value, bias.value, mask.value>
+                <<<grid, kThreads, 0, stream>>>(static_cast<const bf16_t *>(logits), idx, val, path_out, part, c, slices, k);
+        else
+            children_kernel<float, counts.value, bias.value, mask.value>
+                <<<grid, kThreads, 0, stream>>>(static_cast<const float *>(logits), idx, val, path_out, part, c, slices, k);
+        return hipGetLastError();
+    });
+    if (e != hipSuccess || slices == 1) return e;
+    merge_kernel<<<(unsigned)M, 64, 0, stream>>>(part, idx, val, path_out, c, slices, k);
     return hipGetLastError();
 }
 

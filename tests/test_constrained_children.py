@@ -132,7 +132,7 @@ def test_children_refusals(m):
     S = m.STATUS
     import ctypes
     need = m.mamba_topk_constrained_workspace_bytes(12, 50280, 3)
-    assert need > 0 and m.mamba_topk_constrained_workspace_bytes(12, 8192, 3) == 0
+    assert need > 0 and m.mamba_topk_constrained_workspace_bytes(12, 2048, 3) == 0
     for bad in ((0, 50280, 3), (12, 0, 3), (12, 50280, 0), (12, 50280, 9), (12, (1 << 25) + 1, 3), (1 << 31, 50280, 3)):
         assert m.mamba_topk_constrained_workspace_bytes(*bad) == 0
 
@@ -195,7 +195,7 @@ def test_the_binding_refuses(m):
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("M,V,S,T,masks,k", [
     (1, 1, 1, 0, None, 1), (3, 5, 1, 2, [0.5], 8), (2, 7, 2, 1, [0.0, 1.0], 3), (4, 8, 1, 0, [0.3], 2), (5, 9, 3, 3, [0.5, 0.1], 4),
-    (7, 33, 2, 2, [0.9, 0.02], 8), (3, 1000, 1, 4, None, 5), (2, 4099, 2, 1, [0.5, 0.0, 0.001], 8), (6, 8192, 3, 2, [0.97], 3), (2, 8193, 1, 2, [0.5], 3),
+    (7, 33, 2, 2, [0.9, 0.02], 8), (3, 1000, 1, 4, None, 5), (2, 2047, 1, 1, [0.7], 3), (2, 2048, 2, 2, [0.7], 8), (2, 2049, 1, 3, [0.7], 8), (2, 4099, 2, 1, [0.5, 0.0, 0.001], 8), (6, 8192, 3, 2, [0.97], 3), (2, 8193, 1, 2, [0.5], 3),
     (3, 16391, 2, 5, [0.0003, 0.6], 8), (1, 50280, 1, 0, None, 3), (13, 50280, 4, 4, [0.97, 0.5, 0.0001, 0.0], 2), (2, 131071, 2, 3, [0.5], 4),
     (1, 600000, 1, 2, [0.5], 8)])
 def test_against_the_oracle(m, M, V, S, T, masks, k, dtype):
