@@ -418,13 +418,13 @@ int mamba2_state_step(float *h_out, const float *h_in, const int32_t *parent_idx
  * as the scalar-decay layer has them (mamba_state_fork copies them with D = H * P).  N and P each 64 or 128; H a multiple of Hk.
  *
  * mamba_gated_delta_fwd encodes a sequence, bf16 or float32 I/O.  workspace: device scratch of
- * mamba_gated_delta_workspace_bytes(batch, L, H, Hk, P, N) bytes (0 for an unsupported shape), caller-owned; nothing in it has to be
- * kept or cleared between calls.  h_final may be h0 (any other overlap of the two is an error).
+ * mamba_gated_delta_workspace_bytes(batch, L, H, Hk, P, N) bytes (0 for an unsupported shape, and where none is needed: a few tokens),
+ * caller-owned; nothing in it has to be kept or cleared between calls; float32 needs none.  h_final may be h0 (any other overlap of the two is an error).
  * mamba_gated_delta_step advances n_out draft branches by one token (q, k (n_out, Hk, N); v, z, out (n_out, H, P); dt, beta
  * (n_out, H); h_in (n_in, H, P, N), h_out (n_out, H, P, N)); branch j continues from h_in[parent_idx[j]] (device int32[n_out]; NULL:
  * h_in[j], n_in == n_out, and then h_out may be h_in); an index outside [0, n_in) reads nothing and gives NaN for that branch.
  * A NaN or an infinity in the inputs of a token reaches the state from there on, as the equations have it, and may reach the outputs
- * of up to 63 tokens ahead of it.  batch, H, n_out <= 65535; batch * H <= 2^27; L <= 2^31.
+ * of up to 63 tokens ahead of it.  batch, H, n_out <= 65535; batch * H <= 2^19; L <= 2^31.
  */
 size_t mamba_gated_delta_workspace_bytes(int64_t batch, int64_t L, int64_t H, int64_t Hk, int64_t P, int64_t N);
 int mamba_gated_delta_fwd(const void *q, const void *k, const void *v, const void *dt, const float *A, const void *beta,

@@ -497,7 +497,7 @@ def mamba_gated_delta_fwd(q, k, v, dt, A, beta, z=None, norm_w=None, dt_bias=Non
                           scale=None, eps=1e-6, want_state=True, dt_softplus=True, beta_sigmoid=True, qk_norm=True, stream=None):
     """Gated-delta layer core over a sequence: q, k (B,L,Hk,N), v, z (B,L,H,P), dt, beta (B,L,H) bf16|f32; A, dt_bias (H), norm_w (P)
     f32; h0 (B,H,P,N) f32 -> out (B,L,H,P), h_final (B,H,P,N).  scale defaults to N ** -0.5."""
-    if stream is not None and workspace is None:
+    if stream is not None and workspace is None and v.dtype == torch.bfloat16:
         need = mamba_gated_delta_workspace_bytes(*v.shape[:3], q.shape[2], v.shape[3], q.shape[3])
         if need > 0:
             workspace = _scratch(need, v.device, stream)

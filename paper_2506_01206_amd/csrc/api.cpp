@@ -887,7 +887,7 @@ bool delta_shape_ok(int64_t H, int64_t Hk, int64_t P, int64_t N)
 {
     return (P == 64 || P == 128) && (N == 64 || N == 128) && (H == 0 || (Hk > 0 && H % Hk == 0));
 }
-constexpr int64_t kMaxDeltaHeads = (int64_t)1 << 27;                 // batch x H: eight workgroups to a head in one grid dimension
+constexpr int64_t kMaxDeltaHeads = (int64_t)1 << 19;                 // batch x H: 8 workgroups of 512 threads a head, below 2^32 threads
 struct DeltaBytes {
     int64_t key, value, head, state_in, state_out;   // a q or k, a v or out, a dt or beta tensor; the states
 };
@@ -945,7 +945,7 @@ int mamba_gated_delta_fwd(const void *q, const void *k, const void *v, const voi
     const DeltaArgs a{h_final, h0, nullptr, q, k, v, dt, beta, z, A, norm_w, dt_bias, out, static_cast<float *>(workspace),
                       batch, batch, L, H, Hk, (int)P, (int)N, (int)io, scale, eps, dt_softplus, beta_sigmoid, qk_norm};
     if (const int st = delta_pointers(a, b)) return st;
-    const size_t need = gated_delta_workspace_bytes(batch, L, H, Hk, P, N);
+    const size_t need = io == MAMBA_BF16 ? gated_delta_workspace_bytes(batch, L, H, Hk, P, N) : 0;
     if (need > 0) {
         if (!workspace || workspace_bytes < need) return MAMBA_ERR_WORKSPACE;
         const struct { const void *p; int64_t n; } all[] = {{q, b.key}, {k, b.key}, {v, b.value}, {z, b.value}, {dt, b.head}, {beta, b.head},

@@ -37,12 +37,26 @@ __device__ __forceinline__ void load4(const bf16_t *p, float *v)
     v[0] = bf16_lo(f.x), v[1] = bf16_hi(f.x), v[2] = bf16_lo(f.y), v[3] = bf16_hi(f.y);
 }
 
+// Four values as they lie in memory.
+template <typename T> struct RawOf;
+template <> struct RawOf<float> { typedef float4 type; };
+template <> struct RawOf<bf16_t> { typedef uint2 type; };
+template <typename T> using Raw4 = typename RawOf<T>::type;
+template <typename T> __device__ __forceinline__ Raw4<T> raw4(const T *p) { return *reinterpret_cast<const Raw4<T> *>(p); }
+__device__ __forceinline__ void unpack4(float4 w, float *v) { v[0] = w.x, v[1] = w.y, v[2] = w.z, v[3] = w.w; }
+__device__ __forceinline__ void unpack4(uint2 w, float *v)
+{
+    v[0] = bf16_lo(w.x), v[1] = bf16_hi(w.x), v[2] = bf16_lo(w.y), v[3] = bf16_hi(w.y);
+}
+
 __device__ __forceinline__ float sigmoid_f32(float v) { return rcp_hw(1.0f + exp2_hw(-v * kLog2e)); }
 
 // ---------------------------------------------------------------------------------------------------
 // Token after token as the equations stand: one workgroup has a head of one row, its state in registers (16 lanes to a row of S,
 // P / 16 rows to a thread).  For single tokens this is all there is to do: a state is read and written once, both dot products
 // of a row with it come out of one reduction, and the head's P outputs are together for the norm.
+// A new state is written past the caches (nobody reads it in this launch), but an old one is read through them: children of one parent
+// read it one after the other.  128 branches of 64 parents, 32 heads of 128 x 128: 74 us; both past the caches 93, both through them 88.
 // (The states come first and are an aggregate: arguments fetched by the kernel, as in the other steps, see build.py.)
 // grid: (H, rows)
 template <typename T, int N, int P>
@@ -65,7 +79,7 @@ delta_recurrent_kernel(StepStates h, const int32_t *__restrict__ parent, const T
         for (int i = 0; i < R; ++i)
 #pragma unroll
             for (int f = 0; f < F; f += 4) {
-                const f32x4 w = __builtin_nontemporal_load(reinterpret_cast<const f32x4 *>(src + i * N + f * 16));
+                const f32x4 w = *reinterpret_cast<const f32x4 *>(src + i * N + f * 16);
                 S[i][f] = w.x, S[i][f + 1] = w.y, S[i][f + 2] = w.z, S[i][f + 3] = w.w;
             }
     } else {
@@ -75,18 +89,40 @@ delta_recurrent_kernel(StepStates h, const int32_t *__restrict__ parent, const T
             for (int f = 0; f < F; ++f) S[i][f] = 0.0f;
     }
     const float a2 = A[hh] * kLog2e, bias = dt_bias ? dt_bias[hh] : 0.0f;
-    __shared__ float squares[2][kThreads / 64];
-    for (int64_t t = 0; t < L; ++t) {
+    // The 16 lanes of a row group have its R outputs: one each (the rest repeat the last).
+    const int mine = l < R ? l : R - 1;
+    const float weight = norm_w ? norm_w[p0 + mine] : 1.0f;
+    // All that a token brings, as it lies in memory: the next token's is on its way while this one is worked on.
+    struct Token {
+        Raw4<T> k[F / 4], q[F / 4], v[R / 4];
+        T dt, beta, z;
+    };
+    auto fetch = [&](int64_t t) __attribute__((always_inline)) {
+        Token w;
         const int64_t tok = j * L + t;
-        float kv[F], qv[F], vv[R];
 #pragma unroll
-        for (int f = 0; f < F; f += 4) {
-            load4(k + (tok * Hk + hk) * N + f * 16 + 4 * l, kv + f);
-            load4(q + (tok * Hk + hk) * N + f * 16 + 4 * l, qv + f);
+        for (int f = 0; f < F / 4; ++f) {
+            w.k[f] = raw4(k + (tok * Hk + hk) * N + f * 64 + 4 * l);
+            w.q[f] = raw4(q + (tok * Hk + hk) * N + f * 64 + 4 * l);
         }
 #pragma unroll
-        for (int i = 0; i < R; i += 4) load4(v + (tok * H + hh) * P + p0 + i, vv + i);
-        const float x = ld_io(dt, tok * H + hh) + bias, w = ld_io(beta, tok * H + hh);
+        for (int i = 0; i < R / 4; ++i) w.v[i] = raw4(v + (tok * H + hh) * P + p0 + 4 * i);
+        w.dt = dt[tok * H + hh], w.beta = beta[tok * H + hh];
+        w.z = z ? z[(tok * H + hh) * P + p0 + mine] : T{};
+        return w;
+    };
+    __shared__ float squares[2][kThreads / 64];
+    Token next = fetch(0);
+    for (int64_t t = 0; t < L; ++t) {
+        const int64_t tok = j * L + t;
+        const Token c = next;
+        if (t + 1 < L) next = fetch(t + 1);
+        float kv[F], qv[F], vv[R];
+#pragma unroll
+        for (int f = 0; f < F / 4; ++f) unpack4(c.k[f], kv + 4 * f), unpack4(c.q[f], qv + 4 * f);
+#pragma unroll
+        for (int i = 0; i < R / 4; ++i) unpack4(c.v[i], vv + 4 * i);
+        const float x = ld_io(&c.dt, 0) + bias, w = ld_io(&c.beta, 0);
         const float a = exp2_hw((o.softplus ? softplus_f32(x) : x) * a2), b = o.sigmoid ? sigmoid_f32(w) : w;
         float kk = 0.0f, qq = 0.0f, kq = 0.0f, sk[R], sq[R];
 #pragma unroll
@@ -116,17 +152,12 @@ delta_recurrent_kernel(StepStates h, const int32_t *__restrict__ parent, const T
             __syncthreads();                                         // (the next token's go to the other half)
             norm = 1.0f / sqrtf(((squares[t & 1][0] + squares[t & 1][1]) + (squares[t & 1][2] + squares[t & 1][3])) / P + o.eps);
         }
-        // the 16 lanes of a row group have its R outputs: one each
-        float mine = 0.0f;
+        float r = y[0];
 #pragma unroll
-        for (int i = 0; i < R; ++i)
-            if (l == i) mine = y[i];
-        if (l < R) {
-            const int p = p0 + l;
-            if (norm_w) mine *= norm * norm_w[p];
-            if (z) mine *= silu_f32(ld_io(z, (tok * H + hh) * P + p));
-            st_io(out, (tok * H + hh) * P + p, known ? mine : __int_as_float(0x7fc00000));
-        }
+        for (int i = 1; i < R; ++i) r = l == i ? y[i] : r;
+        if (norm_w) r *= norm * weight;
+        if (z) r *= silu_f32(ld_io(&c.z, 0));
+        if (l < R) st_io(out, (tok * H + hh) * P + p0 + l, known ? r : __int_as_float(0x7fc00000));
     }
     if (!h.out) return;
     float *dst = h.out + ((j * H + hh) * P + p0) * N + 4 * l;
@@ -875,7 +906,8 @@ delta_norm_kernel(const float *__restrict__ raw, const bf16_t *__restrict__ z, c
 }
 
 // A long context goes in slabs of chunks, so that what the preparation leaves is still in the last-level cache (256 MB) when the walk takes
-// it, and the workspace does not grow with the context.  (@SLABS@)
+// it, and the workspace does not grow with the context.  32768 tokens of 32 heads of 128 x 128, all launches, by a slab's bytes: 32 MB 1881 us,
+// 64 MB 1520, 128 MB 1333, 256 MB 1502, one slab 1402; 8191 tokens of 8 heads of 64 x 64: 224, 199, 186, 186, 187.
 constexpr int64_t kSlabBytes = (int64_t)128 << 20, kSlabLeast = 8;
 // Where the parts of the workspace lie (bytes from its start): what the preparation leaves of a chunk and value head, fragments of a
 // chunk and key head, outputs ahead of their norm, the states between slabs where the caller takes none.
@@ -948,14 +980,21 @@ hipError_t launch_gated_delta_step(const DeltaArgs &a, hipStream_t stream)
 #undef MAMBA_DELTA
 }
 
+// A context of a few tokens goes token after token, without a workspace: a chunk costs the same whether 1 or 64 of its tokens are there.
+// bf16, with gate and norm, token after token | in a chunk (us): 8 heads of 64 x 64: 6 tokens 8.6 | 12.2, 8: 10.6 | 12.0, 10: 12.7 | 12.1;
+// 32 heads of 128 x 128: 4: 9.8 | 13.1, 6: 13.3 | 13.2, 8: 16.8 | 13.3.  Heads for every CU make a chunk dearer: 256 of 128 x 128: 16 tokens
+// 32.5 | 36.4, 20: 39.2 | 37.0; 512 of 64 x 64: 16: 25.8 | 35.9, 24: 36.4 | 36.1; 2048 of 128 x 128: 16: 147 | 265, 24: 214 | 279.
+static bool few_tokens(int64_t batch, int64_t L, int64_t H) { return L <= (batch * H >= 256 ? 16 : 6); }
+
 size_t gated_delta_workspace_bytes(int64_t batch, int64_t L, int64_t H, int64_t Hk, int64_t P, int64_t N)
 {
+    if (few_tokens(batch, L, H)) return 0;
     return (size_t)delta_plan(batch, L, H, Hk, P, N).bytes;
 }
 
 hipError_t launch_gated_delta(const DeltaArgs &a, hipStream_t stream)
 {
-    if (a.io != kIoBf16) return launch_gated_delta_step(a, stream);
+    if (a.io != kIoBf16 || few_tokens(a.rows, a.L, a.H)) return launch_gated_delta_step(a, stream);
     return a.N == 64 ? chunked<64>(a, stream) : chunked<128>(a, stream);
 }
 

@@ -51,7 +51,7 @@ PyObject *gated_delta_fwd(Args a)
     placed(vt, "v");
     out.unless_given(vt, s, type);
     if (flag(a[13])) h_final.unless_given(vt, {B, H, P, N}, at::kFloat);
-    const Workspace ws(a[12], api.gated_delta_workspace_bytes(B, L, H, Hk, P, N), vt);
+    const Workspace ws(a[12], io == MAMBA_BF16 ? api.gated_delta_workspace_bytes(B, L, H, Hk, P, N) : 0, vt);
     const void *qp = ptr(q, type, {B, L, Hk, N}, "q"), *kp = ptr(a[1], type, {B, L, Hk, N}, "k"), *dtp = ptr(a[3], type, {B, L, H}, "dt");
     const float *A = fptr(a[4], {H}, "A");
     const void *bp = ptr(a[5], type, {B, L, H}, "beta"), *zp = ptr(a[6], type, {B, L, H, P}, "z");

@@ -1,12 +1,12 @@
 """The gated-delta layer core (mamba_gated_delta_fwd, mamba_gated_delta_step): the oracle's own pins, refusals (no GPU needed), and the
 kernels against the oracle.
 
-Tolerances, per element, of max(|reference|, rms of the reference).  States and float32 outputs: 1e-4.  The chunked form carries every
-computed factor of a product as two bfloat16 terms, together off by at most 2^-18 of the factor plus 2^-18 for the left-out product
-of the two remainders, and a term passes through at most four such products inside a chunk of 64 (the inverse, the state, u, the
-state again): 8 * 2^-18 = 3.1e-5 if all of them lean to one side, and float32 sums of 128 terms another 128 * 2^-24 = 8e-6; the state
-forgets what lies more than a chunk or two behind.  bfloat16 outputs: the rounding, half a step = 2^-8, and that: 4.1e-3.  A norm over the
-channels divides by the outputs' own size, which leaves relative errors as they are."""
+Tolerances, per element, of max(|reference|, rms of the reference).  States and float32 outputs: 1e-4.  On the way to the states the
+chunked form carries every computed factor of a product as three bfloat16 terms, exact, and leaves out the three smallest of the nine
+products of two such, 3 * 2^-24 of the whole at most; sums are float32 over 128 terms, 128 * 2^-24 = 8e-6 if every rounding leans to one
+side, and a term passes through four such sums inside a chunk of 64 (the inverse, the state, u, the state again): 3.1e-5, and the state
+forgets what lies more than a chunk or two behind.  bfloat16 outputs take two terms, off by 2^-17: their own rounding, half a step = 2^-8,
+and that: 4.1e-3.  A norm over the channels divides by the outputs' own size, which leaves relative errors as they are."""
 import os
 
 import numpy as np
@@ -143,7 +143,7 @@ def test_fwd_refusals(m):
     for bad in (dict(batch=-1), dict(L=-1), dict(H=-8), dict(Hk=-4), dict(P=-64), dict(N=-128), dict(L=1 << 40, H=1 << 30)):
         assert fwd(m, **bad) == S["BAD_SHAPE"], bad
     for bad in (dict(io=2), dict(io=-1), dict(P=32), dict(P=256), dict(N=16), dict(N=96), dict(Hk=3), dict(Hk=0), dict(Hk=16), dict(batch=70000),
-                dict(H=70000, Hk=1), dict(L=(1 << 31) + 1)):
+                dict(H=70000, Hk=1), dict(batch=1025, H=512), dict(L=(1 << 31) + 1)):
         assert fwd(m, **bad) == S["UNSUPPORTED"], bad
     assert fwd(m, batch=0) == 0 and fwd(m, H=0, Hk=0) == 0 and fwd(m, L=0, hf=None) == 0 and fwd(m, L=0, hf=Pt(9)) == 0
     need = m.mamba_gated_delta_workspace_bytes(1, 100, 8, 4, 64, 128)
@@ -151,6 +151,7 @@ def test_fwd_refusals(m):
         assert fwd(m, ws=None) == S["WORKSPACE"] and fwd(m, ws_bytes=need - 1) == S["WORKSPACE"]
         for name in ("q", "k", "v", "dt", "A", "beta", "z", "nw", "db", "h0", "hf", "out"):
             assert fwd(m, **{name: Pt(12)}) == S["ALIAS"], name                 # over the workspace
+    assert need > 0 and fwd(m, L=0, hf=None, ws=None) == 0
     for bad in ((0, 8, 8, 4, 64, 128), (1, 0, 8, 4, 64, 128), (1, 8, 8, 3, 64, 128), (1, 8, 8, 4, 64, 32), (1, 1 << 50, 1 << 12, 4, 64, 128)):
         assert m.mamba_gated_delta_workspace_bytes(*bad) == 0
 
@@ -258,12 +259,44 @@ def test_fwd_keys_that_lean_to_one_side_and_extreme_decays(m, alike, A, beta):
     c["beta"] = storage(W(c["beta"]) + beta, synth.BF16)
     out, hf = m.mamba_gated_delta_fwd(**device(c))
     ro, rh = oracle_scan(c)
-    # A state that never forgets keeps the error of every token's write, each up to 2^-18 of its size as a factor and 2^-18 as a left-out
-    # product, and keys that are alike make them lean to one side: 200 * 2^-17 = 1.5e-3 of a write (which is no larger than the state's
-    # own elements here), where elsewhere only the last chunk or two count.
-    forgets = A <= -16.0
-    assert_close(values(to_host(out)), ro, TOL_BF16 if forgets else TOL_BF16 + 200 * 2.0 ** -17, "out")
-    assert_close(to_host(hf), rh, TOL_F32 if forgets else 200 * 2.0 ** -17, "final state")
+    assert_close(values(to_host(out)), ro, TOL_BF16, "out")
+    assert_close(to_host(hf), rh, TOL_F32, "final state")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("B,H,L", [(1, 2, 6), (1, 2, 7), (64, 4, 16), (64, 4, 17), (51, 5, 7)])
+def test_fwd_of_a_few_tokens(m, B, H, L):
+    """On both sides of the lengths up to which a context goes token after token."""
+    print("\n[gpu-case] gated delta few tokens B=%d H=%d L=%d" % (B, H, L), flush=True)
+    rng = np.random.default_rng(B + L)
+    c, h0 = case(rng, B, L, H, 1, 64, 64), state(rng, B, H, 64, 64)
+    out, hf = m.mamba_gated_delta_fwd(**device(c), h0=to_dev(h0))
+    ro, rh = oracle_scan(c, h0)
+    assert_close(values(to_host(out)), ro, TOL_BF16, "out")
+    assert_close(to_host(hf), rh, TOL_F32, "final state")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("z,norm", [(True, True), (True, False), (False, False)])
+def test_fwd_of_a_context_in_several_slabs(m, z, norm):
+    """More chunks than one preparation takes at once: the state goes from slab to slab, in the caller's tensor or in the workspace."""
+    print("\n[gpu-case] gated delta slabs z=%s norm=%s" % (z, norm), flush=True)
+    rng = np.random.default_rng(12)
+    B, L, H, Hk, N, P = 8, 17 * 64 + 3, 32, 8, 64, 64
+    assert m.mamba_gated_delta_workspace_bytes(B, 64 * L, H, Hk, P, N) < 2 * m.mamba_gated_delta_workspace_bytes(B, L, H, Hk, P, N)
+    c, h0 = case(rng, B, L, H, Hk, N, P, z=z, norm=norm), state(rng, B, H, P, N)
+    g, h = device(c), to_dev(h0)
+    out, hf = m.mamba_gated_delta_fwd(**g, h0=h)
+    for b, i in ((0, 0), (0, 31), (3, 13), (7, 4), (7, 31)):
+        part = {n: x if x is None or n == "norm_w" else x[i:i + 1] if n in ("A", "dt_bias") else
+                x[b:b + 1, :, i * Hk // H][:, :, None] if n in ("q", "k") else x[b:b + 1, :, i:i + 1] for n, x in c.items()}
+        ro, rh = oracle_scan(part, h0[b:b + 1, i:i + 1])
+        assert_close(values(to_host(out[b:b + 1, :, i:i + 1].contiguous())), ro, TOL_BF16, "out")
+        assert_close(to_host(hf[b:b + 1, i:i + 1].contiguous()), rh, TOL_F32, "final state")
+    o2, none = m.mamba_gated_delta_fwd(**g, h0=h, want_state=False)
+    assert none is None and torch.equal(o2, out)
+    o3, h3 = m.mamba_gated_delta_fwd(**g, h0=h, h_final=h)
+    assert h3 is h and torch.equal(o3, out) and torch.equal(h, hf)
 
 
 @pytest.mark.gpu
