@@ -539,7 +539,9 @@ struct WalkArgs {
     float *h_final;
     bf16_t *out;
     float *raw;
-    int64_t L, H, group, heads, tok0, n_chunks;                   // (of the slab: its first token and its chunks)
+    float *starts, *map;                                          // of parts of the slab
+    int64_t L, H, group, heads, tok0, n_chunks, part;             // (of the slab: its first token and its chunks; chunks of a part)
+    uint32_t first_part, walked, maps;                            // the parts walked for their outputs, and how many of those from 1 on for their maps
     int P;
 };
 constexpr int kWalkPlain = 0, kWalkGate = 1, kWalkRaw = 2;        // outputs as they are, gated, or in float32 for the norm
@@ -557,8 +559,12 @@ template <int N> struct __attribute__((aligned(16))) WalkLds {
 // Where a workgroup and a lane are.
 template <int N> struct WalkPlace {
     int lane, wave, c16, g4, p0;
+    int unit;                                                     // the first of the 16 unit vectors that are the start; -1: none
     int64_t hb, b, h, Hk, hk;
-    const uint16_t *own;                                          // the head's part of the workspace
+    int64_t tok0, first, n_chunks;                                // its part of the slab: first token, chunks ahead of it, chunks
+    const float *h0;                                              // the 16 rows of the state that it has, ahead and behind (or NULL)
+    float *h_final;
+    const uint16_t *own, *frags;                                  // the head's and the key head's parts of the workspace
     uint32_t value_row;                                           // elements of a token
     // where the four adjacent k from 16 tile + 4 g4 of row c16 lie in fragments, and where a lane's eight of fragment i
     __device__ __forceinline__ int in_frags(int tile) const { return (tile >> 1) * kFrag + (c16 + 16 * ((tile & 1) * 2 + (g4 >> 1))) * 8 + 4 * (g4 & 1); }
@@ -584,21 +590,24 @@ template <int N, bool TWO> __device__ __forceinline__ void walk_chain(const Walk
 {
     constexpr int kNT = N / 64, kX = TWO ? 2 : 1;
     const f32x4_t zero = {0.0f, 0.0f, 0.0f, 0.0f};
-    const int n_chunks = (int)a.n_chunks;
+    const int n_chunks = (int)me.n_chunks;
     const uint32_t lane8 = (uint32_t)me.lane * 8;
     // (the state ahead of the operands: what the loop waits for at its head is then never what it has just requested)
     f32x4_t acc[kNT];                                             // [j][i]: state_of(kNT wave + j, 4 g4 + i) of channel p0 + c16
 #pragma unroll
     for (int j = 0; j < kNT; ++j) {
+        const int n = state_of<N>(me.wave * kNT + j, 4 * me.g4);
         acc[j] = zero;
-        if (a.h0) acc[j] = *reinterpret_cast<const f32x4_t *>(a.h0 + (me.hb * a.P + me.p0 + me.c16) * N + state_of<N>(me.wave * kNT + j, 4 * me.g4));
+        if (me.h0) acc[j] = *reinterpret_cast<const f32x4_t *>(me.h0 + me.c16 * N + n);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (me.unit >= 0 && n + i == me.unit + me.c16) acc[j][i] = 1.0f;
     }
     struct Operands {
         uint2 k[4][kNT];
         uint4 x[3][kX];
     };
-    const uint16_t *frags = a.frags + (me.b * me.Hk + me.hk) * a.n_chunks * kKeyHalves<N> + me.wave * kNT * 2 * kFrag;
-    Cursor<uint16_t> keys{frags, kKeyHalves<N>, n_chunks - 1}, xs{me.own, kChunkHalves, n_chunks - 1};
+    Cursor<uint16_t> keys{me.frags + me.wave * kNT * 2 * kFrag, kKeyHalves<N>, n_chunks - 1}, xs{me.own, kChunkHalves, n_chunks - 1};
     auto fetch_k = [&](Operands &f) {
         if constexpr (kNT == 2) {
 #pragma unroll
@@ -736,31 +745,32 @@ template <int N, bool TWO> __device__ __forceinline__ void walk_chain(const Walk
         step(1, odd);
     }
     if (left > 0) step(0, even);
-    if (a.h_final)
+    if (me.h_final)
 #pragma unroll
         for (int j = 0; j < kNT; ++j)
-            *reinterpret_cast<f32x4_t *>(a.h_final + (me.hb * a.P + me.p0 + me.c16) * N + state_of<N>(me.wave * kNT + j, 4 * me.g4)) = acc[j];
+            *reinterpret_cast<f32x4_t *>(me.h_final + me.c16 * N + state_of<N>(me.wave * kNT + j, 4 * me.g4)) = acc[j];
 }
 
-template <int N, int MODE, bool TWO> __device__ __forceinline__ void walk_outputs(const WalkArgs &a, const WalkPlace<N> &me, WalkLds<N> &lds)
+// OUT: or no outputs, only the values for the other role
+template <int N, int MODE, bool TWO, bool OUT> __device__ __forceinline__ void walk_outputs(const WalkArgs &a, const WalkPlace<N> &me, WalkLds<N> &lds)
 {
     constexpr int kSteps = N / 32, kX = TWO ? 2 : 1;
     const f32x4_t zero = {0.0f, 0.0f, 0.0f, 0.0f};
-    const int n_chunks = (int)a.n_chunks;
+    const int n_chunks = (int)me.n_chunks;
     const uint32_t lane8 = (uint32_t)me.lane * 8;
     // V, the gates and the outputs: token lane / 4 of the wavefront's 16, four channels, so that four adjacent lanes have a row's 32 bytes
     // (a request costs a cycle for every run of adjacent lanes that reads adjacent bytes: 64 of them as a fragment has its rows).
     // Behind the end: the last token again.
     const int t_own = me.wave * 16 + (me.lane >> 2), p_own = 4 * (me.lane & 3);
-    const uint32_t live = (uint32_t)min((int64_t)kC, a.L - a.tok0 - (int64_t)(n_chunks - 1) * kC);
+    const uint32_t live = (uint32_t)min((int64_t)kC, a.L - me.tok0 - (int64_t)(n_chunks - 1) * kC);
     const uint32_t value_at = (uint32_t)t_own * me.value_row + (uint32_t)p_own, value_last = min((uint32_t)t_own, live - 1) * me.value_row + (uint32_t)p_own;
-    const int64_t first = ((me.b * a.L + a.tok0) * a.H + me.h) * a.P + me.p0, chunk_values = (int64_t)kC * me.value_row;
+    const int64_t first = ((me.b * a.L + me.tok0) * a.H + me.h) * a.P + me.p0, chunk_values = (int64_t)kC * me.value_row;
     struct Operands {
         uint4 q[kSteps], mx[2][kX];
         uint2 z, v;
         float factor;                                             // number lane % 4 of token lane / 4
     };
-    Cursor<uint16_t> queries{a.frags + (me.b * me.Hk + me.hk) * a.n_chunks * kKeyHalves<N> + N * kC + me.wave * kSteps * kFrag, kKeyHalves<N>, n_chunks - 1};
+    Cursor<uint16_t> queries{me.frags + N * kC + me.wave * kSteps * kFrag, kKeyHalves<N>, n_chunks - 1};
     Cursor<bf16_t> values{a.v + first, chunk_values, n_chunks - 1}, gates{MODE == kWalkGate ? a.z + first : nullptr, chunk_values, n_chunks - 1};
     Cursor<uint16_t> xs{me.own + kAtMX, kChunkHalves, n_chunks - 1};
     Cursor<float> factors{reinterpret_cast<const float *>(me.own + kAtScalars) + me.wave * 64, kChunkHalves / 2, n_chunks - 1};
@@ -794,15 +804,35 @@ template <int N, int MODE, bool TWO> __device__ __forceinline__ void walk_output
     // V of a chunk, the other way round, and the factors of its rows
     auto park_v = [&](int parity, const Operands &f) {
         uint16_t *to = &lds.v[parity][p_own * kRowV + t_own];
-        to[0] = (uint16_t)f.v.x, to[kRowV] = (uint16_t)(f.v.x >> 16), to[2 * kRowV] = (uint16_t)f.v.y, to[3 * kRowV] = (uint16_t)(f.v.y >> 16);
+        const uint32_t x = OUT || me.unit < 0 ? f.v.x : 0u, y = OUT || me.unit < 0 ? f.v.y : 0u;
+        to[0] = (uint16_t)x, to[kRowV] = (uint16_t)(x >> 16), to[2 * kRowV] = (uint16_t)y, to[3 * kRowV] = (uint16_t)(y >> 16);
         if ((me.lane & 3) < 3) lds.factors[parity][me.lane & 3][t_own] = f.factor;
     };
     Operands even, odd;
+    if constexpr (!OUT) {
+        fetch_v(even), fetch_v(odd);
+        park_v(0, even);
+        fetch_v(even);
+        auto step = [&](int parity, Operands &other) __attribute__((always_inline)) {
+            lds_barrier();                                        // A
+            park_v(parity ^ 1, other);
+            fetch_v(other);
+            lds_barrier();                                        // B
+            lds_barrier();                                        // C
+        };
+        int left = n_chunks;
+        for (; left > 1; left -= 2) {
+            step(0, odd);
+            step(1, even);
+        }
+        if (left > 0) step(0, odd);
+        return;
+    }
     fetch_v(even), fetch_v(odd), fetch_q(even), fetch_q(odd), fetch_mx(even), fetch_z(even);
     park_v(0, even);
     fetch_v(even);
     // this lane's outputs of the chunk (ahead of a norm they go into a buffer of the slab)
-    int64_t to = (MODE == kWalkRaw ? (me.b * a.n_chunks * kC * a.H + me.h) * a.P + me.p0 : first) + value_at;
+    int64_t to = (MODE == kWalkRaw ? ((me.b * a.n_chunks + me.first) * kC * a.H + me.h) * a.P + me.p0 : first) + value_at;
     // (what this role requests goes out where the chain has more to do: all of it behind C made the chain wait there)
     auto step = [&](int parity, bool stores, Operands &f, Operands &other) __attribute__((always_inline)) {
         lds_barrier();                                            // A
@@ -861,25 +891,100 @@ template <int N, int MODE, bool TWO> __device__ __forceinline__ void walk_output
     }
 }
 
-// grid: 8 channel blocks (heads / 8 rounded up); the blocks of a head, which read the same fragments, are 8 apart: on one XCD
+// Heads that leave CUs free have their slab in parts of `part` chunks, several at once: what a part makes of a state is a linear map,
+// S -> S F + C, whose C is the walk from nothing and whose F is the walk of the unit vectors without values.  A first launch walks the
+// first part for its outputs and the others but the last for their maps; delta_join_kernel takes the states through the maps; a second
+// launch walks the parts from the second on for their outputs, from their own states.
+// grid: 8 blocks of 16 rows (heads parts / 8 rounded up), first those of the parts for their outputs, then those for their maps; the blocks of
+// a head's part, which read the same fragments, are 8 apart: on one XCD, and the maps begin on the XCD behind the last of the others
 template <int N, int MODE>
 __global__ void __launch_bounds__(2 * kThreads) delta_walk_kernel(WalkArgs a)
 {
     __shared__ WalkLds<N> lds;
-    const uint32_t blocks = (uint32_t)a.P / 16, place = blockIdx.x >> 3;
+    const uint32_t heads = (uint32_t)a.heads, values = (uint32_t)a.P / 16, walks = (heads * a.walked + 7) / 8 * 8 * values;
+    const bool maps = blockIdx.x >= walks;
+    const uint32_t index = maps ? blockIdx.x - walks : blockIdx.x, blocks = maps ? values + N / 16 : values, place = index >> 3;
+    const uint32_t pair = place / blocks * 8 + ((maps ? index - heads * a.walked : index) & 7), block = place % blocks, turn = pair / heads;
+    if (turn >= (maps ? a.maps : a.walked)) return;
+    const bool unit = block >= values;
+    const uint32_t part = turn + (maps ? 1 : a.first_part);
     WalkPlace<N> at;
-    at.hb = (int64_t)(place / blocks) * 8 + (blockIdx.x & 7);
-    if (at.hb >= a.heads) return;
+    at.hb = pair - turn * heads;
     const int role = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     at.lane = threadIdx.x & 63, at.wave = role & 3, at.c16 = at.lane & 15, at.g4 = at.lane >> 4;
     at.b = at.hb / a.H, at.h = at.hb - at.b * a.H, at.Hk = a.H / a.group, at.hk = at.h / a.group;
-    at.p0 = (int)(place % blocks) * 16;
-    at.own = a.ws + at.hb * a.n_chunks * kChunkHalves;
+    at.p0 = unit ? 0 : (int)block * 16;
+    at.unit = unit ? (int)(block - values) * 16 : -1;
+    at.first = part * a.part, at.n_chunks = min(a.part, a.n_chunks - at.first), at.tok0 = a.tok0 + at.first * kC;
+    at.own = a.ws + (at.hb * a.n_chunks + at.first) * kChunkHalves;
+    at.frags = a.frags + ((at.b * at.Hk + at.hk) * a.n_chunks + at.first) * kKeyHalves<N>;
     at.value_row = (uint32_t)(a.H * a.P);
+    // (a.starts: of the parts from the second on)
+    const bool last = at.first + at.n_chunks == a.n_chunks;
+    const int64_t rows = (at.hb * a.P + at.p0) * N, each = a.heads * a.P * N;
+    at.h0 = maps ? nullptr : part > 0 ? a.starts + (part - 1) * each + rows : a.h0 ? a.h0 + rows : nullptr;
+    at.h_final = unit ? a.map + ((turn * a.heads + at.hb) * N + at.unit) * N : last ? a.h_final ? a.h_final + rows : nullptr
+                 : maps || part == 0 ? a.starts + part * each + rows : nullptr;
+    if (maps) {
+        if (role < 2) walk_chain<N, false>(a, at, lds);
+        else if (role < 4) walk_chain<N, true>(a, at, lds);
+        else walk_outputs<N, MODE, false, false>(a, at, lds);
+        return;
+    }
     if (role < 2) walk_chain<N, false>(a, at, lds);
     else if (role < 4) walk_chain<N, true>(a, at, lds);
-    else if (role < 6) walk_outputs<N, MODE, false>(a, at, lds);
-    else walk_outputs<N, MODE, true>(a, at, lds);
+    else if (role < 6) walk_outputs<N, MODE, false, true>(a, at, lds);
+    else walk_outputs<N, MODE, true, true>(a, at, lds);
+}
+
+// The states at the starts of the parts, from that of the second on: S[i + 1] = S[i] F[i] + C[i], C[i] where S[i + 1] will be.  A workgroup
+// has 16 rows of a head and a wavefront 16 of the N columns, in float32: of S^T = F^T S^T + C^T a lane has four adjacent columns of
+// row l % 16, just as the next product's right operand needs them (k in the order 16 q + 4 (l / 16) + j).
+// grid: (heads P / 16); rows: of all heads, head_rows: of one; steps > 0
+template <int N>
+__global__ void __launch_bounds__(4 * N)
+delta_join_kernel(const float *__restrict__ map, float *states, int64_t rows, int64_t head_rows, int steps)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c16 = lane & 15, g4 = lane >> 4;
+    const int64_t row = (int64_t)blockIdx.x * 16 + c16, hb = (int64_t)blockIdx.x * 16 / head_rows;
+    const int64_t f_step = rows / head_rows * N * N, s_step = rows * N;
+    __shared__ f32x4_t tiles[2][N / 16][64];
+    const float *f = map + (hb * N + 4 * g4) * N + wave * 16 + c16;
+    float *s = states + row * N + wave * 16 + 4 * g4;
+    f32x4_t now = *reinterpret_cast<const f32x4_t *>(s);
+    const float *c = s + s_step;
+    struct Operands {
+        float f[N / 4];
+        f32x4_t c;
+    };
+    int left = steps;                                             // that are to be fetched
+    auto fetch = [&](Operands &w) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < N / 4; ++i) w.f[i] = f[(i / 4 * 16 + i % 4) * N];
+        w.c = *reinterpret_cast<const f32x4_t *>(c);
+        --left;
+        f += left > 0 ? f_step : 0, c += left > 0 ? s_step : 0;
+    };
+    auto step = [&](int parity, Operands &w) __attribute__((always_inline)) {
+        tiles[parity][wave][lane] = now;
+        __syncthreads();                                          // (the next step's go to the other half)
+        now = w.c;
+#pragma unroll
+        for (int q = 0; q < N / 16; ++q) {
+            const f32x4_t right = tiles[parity][q][lane];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) now = mma(w.f[q * 4 + j], right[j], now);
+        }
+        s += s_step;
+        *reinterpret_cast<f32x4_t *>(s) = now;
+        fetch(w);
+    };
+    Operands even, odd;
+    fetch(even), fetch(odd);
+    for (int i = 0; i < steps; i += 2) {
+        step(0, even);
+        if (i + 1 < steps) step(1, odd);
+    }
 }
 
 // The norm over a head's channels, which the walk's workgroups have in parts, and the gate: P / 4 lanes to a (token, head).
@@ -907,13 +1012,41 @@ delta_norm_kernel(const float *__restrict__ raw, const bf16_t *__restrict__ z, c
 
 // A long context goes in slabs of chunks, so that what the preparation leaves is still in the last-level cache (256 MB) when the walk takes
 // it, and the workspace does not grow with the context.  32768 tokens of 32 heads of 128 x 128, all launches, by a slab's bytes: 32 MB 1881 us,
-// 64 MB 1520, 128 MB 1333, 256 MB 1502, one slab 1402; 8191 tokens of 8 heads of 64 x 64: 224, 199, 186, 186, 187.
+// 64 MB 1520, 128 MB 1333, 256 MB 1502, one slab 1402; 8191 tokens of 12 heads of N = 64, P = 128: 224, 199, 186, 186, 187.
+constexpr int64_t kMostBlocks = 512;
 constexpr int64_t kSlabBytes = (int64_t)128 << 20, kSlabLeast = 8;
 // Where the parts of the workspace lie (bytes from its start): what the preparation leaves of a chunk and value head, fragments of a
 // chunk and key head, outputs ahead of their norm, the states between slabs where the caller takes none.
 struct DeltaPlan {
-    int64_t chunks, slab, frags_at, raw_at, state_at, bytes;
+    int64_t chunks, slab, part, frags_at, raw_at, state_at, parts_at, map_at, bytes;
 };
+// The parts of a slab of n chunks, those of the least time (us): a CU (32 to an XCD) walks one block of 16 rows at a time, a chunk in about
+// 1.1 (N = 64) or 1.25 (128), and takes 3 to begin; a part more is a step of the join; two more launches.
+// All launches of 8191 tokens, in one part | in several: 2 heads of 64 x 64 153 | 50 (16 parts), 2 of 128 x 128 158 | 77 (9), 8 of N = 64,
+// P = 64 156 | 84 (9), 8 of 128 x 128 169 | 129 (5), 12 of N = 64, P = 128 161 | 129 (3); 24 of N = 128, P = 64 have work for all CUs:
+// 233 | 305 (3).  2048 tokens: 2 heads of 64 x 64 46 | 30, 12 of N = 64, P = 128 53.5 | 51.6; 1000 tokens of 8 heads of 64 x 64 29 | 30.
+int64_t delta_parts(int64_t heads, int64_t P, int64_t N, int64_t n)
+{
+    const double chunk = N == 64 ? 1.1 : 1.25, join = N == 64 ? 0.75 : 2.0;
+    auto walks = [&](int64_t walked, int64_t maps, int64_t chunks) {
+        int64_t most = 0;
+        for (int64_t xcd = 0; xcd < 8; ++xcd) {
+            const int64_t behind = (xcd - heads * walked % 8 + 8) % 8;
+            const int64_t blocks = (heads * walked + 7 - xcd) / 8 * (P / 16) + (heads * maps + 7 - behind) / 8 * ((P + N) / 16);
+            most = blocks > most ? blocks : most;
+        }
+        return (double)((most + 31) / 32) * (3.0 + chunk * (double)chunks);
+    };
+    int64_t best = 1;
+    double least = walks(1, 0, n);
+    for (int64_t parts = 3; parts <= n && heads * (P / 16) * (parts - 1) <= kMostBlocks; ++parts) {
+        const int64_t part = (n + parts - 1) / parts;
+        if ((n + part - 1) / part != parts) continue;
+        const double t = walks(1, parts - 2, part) + walks(parts - 1, 0, part) + join * (double)(parts - 2) + 6.0;
+        if (t < least) least = t, best = parts;
+    }
+    return best;
+}
 DeltaPlan delta_plan(int64_t batch, int64_t L, int64_t H, int64_t Hk, int64_t P, int64_t N)
 {
     DeltaPlan p;
@@ -926,13 +1059,21 @@ DeltaPlan delta_plan(int64_t batch, int64_t L, int64_t H, int64_t Hk, int64_t P,
     p.frags_at = batch * H * p.slab * kChunkHalves * 2;
     p.raw_at = p.frags_at + batch * Hk * p.slab * 2 * N * kC * 2;
     p.state_at = p.raw_at + batch * p.slab * kC * H * P * 4;
-    p.bytes = p.state_at + (slabs > 1 ? batch * H * P * N * 4 : 0);
+    const int64_t parts = delta_parts(batch * H, P, N, p.slab);   // (two are never chosen: one after the other they gain nothing)
+    p.part = (p.slab + parts - 1) / parts;
+    p.parts_at = p.state_at + (slabs > 1 ? batch * H * P * N * 4 : 0);
+    p.map_at = p.parts_at + (parts - 1) * batch * H * P * N * 4;
+    p.bytes = p.map_at + (parts > 2 ? parts - 2 : 0) * batch * H * N * N * 4;
     return p;
 }
 
-template <int N, int MODE> void walk(const DeltaArgs &a, const WalkArgs &w, hipStream_t stream)
+template <int N> hipError_t walk(const WalkArgs &w, hipStream_t stream)
 {
-    delta_walk_kernel<N, MODE><<<(unsigned)((w.heads + 7) / 8 * 8 * (a.P / 16)), 2 * kThreads, 0, stream>>>(w);
+    const int64_t blocks = (w.heads * w.walked + 7) / 8 * 8 * (w.P / 16) + (w.heads * w.maps + 7) / 8 * 8 * ((w.P + N) / 16);
+    if (w.raw) delta_walk_kernel<N, kWalkRaw><<<(unsigned)blocks, 2 * kThreads, 0, stream>>>(w);
+    else if (w.z) delta_walk_kernel<N, kWalkGate><<<(unsigned)blocks, 2 * kThreads, 0, stream>>>(w);
+    else delta_walk_kernel<N, kWalkPlain><<<(unsigned)blocks, 2 * kThreads, 0, stream>>>(w);
+    return hipGetLastError();
 }
 
 template <int N> hipError_t chunked(const DeltaArgs &a, hipStream_t stream)
@@ -952,12 +1093,20 @@ template <int N> hipError_t chunked(const DeltaArgs &a, hipStream_t stream)
             a.A, a.dt_bias, reinterpret_cast<uint16_t *>(ws), frags, tok0, a.L, a.H, a.H / a.Hk,
             DeltaOptions{a.scale, a.eps, a.dt_softplus, a.beta_sigmoid, a.qk_norm});
         if (hipError_t e = hipGetLastError()) return e;
-        const WalkArgs w{static_cast<const bf16_t *>(a.v), z, reinterpret_cast<const uint16_t *>(ws), frags, first == 0 ? a.h_in : state,
-                         last ? a.h_out : state, out, raw, a.L, a.H, a.H / a.Hk, a.rows * a.H, tok0, n, a.P};
-        if (raw) walk<N, kWalkRaw>(a, w, stream);
-        else if (z) walk<N, kWalkGate>(a, w, stream);
-        else walk<N, kWalkPlain>(a, w, stream);
-        if (hipError_t e = hipGetLastError()) return e;
+        const int64_t heads = a.rows * a.H;
+        const uint32_t parts = (uint32_t)((n + p.part - 1) / p.part);
+        float *starts = reinterpret_cast<float *>(ws + p.parts_at), *map = reinterpret_cast<float *>(ws + p.map_at);
+        WalkArgs w{static_cast<const bf16_t *>(a.v), z, reinterpret_cast<const uint16_t *>(ws), frags, first == 0 ? a.h_in : state,
+                   last ? a.h_out : state, out, raw, starts, map, a.L, a.H, a.H / a.Hk, heads, tok0, n, p.part, 0, 1, parts > 2 ? parts - 2 : 0, a.P};
+        if (hipError_t e = walk<N>(w, stream)) return e;
+        if (w.maps > 0) {
+            delta_join_kernel<N><<<(unsigned)(heads * a.P / 16), 4 * N, 0, stream>>>(map, starts, heads * a.P, a.P, (int)w.maps);
+            if (hipError_t e = hipGetLastError()) return e;
+        }
+        if (parts > 1) {
+            w.first_part = 1, w.walked = parts - 1, w.maps = 0;
+            if (hipError_t e = walk<N>(w, stream)) return e;
+        }
         if (!raw) continue;
         const int64_t token = a.H * a.P / 4, tokens = last ? a.L - tok0 : n * kC;
         const dim3 grid((unsigned)((tokens * token + kThreads - 1) / kThreads), (unsigned)a.rows);

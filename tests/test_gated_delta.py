@@ -300,6 +300,37 @@ def test_fwd_of_a_context_in_several_slabs(m, z, norm):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("B,L,H,Hk,N,P,A,z,norm", [(1, 2100, 2, 1, 64, 64, None, True, True), (2, 1999, 2, 2, 128, 64, -0.01, True, False),
+                                                   (1, 3001, 3, 3, 64, 128, None, False, False), (1, 2305, 1, 1, 128, 128, -0.01, False, True),
+                                                   (1, 17001, 8, 4, 64, 64, None, True, False), (1, 961, 1, 1, 64, 64, -300.0, False, False)])
+def test_fwd_of_long_contexts_of_few_heads(m, B, L, H, Hk, N, P, A, z, norm):
+    """The parts of a long context at once, joined by their maps of the state; with decays that keep a state through all of it, and with
+    ones that leave nothing of it."""
+    print("\n[gpu-case] gated delta parts B=%d L=%d H=%d/%d N=%d P=%d A=%s" % (B, L, H, Hk, N, P, A), flush=True)
+    rng = np.random.default_rng(L)
+    c, h0 = case(rng, B, L, H, Hk, N, P, z=z, norm=norm), state(rng, B, H, P, N)
+    if A is not None:
+        c["A"] = np.full(H, A, np.float32)
+    g, h = device(c), to_dev(h0)
+    ro, rh = oracle_scan(c, h0)
+    out, hf = m.mamba_gated_delta_fwd(**g, h0=h)
+    assert_close(values(to_host(out)), ro, TOL_BF16, "out")
+    assert_close(to_host(hf), rh, TOL_F32, "final state")
+    for _ in range(2):
+        o2, h2 = m.mamba_gated_delta_fwd(**g, h0=h)
+        assert torch.equal(o2, out) and torch.equal(h2, hf)
+    o2, none = m.mamba_gated_delta_fwd(**g, h0=h, want_state=False)
+    assert none is None and torch.equal(o2, out)
+    o2, h2 = m.mamba_gated_delta_fwd(**g, h0=h, h_final=h)
+    assert h2 is h and torch.equal(o2, out) and torch.equal(h, hf)
+    g["v"][0, L // 2, 0, 5] = float("nan")                       # a channel's NaN stays in the channel, also on its way through the joins
+    _, h2 = m.mamba_gated_delta_fwd(**g, h0=to_dev(h0))
+    want = hf.clone()
+    want[0, 0, 5] = float("nan")
+    assert torch.equal(torch.isnan(h2), torch.isnan(want)) and torch.equal(torch.nan_to_num(h2), torch.nan_to_num(want))
+
+
+@pytest.mark.gpu
 def test_fwd_without_tokens_and_empty(m):
     rng = np.random.default_rng(5)
     h0 = to_dev(state(rng, 2, 4, 64, 128))
