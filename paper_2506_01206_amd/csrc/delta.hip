@@ -531,7 +531,9 @@ delta_prepare_kernel(const bf16_t *__restrict__ q, const bf16_t *__restrict__ k,
 //            U = X R of those tokens, with their decay to the end                                                         | C
 //            the write to its states
 //   outputs  wavefront w has the tokens 16 w ..: Q S^T after B, (M X) R after C, gate and store, with the next chunk under way in the chain
-// All operands but S, R and U come from memory, requested two chunks ahead into two sets of registers used in turn.
+// All operands but S, R and U come from memory, requested a chunk ahead, the chain's into the registers that the last use has just left: with
+// two sets used in turn it took 156 registers, a CU held one workgroup, and 4 contexts of 1000 tokens of 16 heads of 128 x 128 took 48 us
+// (now 39); alone on its CU a workgroup is no slower for it.
 struct WalkArgs {
     const bf16_t *v, *z;
     const uint16_t *ws, *frags;
@@ -645,15 +647,15 @@ template <int N, bool TWO> __device__ __forceinline__ void walk_chain(const Walk
         return make_uint2(__builtin_amdgcn_perm(__float_as_uint(d[1]), __float_as_uint(d[0]), 0x07060302),
                           __builtin_amdgcn_perm(__float_as_uint(d[3]), __float_as_uint(d[2]), 0x07060302));
     };
-    Operands even, odd;
-    fetch_k(even), fetch_x(even), fetch_k(odd), fetch_x(odd);
+    Operands f;
+    fetch_k(f), fetch_x(f);
     __builtin_amdgcn_s_setprio(1);                                // the chain's instructions ahead of the other role's
     const int at = me.in_frags(me.wave);
     // the write to the state takes the tokens of two tiles in turns of four, as K^T comes out of its products
     const int u_at = me.of_lane(me.wave >> 1) + 4 * (me.wave & 1);
     // (requests go out where the wavefront waits for LDS anyway: a request holds its wavefront for some 14 cycles, and 12 of them at once
     // are a sixth of a chunk)
-    auto step = [&](int parity, Operands &f) __attribute__((always_inline)) {
+    auto step = [&](int parity) __attribute__((always_inline)) {
         Terms s[kNT];
 #pragma unroll
         for (int j = 0; j < kNT; ++j) s[j] = terms_of(acc[j]);
@@ -739,12 +741,12 @@ template <int N, bool TWO> __device__ __forceinline__ void walk_chain(const Walk
 #pragma unroll
                 for (int j = 0; j < kNT; ++j) acc[j] = mma(as_frag(kt[2 * i][j], kt[2 * i + 1][j]), uf[n][i], acc[j]);
     };
-    int left = n_chunks;                                          // (in pairs: the loads in flight are then the same at every turn)
+    int left = n_chunks;
     for (; left > 1; left -= 2) {
-        step(0, even);
-        step(1, odd);
+        step(0);
+        step(1);
     }
-    if (left > 0) step(0, even);
+    if (left > 0) step(0);
     if (me.h_final)
 #pragma unroll
         for (int j = 0; j < kNT; ++j)
@@ -1020,6 +1022,17 @@ constexpr int64_t kSlabBytes = (int64_t)128 << 20, kSlabLeast = 8;
 struct DeltaPlan {
     int64_t chunks, slab, part, frags_at, raw_at, state_at, parts_at, map_at, bytes;
 };
+// workgroups of a walk on the XCD that has most
+int64_t fullest_xcd(int64_t heads, int64_t P, int64_t N, int64_t walked, int64_t maps)
+{
+    int64_t most = 0;
+    for (int64_t xcd = 0; xcd < 8; ++xcd) {
+        const int64_t behind = (xcd - heads * walked % 8 + 8) % 8;
+        const int64_t blocks = (heads * walked + 7 - xcd) / 8 * (P / 16) + (heads * maps + 7 - behind) / 8 * ((P + N) / 16);
+        most = blocks > most ? blocks : most;
+    }
+    return most;
+}
 // The parts of a slab of n chunks, those of the least time (us): a CU (32 to an XCD) walks one block of 16 rows at a time, a chunk in about
 // 1.1 (N = 64) or 1.25 (128), and takes 3 to begin; a part more is a step of the join; two more launches.
 // All launches of 8191 tokens, in one part | in several: 2 heads of 64 x 64 153 | 50 (16 parts), 2 of 128 x 128 158 | 77 (9), 8 of N = 64,
@@ -1029,13 +1042,7 @@ int64_t delta_parts(int64_t heads, int64_t P, int64_t N, int64_t n)
 {
     const double chunk = N == 64 ? 1.1 : 1.25, join = N == 64 ? 0.75 : 2.0;
     auto walks = [&](int64_t walked, int64_t maps, int64_t chunks) {
-        int64_t most = 0;
-        for (int64_t xcd = 0; xcd < 8; ++xcd) {
-            const int64_t behind = (xcd - heads * walked % 8 + 8) % 8;
-            const int64_t blocks = (heads * walked + 7 - xcd) / 8 * (P / 16) + (heads * maps + 7 - behind) / 8 * ((P + N) / 16);
-            most = blocks > most ? blocks : most;
-        }
-        return (double)((most + 31) / 32) * (3.0 + chunk * (double)chunks);
+        return (double)((fullest_xcd(heads, P, N, walked, maps) + 31) / 32) * (3.0 + chunk * (double)chunks);
     };
     int64_t best = 1;
     double least = walks(1, 0, n);
@@ -1070,9 +1077,12 @@ DeltaPlan delta_plan(int64_t batch, int64_t L, int64_t H, int64_t Hk, int64_t P,
 template <int N> hipError_t walk(const WalkArgs &w, hipStream_t stream)
 {
     const int64_t blocks = (w.heads * w.walked + 7) / 8 * 8 * (w.P / 16) + (w.heads * w.maps + 7) / 8 * 8 * ((w.P + N) / 16);
-    if (w.raw) delta_walk_kernel<N, kWalkRaw><<<(unsigned)blocks, 2 * kThreads, 0, stream>>>(w);
-    else if (w.z) delta_walk_kernel<N, kWalkGate><<<(unsigned)blocks, 2 * kThreads, 0, stream>>>(w);
-    else delta_walk_kernel<N, kWalkPlain><<<(unsigned)blocks, 2 * kThreads, 0, stream>>>(w);
+    // Two workgroups fit on a CU, but each takes its time then: where a CU can be had for each, LDS that nobody uses keeps the second away
+    // (8191 tokens of 12 heads of N = 64, P = 128: 145 -> 133 us; without it two go to one CU while others stay empty).
+    const unsigned alone = fullest_xcd(w.heads, w.P, N, w.walked, w.maps) <= 32 ? 40960 : 0;
+    if (w.raw) delta_walk_kernel<N, kWalkRaw><<<(unsigned)blocks, 2 * kThreads, alone, stream>>>(w);
+    else if (w.z) delta_walk_kernel<N, kWalkGate><<<(unsigned)blocks, 2 * kThreads, alone, stream>>>(w);
+    else delta_walk_kernel<N, kWalkPlain><<<(unsigned)blocks, 2 * kThreads, alone, stream>>>(w);
     return hipGetLastError();
 }
 
