@@ -467,7 +467,7 @@ int mamba_gated_delta_step(float *h_out, const float *h_in, const int32_t *paren
  *   bias (V) float, the same for all rows
  *   mask (n_masks, ceil(V / 32)): bit v % 32 of word v / 32 set where v is allowed; mask_idx (M): the row's mask, -1 for none; NULL: as seq_idx
  * A row whose seq_idx or mask_idx is out of range reads nothing out of bounds: NaN in all of out, no token left in the choice.
- * M (V / 2048 rounded up) <= 2^31 - 1, V <= 2^25, path_len <= 4096.
+ * M (V / 2048 rounded up) < 2^24, n_seq (V / 8192 rounded up) < 2^22, V <= 2^25, path_len <= 4096.
  */
 typedef struct {
     const int32_t *counts;

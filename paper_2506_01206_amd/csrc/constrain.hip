@@ -364,8 +364,9 @@ int64_t slices_of(int64_t V) { return (V + kSlice - 1) / kSlice; }
 
 }  // namespace
 
-bool constrain_grid_ok(int64_t M, int64_t V) { return M <= 0x7fffffff / (slices_of(V) > 0 ? slices_of(V) : 1); }
-bool token_counts_grid_ok(int64_t n_seq, int64_t V) { return n_seq <= 0x7fffffff / ((V + kCountRange - 1) / kCountRange); }
+// (a launch has fewer than 2^32 threads)
+bool constrain_grid_ok(int64_t M, int64_t V) { return M <= (0xffffffff / kThreads) / (slices_of(V) > 0 ? slices_of(V) : 1); }
+bool token_counts_grid_ok(int64_t n_seq, int64_t V) { return n_seq <= (0xffffffff / kCountThreads) / ((V + kCountRange - 1) / kCountRange); }
 
 size_t children_workspace_bytes(int64_t M, int64_t V, int k)
 {

@@ -116,6 +116,7 @@ def test_constrain_refusals(m):
         return m.lib.mamba_logits_constrain_fwd(logits, None if none else ctypes.byref(r), out, M, V, io, None)
     assert call(none=True) == S["NULL_POINTER"] and call(logits=None) == S["NULL_POINTER"] and call(out=None) == S["NULL_POINTER"]
     assert call(io=3) == S["UNSUPPORTED"] and call(V=(1 << 25) + 1) == S["UNSUPPORTED"] and call(M=1 << 30) == S["UNSUPPORTED"]
+    assert call(M=1 << 24, V=1) == S["UNSUPPORTED"] and call(M=1 << 20, V=16 * 2048) == S["UNSUPPORTED"]
     assert call(M=-1) == S["BAD_SHAPE"] and call(V=-1) == S["BAD_SHAPE"]
     assert call(logits=P(0) + 8) == S["MISALIGNED"] and call(out=P(1) + 2) == S["MISALIGNED"] and call(out=P(0) + 16) == S["ALIAS"]
     for name in RULE_NAMES:
@@ -164,6 +165,7 @@ def test_token_counts_refusals(m):
     assert call(tokens=P(0) + 4) == S["MISALIGNED"] and call(counts=P(1) + 4) == S["MISALIGNED"] and call(counts=P(0)) == S["ALIAS"]
     assert call(n_seq=-1) == S["BAD_SHAPE"] and call(L=-1) == S["BAD_SHAPE"] and call(V=-1) == S["BAD_SHAPE"]
     assert call(V=(1 << 25) + 1) == S["UNSUPPORTED"] and call(L=1 << 31) == S["UNSUPPORTED"] and call(n_seq=1 << 31) == S["UNSUPPORTED"]
+    assert call(n_seq=1 << 22, V=1) == S["UNSUPPORTED"] and call(n_seq=1 << 20, V=4 * 8192) == S["UNSUPPORTED"]
     assert call(n_seq=0) == 0 and call(V=0) == 0 and call(L=0, accumulate=1) == 0
 
 
