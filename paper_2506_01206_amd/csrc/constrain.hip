@@ -18,8 +18,8 @@ namespace {
 
 constexpr int kThreads = 256;
 // Vectors of 8 tokens to a lane.  One: what a lane does once is long (a division that rounds right, the rules, the search), and every turn
-// repeats it in the code, which a workgroup fetches as it goes: 3 children of one row of 50280 6.2 us with one turn, 8.4 with two, 13.0
-// with four; logits of 19 rows 4.3, 5.1 and 7.6.
+// repeats it in the code, which a workgroup fetches as it goes: 3 children of one row of 50280 5.9 us with one turn, 8.2 with two, 13.3
+// with four; logits of 19 rows 3.6, 4.2 and 5.8.
 constexpr int kTurns = 1;
 constexpr int kSlice = kThreads * kTurns * 8;                        // tokens to a workgroup
 constexpr int32_t kNoKey = INT32_MIN;                                // below every key
@@ -62,6 +62,10 @@ __device__ __forceinline__ void store8(bf16_t *p, const float *x)
     *reinterpret_cast<u32x4_any *>(p) = a;
 }
 
+// A grid of slices by rows has the rows in two of its dimensions: no number of a workgroup is divided.
+constexpr int64_t kRowsY = 65535;
+__device__ __forceinline__ int64_t row_of_block() { return (int64_t)blockIdx.z * kRowsY + blockIdx.y; }
+
 // What holds for one row of logits.
 struct RowRules {
     bool known;                                                      // its indices are in range
@@ -87,19 +91,47 @@ template <bool COUNTS, bool MASK> __device__ __forceinline__ RowRules rules_of(c
     return r;
 }
 
-__device__ __forceinline__ float adjusted(const RowRules &r, float x, int32_t count)
+// x / d rounded to nearest from y = 1 / d rounded to nearest: two corrections of x y by the exact remainder (P. Markstein, Computation of
+// elementary functions on the IBM RISC System/6000 processor, 1990: with y so rounded and q off by less than one unit, q + (x - q d) y is
+// rounded right).  Holds where nothing over- or underflows on the way; elsewhere the division itself.
+__device__ __forceinline__ float divided(float x, float d, float y)
+{
+    float q = x * y;
+    q = fmaf(fmaf(-q, d, x), y, q);
+    return fmaf(fmaf(-q, d, x), y, q);
+}
+constexpr float kLeast = 0x1p-40f, kMost = 0x1p40f;
+
+// The penalties on a lane's n logits.  Without branches, as a wavefront has tokens of all kinds.
+template <int n> __device__ __forceinline__ void penalise(const RowRules &r, float (&x)[n], const int32_t (&count)[n])
 {
 #pragma clang fp contract(off)
-    const int32_t times = count & 0x7fffffff;
-    if (count != 0) {
-        x = x > 0.0f ? x / r.repetition : x * r.repetition;
-        if (times > 0) {
-            const float f = r.frequency * (float)times;
-            x = x - f;
-            x = x - r.presence;
+    const float y = 1.0f / r.repetition;
+    float less[n], least = kMost, most = kLeast;                     // (only what is above zero is divided)
+#pragma unroll
+    for (int i = 0; i < n; ++i) {
+        least = fminf(least, fabsf(x[i])), most = fmaxf(most, x[i]);
+        less[i] = divided(x[i], r.repetition, y);
+    }
+    if (!__all(least >= kLeast && most <= kMost && r.repetition >= kLeast && r.repetition <= kMost)) {
+#pragma unroll 1
+        for (int i = 0; i < n; ++i) {                                // (rolled up: seldom run, and not to be fetched by the others)
+            const float first = x[0], q = first / r.repetition;
+#pragma unroll
+            for (int j = 0; j + 1 < n; ++j) less[j] = less[j + 1], x[j] = x[j + 1];
+            less[n - 1] = q, x[n - 1] = first;
         }
     }
-    return x;
+#pragma unroll
+    for (int i = 0; i < n; ++i) {
+        const int32_t times = count[i] & 0x7fffffff;
+        float v = x[i] > 0.0f ? less[i] : x[i] * r.repetition;
+        v = count[i] != 0 ? v : x[i];
+        const float f = r.frequency * (float)times;
+        float w = v - f;
+        w = w - r.presence;
+        x[i] = times > 0 ? w : v;
+    }
 }
 
 // A lane's tokens of a slice of a row, kTurns vectors of 8: their adjusted logits, and which of them count (allowed, of this row and
@@ -108,16 +140,16 @@ __device__ __forceinline__ float adjusted(const RowRules &r, float x, int32_t co
 // than 8 tokens is read token by token.)
 // COUNTS: penalties with counts; BIAS, MASK: there are such
 template <typename T, bool COUNTS, bool BIAS, bool MASK> struct Share {
-    int64_t start[kTurns];                                           // first token of a vector as it was read
+    int32_t start[kTurns];                                           // first token of a vector as it was read
     float x[kTurns][8];
     uint32_t valid[kTurns];
 
-    __device__ __forceinline__ void load(const ConstrainArgs &c, const T *row, int64_t m, int64_t slice, RowRules &r)
+    __device__ __forceinline__ void load(const ConstrainArgs &c, const T *row, int64_t m, int32_t slice, RowRules &r)
     {
         int32_t counts[kTurns][8];
         float bias[kTurns][8];
         uint32_t mask[kTurns][2];
-        const int64_t v0 = slice * kSlice + threadIdx.x * 8, V = c.V;
+        const int32_t v0 = slice * kSlice + (int32_t)threadIdx.x * 8, V = (int32_t)c.V;
         if (V >= 8) {
 #pragma unroll
             for (int u = 0; u < kTurns; ++u) {
@@ -126,13 +158,13 @@ template <typename T, bool COUNTS, bool BIAS, bool MASK> struct Share {
                 if constexpr (BIAS) load8(c.bias + start[u], bias[u]);
             }
             r = rules_of<COUNTS, MASK>(c, m);
-            const int64_t last = (V + 31) / 32 * 4 - 1;
+            const int32_t last = (V + 31) / 32 * 4 - 1;
             const uint8_t *bits = r.mask ? r.mask : reinterpret_cast<const uint8_t *>(c.mask);
 #pragma unroll
             for (int u = 0; u < kTurns; ++u) {
                 if constexpr (COUNTS) load8(r.counts + start[u], counts[u]);
                 if constexpr (MASK) {
-                    const int64_t at = start[u] >> 3;
+                    const int32_t at = start[u] >> 3;
                     mask[u][0] = bits[at], mask[u][1] = bits[min(at + 1, last)];
                 }
             }
@@ -145,7 +177,7 @@ template <typename T, bool COUNTS, bool BIAS, bool MASK> struct Share {
                 if constexpr (MASK) mask[u][0] = r.mask ? r.mask[0] : 0, mask[u][1] = 0;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const int64_t v = min<int64_t>(i, V - 1);        // (only the first vector counts)
+                    const int32_t v = min(i, V - 1);        // (only the first vector counts)
                     x[u][i] = ld_io(row, v);
                     if constexpr (BIAS) bias[u][i] = c.bias[v];
                     if constexpr (COUNTS) counts[u][i] = r.counts[v];
@@ -170,32 +202,33 @@ template <typename T, bool COUNTS, bool BIAS, bool MASK> struct Share {
 #pragma unroll
                     for (int u = 0; u < kTurns; ++u)
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) counts[u][i] += (int32_t)start[u] + i == one;
+                        for (int i = 0; i < 8; ++i) counts[u][i] += start[u] + i == one;
                 }
             }
         }
 #pragma unroll
         for (int u = 0; u < kTurns; ++u) {
-            const int64_t v = v0 + u * kThreads * 8;
+            const int32_t v = v0 + u * kThreads * 8;
             valid[u] = 0xff;
             if constexpr (MASK) valid[u] = r.mask ? (mask[u][0] | mask[u][1] << 8) >> (start[u] & 7) & 0xff : 0xff;
             if (V >= 8) valid[u] &= v < V ? 0xffu << (v - start[u]) : 0u;        // (the shift is 0 but in a row's last vector)
             else valid[u] &= v == 0 ? 0xffu >> (8 - V) : 0u;
             if (!r.known) valid[u] = 0;
+            if (c.penalties) penalise(r, x[u], counts[u]);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                x[u][i] = adjusted(r, x[u][i], counts[u][i]);
+            for (int i = 0; i < 8; ++i)
                 if constexpr (BIAS) x[u][i] = x[u][i] + bias[u][i];
-            }
         }
     }
 };
 
-// grid: (rows x slices); out may be logits (a thread writes what it alone has read)
+// grid: slices and rows (see row_of_block); out may be logits (a thread writes what it alone has read)
 template <typename T, bool COUNTS, bool BIAS, bool MASK>
-__global__ void __launch_bounds__(kThreads) constrain_kernel(const T *logits, T *out, ConstrainArgs c, int64_t slices)
+__global__ void __launch_bounds__(kThreads) constrain_kernel(const T *logits, T *out, ConstrainArgs c, int64_t M)
 {
-    const int64_t m = blockIdx.x / slices, slice = blockIdx.x - m * slices, v0 = slice * kSlice + threadIdx.x * 8;
+    const int64_t m = row_of_block();
+    if (m >= M) return;
+    const int32_t slice = blockIdx.x, v0 = slice * kSlice + (int32_t)threadIdx.x * 8, V = (int32_t)c.V;
     RowRules r;
     Share<T, COUNTS, BIAS, MASK> s;
     s.load(c, logits + m * c.V, m, slice, r);
@@ -203,16 +236,16 @@ __global__ void __launch_bounds__(kThreads) constrain_kernel(const T *logits, T 
     const float nan = __int_as_float(0x7fc00000);
 #pragma unroll
     for (int u = 0; u < kTurns; ++u) {
-        const int64_t v = v0 + u * kThreads * 8;
+        const int32_t v = v0 + u * kThreads * 8;
 #pragma unroll
         for (int i = 0; i < 8; ++i) s.x[u][i] = !r.known ? nan : (s.valid[u] >> i & 1) ? s.x[u][i] : -INFINITY;
-        if (v + 8 <= c.V) {
+        if (v + 8 <= V) {
             store8(to + v, s.x[u]);
-        } else if (v < c.V) {                                        // (the end of a row: only what is not another lane's)
-            const int64_t first = c.V >= 8 ? v - s.start[u] : 0, end = c.V >= 8 ? 8 : c.V;
+        } else if (v < V) {                                          // (the end of a row: only what is not another lane's)
+            const int32_t first = V >= 8 ? v - s.start[u] : 0, end = V >= 8 ? 8 : V;
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                if (i >= first && i < end) st_io(to, (c.V >= 8 ? s.start[u] : 0) + i, s.x[u][i]);
+                if (i >= first && i < end) st_io(to, (V >= 8 ? s.start[u] : 0) + i, s.x[u][i]);
         }
     }
 }
@@ -253,13 +286,15 @@ __device__ __forceinline__ void write_child(const ConstrainArgs &c, int64_t m, i
 
 // The k best of one slice of one row.  A lane keeps its 8 tokens' keys in registers and offers the best; the workgroup's best is
 // found k times, and only the wavefront that owned it looks through its registers again.
-// grid: (rows x slices); with one slice the result is the row's, with more the slices' go to `part` and merge_kernel takes over
+// grid: slices and rows; with one slice the result is the row's, with more the slices' go to `part` and merge_kernel takes over
 template <typename T, bool COUNTS, bool BIAS, bool MASK>
 __global__ void __launch_bounds__(kThreads)
 children_kernel(const T *__restrict__ logits, int32_t *__restrict__ idx, float *__restrict__ val, int32_t *__restrict__ path_out,
-                int2 *__restrict__ part, ConstrainArgs c, int64_t slices, int k)
+                int2 *__restrict__ part, ConstrainArgs c, int64_t M, int k)
 {
-    const int64_t m = blockIdx.x / slices, slice = blockIdx.x - m * slices;
+    const int64_t m = row_of_block(), slices = gridDim.x;
+    if (m >= M) return;
+    const int32_t slice = blockIdx.x;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     RowRules r;
     Share<T, COUNTS, BIAS, MASK> s;
@@ -274,7 +309,7 @@ children_kernel(const T *__restrict__ logits, int32_t *__restrict__ idx, float *
             if (key[u][i] > best) best = key[u][i], best_at = u * 8 + i;
         }
     // a token's number in the row from its place in the lane
-    const int32_t v0 = (int32_t)(slice * kSlice) + tid * 8, last = c.V >= 8 ? (int32_t)c.V - 8 : INT32_MAX;
+    const int32_t v0 = slice * kSlice + tid * 8, last = c.V >= 8 ? (int32_t)c.V - 8 : INT32_MAX;
     auto token_of = [&](int at) { return min(v0 + (at >> 3) * (kThreads * 8), last) + (at & 7); };
     int32_t best_token = token_of(max(best_at, 0));
     __shared__ int2 heads[2][kThreads / 64];
@@ -335,16 +370,20 @@ merge_kernel(const int2 *__restrict__ part, int32_t *__restrict__ idx, float *__
 // Occurrences of every token in its sequence.  A workgroup has a range of the vocabulary and counts in LDS, over all of the
 // sequence's tokens (numbers outside the vocabulary, such as the -1 of a padded row, are in no range), and writes its range whole:
 // no clearing beforehand, and integer sums, whatever their order.
-constexpr int kCountThreads = 1024, kCountRange = 8192;
+// Narrow ranges while all their workgroups, two to a CU, are there at once: every one reads all of its sequence's tokens, but clears and
+// writes a quarter.  Narrow | wide (us), a vocabulary of 50280: 1 sequence of 333 tokens 2.9 | 4.1, 8 of 8000 4.7 | 5.8, 16 of 8000
+// 5.7 | 6.0, 32 of 16000 11.9 | 7.8, 64 of 2000 11.5 | 7.8.
+constexpr int kCountThreads = 1024, kCountRange = 8192, kCountNarrow = 2048;
 __global__ void __launch_bounds__(kCountThreads)
-token_counts_kernel(const int32_t *__restrict__ tokens, int32_t *__restrict__ counts, int64_t L, int64_t V, int64_t ranges, int accumulate, int prompt)
+token_counts_kernel(const int32_t *__restrict__ tokens, int32_t *__restrict__ counts, int64_t L, int64_t V, int32_t range, int64_t n_seq, int accumulate, int prompt)
 {
     __shared__ int32_t n[kCountRange];
-    const int64_t s = blockIdx.x / ranges, v0 = (blockIdx.x - s * ranges) * kCountRange;
-    const int len = (int)min((int64_t)kCountRange, V - v0);
+    const int64_t s = row_of_block(), v0 = (int64_t)blockIdx.x * range;
+    if (s >= n_seq) return;
+    const int len = (int)min((int64_t)range, V - v0);
     for (int i = threadIdx.x; i < len; i += kCountThreads) n[i] = 0;
     __syncthreads();
-    constexpr int kAhead = 4;
+    constexpr int kAhead = 8;
     for (int64_t t0 = threadIdx.x; t0 < L; t0 += kCountThreads * kAhead) {
         int64_t v[kAhead];
 #pragma unroll
@@ -375,6 +414,11 @@ size_t children_workspace_bytes(int64_t M, int64_t V, int k)
 }
 
 namespace {
+dim3 grid_of(int64_t M, int64_t V)
+{
+    return dim3((unsigned)slices_of(V), (unsigned)(M < kRowsY ? M : kRowsY), (unsigned)((M + kRowsY - 1) / kRowsY));
+}
+
 // F with the rules that a call has as constants: their absence costs nothing then, and what there is is requested without conditions
 template <typename F> auto with_rules(const ConstrainArgs &c, F f)
 {
@@ -394,15 +438,14 @@ template <typename F> auto with_rules(const ConstrainArgs &c, F f)
 
 hipError_t launch_constrain(const void *logits, void *out, const ConstrainArgs &c, int64_t M, int io, hipStream_t stream)
 {
-    const int64_t slices = slices_of(c.V);
-    const unsigned grid = (unsigned)(M * slices);
+    const dim3 grid = grid_of(M, c.V);
     return with_rules(c, [&](auto counts, auto bias, auto mask) {
         if (io == kIoBf16)
             constrain_kernel<bf16_t, counts.value, bias.value, mask.value>
-                <<<grid, kThreads, 0, stream>>>(static_cast<const bf16_t *>(logits), static_cast<bf16_t *>(out), c, slices);
+                <<<grid, kThreads, 0, stream>>>(static_cast<const bf16_t *>(logits), static_cast<bf16_t *>(out), c, M);
         else
             constrain_kernel<float, counts.value, bias.value, mask.value>
-                <<<grid, kThreads, 0, stream>>>(static_cast<const float *>(logits), static_cast<float *>(out), c, slices);
+                <<<grid, kThreads, 0, stream>>>(static_cast<const float *>(logits), static_cast<float *>(out), c, M);
         return hipGetLastError();
     });
 }
@@ -411,15 +454,15 @@ hipError_t launch_children(const void *logits, int32_t *idx, float *val, int32_t
                            hipStream_t stream)
 {
     const int64_t slices = slices_of(c.V);
-    const unsigned grid = (unsigned)(M * slices);
+    const dim3 grid = grid_of(M, c.V);
     int2 *part = static_cast<int2 *>(ws);
     const hipError_t e = with_rules(c, [&](auto counts, auto bias, auto mask) {
         if (io == kIoBf16)
             children_kernel<bf16_t, counts.value, bias.value, mask.value>
-                <<<grid, kThreads, 0, stream>>>(static_cast<const bf16_t *>(logits), idx, val, path_out, part, c, slices, k);
+                <<<grid, kThreads, 0, stream>>>(static_cast<const bf16_t *>(logits), idx, val, path_out, part, c, M, k);
         else
             children_kernel<float, counts.value, bias.value, mask.value>
-                <<<grid, kThreads, 0, stream>>>(static_cast<const float *>(logits), idx, val, path_out, part, c, slices, k);
+                <<<grid, kThreads, 0, stream>>>(static_cast<const float *>(logits), idx, val, path_out, part, c, M, k);
         return hipGetLastError();
     });
     if (e != hipSuccess || slices == 1) return e;
@@ -430,8 +473,10 @@ hipError_t launch_children(const void *logits, int32_t *idx, float *val, int32_t
 hipError_t launch_token_counts(const int32_t *tokens, int32_t *counts, int64_t n_seq, int64_t L, int64_t V, int accumulate, int prompt,
                                hipStream_t stream)
 {
-    const int64_t ranges = (V + kCountRange - 1) / kCountRange;
-    token_counts_kernel<<<(unsigned)(n_seq * ranges), kCountThreads, 0, stream>>>(tokens, counts, L, V, ranges, accumulate, prompt);
+    const int64_t narrow = (V + kCountNarrow - 1) / kCountNarrow;
+    const int range = n_seq * narrow <= 512 ? kCountNarrow : kCountRange;
+    const dim3 grid((unsigned)((V + range - 1) / range), (unsigned)(n_seq < kRowsY ? n_seq : kRowsY), (unsigned)((n_seq + kRowsY - 1) / kRowsY));
+    token_counts_kernel<<<grid, kCountThreads, 0, stream>>>(tokens, counts, L, V, range, n_seq, accumulate, prompt);
     return hipGetLastError();
 }
 

@@ -235,6 +235,26 @@ def test_ties_infinities_and_nans(m):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("ordinary", [True, False])
+def test_penalties_of_all_sizes_divide_as_float32_does(m, ordinary):
+    """Quotients bit for bit: logits of all sizes by penalties of all sizes, among them those whose quotient, or its way there, is
+    subnormal or too large, and neighbours of powers of two."""
+    print("\n[gpu-case] penalties of all sizes, ordinary=%s" % ordinary, flush=True)
+    rng = np.random.default_rng(8)
+    f = np.float32
+    by = [1.0, 1.3, 0.7, 3.0, 1.1, np.nextafter(f(1), f(2)), np.nextafter(f(1), f(0)), np.nextafter(f(2), f(0)), 2.0 ** -40, 2.0 ** 40, 1e6, 1e-6,
+          3e-39, 1e-30, 1e38, 2.0 ** -126, 1.7e-45]
+    M, V = len(by), 20000
+    bits = rng.integers(0, 1 << 32, (M, V), dtype=np.uint64).astype(np.uint32)
+    x = bits.view(f)
+    if ordinary:                                                 # of all mantissas, exponents -40 .. 39
+        x = ((bits & 0x807fffff) | (rng.integers(87, 167, (M, V)).astype(np.uint32) << 23)).view(f)
+    c = dict(logits=torch.from_numpy(x.copy()), counts=torch.ones(M, V, dtype=I32), seq_idx=torch.arange(M, dtype=I32),
+             penalties=torch.from_numpy(np.array([[b, 0.0, 0.0] for b in by], f)))
+    check(m, c, 4)
+
+
+@pytest.mark.gpu
 def test_a_path_that_repeats_a_token_and_a_row_without_choice(m):
     rng = np.random.default_rng(4)
     c = case(rng, 3, 9000, 1, 0, [0.0], bias=False)
