@@ -1022,16 +1022,13 @@ constexpr int64_t kSlabBytes = (int64_t)128 << 20, kSlabLeast = 8;
 struct DeltaPlan {
     int64_t chunks, slab, part, frags_at, raw_at, state_at, parts_at, map_at, bytes;
 };
-// workgroups of a walk on the XCD that has most
+// Workgroups of a walk on the XCD that has most: the maps go on where the other parts end, so that only where both leave more than 8 behind
+// does one XCD have one more of each.
 int64_t fullest_xcd(int64_t heads, int64_t P, int64_t N, int64_t walked, int64_t maps)
 {
-    int64_t most = 0;
-    for (int64_t xcd = 0; xcd < 8; ++xcd) {
-        const int64_t behind = (xcd - heads * walked % 8 + 8) % 8;
-        const int64_t blocks = (heads * walked + 7 - xcd) / 8 * (P / 16) + (heads * maps + 7 - behind) / 8 * ((P + N) / 16);
-        most = blocks > most ? blocks : most;
-    }
-    return most;
+    const int64_t blocks = P / 16, map_blocks = (P + N) / 16, a = heads * walked, b = heads * maps;
+    const int64_t more = a % 8 + b % 8 > 8 ? blocks + map_blocks : b % 8 > 0 ? map_blocks : a % 8 > 0 ? blocks : 0;
+    return a / 8 * blocks + b / 8 * map_blocks + more;
 }
 // The parts of a slab of n chunks, those of the least time (us): a CU (32 to an XCD) walks one block of 16 rows at a time, a chunk in about
 // 1.1 (N = 64) or 1.25 (128), and takes 3 to begin; a part more is a step of the join; two more launches.
