@@ -17,11 +17,10 @@ namespace mamba {
 namespace {
 
 constexpr int kThreads = 256;
-// Vectors of 8 tokens to a lane.  One: what a lane does once is long (a division that rounds right, the rules, the search), and every turn
-// repeats it in the code, which a workgroup fetches as it goes: 3 children of one row of 50280 5.9 us with one turn, 8.2 with two, 13.3
-// with four; logits of 19 rows 3.6, 4.2 and 5.8.
-constexpr int kTurns = 1;
-constexpr int kSlice = kThreads * kTurns * 8;                        // tokens to a workgroup
+// A lane has one vector of 8 tokens.  What it does with a vector is long (quotients that round right, the rules, the search), and more vectors
+// repeat it in the code, which a workgroup fetches as it goes: 3 children of one row of 50280 5.9 us with one, 8.2 with two, 13.3 with
+// four (4.5 with one since the search is without branches); logits of 19 rows 3.6, 4.2 and 5.8.
+constexpr int kSlice = kThreads * 8;                                 // tokens to a workgroup
 constexpr int32_t kNoKey = INT32_MIN;                                // below every key
 
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));      // rows of V elements start anywhere
@@ -134,61 +133,49 @@ template <int n> __device__ __forceinline__ void penalise(const RowRules &r, flo
     }
 }
 
-// A lane's tokens of a slice of a row, kTurns vectors of 8: their adjusted logits, and which of them count (allowed, of this row and
-// no other lane's).  Everything is requested ahead of the first use, at addresses that do not depend on a condition: a vector past
-// the row's end is the last 8 tokens of the row again, of which those that stand in the vector before it are left out.  (A row of fewer
-// than 8 tokens is read token by token.)
+// A lane's 8 tokens of a slice of a row: their adjusted logits, and which of them count (allowed, of this row and no other lane's).
+// Everything is requested ahead of the first use, at addresses that do not depend on a condition: a vector past the row's end is the last 8
+// tokens of the row again, of which those that stand in the vector before it are left out.  (A row of fewer than 8 tokens is read token by
+// token.)
 // COUNTS: penalties with counts; BIAS, MASK: there are such
 template <typename T, bool COUNTS, bool BIAS, bool MASK> struct Share {
-    int32_t start[kTurns];                                           // first token of a vector as it was read
-    float x[kTurns][8];
-    uint32_t valid[kTurns];
+    int32_t start;                                                   // first token of the vector as it was read
+    float x[8];
+    uint32_t valid;
 
     __device__ __forceinline__ void load(const ConstrainArgs &c, const T *row, int64_t m, int32_t slice, RowRules &r)
     {
-        int32_t counts[kTurns][8];
-        float bias[kTurns][8];
-        uint32_t mask[kTurns][2];
+        int32_t counts[8];
+        float bias[8];
+        uint32_t mask[2];
         const int32_t v0 = slice * kSlice + (int32_t)threadIdx.x * 8, V = (int32_t)c.V;
         if (V >= 8) {
-#pragma unroll
-            for (int u = 0; u < kTurns; ++u) {
-                start[u] = min(v0 + u * kThreads * 8, V - 8);
-                load8(row + start[u], x[u]);
-                if constexpr (BIAS) load8(c.bias + start[u], bias[u]);
-            }
+            start = min(v0, V - 8);
+            load8(row + start, x);
+            if constexpr (BIAS) load8(c.bias + start, bias);
             r = rules_of<COUNTS, MASK>(c, m);
-            const int32_t last = (V + 31) / 32 * 4 - 1;
-            const uint8_t *bits = r.mask ? r.mask : reinterpret_cast<const uint8_t *>(c.mask);
-#pragma unroll
-            for (int u = 0; u < kTurns; ++u) {
-                if constexpr (COUNTS) load8(r.counts + start[u], counts[u]);
-                if constexpr (MASK) {
-                    const int32_t at = start[u] >> 3;
-                    mask[u][0] = bits[at], mask[u][1] = bits[min(at + 1, last)];
-                }
+            if constexpr (COUNTS) load8(r.counts + start, counts);
+            if constexpr (MASK) {
+                const int32_t last = (V + 31) / 32 * 4 - 1, at = start >> 3;
+                const uint8_t *bits = r.mask ? r.mask : reinterpret_cast<const uint8_t *>(c.mask);
+                mask[0] = bits[at], mask[1] = bits[min(at + 1, last)];
             }
             __builtin_amdgcn_sched_barrier(0);
         } else {
             r = rules_of<COUNTS, MASK>(c, m);
+            start = v0;
+            if constexpr (MASK) mask[0] = mask[1] = r.mask ? r.mask[0] : 0;   // (the second is not looked at)
 #pragma unroll
-            for (int u = 0; u < kTurns; ++u) {
-                start[u] = v0 + u * kThreads * 8;
-                if constexpr (MASK) mask[u][0] = r.mask ? r.mask[0] : 0, mask[u][1] = 0;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int32_t v = min(i, V - 1);        // (only the first vector counts)
-                    x[u][i] = ld_io(row, v);
-                    if constexpr (BIAS) bias[u][i] = c.bias[v];
-                    if constexpr (COUNTS) counts[u][i] = r.counts[v];
-                }
+            for (int i = 0; i < 8; ++i) {
+                const int32_t v = min(i, V - 1);                     // (only the first vector counts)
+                x[i] = ld_io(row, v);
+                if constexpr (BIAS) bias[i] = c.bias[v];
+                if constexpr (COUNTS) counts[i] = r.counts[v];
             }
         }
         if constexpr (!COUNTS) {
 #pragma unroll
-            for (int u = 0; u < kTurns; ++u)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) counts[u][i] = 0;
+            for (int i = 0; i < 8; ++i) counts[i] = 0;
         }
         // The row's path: a lane of each wavefront has a token of it, and those that stand in this slice are handed to all lanes.
         if (c.path && c.penalties) {
@@ -200,25 +187,19 @@ template <typename T, bool COUNTS, bool BIAS, bool MASK> struct Share {
                     const int32_t one = __builtin_amdgcn_readlane(token, __builtin_ctzll(here));
                     here &= here - 1;
 #pragma unroll
-                    for (int u = 0; u < kTurns; ++u)
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) counts[u][i] += start[u] + i == one;
+                    for (int i = 0; i < 8; ++i) counts[i] += start + i == one;
                 }
             }
         }
+        valid = 0xff;
+        if constexpr (MASK) valid = r.mask ? (mask[0] | mask[1] << 8) >> (start & 7) & 0xff : 0xff;
+        if (V >= 8) valid &= v0 < V ? 0xffu << (v0 - start) : 0u;    // (the shift is 0 but in a row's last vector)
+        else valid &= v0 == 0 ? 0xffu >> (8 - V) : 0u;
+        if (!r.known) valid = 0;
+        if (c.penalties) penalise(r, x, counts);
 #pragma unroll
-        for (int u = 0; u < kTurns; ++u) {
-            const int32_t v = v0 + u * kThreads * 8;
-            valid[u] = 0xff;
-            if constexpr (MASK) valid[u] = r.mask ? (mask[u][0] | mask[u][1] << 8) >> (start[u] & 7) & 0xff : 0xff;
-            if (V >= 8) valid[u] &= v < V ? 0xffu << (v - start[u]) : 0u;        // (the shift is 0 but in a row's last vector)
-            else valid[u] &= v == 0 ? 0xffu >> (8 - V) : 0u;
-            if (!r.known) valid[u] = 0;
-            if (c.penalties) penalise(r, x[u], counts[u]);
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if constexpr (BIAS) x[u][i] = x[u][i] + bias[u][i];
-        }
+        for (int i = 0; i < 8; ++i)
+            if constexpr (BIAS) x[i] = x[i] + bias[i];
     }
 };
 
@@ -228,31 +209,26 @@ __global__ void __launch_bounds__(kThreads) constrain_kernel(const T *logits, T 
 {
     const int64_t m = row_of_block();
     if (m >= M) return;
-    const int32_t slice = blockIdx.x, v0 = slice * kSlice + (int32_t)threadIdx.x * 8, V = (int32_t)c.V;
+    const int32_t slice = blockIdx.x, v = slice * kSlice + (int32_t)threadIdx.x * 8, V = (int32_t)c.V;
     RowRules r;
     Share<T, COUNTS, BIAS, MASK> s;
     s.load(c, logits + m * c.V, m, slice, r);
     T *to = out + m * c.V;
-    const float nan = __int_as_float(0x7fc00000);
 #pragma unroll
-    for (int u = 0; u < kTurns; ++u) {
-        const int32_t v = v0 + u * kThreads * 8;
+    for (int i = 0; i < 8; ++i) s.x[i] = !r.known ? __int_as_float(0x7fc00000) : (s.valid >> i & 1) ? s.x[i] : -INFINITY;
+    if (v + 8 <= V) {
+        store8(to + v, s.x);
+    } else if (v < V) {                                              // (the end of a row: only what is not another lane's)
+        const int32_t first = V >= 8 ? v - s.start : 0, end = V >= 8 ? 8 : V;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s.x[u][i] = !r.known ? nan : (s.valid[u] >> i & 1) ? s.x[u][i] : -INFINITY;
-        if (v + 8 <= V) {
-            store8(to + v, s.x[u]);
-        } else if (v < V) {                                          // (the end of a row: only what is not another lane's)
-            const int32_t first = V >= 8 ? v - s.start[u] : 0, end = V >= 8 ? 8 : V;
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (i >= first && i < end) st_io(to, (V >= 8 ? s.start[u] : 0) + i, s.x[u][i]);
-        }
+        for (int i = 0; i < 8; ++i)
+            if (i >= first && i < end) st_io(to, s.start + i, s.x[i]);
     }
 }
 
 template <int CTRL> __device__ __forceinline__ int32_t lane_max(int32_t v)
 {
-    return max(v, __builtin_amdgcn_update_dpp(v, v, CTRL, 0xf, 0xf, false));
+    return max(v, __builtin_amdgcn_update_dpp(INT32_MIN, v, CTRL, 0xf, 0xf, false));
 }
 // largest of the 64 lanes: quad_perm [1,0,3,2], [2,3,0,1], row_half_mirror, row_mirror, row_bcast:15, row_bcast:31
 __device__ __forceinline__ int32_t wave_max(int32_t v)
@@ -299,45 +275,39 @@ children_kernel(const T *__restrict__ logits, int32_t *__restrict__ idx, float *
     RowRules r;
     Share<T, COUNTS, BIAS, MASK> s;
     s.load(c, logits + m * c.V, m, slice, r);
-    int32_t key[kTurns][8];
-    int32_t best = kNoKey, best_at = -1;                             // first of the lane's largest
+    int32_t key[8], best = kNoKey, best_at = 0;                      // first of the lane's largest
 #pragma unroll
-    for (int u = 0; u < kTurns; ++u)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            key[u][i] = (s.valid[u] >> i & 1) ? key_of(s.x[u][i]) : kNoKey;
-            if (key[u][i] > best) best = key[u][i], best_at = u * 8 + i;
-        }
-    // a token's number in the row from its place in the lane
-    const int32_t v0 = slice * kSlice + tid * 8, last = c.V >= 8 ? (int32_t)c.V - 8 : INT32_MAX;
-    auto token_of = [&](int at) { return min(v0 + (at >> 3) * (kThreads * 8), last) + (at & 7); };
-    int32_t best_token = token_of(max(best_at, 0));
+    for (int i = 0; i < 8; ++i) {
+        const int32_t on = (int32_t)(s.valid << (31 - i)) >> 31;     // (all bits of one: no branch)
+        key[i] = (key_of(s.x[i]) & on) | (kNoKey & ~on);
+        const bool ahead = key[i] > best;
+        best = max(best, key[i]), best_at = ahead ? i : best_at;
+    }
     __shared__ int2 heads[2][kThreads / 64];
     for (int n = 0; n < k; ++n) {
-        const int32_t wk = wave_max(best), wt = wave_max(best == wk ? ~best_token : INT32_MIN);
+        // (lanes, and wavefronts, have the tokens in their order: the first of equals has the lowest)
+        const int32_t wk = wave_max(best), wt = __builtin_amdgcn_readlane(s.start + best_at, __builtin_ctzll(__ballot(best == wk)));
         if (lane == 0) heads[n & 1][wave] = make_int2(wk, wt);       // (the other half may still be being read)
         __syncthreads();
-        int32_t win = kNoKey, not_token = INT32_MIN;
+        int32_t win = kNoKey, token = -1;
 #pragma unroll
         for (int w = 0; w < kThreads / 64; ++w) {
             const int2 h = heads[n & 1][w];
-            if (h.x > win || (h.x == win && h.y > not_token)) win = h.x, not_token = h.y;
+            if (h.x > win) win = h.x, token = h.y;
         }
-        const int32_t token = ~not_token;
         if (wave == 0) {
             if (slices == 1) write_child(c, m, n, k, win, token, idx, val, path_out, lane);
             else if (lane == 0) part[(m * slices + slice) * k + n] = make_int2(win, token);
         }
-        if (win != kNoKey && best == win && best_token == token) {   // the owner's next: the best behind the one that was taken
-            best = kNoKey, best_at = -1;
+        if (best == win && s.start + best_at == token) {             // the owner's next
+            const int32_t taken = best_at;
+            best = kNoKey, best_at = 0;
 #pragma unroll
-            for (int u = 0; u < kTurns; ++u)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int32_t q = key[u][i];
-                    if ((q < win || (q == win && token_of(u * 8 + i) > token)) && q > best) best = q, best_at = u * 8 + i;
-                }
-            best_token = token_of(max(best_at, 0));
+            for (int i = 0; i < 8; ++i) {
+                key[i] = taken == i ? kNoKey : key[i];
+                const bool ahead = key[i] > best;
+                best = max(best, key[i]), best_at = ahead ? i : best_at;
+            }
         }
     }
 }
