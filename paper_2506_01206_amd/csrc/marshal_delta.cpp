@@ -116,6 +116,9 @@ mamba_constraints_t constraints(Args a, int64_t M, int64_t V)
     if (a[1] != Py_None) c.n_seq = sizes(a[1], "penalties", 2)[0];
     if (a[3] != Py_None) c.path_len = sizes(a[3], "path", 2)[1];
     if (a[5] != Py_None) c.n_masks = sizes(a[5], "mask", 2)[0];
+    // (a tensor of no rows has no address, and would pass for a rule that is left out)
+    if (M > 0 && a[5] != Py_None && c.n_masks == 0) fail(PyExc_ValueError, "%s must have a row", "mask");
+    if (M > 0 && (a[0] != Py_None || a[1] != Py_None) && c.n_seq == 0) fail(PyExc_ValueError, "%s must have a row", a[0] != Py_None ? "counts" : "penalties");
     c.counts = static_cast<const int32_t *>(ptr(a[0], at::kInt, {c.n_seq, V}, "counts"));
     c.penalties = fptr(a[1], {c.n_seq, 3}, "penalties");
     c.seq_idx = static_cast<const int32_t *>(ptr(a[2], at::kInt, {M}, "seq_idx"));

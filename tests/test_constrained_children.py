@@ -276,6 +276,19 @@ def test_indices_out_of_range_read_nothing(m):
 
 
 @pytest.mark.gpu
+def test_rules_without_rows_are_refused_where_there_are_logits(m):
+    logits, none = torch.zeros(2, 40, dtype=BF16, device=DEV), lambda *s, dtype=I32: torch.zeros(*s, dtype=dtype, device=DEV)
+    for rule in (dict(mask=none(0, 2)), dict(counts=none(0, 40)), dict(penalties=none(0, 3, dtype=F32)),
+                 dict(counts=none(0, 40), penalties=none(0, 3, dtype=F32))):
+        with pytest.raises(ValueError, match="must have a row"):
+            m.mamba_logits_constrain_fwd(logits, **rule)
+        with pytest.raises(ValueError, match="must have a row"):
+            m.mamba_topk_constrained_fwd(logits, 2, **rule)
+        assert m.mamba_logits_constrain_fwd(logits[:0], **rule).shape == (0, 40)
+        assert [tuple(x.shape) for x in m.mamba_topk_constrained_fwd(logits[:0], 2, **rule)[:2]] == [(0, 2), (0, 2)]
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("S,L,V", [(1, 1, 1), (3, 17, 5), (2, 4097, 8193), (4, 8000, 50280), (1, 100000, 20000), (2, 0, 30)])
 def test_token_counts(m, S, L, V):
     from oracle import constrain as oc
