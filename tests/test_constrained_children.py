@@ -276,6 +276,26 @@ def test_indices_out_of_range_read_nothing(m):
 
 
 @pytest.mark.gpu
+def test_rows_beyond_32_bit_offsets(m):
+    """65 rows of the widest vocabulary: more than 2^31 logits."""
+    print("\n[gpu-case] constrained logits beyond 2^31 elements", flush=True)
+    M, wide = 65, 1 << 25
+    logits = torch.zeros(M, wide, dtype=BF16, device=DEV)
+    logits[M - 1, wide - 1], logits[M - 1, 7], logits[M - 1, 8] = 5.0, 4.0, 6.0
+    logits[M - 2, 3] = 3.0
+    counts = torch.zeros(1, wide, dtype=I32, device=DEV)
+    counts[0, 7], counts[0, wide - 1] = 2, 1
+    rules = dict(counts=counts, penalties=torch.tensor([[2.0, 0.25, 0.5]], device=DEV))
+    idx, val, _ = m.mamba_topk_constrained_fwd(logits, 3, **rules)
+    assert idx[M - 1].tolist() == [8, wide - 1, 7] and val[M - 1].tolist() == [6.0, 2.5 - 0.5 - 0.25, 2.0 - 1.0 - 0.25]
+    assert idx[M - 2].tolist() == [3, 0, 1]
+    out = m.mamba_logits_constrain_fwd(logits, **rules, out=logits)
+    assert out is logits and out[M - 1, [7, 8, wide - 1]].tolist() == [0.75, 6.0, 1.75] and out[M - 2, [3, 7, wide - 1]].tolist() == [3.0, -1.25, -0.75]
+    del logits, out
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.gpu
 def test_rules_without_rows_are_refused_where_there_are_logits(m):
     logits, none = torch.zeros(2, 40, dtype=BF16, device=DEV), lambda *s, dtype=I32: torch.zeros(*s, dtype=dtype, device=DEV)
     for rule in (dict(mask=none(0, 2)), dict(counts=none(0, 40)), dict(penalties=none(0, 3, dtype=F32)),

@@ -374,6 +374,45 @@ def test_fwd_nan_stays_in_its_sequence_and_head(m):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("norm", [False, True])
+def test_fwd_beyond_32_bit_offsets(m, norm):
+    """More than 2^31 values: the last head's outputs and state are those of that head by itself, which goes in other slabs and parts."""
+    print("\n[gpu-case] gated delta beyond 2^31 elements norm=%s" % norm, flush=True)
+    L, H, N, P = 131072 + 70, 128, 64, 128
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    n = lambda *s: torch.randn(*s, generator=gen, device=DEV).to(torch.bfloat16)
+    q, k, v, dt, beta = n(1, L, 1, N), n(1, L, 1, N), n(1, L, 1, P), n(1, L, 1), n(1, L, 1)
+    A, bias, w = -torch.linspace(0.05, 4, H, device=DEV), torch.full((H,), -3.0, device=DEV), torch.ones(P, device=DEV) if norm else None
+    heads = lambda x: x.expand(1, L, H, *x.shape[3:]).contiguous()
+    out, hf = m.mamba_gated_delta_fwd(q, k, heads(v), heads(dt), A, heads(beta), norm_w=w, dt_bias=bias)
+    for h in (0, H - 1):
+        ro, rh = m.mamba_gated_delta_fwd(q, k, v, dt, A[h:h + 1].clone(), beta, norm_w=w, dt_bias=bias[:1])
+        # both within TOL_BF16 of the same
+        assert_close(values(to_host(out[:, -200:, h:h + 1].contiguous())), values(to_host(ro[:, -200:].contiguous())), 2 * TOL_BF16, "out")
+        assert_close(to_host(hf[:, h:h + 1].contiguous()), values(to_host(rh)), 2 * TOL_F32, "state")
+    del out
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.gpu
+def test_step_beyond_32_bit_offsets(m):
+    print("\n[gpu-case] gated delta step beyond 2^31 elements", flush=True)
+    rng = np.random.default_rng(13)
+    n_out, H, N, P = 1030, 128, 128, 128
+    c = {n: x[:, 0] if n in ("q", "k", "v", "dt", "beta", "z") and x is not None else x for n, x in case(rng, 2, 1, H, 2, N, P).items()}
+    g, h = device(c), to_dev(state(rng, 2, H, P, N))
+    rh, ro = m.mamba_gated_delta_step(h, **g)
+    many = {n: x.repeat(n_out // 2, *[1] * (x.dim() - 1)) if n in ("q", "k", "v", "dt", "beta", "z") else x for n, x in g.items()}
+    parent = torch.arange(n_out, device=DEV, dtype=torch.int32) % 2
+    ho, out = m.mamba_gated_delta_step(h, **many, parent_idx=parent)
+    assert torch.equal(ho[-2:], rh) and torch.equal(out[-2:], ro) and torch.equal(ho[:2], rh)
+    h2, o2 = m.mamba_gated_delta_step(ho, **many, parent_idx=torch.arange(n_out, device=DEV, dtype=torch.int32).flip(0))
+    assert torch.equal(h2[0], h2[-2]) and torch.equal(h2[1], h2[-1]) and not torch.equal(h2[0], ho[0])
+    del ho, h2
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("io", [synth.BF16, synth.F32])
 @pytest.mark.parametrize("n_out,n_in,H,Hk,N,P,z,norm", [
     (1, 1, 1, 1, 64, 64, True, True), (6, 3, 4, 2, 128, 64, True, False), (18, 9, 3, 1, 64, 128, False, True), (33, 33, 2, 2, 128, 128, True, True),
