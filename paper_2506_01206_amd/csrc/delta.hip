@@ -269,6 +269,8 @@ template <int N> __device__ __forceinline__ int state_of(int tile, int row)
 
 // One chunk of one head.  Eight wavefronts, and what the chain of phases needs comes first: T by all of them; then one inverts the blocks
 // on its diagonal while the others form M and write the fragments of keys and queries.
+// Bound by the latency of those phases, three workgroups to a CU: one chunk 6.6 us, 768 chunks (24 heads, N = 128) 16.7, 1504 (32 heads, N = 128)
+// 28, which then write their 70 MB at 2.5 TB/s.
 // grid: (chunks of the slab, H, batch); tok_slab: the slab's first token
 constexpr int kPrepThreads = 512;
 template <int N>
@@ -534,6 +536,8 @@ delta_prepare_kernel(const bf16_t *__restrict__ q, const bf16_t *__restrict__ k,
 // All operands but S, R and U come from memory, requested a chunk ahead, the chain's into the registers that the last use has just left: with
 // two sets used in turn it took 156 registers, a CU held one workgroup, and 4 contexts of 1000 tokens of 16 heads of 128 x 128 took 48 us
 // (now 39); alone on its CU a workgroup is no slower for it.
+// Bound by the latency of a chunk's chain: N = 64 1.1, N = 128 1.25 us, of which the matrix pipe is busy for a fifth; 24 heads of N = 128,
+// P = 64 and 2048 tokens 41 us.  Where all CUs have one or two workgroups the instructions of both roles are two thirds of the time.
 struct WalkArgs {
     const bf16_t *v, *z;
     const uint16_t *ws, *frags;
@@ -942,6 +946,7 @@ __global__ void __launch_bounds__(2 * kThreads) delta_walk_kernel(WalkArgs a)
 // The states at the starts of the parts, from that of the second on: S[i + 1] = S[i] F[i] + C[i], C[i] where S[i + 1] will be.  A workgroup
 // has 16 rows of a head and a wavefront 16 of the N columns, in float32: of S^T = F^T S^T + C^T a lane has four adjacent columns of
 // row l % 16, just as the next product's right operand needs them (k in the order 16 q + 4 (l / 16) + j).
+// Bound by the float32 matrix rate of a CU (N = 128: 0.9 us a step) and the exchange: 0.75 us a step with N = 64, 2 with N = 128.
 // grid: (heads P / 16); rows: of all heads, head_rows: of one; steps > 0
 template <int N>
 __global__ void __launch_bounds__(4 * N)
@@ -989,7 +994,8 @@ delta_join_kernel(const float *__restrict__ map, float *states, int64_t rows, in
     }
 }
 
-// The norm over a head's channels, which the walk's workgroups have in parts, and the gate: P / 4 lanes to a (token, head).
+// The norm over a head's channels, which the walk's workgroups have in parts, and the gate: P / 4 lanes to a (token, head).  Bound by bytes:
+// 3008 tokens of 32 heads of 128 channels, 99 MB, in 15 us.
 // grid: (workgroups, batch); n: quadruples of a batch row, raw_row and row those from one batch row to the next
 template <int P>
 __global__ void __launch_bounds__(kThreads)
@@ -1013,8 +1019,9 @@ delta_norm_kernel(const float *__restrict__ raw, const bf16_t *__restrict__ z, c
 }
 
 // A long context goes in slabs of chunks, so that what the preparation leaves is still in the last-level cache (256 MB) when the walk takes
-// it, and the workspace does not grow with the context.  32768 tokens of 32 heads of 128 x 128, all launches, by a slab's bytes: 32 MB 1881 us,
-// 64 MB 1520, 128 MB 1333, 256 MB 1502, one slab 1402; 8191 tokens of 12 heads of N = 64, P = 128: 224, 199, 186, 186, 187.
+// it, and the workspace does not grow with the context.  32768 tokens of 32 heads of 128 x 128, all launches, by a slab's bytes: 32 MB 1625 us,
+// 64 MB 1345, 128 MB 1152, 256 MB 1261, one slab 1174 (and 1.2 GB of workspace); 8191 tokens of 12 heads of N = 64, P = 128: 192, 148, 133 from
+// 128 MB on, which are one slab.
 constexpr int64_t kMostBlocks = 512;
 constexpr int64_t kSlabBytes = (int64_t)128 << 20, kSlabLeast = 8;
 // Where the parts of the workspace lie (bytes from its start): what the preparation leaves of a chunk and value head, fragments of a
