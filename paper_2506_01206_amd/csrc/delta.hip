@@ -204,8 +204,8 @@ constexpr int kTiles = 6;                                         // 16 x 32 fra
 constexpr int kFrag = 512;                                        // bf16 of a fragment
 constexpr int kTri = kTiles * kFrag;
 constexpr int kScalars = 256;                                     // floats, four to a token: its factors of k S and of q S, the chunk's decay
-// 16-bit words of a chunk and head: X times the decay to the end (three terms), M X (two), scalars
-constexpr int kAtMX = 3 * kTri, kAtScalars = 5 * kTri, kChunkHalves = 5 * kTri + 2 * kScalars;
+// 16-bit words of a chunk and head: X times the decay to the end, M X (three terms each), scalars
+constexpr int kAtMX = 3 * kTri, kAtScalars = 6 * kTri, kChunkHalves = 6 * kTri + 2 * kScalars;
 __device__ __forceinline__ int tile_at(int t_tile, int k_step) { return (t_tile < 2 ? t_tile : 2 * t_tile - 2) + k_step; }
 
 __device__ __forceinline__ bf16x8 as_frag(uint4 q) { return __builtin_bit_cast(bf16x8, q); }
@@ -521,7 +521,7 @@ delta_prepare_kernel(const bf16_t *__restrict__ q, const bf16_t *__restrict__ k,
         const int t_tile = wave < 2 ? wave : wave < 4 ? 2 : 3, step = wave < 2 ? 0 : wave & 1, at = kAtMX + wave * kFrag + lane * 8;
         Terms w[2];
         fragment(sys, t_tile * 16 + c16, step * 32 + g4 * 8, 1.0f, w);
-        write(at, w[0].hi, w[1].hi), write(kTri + at, w[0].mid, w[1].mid);
+        write(at, w[0].hi, w[1].hi), write(kTri + at, w[0].mid, w[1].mid), write(2 * kTri + at, w[0].lo, w[1].lo);
     }
 }
 
@@ -555,7 +555,7 @@ constexpr int kRowV = kC + 4;
 // What is exchanged lies in LDS as the fragments that will be read, a kilobyte each: whole lines both ways, no bank conflicts.
 template <int N> struct __attribute__((aligned(16))) WalkLds {
     float part[4 * 4 * 256];                                      // parts of K S^T, [token tile][wavefront][lane][4]
-    uint16_t s_hi[N / 32 * kFrag], s_mid[N / 32 * kFrag];         // S, channels by states
+    uint16_t s_hi[N / 32 * kFrag], s_mid[N / 32 * kFrag], s_lo[N / 32 * kFrag];   // S, channels by states
     uint16_t r_hi[2 * kFrag], r_mid[2 * kFrag], r_lo[2 * kFrag];  // R, channels by tokens
     uint16_t u_hi[2 * kFrag], u_mid[2 * kFrag], u_lo[2 * kFrag];  // decayed U
     uint16_t v[2][16 * kRowV];                                    // V, [channel][token], two chunks
@@ -666,9 +666,11 @@ template <int N, bool TWO> __device__ __forceinline__ void walk_chain(const Walk
         if constexpr (kNT == 2) {
             *reinterpret_cast<uint4 *>(&lds.s_hi[me.of_lane(me.wave)]) = make_uint4(s[0].hi.x, s[0].hi.y, s[1].hi.x, s[1].hi.y);
             *reinterpret_cast<uint4 *>(&lds.s_mid[me.of_lane(me.wave)]) = make_uint4(s[0].mid.x, s[0].mid.y, s[1].mid.x, s[1].mid.y);
+            *reinterpret_cast<uint4 *>(&lds.s_lo[me.of_lane(me.wave)]) = make_uint4(s[0].lo.x, s[0].lo.y, s[1].lo.x, s[1].lo.y);
         } else {
             put(&lds.s_hi[at], s[0].hi);
             put(&lds.s_mid[at], s[0].mid);
+            put(&lds.s_lo[at], s[0].lo);
         }
         f32x4_t sum[4];
         if constexpr (kNT == 2) {
@@ -772,10 +774,11 @@ template <int N, int MODE, bool TWO, bool OUT> __device__ __forceinline__ void w
     const uint32_t value_at = (uint32_t)t_own * me.value_row + (uint32_t)p_own, value_last = min((uint32_t)t_own, live - 1) * me.value_row + (uint32_t)p_own;
     const int64_t first = ((me.b * a.L + me.tok0) * a.H + me.h) * a.P + me.p0, chunk_values = (int64_t)kC * me.value_row;
     struct Operands {
-        uint4 q[kSteps], mx[2][kX];
+        uint4 q[kSteps];
         uint2 z, v;
         float factor;                                             // number lane % 4 of token lane / 4
     };
+    uint4 mx[3][kX];                                              // (one set: the next chunk's are requested when this one's have been used)
     Cursor<uint16_t> queries{me.frags + N * kC + me.wave * kSteps * kFrag, kKeyHalves<N>, n_chunks - 1};
     Cursor<bf16_t> values{a.v + first, chunk_values, n_chunks - 1}, gates{MODE == kWalkGate ? a.z + first : nullptr, chunk_values, n_chunks - 1};
     Cursor<uint16_t> xs{me.own + kAtMX, kChunkHalves, n_chunks - 1};
@@ -786,11 +789,11 @@ template <int N, int MODE, bool TWO, bool OUT> __device__ __forceinline__ void w
         queries.advance();
         requested();
     };
-    auto fetch_mx = [&](Operands &f) {
+    auto fetch_mx = [&]() {
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
+        for (int n = 0; n < 3; ++n)
 #pragma unroll
-            for (int i = 0; i < kX; ++i) f.mx[n][i] = *reinterpret_cast<const uint4 *>(xs.p + n * kTri + tile_at(me.wave, i) * kFrag + lane8);
+            for (int i = 0; i < kX; ++i) mx[n][i] = *reinterpret_cast<const uint4 *>(xs.p + n * kTri + tile_at(me.wave, i) * kFrag + lane8);
         xs.advance();
         requested();
     };
@@ -834,7 +837,7 @@ template <int N, int MODE, bool TWO, bool OUT> __device__ __forceinline__ void w
         if (left > 0) step(0, odd);
         return;
     }
-    fetch_v(even), fetch_v(odd), fetch_q(even), fetch_q(odd), fetch_mx(even), fetch_z(even);
+    fetch_v(even), fetch_v(odd), fetch_q(even), fetch_q(odd), fetch_mx(), fetch_z(even);
     park_v(0, even);
     fetch_v(even);
     // this lane's outputs of the chunk (ahead of a norm they go into a buffer of the slab)
@@ -844,10 +847,11 @@ template <int N, int MODE, bool TWO, bool OUT> __device__ __forceinline__ void w
         lds_barrier();                                            // A
         park_v(parity ^ 1, other);
         fetch_v(other);
-        fetch_mx(other);
         fetch_z(other);
-        lds_barrier();                                            // B (the chain is short between the two, and would wait for this role)
         f32x4_t o = zero, o2 = zero;
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) o2 = mma(lds_frag(&lds.s_lo[me.of_lane(i)]), as_frag(f.q[i]), o2);
+        lds_barrier();                                            // B (the chain is short between the two, and would wait for this role)
         const float q_factor = lds.factors[parity][1][me.wave * 16 + me.c16];
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
@@ -856,16 +860,23 @@ template <int N, int MODE, bool TWO, bool OUT> __device__ __forceinline__ void w
             o = mma(lds_frag(&lds.s_hi[from]), as_frag(f.q[i]), o);
         }
         o = (o + o2) * q_factor;
+        o2 = zero;
         lds_barrier();                                            // C
         fetch_q(f);
 #pragma unroll
         for (int i = 0; i < kX; ++i) {
             const int from = me.of_lane(i);
-            const bf16x8 rh = lds_frag(&lds.r_hi[from]), rm = lds_frag(&lds.r_mid[from]);
-            o = mma(rm, as_frag(f.mx[0][i]), o);
-            o = mma(rh, as_frag(f.mx[1][i]), o);
-            o = mma(rh, as_frag(f.mx[0][i]), o);
+            const bf16x8 rh = lds_frag(&lds.r_hi[from]), rm = lds_frag(&lds.r_mid[from]), rl = lds_frag(&lds.r_lo[from]);
+            const bf16x8 xh = as_frag(mx[0][i]), xm = as_frag(mx[1][i]), xl = as_frag(mx[2][i]);
+            o2 = mma(rh, xl, o2);
+            o = mma(rh, xm, o);
+            o2 = mma(rl, xh, o2);
+            o = mma(rm, xh, o);
+            o2 = mma(rm, xm, o2);
+            o = mma(rh, xh, o);
         }
+        fetch_mx();
+        o += o2;
         // a lane has a token's four channels 4 g4 ..: to the order of the rows, within the wavefront
         *reinterpret_cast<f32x4_t *>(&lds.o[me.wave][me.c16 * 16 + 4 * me.g4]) = o;
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
