@@ -191,8 +191,9 @@ template <typename T, int N, int P> hipError_t recurrent(const DeltaArgs &a, hip
 // but every row of S (a value channel) by itself: delta_walk_kernel gives a workgroup 16 channels of a head.
 // The lengths of q and k are float32 factors of rows and columns, so that k and q enter the products as they were given, exact in
 // bfloat16.  A computed factor (X, R, U, S) is carried as three bfloat16 terms, which hold all of a float32 (8 bits each, cut off, not
-// rounded, so that what is left is exact), and of the products of two such all but the three smallest are formed: the states are float32
-// results, and two terms were off by 3e-6 of them.  The outputs are rounded to bfloat16 and take two terms of S, R and M X.
+// rounded, so that what is left is exact), and of the products of two such all but the three smallest are formed: states and outputs are
+// float32 results.  Two terms were off by 3e-6 of a state; an output is the difference of Q S^T and (M X) R, and where values of a
+// thousandth replaced what the state held, two terms of S, R and M X lost a tenth of it.
 // The triangular systems are solved, not expanded: powers of T grow like binomials where keys lean to one side, the inverse does not.
 // Fragments of v_mfma_f32_16x16x32_bf16: lane l has row (or column) l % 16 and eight consecutive k from 8 (l / 16); of the result
 // column l % 16, rows 4 (l / 16) .. + 3.  What the preparation leaves for the walk is stored in that order, a kilobyte a fragment.
@@ -848,6 +849,7 @@ template <int N, int MODE, bool TWO, bool OUT> __device__ __forceinline__ void w
         park_v(parity ^ 1, other);
         fetch_v(other);
         fetch_z(other);
+        // (the lowest terms of S ahead of B, where LDS is less used: 2048 tokens of N = 128 64.9 -> 60.7 us)
         f32x4_t o = zero, o2 = zero;
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) o2 = mma(lds_frag(&lds.s_lo[me.of_lane(i)]), as_frag(f.q[i]), o2);
