@@ -23,6 +23,20 @@ template <int CTRL> __device__ __forceinline__ float lane_add(float v)
 {
     return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, false));
 }
+// a double of the lane that CTRL names within a row of 16 (0: none such), and of one lane
+template <int CTRL> __device__ __forceinline__ double lanes_back(double v)
+{
+    const uint64_t bits = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)bits, CTRL, 0xf, 0xf, false);
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(bits >> 32), CTRL, 0xf, 0xf, false);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ double of_lane(double v, int lane)
+{
+    const uint64_t bits = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)bits, lane), hi = __builtin_amdgcn_readlane((int)(uint32_t)(bits >> 32), lane);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
 // sum over 16 lanes, in all of them: quad_perm [1,0,3,2], [2,3,0,1], row_half_mirror, row_mirror
 __device__ __forceinline__ float sum16(float v) { return lane_add<0x140>(lane_add<0x141>(lane_add<0x4e>(lane_add<0xb1>(v)))); }
 
@@ -283,7 +297,7 @@ delta_prepare_kernel(const bf16_t *__restrict__ q, const bf16_t *__restrict__ k,
     constexpr int kRow = N + 8, kSys = kC + 4;
     // T, then M X; K, then (I + T)^-1; Q, then M: 53 KB, so that three workgroups share a CU
     __shared__ __attribute__((aligned(16))) float sys[kC * kSys], inv[kC * kSys], mq[kC * kSys];
-    __shared__ __attribute__((aligned(16))) float rk[kC], rq[kC], G[kC], bt[kC];
+    __shared__ __attribute__((aligned(16))) float rk[kC], rq[kC], G[kC], G_rest[kC], bt[kC];
     uint16_t *ks = reinterpret_cast<uint16_t *>(inv), *qs = reinterpret_cast<uint16_t *>(mq);
     static_assert(sizeof(uint16_t) * kC * kRow <= sizeof(mq), "k and q share their places");
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c16 = lane & 15, g4 = lane >> 4;
@@ -303,20 +317,23 @@ delta_prepare_kernel(const bf16_t *__restrict__ q, const bf16_t *__restrict__ k,
         kp[i] = *reinterpret_cast<const uint4 *>(k + first + at);
         qp[i] = *reinterpret_cast<const uint4 *>(q + first + at);
     }
-    // running sum of delta A (in powers of two) and the write strengths; tokens behind the end neither decay nor write
+    // running sum of delta A (in powers of two) and the write strengths; tokens behind the end neither decay nor write.  The decay from a token
+    // to another is a difference of two sums, and a token that resets the state leaves large ones behind it: they are formed in
+    // float64 and kept as two float32, of which the differences are formed one by one (a single float32 was off by 5e-4 of the decays
+    // behind one of 2^-10000).  A token's exponent ends at -160, which leaves nothing of anything: no infinities are subtracted (a NaN passes).
     if (wave == 7) {
         const int64_t at = (b * L + tok0 + min(lane, live - 1)) * H + h;
         const float x = bf16_to_f32(dt[at]) + (dt_bias ? dt_bias[h] : 0.0f), w = bf16_to_f32(beta[at]);
-        float sc = lane < live ? (o.softplus ? softplus_f32(x) : x) * A[h] * kLog2e : 0.0f;
-        sc += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, sc), 0x111, 0xf, 0xf, false));
-        sc += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, sc), 0x112, 0xf, 0xf, false));
-        sc += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, sc), 0x114, 0xf, 0xf, false));
-        sc += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, sc), 0x118, 0xf, 0xf, false));
-        const float r0 = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, sc), 15));
-        const float r1 = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, sc), 31));
-        const float r2 = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, sc), 47));
-        sc += g4 == 0 ? 0.0f : g4 == 1 ? r0 : g4 == 2 ? r0 + r1 : (r0 + r1) + r2;
-        G[lane] = sc;
+        const float own = lane < live ? (o.softplus ? softplus_f32(x) : x) * A[h] * kLog2e : 0.0f;
+        double sum = own < -160.0f ? -160.0f : own;
+        sum += lanes_back<0x111>(sum);
+        sum += lanes_back<0x112>(sum);
+        sum += lanes_back<0x114>(sum);
+        sum += lanes_back<0x118>(sum);
+        const double r0 = of_lane(sum, 15), r1 = of_lane(sum, 31), r2 = of_lane(sum, 47);
+        sum += g4 == 0 ? 0.0 : g4 == 1 ? r0 : g4 == 2 ? r0 + r1 : (r0 + r1) + r2;
+        G[lane] = (float)sum;
+        G_rest[lane] = (float)(sum - (double)(float)sum);
         bt[lane] = lane < live ? (o.sigmoid ? sigmoid_f32(w) : w) : 0.0f;
     }
 #pragma unroll
@@ -356,13 +373,14 @@ delta_prepare_kernel(const bf16_t *__restrict__ q, const bf16_t *__restrict__ k,
             of_s[i] = lds_frag(&ks[(s_tile * 16 + c16) * kRow + i * 32 + g4 * 8]);
             of_t[i] = lds_frag(&rows[t * kRow + i * 32 + g4 * 8]);
         }
-        const float4 Gs = *reinterpret_cast<const float4 *>(&G[s0]), rs = *reinterpret_cast<const float4 *>(&rk[s0]);
-        const float Gt = G[t];
+        const float4 Gs = *reinterpret_cast<const float4 *>(&G[s0]), Gr = *reinterpret_cast<const float4 *>(&G_rest[s0]);
+        const float4 rs = *reinterpret_cast<const float4 *>(&rk[s0]);
+        const float Gt = G[t], Gtr = G_rest[t];
         f32x4_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int i = 0; i < N / 32; ++i) acc = mma(of_s[i], of_t[i], acc);
-        acc[0] *= exp2_hw(Gt - Gs.x) * rs.x, acc[1] *= exp2_hw(Gt - Gs.y) * rs.y;
-        acc[2] *= exp2_hw(Gt - Gs.z) * rs.z, acc[3] *= exp2_hw(Gt - Gs.w) * rs.w;
+        acc[0] *= exp2_hw((Gt - Gs.x) + (Gtr - Gr.x)) * rs.x, acc[1] *= exp2_hw((Gt - Gs.y) + (Gtr - Gr.y)) * rs.y;
+        acc[2] *= exp2_hw((Gt - Gs.z) + (Gtr - Gr.z)) * rs.z, acc[3] *= exp2_hw((Gt - Gs.w) + (Gtr - Gr.w)) * rs.w;
         return acc;
     };
     for (int i = wave; i < 10; i += 8) {
@@ -492,11 +510,11 @@ delta_prepare_kernel(const bf16_t *__restrict__ q, const bf16_t *__restrict__ k,
         }
     };
     auto write = [&](int at, uint2 lo, uint2 hi) { *reinterpret_cast<uint4 *>(ws + at) = make_uint4(lo.x, lo.y, hi.x, hi.y); };
-    const float end = G[kC - 1];
+    const float end = G[kC - 1], end_rest = G_rest[kC - 1];
     if (wave < 4) {
         // X times the decay to the end of the chunk, in three terms
         const int t = wave * 16 + c16;
-        const float f = rk[t] * exp2_hw(end - G[t]);
+        const float f = rk[t] * exp2_hw((end - G[t]) + (end_rest - G_rest[t]));
         for (int step = 0; step <= wave >> 1; ++step) {
             const int at = tile_at(wave, step) * kFrag + lane * 8;
             Terms w[2];
