@@ -51,21 +51,24 @@ class MambaDrafter:
         if not repetition > 0:
             raise ValueError("repetition must be above zero, got %r" % (repetition,))
         words = (self.V + 31) // 32
-        if self._rules is None:
-            full = lambda *shape: torch.full(shape, -1, dtype=torch.int32, device=self.dev)
-            self._rules = dict(counts=torch.zeros((1, self.V), dtype=torch.int32, device=self.dev),
-                               penalties=torch.empty((1, 3), dtype=torch.float32, device=self.dev),
-                               bias=torch.empty((self.V,), dtype=torch.float32, device=self.dev),
-                               masks=[full(1, words) for _ in range(m.MAMBA_MAX_DEPTH)])
-            for bufs in self._trees.values():
-                bufs["constrained_graph"] = None         # (of buffers that were dropped)
-        r = self._rules
-        mask = None if mask is None else mask.reshape(-1, mask.shape[-1])
+        # (everything is checked before anything changes: a call that is refused leaves the rules, or their absence, as they were)
         if bias is not None and tuple(bias.shape) != (self.V,):
             raise ValueError("bias must have shape %s, got %s" % ((self.V,), tuple(bias.shape)))
-        if mask is not None and (mask.dtype != torch.int32 or mask.shape[1] != words or not 1 <= mask.shape[0] <= m.MAMBA_MAX_DEPTH):
-            raise ValueError("mask must be int32 with %d words a row and 1 to %d rows" % (words, m.MAMBA_MAX_DEPTH))
-        r["penalties"].copy_(torch.tensor([[repetition, presence, frequency]], dtype=torch.float32))
+        if mask is not None:
+            if mask.dim() == 0 or mask.dtype != torch.int32 or mask.shape[-1] != words or not 1 <= mask.numel() // words <= m.MAMBA_MAX_DEPTH:
+                raise ValueError("mask must be int32 with %d words a row and 1 to %d rows" % (words, m.MAMBA_MAX_DEPTH))
+            mask = mask.reshape(-1, words)
+        penalties = torch.tensor([[repetition, presence, frequency]], dtype=torch.float32)
+        if self._rules is None:
+            rules = dict(counts=torch.zeros((1, self.V), dtype=torch.int32, device=self.dev),
+                         penalties=penalties.to(self.dev),
+                         bias=torch.zeros((self.V,), dtype=torch.float32, device=self.dev),
+                         masks=[torch.full((1, words), -1, dtype=torch.int32, device=self.dev) for _ in range(m.MAMBA_MAX_DEPTH)])
+            for bufs in self._trees.values():
+                bufs["constrained_graph"] = None         # (of buffers that were dropped)
+            self._rules = rules
+        r = self._rules
+        r["penalties"].copy_(penalties)
         r["bias"].zero_() if bias is None else r["bias"].copy_(bias)
         for i, row in enumerate(r["masks"]):
             row.fill_(-1) if mask is None else row[0].copy_(mask[min(i, mask.shape[0] - 1)])
