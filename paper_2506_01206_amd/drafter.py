@@ -41,8 +41,8 @@ class MambaDrafter:
     def constrain(self, repetition=1.0, presence=0.0, frequency=0.0, bias=None, mask=None):
         """Draft under the rules that the verifier decodes by: penalties for repeated tokens, bias (V) f32 on the logits, mask int32
         (ceil(V/32)) or (positions, ceil(V/32)) with a set bit where a token is allowed (the last row holds for deeper positions).  The
-        next ``prefill`` takes its tokens as the prompt, ``observe`` adds what was generated since; tokens on the way from the root of
-        the tree count as generated.  A branch that may take fewer tokens than the tree has children there gets token -1 for the
+        next ``prefill`` counts its tokens, as the prompt or as generated, ``observe`` adds what was generated since; tokens on the way from
+        the root of the tree count as generated.  A branch that may take fewer tokens than the tree has children there gets token -1 for the
         others, whose own descendants are of no use.  Calling it again changes the rules in place (captured rounds follow); None for
         ``repetition`` drops them."""
         if repetition is None:
@@ -74,19 +74,22 @@ class MambaDrafter:
             row.fill_(-1) if mask is None else row[0].copy_(mask[min(i, mask.shape[0] - 1)])
 
     def observe(self, tokens):
-        """Tokens (int32[n]) that were generated behind the prompt: what was accepted, not what was drafted."""
+        """Tokens (int32[n]) that were generated behind those of the last ``prefill``: what was accepted, not what was drafted.  They count
+        until the next ``prefill``, which counts its own tokens anew."""
         if self._rules is None:
             raise RuntimeError("observe() is for a drafter under rules: call constrain() first")
         m.mamba_token_counts(tokens.view(1, -1), self.V, counts=self._rules["counts"])
 
     # ------------------------------------------------------------------ prefix encoding
-    def prefill(self, tokens):
+    def prefill(self, tokens, prompt_len=None):
         """Encode a prefix (int32[L]); returns the logits of the next token (1, V) and keeps the
-        per-layer states of the prefix as the root of later draft trees."""
+        per-layer states of the prefix as the root of later draft trees.  Under rules (``constrain``) its first
+        ``prompt_len`` tokens (None: all of them) count as the prompt, the others as generated: a prefix that is
+        encoded again with what was accepted since is ``prefill(prompt_and_accepted, prompt_len=len(prompt))``."""
         L = tokens.shape[0]
-        if self._rules is not None:
-            self._rules["counts"].zero_()
-            m.mamba_token_counts(tokens.view(1, -1), self.V, counts=self._rules["counts"], prompt=True)
+        n_prompt = L if prompt_len is None else int(prompt_len)
+        if not 0 <= n_prompt <= L:
+            raise ValueError("prompt_len must be from 0 to %d, got %r" % (L, prompt_len))
         hid = m.mamba_embedding_fwd(tokens, self.embedding).view(1, L, self.dm)
         ws = torch.empty(max(m.mamba_block_workspace_bytes(self.blocks[0], 1, L), 16), dtype=torch.uint8, device=self.dev)
         for l, blk in enumerate(self.blocks):
@@ -94,6 +97,12 @@ class MambaDrafter:
                               workspace=ws)
         last = m.mamba_rmsnorm_fwd(hid[0, L - 1:L].contiguous(), self.norm_f, self.eps)
         m.mamba_linear_fwd(last, self.lm_head, outs=[self.root_logits])
+        if self._rules is not None:
+            counts = self._rules["counts"]
+            counts.zero_()
+            m.mamba_token_counts(tokens[:n_prompt].view(1, -1), self.V, counts=counts, prompt=True)
+            if n_prompt < L:                             # (a copy: the call takes aligned tokens)
+                m.mamba_token_counts(tokens[n_prompt:].clone().view(1, -1), self.V, counts=counts)
         return self.root_logits
 
     # ------------------------------------------------------------------ tree drafting

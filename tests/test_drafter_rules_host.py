@@ -1,4 +1,4 @@
-"""MambaDrafter.constrain without a GPU: what it refuses changes nothing.  The drafter's buffers are host tensors here, no kernel is called."""
+"""MambaDrafter.constrain and prefill without a GPU: what they refuse changes nothing.  The drafter's buffers are host tensors here, no kernel is called."""
 import os
 from types import SimpleNamespace
 
@@ -61,3 +61,20 @@ def test_rules_as_they_are_set(drafter):
     assert all(torch.equal(x[0], torch.arange(WORDS, dtype=torch.int32)) for x in r["masks"]) and bool((r["bias"] == 0).all())
     drafter.constrain(None)
     assert drafter._rules is None
+
+
+@pytest.mark.parametrize("prompt_len", [-1, 6, 10 ** 9])
+def test_a_prompt_longer_than_the_prefix_is_refused(drafter, prompt_len):
+    drafter.constrain()
+    drafter._rules["counts"].fill_(3)
+    with pytest.raises(ValueError, match="prompt_len"):
+        drafter.prefill(torch.zeros(5, dtype=torch.int32), prompt_len=prompt_len)
+    assert bool((drafter._rules["counts"] == 3).all())
+
+
+def test_a_refused_prefix_leaves_the_counts(drafter):
+    drafter.constrain()
+    drafter._rules["counts"].fill_(3)
+    with pytest.raises(ValueError, match="GPU"):
+        drafter.prefill(torch.zeros(5, dtype=torch.int32))
+    assert bool((drafter._rules["counts"] == 3).all())
