@@ -423,8 +423,9 @@ int mamba2_state_step(float *h_out, const float *h_in, const int32_t *parent_idx
  * mamba_gated_delta_step advances n_out draft branches by one token (q, k (n_out, Hk, N); v, z, out (n_out, H, P); dt, beta
  * (n_out, H); h_in (n_in, H, P, N), h_out (n_out, H, P, N)); branch j continues from h_in[parent_idx[j]] (device int32[n_out]; NULL:
  * h_in[j], n_in == n_out, and then h_out may be h_in); an index outside [0, n_in) reads nothing and gives NaN for that branch.
- * A NaN or an infinity in the inputs of a token reaches the state from there on, as the equations have it, and may reach the outputs
- * of up to 63 tokens ahead of it.  batch, H, n_out <= 65535; batch * H <= 2^19; L <= 2^31.
+ * A NaN or an infinity in the inputs of a token reaches what the equations take it to, as NaN where they may have an infinity; what is
+ * ahead of the token does not change.  A decay of exp(-infinity) is a reset of the state.
+ * batch, H, n_out <= 65535; batch * H <= 2^19; L <= 2^31.
  */
 size_t mamba_gated_delta_workspace_bytes(int64_t batch, int64_t L, int64_t H, int64_t Hk, int64_t P, int64_t N);
 int mamba_gated_delta_fwd(const void *q, const void *k, const void *v, const void *dt, const float *A, const void *beta,

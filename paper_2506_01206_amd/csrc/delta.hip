@@ -63,6 +63,7 @@ __device__ __forceinline__ void unpack4(uint2 w, float *v)
     v[0] = bf16_lo(w.x), v[1] = bf16_hi(w.x), v[2] = bf16_lo(w.y), v[3] = bf16_hi(w.y);
 }
 
+__device__ __forceinline__ bool finite(float v) { return __builtin_isfinite(v); }
 __device__ __forceinline__ float sigmoid_f32(float v) { return rcp_hw(1.0f + exp2_hw(-v * kLog2e)); }
 
 // ---------------------------------------------------------------------------------------------------
@@ -334,7 +335,8 @@ delta_prepare_kernel(const bf16_t *__restrict__ q, const bf16_t *__restrict__ k,
         sum += g4 == 0 ? 0.0 : g4 == 1 ? r0 : g4 == 2 ? r0 + r1 : (r0 + r1) + r2;
         G[lane] = (float)sum;
         G_rest[lane] = (float)(sum - (double)(float)sum);
-        bt[lane] = lane < live ? (o.sigmoid ? sigmoid_f32(w) : w) : 0.0f;
+        const float b = lane < live ? (o.sigmoid ? sigmoid_f32(w) : w) : 0.0f;
+        bt[lane] = finite((float)sum) ? b : __int_as_float(0x7fc00000);
     }
 #pragma unroll
     for (int i = 0; i < kMine; ++i) {
@@ -349,18 +351,22 @@ delta_prepare_kernel(const bf16_t *__restrict__ q, const bf16_t *__restrict__ k,
         const int t_tile = wave & 3, t = t_tile * 16 + c16;
         const uint16_t *rows = wave < 4 ? ks : qs;
         f32x4_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (o.qk_norm) {
 #pragma unroll
-            for (int i = 0; i < N / 32; ++i) {
-                const bf16x8 f = lds_frag(&rows[t * kRow + i * 32 + g4 * 8]);
-                acc = mma(f, f, acc);
-            }
+        for (int i = 0; i < N / 32; ++i) {
+            const bf16x8 f = lds_frag(&rows[t * kRow + i * 32 + g4 * 8]);
+            acc = mma(f, f, acc);
         }
         const float square = (c16 & 2) ? (c16 & 1) ? acc[3] : acc[2] : (c16 & 1) ? acc[1] : acc[0];
         const float inverse = t >= live ? 0.0f : o.qk_norm ? 1.0f / sqrtf(square + o.eps) : 1.0f;
-        if (g4 == c16 >> 2) (wave < 4 ? rk : rq)[t] = wave < 4 ? inverse : inverse * o.scale;
+        if (g4 == c16 >> 2) (wave < 4 ? rk : rq)[t] = wave >= 4 ? inverse * o.scale : finite(square) ? inverse : __int_as_float(0x7fc00000);
     }
     lds_barrier();
+    // From the first token on whose key, decay or write strength is not a number the state is none either, and so are the outputs: such tokens
+    // are left out of the chunk's systems, where products with the zeros above a diagonal would take them to the tokens ahead, and their
+    // factors say so.  (A query is a row of its own, a value a channel: the walk sees to it.)
+    const uint64_t no_key = __ballot(!finite(rk[lane])), none = no_key | __ballot(!finite(bt[lane]));
+    const int good = none ? __builtin_ctzll(none) : kC, keys = no_key ? __builtin_ctzll(no_key) : kC;
+    auto row_end = [&](int t, int end) { return t < good ? end : 0; };
 
     // T and M, tile by tile of 16 x 16: lane has token t = l % 16 of the tile and four s.  The ten tiles of a lower triangle by number:
     // row 0 of tiles, row 1, ...
@@ -388,7 +394,7 @@ delta_prepare_kernel(const bf16_t *__restrict__ q, const bf16_t *__restrict__ k,
         f32x4_t v = tile(ks, t_tile, s_tile);
         const float f = bt[t] * rk[t];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = s0 + j < t ? v[j] * f : 0.0f;
+        for (int j = 0; j < 4; ++j) v[j] = s0 + j < row_end(t, t) ? v[j] * f : 0.0f;
         *reinterpret_cast<f32x4_t *>(&sys[t * kSys + s0]) = v;
     }
     lds_barrier();
@@ -412,20 +418,24 @@ delta_prepare_kernel(const bf16_t *__restrict__ q, const bf16_t *__restrict__ k,
             m[j] = tile(qs, t_tile, s_tile);
             const float f = rq[t];
 #pragma unroll
-            for (int n = 0; n < 4; ++n) m[j][n] = s0 + n <= t ? m[j][n] * f : 0.0f;
+            for (int n = 0; n < 4; ++n) m[j][n] = s0 + n < row_end(t, t + 1) ? m[j][n] * f : 0.0f;
         }
         // keys and queries as the fragments that the walk takes: once for the value heads that share them
         if (h % group == 0) {
             uint16_t *to = frags + ((b * Hk + hk) * n_chunks + chunk) * kKeyHalves<N> + lane * 8;
             for (int f = wave - 1; f < N / 8; f += 7) {
                 // K: rows are tokens, columns the states of the walk's wavefront f / (N / 32); with 64 states two tiles of tokens side by side
+                // (none of those from the first on that is not a number)
                 uint4 piece;
                 if constexpr (N == 128) {
                     piece = *reinterpret_cast<const uint4 *>(&ks[((f & 3) * 16 + c16) * kRow + (f >> 2) * 32 + 8 * g4]);
+                    if ((f & 3) * 16 + c16 >= keys) piece = make_uint4(0, 0, 0, 0);
                 } else {
                     const uint16_t *at = &ks[((f & 1) * 32 + c16) * kRow + (f >> 1) * 16 + 4 * g4];
                     const uint2 lo = *reinterpret_cast<const uint2 *>(at), hi = *reinterpret_cast<const uint2 *>(at + 16 * kRow);
                     piece = make_uint4(lo.x, lo.y, hi.x, hi.y);
+                    if ((f & 1) * 32 + c16 >= keys) piece.x = piece.y = 0;
+                    if ((f & 1) * 32 + 16 + c16 >= keys) piece.z = piece.w = 0;
                 }
                 *reinterpret_cast<uint4 *>(to + f * kFrag) = piece;
                 // Q: rows are tokens, columns states
@@ -505,7 +515,7 @@ delta_prepare_kernel(const bf16_t *__restrict__ q, const bf16_t *__restrict__ k,
             f32x4_t v = *reinterpret_cast<const f32x4_t *>(&rows[t * kSys + s0 + 4 * i]);
             const f32x4_t strength = *reinterpret_cast<const f32x4_t *>(&bt[s0 + 4 * i]);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = s0 + 4 * i + j <= t ? v[j] * strength[j] * f : 0.0f;
+            for (int j = 0; j < 4; ++j) v[j] = s0 + 4 * i + j < row_end(t, t + 1) ? v[j] * strength[j] * f : 0.0f;
             w[i] = terms_of(v);
         }
     };
@@ -531,7 +541,9 @@ delta_prepare_kernel(const bf16_t *__restrict__ q, const bf16_t *__restrict__ k,
     } else if (wave == 6) {
         out_block(2, 0);
         const float e = exp2_hw(G[lane]);
-        reinterpret_cast<float4 *>(ws + kAtScalars)[lane] = make_float4(rk[lane] * e, rq[lane] * e, exp2_hw(end), 0.0f);
+        const float nan = __int_as_float(0x7fc00000);
+        reinterpret_cast<float4 *>(ws + kAtScalars)[lane] =
+            make_float4(lane < good ? rk[lane] * e : 0.0f, lane < good ? rq[lane] * e : nan, good == kC ? exp2_hw(end) : nan, 0.0f);
     } else {
         out_block(1, 0), out_block(2, 1);
     }
@@ -580,6 +592,8 @@ template <int N> struct __attribute__((aligned(16))) WalkLds {
     uint16_t v[2][16 * kRowV];                                    // V, [channel][token], two chunks
     float factors[2][3][kC];                                      // of the rows of K S^T and of Q S^T; the chunk's decay
     float o[4][16 * 16];                                          // a wavefront's outputs, [token][channel]
+    int ended[4];                                                 // has a wavefront come by a value that is not a number
+    int ends[16];                                                 // if one has: a channel's first token (of the part) with such a value
 };
 // Where a workgroup and a lane are.
 template <int N> struct WalkPlace {
@@ -609,6 +623,11 @@ template <typename T> struct Cursor {
         left -= left > 0;
     }
 };
+
+template <int N> __device__ __forceinline__ bool any_ended(const WalkLds<N> &lds)
+{
+    return __builtin_amdgcn_readfirstlane(lds.ended[0] | lds.ended[1] | lds.ended[2] | lds.ended[3]) != 0;
+}
 
 // TWO: the wavefront's row of tiles has two fragments of 32 columns (wavefronts 2 and 3)
 template <int N, bool TWO> __device__ __forceinline__ void walk_chain(const WalkArgs &a, const WalkPlace<N> &me, WalkLds<N> &lds)
@@ -772,6 +791,13 @@ template <int N, bool TWO> __device__ __forceinline__ void walk_chain(const Walk
         step(1);
     }
     if (left > 0) step(0);
+    lds_barrier();                                                // (a value that is not a number: the other role says whether, and then where)
+    if (any_ended(lds)) {
+        __syncthreads();
+        if (lds.ends[me.c16] != INT32_MAX)
+#pragma unroll
+            for (int j = 0; j < kNT; ++j) acc[j] = zero + __int_as_float(0x7fc00000);
+    }
     if (me.h_final)
 #pragma unroll
         for (int j = 0; j < kNT; ++j)
@@ -793,18 +819,17 @@ template <int N, int MODE, bool TWO, bool OUT> __device__ __forceinline__ void w
     const uint32_t value_at = (uint32_t)t_own * me.value_row + (uint32_t)p_own, value_last = min((uint32_t)t_own, live - 1) * me.value_row + (uint32_t)p_own;
     const int64_t first = ((me.b * a.L + me.tok0) * a.H + me.h) * a.P + me.p0, chunk_values = (int64_t)kC * me.value_row;
     struct Operands {
-        uint4 q[kSteps];
         uint2 z, v;
         float factor;                                             // number lane % 4 of token lane / 4
     };
-    uint4 mx[3][kX];                                              // (one set: the next chunk's are requested when this one's have been used)
+    uint4 q[kSteps], mx[3][kX];                                   // (one set: the next chunk's are requested when this one's have been used)
     Cursor<uint16_t> queries{me.frags + N * kC + me.wave * kSteps * kFrag, kKeyHalves<N>, n_chunks - 1};
     Cursor<bf16_t> values{a.v + first, chunk_values, n_chunks - 1}, gates{MODE == kWalkGate ? a.z + first : nullptr, chunk_values, n_chunks - 1};
     Cursor<uint16_t> xs{me.own + kAtMX, kChunkHalves, n_chunks - 1};
     Cursor<float> factors{reinterpret_cast<const float *>(me.own + kAtScalars) + me.wave * 64, kChunkHalves / 2, n_chunks - 1};
-    auto fetch_q = [&](Operands &f) {
+    auto fetch_q = [&]() {
 #pragma unroll
-        for (int i = 0; i < kSteps; ++i) f.q[i] = *reinterpret_cast<const uint4 *>(queries.p + i * kFrag + lane8);
+        for (int i = 0; i < kSteps; ++i) q[i] = *reinterpret_cast<const uint4 *>(queries.p + i * kFrag + lane8);
         queries.advance();
         requested();
     };
@@ -829,6 +854,21 @@ template <int N, int MODE, bool TWO, bool OUT> __device__ __forceinline__ void w
             requested();
         }
     };
+    // A value that is not a number ends its channel: the outputs are none from its token on, nor is the state at the end.  The walk takes a 0 for
+    // it, which the zeros above the diagonals of X and M X leave alone, and remembers only that there was one: 9 instructions a chunk, without a
+    // branch (one that found the token at once took 250 cycles of a chunk's 3000); ends_of_channels has the rest, seldom called.
+    uint32_t ended = 0;                                           // bits 15 and 31
+    auto number = [&](uint32_t &pair) {
+        typedef int16_t short2_t __attribute__((ext_vector_type(2)));
+        const uint32_t top = (pair & 0x7f807f80u) + 0x00800080u;  // an exponent of ones carries into the bit above it
+        pair &= ~__builtin_bit_cast(uint32_t, __builtin_bit_cast(short2_t, top) >> 15);
+        ended |= top;
+    };
+    auto numbers = [&](Operands &f) { number(f.v.x), number(f.v.y); };
+    auto say_ended = [&]() {
+        const bool some = __any((ended & 0x80008000u) != 0);
+        if (me.lane == 0) lds.ended[me.wave] = (OUT || me.unit < 0) && some;
+    };
     // V of a chunk, the other way round, and the factors of its rows
     auto park_v = [&](int parity, const Operands &f) {
         uint16_t *to = &lds.v[parity][p_own * kRowV + t_own];
@@ -836,12 +876,42 @@ template <int N, int MODE, bool TWO, bool OUT> __device__ __forceinline__ void w
         to[0] = (uint16_t)x, to[kRowV] = (uint16_t)(x >> 16), to[2 * kRowV] = (uint16_t)y, to[3 * kRowV] = (uint16_t)(y >> 16);
         if ((me.lane & 3) < 3) lds.factors[parity][me.lane & 3][t_own] = f.factor;
     };
+    // Where there were such values: each wavefront looks for the first in four of the channels, and writes their outputs anew.
+    auto ends_of_channels = [&]() {
+        const int64_t tokens = min((int64_t)n_chunks * kC, a.L - me.tok0);
+        const bf16_t *v = a.v + first + 4 * me.wave;
+        int64_t ends[4] = {tokens, tokens, tokens, tokens};
+        for (int64_t t0 = 0; t0 < tokens; t0 += 64) {
+            const int64_t t = t0 + me.lane;
+            const uint2 w = t < tokens ? *reinterpret_cast<const uint2 *>(v + t * me.value_row) : make_uint2(0, 0);
+            const float x[4] = {bf16_lo(w.x), bf16_hi(w.x), bf16_lo(w.y), bf16_hi(w.y)};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint64_t none = __ballot(!finite(x[i]));
+                if (none && ends[i] == tokens) ends[i] = t0 + __builtin_ctzll(none);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) lds.ends[4 * me.wave + i] = ends[i] < tokens ? (int)ends[i] : INT32_MAX;
+        __threadfence();                                          // the outputs as they are, of all wavefronts, are written
+        __syncthreads();
+        if constexpr (!OUT) return;
+        const int64_t at = (MODE == kWalkRaw ? ((me.b * a.n_chunks + me.first) * kC * a.H + me.h) * a.P + me.p0 : first) + 4 * me.wave;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            for (int64_t t = ends[i] + me.lane; t < tokens; t += 64) {
+                if constexpr (MODE == kWalkRaw) a.raw[at + i + t * me.value_row] = __int_as_float(0x7fc00000);
+                else a.out[at + i + t * me.value_row] = 0x7fc0;
+            }
+    };
     Operands even, odd;
     if constexpr (!OUT) {
         fetch_v(even), fetch_v(odd);
+        numbers(even);
         park_v(0, even);
         fetch_v(even);
         auto step = [&](int parity, Operands &other) __attribute__((always_inline)) {
+            numbers(other);
             lds_barrier();                                        // A
             park_v(parity ^ 1, other);
             fetch_v(other);
@@ -854,9 +924,13 @@ template <int N, int MODE, bool TWO, bool OUT> __device__ __forceinline__ void w
             step(1, even);
         }
         if (left > 0) step(0, odd);
+        say_ended();
+        lds_barrier();
+        if (any_ended(lds)) ends_of_channels();
         return;
     }
-    fetch_v(even), fetch_v(odd), fetch_q(even), fetch_q(odd), fetch_mx(), fetch_z(even);
+    fetch_v(even), fetch_v(odd), fetch_q(), fetch_mx(), fetch_z(even);
+    numbers(even), numbers(odd);
     park_v(0, even);
     fetch_v(even);
     // this lane's outputs of the chunk (ahead of a norm they go into a buffer of the slab)
@@ -870,19 +944,20 @@ template <int N, int MODE, bool TWO, bool OUT> __device__ __forceinline__ void w
         // (the lowest terms of S ahead of B, where LDS is less used: 2048 tokens of N = 128 64.9 -> 60.7 us)
         f32x4_t o = zero, o2 = zero;
 #pragma unroll
-        for (int i = 0; i < kSteps; ++i) o2 = mma(lds_frag(&lds.s_lo[me.of_lane(i)]), as_frag(f.q[i]), o2);
+        for (int i = 0; i < kSteps; ++i) o2 = mma(lds_frag(&lds.s_lo[me.of_lane(i)]), as_frag(q[i]), o2);
         lds_barrier();                                            // B (the chain is short between the two, and would wait for this role)
         const float q_factor = lds.factors[parity][1][me.wave * 16 + me.c16];
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
             const int from = me.of_lane(i);
-            o2 = mma(lds_frag(&lds.s_mid[from]), as_frag(f.q[i]), o2);
-            o = mma(lds_frag(&lds.s_hi[from]), as_frag(f.q[i]), o);
+            o2 = mma(lds_frag(&lds.s_mid[from]), as_frag(q[i]), o2);
+            o = mma(lds_frag(&lds.s_hi[from]), as_frag(q[i]), o);
         }
         o = (o + o2) * q_factor;
         o2 = zero;
         lds_barrier();                                            // C
-        fetch_q(f);
+        fetch_q();
+        numbers(f);
 #pragma unroll
         for (int i = 0; i < kX; ++i) {
             const int from = me.of_lane(i);
@@ -926,6 +1001,9 @@ template <int N, int MODE, bool TWO, bool OUT> __device__ __forceinline__ void w
     } else {
         step(0, last, even, odd);
     }
+    say_ended();
+    lds_barrier();
+    if (any_ended(lds)) ends_of_channels();
 }
 
 // Heads that leave CUs free have their slab in parts of `part` chunks, several at once: what a part makes of a state is a linear map,
