@@ -888,6 +888,10 @@ bool delta_shape_ok(int64_t H, int64_t Hk, int64_t P, int64_t N)
     return (P == 64 || P == 128) && (N == 64 || N == 128) && (H == 0 || (Hk > 0 && H % Hk == 0));
 }
 constexpr int64_t kMaxDeltaHeads = (int64_t)1 << 19;                 // batch x H: 8 workgroups of 512 threads a head, below 2^32 threads
+bool delta_context_ok(int64_t batch, int64_t L, int64_t H, int64_t Hk, int64_t P, int64_t N)
+{
+    return delta_shape_ok(H, Hk, P, N) && batch <= kMaxGridYZ && H <= kMaxGridYZ && batch * H <= kMaxDeltaHeads && L <= (int64_t)1 << 31;
+}
 struct DeltaBytes {
     int64_t key, value, head, state_in, state_out;   // a q or k, a v or out, a dt or beta tensor; the states
 };
@@ -919,7 +923,7 @@ int delta_pointers(const DeltaArgs &a, const DeltaBytes &b)
 size_t mamba_gated_delta_workspace_bytes(int64_t batch, int64_t L, int64_t H, int64_t Hk, int64_t P, int64_t N)
 {
     DeltaBytes b;
-    if (batch <= 0 || L <= 0 || H <= 0 || !delta_shape_ok(H, Hk, P, N) || !delta_bytes(batch, batch, L, H, Hk, P, N, 4, &b)) return 0;
+    if (batch <= 0 || L <= 0 || H <= 0 || !delta_context_ok(batch, L, H, Hk, P, N) || !delta_bytes(batch, batch, L, H, Hk, P, N, 4, &b)) return 0;
     return gated_delta_workspace_bytes(batch, L, H, Hk, P, N);
 }
 
@@ -933,8 +937,7 @@ int mamba_gated_delta_fwd(const void *q, const void *k, const void *v, const voi
     if (batch < 0 || L < 0 || H < 0 || Hk < 0 || P < 0 || N < 0) return MAMBA_ERR_BAD_SHAPE;
     DeltaBytes b;
     if (!delta_bytes(batch, batch, L, H, Hk, P, N, e, &b)) return MAMBA_ERR_BAD_SHAPE;
-    if (!delta_shape_ok(H, Hk, P, N) || batch > kMaxGridYZ || H > kMaxGridYZ || batch * H > kMaxDeltaHeads || L > ((int64_t)1 << 31))
-        return MAMBA_ERR_UNSUPPORTED;
+    if (!delta_context_ok(batch, L, H, Hk, P, N)) return MAMBA_ERR_UNSUPPORTED;
     if (batch == 0 || H == 0) return MAMBA_OK;
     if (L == 0) {
         if (!h_final || h_final == h0) return MAMBA_OK;
