@@ -215,13 +215,14 @@ template <typename T, int N, int P> hipError_t recurrent(const DeltaArgs &a, hip
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
-constexpr int kC = 64;                                            // tokens of a chunk
+constexpr int kC = kDeltaChunk;                                   // tokens of a chunk
 constexpr int kTiles = 6;                                         // 16 x 32 fragments of a lower triangle: 1, 1, 2, 2 to a row of tiles
 constexpr int kFrag = 512;                                        // bf16 of a fragment
 constexpr int kTri = kTiles * kFrag;
 constexpr int kScalars = 256;                                     // floats, four to a token: its factors of k S and of q S, the chunk's decay
 // 16-bit words of a chunk and head: X times the decay to the end, M X (three terms each), scalars
 constexpr int kAtMX = 3 * kTri, kAtScalars = 6 * kTri, kChunkHalves = 6 * kTri + 2 * kScalars;
+static_assert(kC == 64 && kChunkHalves == kDeltaChunkHalves, "as the workspace is planned");
 __device__ __forceinline__ int tile_at(int t_tile, int k_step) { return (t_tile < 2 ? t_tile : 2 * t_tile - 2) + k_step; }
 
 __device__ __forceinline__ bf16x8 as_frag(uint4 q) { return __builtin_bit_cast(bf16x8, q); }
@@ -1127,72 +1128,12 @@ delta_norm_kernel(const float *__restrict__ raw, const bf16_t *__restrict__ z, c
     if (at < n) *reinterpret_cast<uint2 *>(out + to * 4) = make_uint2(f32x2_to_bf16x2(y[0], y[1]), f32x2_to_bf16x2(y[2], y[3]));
 }
 
-// A long context goes in slabs of chunks, so that what the preparation leaves is still in the last-level cache (256 MB) when the walk takes
-// it, and the workspace does not grow with the context.  32768 tokens of 32 heads of 128 x 128, all launches, by a slab's bytes: 32 MB 1625 us,
-// 64 MB 1345, 128 MB 1152, 256 MB 1261, one slab 1174 (and 1.2 GB of workspace); 8191 tokens of 12 heads of N = 64, P = 128: 192, 148, 133 from
-// 128 MB on, which are one slab.
-constexpr int64_t kMostBlocks = 512;
-constexpr int64_t kSlabBytes = (int64_t)128 << 20, kSlabLeast = 8;
-// Where the parts of the workspace lie (bytes from its start): what the preparation leaves of a chunk and value head, fragments of a
-// chunk and key head, outputs ahead of their norm, the states between slabs where the caller takes none.
-struct DeltaPlan {
-    int64_t chunks, slab, part, frags_at, raw_at, state_at, parts_at, map_at, bytes;
-};
-// Workgroups of a walk on the XCD that has most: the maps go on where the other parts end, so that only where both leave more than 8 behind
-// does one XCD have one more of each.
-int64_t fullest_xcd(int64_t heads, int64_t P, int64_t N, int64_t walked, int64_t maps)
-{
-    const int64_t blocks = P / 16, map_blocks = (P + N) / 16, a = heads * walked, b = heads * maps;
-    const int64_t more = a % 8 + b % 8 > 8 ? blocks + map_blocks : b % 8 > 0 ? map_blocks : a % 8 > 0 ? blocks : 0;
-    return a / 8 * blocks + b / 8 * map_blocks + more;
-}
-// The parts of a slab of n chunks, those of the least time (us): a CU (32 to an XCD) walks one block of 16 rows at a time, a chunk in about
-// 1.1 (N = 64) or 1.25 (128), and takes 3 to begin; a part more is a step of the join; two more launches.
-// All launches of 8191 tokens, in one part | in several: 2 heads of 64 x 64 153 | 50 (16 parts), 2 of 128 x 128 158 | 77 (9), 8 of N = 64,
-// P = 64 156 | 84 (9), 8 of 128 x 128 169 | 129 (5), 12 of N = 64, P = 128 161 | 129 (3); 24 of N = 128, P = 64 have work for all CUs:
-// 233 | 305 (3).  2048 tokens: 2 heads of 64 x 64 46 | 30, 12 of N = 64, P = 128 53.5 | 51.6; 1000 tokens of 8 heads of 64 x 64 29 | 30.
-int64_t delta_parts(int64_t heads, int64_t P, int64_t N, int64_t n)
-{
-    const double chunk = N == 64 ? 1.1 : 1.25, join = N == 64 ? 0.75 : 2.0;
-    auto walks = [&](int64_t walked, int64_t maps, int64_t chunks) {
-        return (double)((fullest_xcd(heads, P, N, walked, maps) + 31) / 32) * (3.0 + chunk * (double)chunks);
-    };
-    int64_t best = 1;
-    double least = walks(1, 0, n);
-    for (int64_t parts = 3; parts <= n && heads * (P / 16) * (parts - 1) <= kMostBlocks; ++parts) {
-        const int64_t part = (n + parts - 1) / parts;
-        if ((n + part - 1) / part != parts) continue;
-        const double t = walks(1, parts - 2, part) + walks(parts - 1, 0, part) + join * (double)(parts - 2) + 6.0;
-        if (t < least) least = t, best = parts;
-    }
-    return best;
-}
-DeltaPlan delta_plan(int64_t batch, int64_t L, int64_t H, int64_t Hk, int64_t P, int64_t N)
-{
-    DeltaPlan p;
-    p.chunks = (L + kC - 1) / kC;
-    const int64_t chunk_bytes = batch * (H * (kChunkHalves * 2 + kC * P * 4) + Hk * 2 * N * kC * 2);
-    int64_t most = kSlabBytes / chunk_bytes;
-    most = most < kSlabLeast ? kSlabLeast : most;
-    const int64_t slabs = (p.chunks + most - 1) / most;
-    p.slab = (p.chunks + slabs - 1) / slabs;
-    p.frags_at = batch * H * p.slab * kChunkHalves * 2;
-    p.raw_at = p.frags_at + batch * Hk * p.slab * 2 * N * kC * 2;
-    p.state_at = p.raw_at + batch * p.slab * kC * H * P * 4;
-    const int64_t parts = delta_parts(batch * H, P, N, p.slab);   // (two are never chosen: one after the other they gain nothing)
-    p.part = (p.slab + parts - 1) / parts;
-    p.parts_at = p.state_at + (slabs > 1 ? batch * H * P * N * 4 : 0);
-    p.map_at = p.parts_at + (parts - 1) * batch * H * P * N * 4;
-    p.bytes = p.map_at + (parts > 2 ? parts - 2 : 0) * batch * H * N * N * 4;
-    return p;
-}
-
 template <int N> hipError_t walk(const WalkArgs &w, hipStream_t stream)
 {
-    const int64_t blocks = (w.heads * w.walked + 7) / 8 * 8 * (w.P / 16) + (w.heads * w.maps + 7) / 8 * 8 * ((w.P + N) / 16);
+    const int64_t blocks = delta_walk_blocks(w.heads, w.P, N, w.walked, w.maps);
     // Two workgroups fit on a CU, but each takes its time then: where a CU can be had for each, LDS that nobody uses keeps the second away
     // (8191 tokens of 12 heads of N = 64, P = 128: 145 -> 133 us; without it two go to one CU while others stay empty).
-    const unsigned alone = fullest_xcd(w.heads, w.P, N, w.walked, w.maps) <= 32 ? 40960 : 0;
+    const unsigned alone = delta_fullest_xcd(w.heads, w.P, N, w.walked, w.maps) <= 32 ? 40960 : 0;
     if (w.raw) delta_walk_kernel<N, kWalkRaw><<<(unsigned)blocks, 2 * kThreads, alone, stream>>>(w);
     else if (w.z) delta_walk_kernel<N, kWalkGate><<<(unsigned)blocks, 2 * kThreads, alone, stream>>>(w);
     else delta_walk_kernel<N, kWalkPlain><<<(unsigned)blocks, 2 * kThreads, alone, stream>>>(w);
@@ -1209,7 +1150,8 @@ template <int N> hipError_t chunked(const DeltaArgs &a, hipStream_t stream)
     const bf16_t *z = static_cast<const bf16_t *>(a.z);
     bf16_t *out = static_cast<bf16_t *>(a.out);
     for (int64_t first = 0; first < p.chunks; first += p.slab) {
-        const int64_t n = p.slab < p.chunks - first ? p.slab : p.chunks - first, tok0 = first * kC;
+        const DeltaSlab slab = delta_slab(p, first);
+        const int64_t n = slab.chunks, tok0 = first * kC;
         const bool last = first + n == p.chunks;
         delta_prepare_kernel<N><<<dim3((unsigned)n, (unsigned)a.H, (unsigned)a.rows), kPrepThreads, 0, stream>>>(
             static_cast<const bf16_t *>(a.q), static_cast<const bf16_t *>(a.k), static_cast<const bf16_t *>(a.dt), static_cast<const bf16_t *>(a.beta),
@@ -1217,10 +1159,10 @@ template <int N> hipError_t chunked(const DeltaArgs &a, hipStream_t stream)
             DeltaOptions{a.scale, a.eps, a.dt_softplus, a.beta_sigmoid, a.qk_norm});
         if (hipError_t e = hipGetLastError()) return e;
         const int64_t heads = a.rows * a.H;
-        const uint32_t parts = (uint32_t)((n + p.part - 1) / p.part);
+        const uint32_t parts = (uint32_t)slab.parts;
         float *starts = reinterpret_cast<float *>(ws + p.parts_at), *map = reinterpret_cast<float *>(ws + p.map_at);
         WalkArgs w{static_cast<const bf16_t *>(a.v), z, reinterpret_cast<const uint16_t *>(ws), frags, first == 0 ? a.h_in : state,
-                   last ? a.h_out : state, out, raw, starts, map, a.L, a.H, a.H / a.Hk, heads, tok0, n, p.part, 0, 1, parts > 2 ? parts - 2 : 0, a.P};
+                   last ? a.h_out : state, out, raw, starts, map, a.L, a.H, a.H / a.Hk, heads, tok0, n, p.part, 0, 1, (uint32_t)slab.maps, a.P};
         if (hipError_t e = walk<N>(w, stream)) return e;
         if (w.maps > 0) {
             delta_join_kernel<N><<<(unsigned)(heads * a.P / 16), 4 * N, 0, stream>>>(map, starts, heads * a.P, a.P, (int)w.maps);
@@ -1252,21 +1194,15 @@ hipError_t launch_gated_delta_step(const DeltaArgs &a, hipStream_t stream)
 #undef MAMBA_DELTA
 }
 
-// A context of a few tokens goes token after token, without a workspace: a chunk costs the same whether 1 or 64 of its tokens are there.
-// bf16, with gate and norm, token after token | in a chunk (us): 8 heads of 64 x 64: 6 tokens 8.6 | 12.2, 8: 10.6 | 12.0, 10: 12.7 | 12.1;
-// 32 heads of 128 x 128: 4: 9.8 | 13.1, 6: 13.3 | 13.2, 8: 16.8 | 13.3.  Heads for every CU make a chunk dearer: 256 of 128 x 128: 16 tokens
-// 32.5 | 36.4, 20: 39.2 | 37.0; 512 of 64 x 64: 16: 25.8 | 35.9, 24: 36.4 | 36.1; 2048 of 128 x 128: 16: 147 | 265, 24: 214 | 279.
-static bool few_tokens(int64_t batch, int64_t L, int64_t H) { return L <= (batch * H >= 256 ? 16 : 6); }
-
 size_t gated_delta_workspace_bytes(int64_t batch, int64_t L, int64_t H, int64_t Hk, int64_t P, int64_t N)
 {
-    if (few_tokens(batch, L, H)) return 0;
+    if (delta_few_tokens(batch, L, H)) return 0;
     return (size_t)delta_plan(batch, L, H, Hk, P, N).bytes;
 }
 
 hipError_t launch_gated_delta(const DeltaArgs &a, hipStream_t stream)
 {
-    if (a.io != kIoBf16 || few_tokens(a.rows, a.L, a.H)) return launch_gated_delta_step(a, stream);
+    if (a.io != kIoBf16 || delta_few_tokens(a.rows, a.L, a.H)) return launch_gated_delta_step(a, stream);
     return a.N == 64 ? chunked<64>(a, stream) : chunked<128>(a, stream);
 }
 

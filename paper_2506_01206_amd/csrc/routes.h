@@ -486,4 +486,90 @@ inline int xdt_plan(int64_t M, int64_t d_inner, int64_t dt_rank, int64_t N, unsi
     return rows;
 }
 
+// The gated-delta core (delta.hip).
+// A long context goes in slabs of chunks, so that what the preparation leaves is still in the last-level cache (256 MB) when the walk takes
+// it, and the workspace does not grow with the context.  32768 tokens of 32 heads of 128 x 128, all launches, by a slab's bytes: 32 MB 1625 us,
+// 64 MB 1345, 128 MB 1152, 256 MB 1261, one slab 1174 (and 1.2 GB of workspace); 8191 tokens of 12 heads of N = 64, P = 128: 192, 148, 133 from
+// 128 MB on, which are one slab.
+// (a chunk's tokens, and what the preparation leaves of a chunk and value head in 16-bit words: X and M X in three terms each, 6 fragments of 512 to
+// a term, and 256 floats)
+constexpr int64_t kDeltaChunk = 64, kDeltaChunkHalves = 2 * 3 * 6 * 512 + 2 * 256;
+constexpr int64_t kDeltaMostBlocks = 512;
+constexpr int64_t kDeltaSlabBytes = (int64_t)128 << 20, kDeltaSlabLeast = 8;
+// Where the parts of the workspace lie (bytes from its start): what the preparation leaves of a chunk and value head, fragments of a
+// chunk and key head, outputs ahead of their norm, the states between slabs where the caller takes none.
+struct DeltaPlan {
+    int64_t chunks, slab, part, frags_at, raw_at, state_at, parts_at, map_at, bytes;
+};
+// Workgroups of a walk on the XCD that has most: the maps go on where the other parts end, so that only where both leave more than 8 behind
+// does one XCD have one more of each.
+inline int64_t delta_fullest_xcd(int64_t heads, int64_t P, int64_t N, int64_t walked, int64_t maps)
+{
+    const int64_t blocks = P / 16, map_blocks = (P + N) / 16, a = heads * walked, b = heads * maps;
+    const int64_t more = a % 8 + b % 8 > 8 ? blocks + map_blocks : b % 8 > 0 ? map_blocks : a % 8 > 0 ? blocks : 0;
+    return a / 8 * blocks + b / 8 * map_blocks + more;
+}
+// The parts of a slab of n chunks, those of the least time (us): a CU (32 to an XCD) walks one block of 16 rows at a time, a chunk in about
+// 1.1 (N = 64) or 1.25 (128), and takes 3 to begin; a part more is a step of the join; two more launches.
+// All launches of 8191 tokens, in one part | in several: 2 heads of 64 x 64 153 | 50 (16 parts), 2 of 128 x 128 158 | 77 (9), 8 of N = 64,
+// P = 64 156 | 84 (9), 8 of 128 x 128 169 | 129 (5), 12 of N = 64, P = 128 161 | 129 (3); 24 of N = 128, P = 64 have work for all CUs:
+// 233 | 305 (3).  2048 tokens: 2 heads of 64 x 64 46 | 30, 12 of N = 64, P = 128 53.5 | 51.6; 1000 tokens of 8 heads of 64 x 64 29 | 30.
+inline int64_t delta_parts(int64_t heads, int64_t P, int64_t N, int64_t n)
+{
+    const double chunk = N == 64 ? 1.1 : 1.25, join = N == 64 ? 0.75 : 2.0;
+    auto walks = [&](int64_t walked, int64_t maps, int64_t chunks) {
+        return (double)((delta_fullest_xcd(heads, P, N, walked, maps) + 31) / 32) * (3.0 + chunk * (double)chunks);
+    };
+    int64_t best = 1;
+    double least = walks(1, 0, n);
+    for (int64_t parts = 3; parts <= n && heads * (P / 16) * (parts - 1) <= kDeltaMostBlocks; ++parts) {
+        const int64_t part = (n + parts - 1) / parts;
+        if ((n + part - 1) / part != parts) continue;
+        const double t = walks(1, parts - 2, part) + walks(parts - 1, 0, part) + join * (double)(parts - 2) + 6.0;
+        if (t < least) least = t, best = parts;
+    }
+    return best;
+}
+inline DeltaPlan delta_plan(int64_t batch, int64_t L, int64_t H, int64_t Hk, int64_t P, int64_t N)
+{
+    DeltaPlan p;
+    p.chunks = (L + kDeltaChunk - 1) / kDeltaChunk;
+    const int64_t chunk_bytes = batch * (H * (kDeltaChunkHalves * 2 + kDeltaChunk * P * 4) + Hk * 2 * N * kDeltaChunk * 2);
+    int64_t most = kDeltaSlabBytes / chunk_bytes;
+    most = most < kDeltaSlabLeast ? kDeltaSlabLeast : most;
+    const int64_t slabs = (p.chunks + most - 1) / most;
+    p.slab = (p.chunks + slabs - 1) / slabs;
+    p.frags_at = batch * H * p.slab * kDeltaChunkHalves * 2;
+    p.raw_at = p.frags_at + batch * Hk * p.slab * 2 * N * kDeltaChunk * 2;
+    p.state_at = p.raw_at + batch * p.slab * kDeltaChunk * H * P * 4;
+    const int64_t parts = delta_parts(batch * H, P, N, p.slab);   // (two are never chosen: one after the other they gain nothing)
+    p.part = (p.slab + parts - 1) / parts;
+    p.parts_at = p.state_at + (slabs > 1 ? batch * H * P * N * 4 : 0);
+    p.map_at = p.parts_at + (parts - 1) * batch * H * P * N * 4;
+    p.bytes = p.map_at + (parts > 2 ? parts - 2 : 0) * batch * H * N * N * 4;
+    return p;
+}
+
+// The slab that begins with chunk `first`: its chunks, the parts it is walked in, and how many of those from the second on for their maps of the
+// state.  (The last slab may be shorter: fewer parts, of the same length.)
+struct DeltaSlab {
+    int64_t chunks, parts, maps;
+};
+inline DeltaSlab delta_slab(const DeltaPlan &p, int64_t first)
+{
+    const int64_t n = p.slab < p.chunks - first ? p.slab : p.chunks - first, parts = (n + p.part - 1) / p.part;
+    return {n, parts, parts > 2 ? parts - 2 : 0};
+}
+// Workgroups of a walk: whole groups of 8, one to an XCD, first of what is walked for outputs, then of what is for maps.
+inline int64_t delta_walk_blocks(int64_t heads, int64_t P, int64_t N, int64_t walked, int64_t maps)
+{
+    return (heads * walked + 7) / 8 * 8 * (P / 16) + (heads * maps + 7) / 8 * 8 * ((P + N) / 16);
+}
+
+// A context of a few tokens goes token after token, without a workspace: a chunk costs the same whether 1 or 64 of its tokens are there.
+// bf16, with gate and norm, token after token | in a chunk (us): 8 heads of 64 x 64: 6 tokens 8.6 | 12.2, 8: 10.6 | 12.0, 10: 12.7 | 12.1;
+// 32 heads of 128 x 128: 4: 9.8 | 13.1, 6: 13.3 | 13.2, 8: 16.8 | 13.3.  Heads for every CU make a chunk dearer: 256 of 128 x 128: 16 tokens
+// 32.5 | 36.4, 20: 39.2 | 37.0; 512 of 64 x 64: 16: 25.8 | 35.9, 24: 36.4 | 36.1; 2048 of 128 x 128: 16: 147 | 265, 24: 214 | 279.
+inline bool delta_few_tokens(int64_t batch, int64_t L, int64_t H) { return L <= (batch * H >= 256 ? 16 : 6); }
+
 }  // namespace mamba
