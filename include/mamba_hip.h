@@ -445,8 +445,8 @@ int mamba_gated_delta_step(float *h_out, const float *h_in, const int32_t *paren
  *
  * mamba_token_counts: occurrences of every token in each of n_seq sequences, tokens (n_seq, L) device int32 (numbers outside [0,V),
  *   such as the -1 of a padded row, are skipped), into counts (n_seq, V) device int32.  An entry's lower 31 bits are the
- *   occurrences in the generated text, bit 31 says that the token stands in the prompt: with prompt = 0 the call adds
- *   occurrences, with prompt = 1 it sets that bit.  accumulate = 0: counts are written from scratch, else what they hold is kept
+ *   occurrences in the generated text (2^31 - 1 where there are more), bit 31 says that the token stands in the prompt: with prompt = 0 the
+ *   call adds occurrences, with prompt = 1 it sets that bit.  accumulate = 0: counts are written from scratch, else what they hold is kept
  *   and added to.  V <= 2^25.
  * mamba_logits_constrain_fwd: out[m,v] from logits[m,v], (M,V) bf16 or float32 both, out may be logits itself:
  *   c = generated occurrences of v in the row's sequence, and in the row's path

@@ -187,7 +187,7 @@ template <typename T, bool COUNTS, bool BIAS, bool MASK> struct Share {
                     const int32_t one = __builtin_amdgcn_readlane(token, __builtin_ctzll(here));
                     here &= here - 1;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) counts[i] += start + i == one;
+                    for (int i = 0; i < 8; ++i) counts[i] += start + i == one && (counts[i] & 0x7fffffff) != 0x7fffffff;
                 }
             }
         }
@@ -368,7 +368,8 @@ token_counts_kernel(const int32_t *__restrict__ tokens, int32_t *__restrict__ co
     __syncthreads();
     for (int i = threadIdx.x; i < len; i += kCountThreads) {
         const uint32_t old = accumulate ? (uint32_t)counts[s * V + v0 + i] : 0u, more = (uint32_t)n[i];
-        counts[s * V + v0 + i] = (int32_t)(prompt ? old | (more ? 0x80000000u : 0u) : (old & 0x80000000u) | ((old + more) & 0x7fffffffu));
+        const uint32_t sum = min((old & 0x7fffffffu) + more, 0x7fffffffu);
+        counts[s * V + v0 + i] = (int32_t)(prompt ? old | (more ? 0x80000000u : 0u) : (old & 0x80000000u) | sum);
     }
 }
 
