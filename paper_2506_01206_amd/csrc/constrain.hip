@@ -106,13 +106,16 @@ template <int n> __device__ __forceinline__ void penalise(const RowRules &r, flo
 {
 #pragma clang fp contract(off)
     const float y = 1.0f / r.repetition;
-    float less[n], least = kMost, most = kLeast;                     // (only what is above zero is divided)
+    // Only what is above zero is divided.  As unsigned integers less one such values are in order, and zeros, negative values and NaN are beyond them:
+    // a zero does not send its wavefront to the slow division (2 children of 96 rows with zeros among them 18.7 -> 16.5 us).
+    uint32_t least = UINT32_MAX;
+    float less[n], most = kLeast;
 #pragma unroll
     for (int i = 0; i < n; ++i) {
-        least = fminf(least, fabsf(x[i])), most = fmaxf(most, x[i]);
+        least = min(least, __float_as_uint(x[i]) - 1u), most = fmaxf(most, x[i]);
         less[i] = divided(x[i], r.repetition, y);
     }
-    if (!__all(least >= kLeast && most <= kMost && r.repetition >= kLeast && r.repetition <= kMost)) {
+    if (!__all(least >= __builtin_bit_cast(uint32_t, kLeast) - 1u && most <= kMost && r.repetition >= kLeast && r.repetition <= kMost)) {
 #pragma unroll 1
         for (int i = 0; i < n; ++i) {                                // (rolled up: seldom run, and not to be fetched by the others)
             const float first = x[0], q = first / r.repetition;
