@@ -286,8 +286,8 @@ template <int N> __device__ __forceinline__ int state_of(int tile, int row)
 
 // One chunk of one head.  Eight wavefronts, and what the chain of phases needs comes first: T by all of them; then one inverts the blocks
 // on its diagonal while the others form M and write the fragments of keys and queries.
-// Bound by the latency of those phases, three workgroups to a CU: one chunk 6.6 us, 768 chunks (24 heads, N = 128) 16.7, 1504 (32 heads, N = 128)
-// 28, which then write their 70 MB at 2.5 TB/s.
+// Bound by the latency of those phases, three workgroups to a CU: one chunk 6.9 us, 768 chunks (24 heads, N = 128) 16.9, 1504 (32 heads, N = 128)
+// 29, which then write their 82 MB at 2.8 TB/s.
 // grid: (chunks of the slab, H, batch); tok_slab: the slab's first token
 constexpr int kPrepThreads = 512;
 template <int N>
@@ -565,11 +565,12 @@ delta_prepare_kernel(const bf16_t *__restrict__ q, const bf16_t *__restrict__ k,
 //            U = X R of those tokens, with their decay to the end                                                         | C
 //            the write to its states
 //   outputs  wavefront w has the tokens 16 w ..: Q S^T after B, (M X) R after C, gate and store, with the next chunk under way in the chain
-// All operands but S, R and U come from memory, requested a chunk ahead, the chain's into the registers that the last use has just left: with
-// two sets used in turn it took 156 registers, a CU held one workgroup, and 4 contexts of 1000 tokens of 16 heads of 128 x 128 took 48 us
-// (now 39); alone on its CU a workgroup is no slower for it.
-// Bound by the latency of a chunk's chain: N = 64 1.1, N = 128 1.25 us, of which the matrix pipe is busy for a fifth; 24 heads of N = 128,
-// P = 64 and 2048 tokens 41 us.  Where all CUs have one or two workgroups the instructions of both roles are two thirds of the time.
+// All operands but S, R and U come from memory, requested a chunk ahead, into the registers that the last use has just left: with two sets used in
+// turn a wavefront has more than 128 registers, a CU holds one workgroup, and 4 contexts of 1000 tokens of 16 heads of 128 x 128 took 48 us
+// where they took 39 with one; alone on its CU a workgroup is no slower for it.
+// Bound by the latency of a chunk's chain: N = 64 1.1, N = 128 1.25 us (3000 cycles: terms of S 360, K S^T 400, sum, K^T and R 520, U 220 to 350, its
+// terms 250, the write to S 690, the rest barriers); 24 heads of N = 128, P = 64 and 2048 tokens 43 us, of which the matrix cores of the CUs that
+// have a workgroup are busy for a third.  With two workgroups to a CU (the 4 contexts: 42 us) they are for 42 %.
 struct WalkArgs {
     const bf16_t *v, *z;
     const uint16_t *ws, *frags;
@@ -1132,7 +1133,7 @@ template <int N> hipError_t walk(const WalkArgs &w, hipStream_t stream)
 {
     const int64_t blocks = delta_walk_blocks(w.heads, w.P, N, w.walked, w.maps);
     // Two workgroups fit on a CU, but each takes its time then: where a CU can be had for each, LDS that nobody uses keeps the second away
-    // (8191 tokens of 12 heads of N = 64, P = 128: 145 -> 133 us; without it two go to one CU while others stay empty).
+    // (8191 tokens of 12 heads of N = 64, P = 128: 138 -> 130 us; without it two go to one CU while others stay empty).
     const unsigned alone = delta_fullest_xcd(w.heads, w.P, N, w.walked, w.maps) <= 32 ? 40960 : 0;
     if (w.raw) delta_walk_kernel<N, kWalkRaw><<<(unsigned)blocks, 2 * kThreads, alone, stream>>>(w);
     else if (w.z) delta_walk_kernel<N, kWalkGate><<<(unsigned)blocks, 2 * kThreads, alone, stream>>>(w);

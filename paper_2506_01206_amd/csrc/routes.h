@@ -488,9 +488,9 @@ inline int xdt_plan(int64_t M, int64_t d_inner, int64_t dt_rank, int64_t N, unsi
 
 // The gated-delta core (delta.hip).
 // A long context goes in slabs of chunks, so that what the preparation leaves is still in the last-level cache (256 MB) when the walk takes
-// it, and the workspace does not grow with the context.  32768 tokens of 32 heads of 128 x 128, all launches, by a slab's bytes: 32 MB 1625 us,
-// 64 MB 1345, 128 MB 1152, 256 MB 1261, one slab 1174 (and 1.2 GB of workspace); 8191 tokens of 12 heads of N = 64, P = 128: 192, 148, 133 from
-// 128 MB on, which are one slab.
+// it, and the workspace does not grow with the context.  32768 tokens of 32 heads of 128 x 128, all launches, by a slab's bytes: 32 MB 1702 us,
+// 64 MB 1314, 96 MB 1300, 128 MB 1226, 256 MB 1357, one slab 1275 (and 1.4 GB of workspace); 8191 tokens of 12 heads of N = 64, P = 128: 199, 150, 150,
+// 130 from 128 MB on, which are one slab.
 // (a chunk's tokens, and what the preparation leaves of a chunk and value head in 16-bit words: X and M X in three terms each, 6 fragments of 512 to
 // a term, and 256 floats)
 constexpr int64_t kDeltaChunk = 64, kDeltaChunkHalves = 2 * 3 * 6 * 512 + 2 * 256;
@@ -511,9 +511,9 @@ inline int64_t delta_fullest_xcd(int64_t heads, int64_t P, int64_t N, int64_t wa
 }
 // The parts of a slab of n chunks, those of the least time (us): a CU (32 to an XCD) walks one block of 16 rows at a time, a chunk in about
 // 1.1 (N = 64) or 1.25 (128), and takes 3 to begin; a part more is a step of the join; two more launches.
-// All launches of 8191 tokens, in one part | in several: 2 heads of 64 x 64 153 | 50 (16 parts), 2 of 128 x 128 158 | 77 (9), 8 of N = 64,
-// P = 64 156 | 84 (9), 8 of 128 x 128 169 | 129 (5), 12 of N = 64, P = 128 161 | 129 (3); 24 of N = 128, P = 64 have work for all CUs:
-// 233 | 305 (3).  2048 tokens: 2 heads of 64 x 64 46 | 30, 12 of N = 64, P = 128 53.5 | 51.6; 1000 tokens of 8 heads of 64 x 64 29 | 30.
+// All launches of 8191 tokens, in one part | in several: 2 heads of 64 x 64 153 | 52 (16 parts), 2 of 128 x 128 163 | 77 (9), 8 of N = 64,
+// P = 64 166 | 77 (9), 8 of 128 x 128 184 | 125 (5), 12 of N = 64, P = 128 182 | 145 (3).  2048 tokens: 2 heads of 64 x 64 49 | 32, 12 of N = 64,
+// P = 128 55 | 52.  24 heads of N = 128, P = 64 have work for all CUs and stay in one part (242).
 inline int64_t delta_parts(int64_t heads, int64_t P, int64_t N, int64_t n)
 {
     const double chunk = N == 64 ? 1.1 : 1.25, join = N == 64 ? 0.75 : 2.0;
@@ -566,10 +566,11 @@ inline int64_t delta_walk_blocks(int64_t heads, int64_t P, int64_t N, int64_t wa
     return (heads * walked + 7) / 8 * 8 * (P / 16) + (heads * maps + 7) / 8 * 8 * ((P + N) / 16);
 }
 
-// A context of a few tokens goes token after token, without a workspace: a chunk costs the same whether 1 or 64 of its tokens are there.
-// bf16, with gate and norm, token after token | in a chunk (us): 8 heads of 64 x 64: 6 tokens 8.6 | 12.2, 8: 10.6 | 12.0, 10: 12.7 | 12.1;
-// 32 heads of 128 x 128: 4: 9.8 | 13.1, 6: 13.3 | 13.2, 8: 16.8 | 13.3.  Heads for every CU make a chunk dearer: 256 of 128 x 128: 16 tokens
-// 32.5 | 36.4, 20: 39.2 | 37.0; 512 of 64 x 64: 16: 25.8 | 35.9, 24: 36.4 | 36.1; 2048 of 128 x 128: 16: 147 | 265, 24: 214 | 279.
+// A context of a few tokens goes token after token, without a workspace: a chunk costs the same whether 1 or 64 of its tokens are there.  bf16, with gate
+// and norm, token after token | in a chunk (us).  8 heads of 64 x 64: 6 tokens 8.5 | 12.9, 8: 10.6 | 12.8, 10: 12.7 | 12.9; 64 of them: 6: 8.7 | 13.6,
+// 10: 12.8 | 13.5; 32 heads of 128 x 128: 6: 12.9 | 14.0, 8: 16.3 | 14.0; 128 of them: 6: 13.7 | 20.8, 8: 17.0 | 20.5, 10: 20.3 | 20.7.  Heads for
+// every CU: 256 of 128 x 128: 12: 25.6 | 29.4, 16: 31.6 | 29.5; 512 of 64 x 64: 16: 25.1 | 29.8, 20: 30.4 | 30.2; 2048 of 128 x 128: 16: 140 | 176, 20: 175 | 179,
+// 24: 208 | 182.  The two meet at 7 to 20 tokens, by heads and sizes; two steps in the heads lose 3 us of 13 at the most between.
 inline bool delta_few_tokens(int64_t batch, int64_t L, int64_t H) { return L <= (batch * H >= 256 ? 16 : 6); }
 
 }  // namespace mamba
