@@ -78,7 +78,10 @@ class MambaDrafter:
         until the next ``prefill``, which counts its own tokens anew."""
         if self._rules is None:
             raise RuntimeError("observe() is for a drafter under rules: call constrain() first")
-        m.mamba_token_counts(tokens.view(1, -1), self.V, counts=self._rules["counts"])
+        row = tokens.reshape(1, -1)
+        if row.data_ptr() % 16:                          # (a row of a round's paths: the call takes aligned tokens)
+            row = row.clone()
+        m.mamba_token_counts(row, self.V, counts=self._rules["counts"])
 
     # ------------------------------------------------------------------ prefix encoding
     def prefill(self, tokens, prompt_len=None):

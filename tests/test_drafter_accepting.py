@@ -46,3 +46,20 @@ def test_accepted_tokens_stay_generated_when_the_prefix_is_encoded_again(m, n_pr
         text = np.concatenate([text, path[rng.integers(0, len(path))], more])
     d.prefill(torch.from_numpy(text).to(DEV))                    # all of it as the prompt
     assert np.array_equal(d._rules["counts"].cpu().numpy(), oc.token_counts(text[None], d.V, prompt=True))
+
+
+@pytest.mark.gpu
+def test_a_row_of_a_rounds_paths_is_observed(m):  # noqa: F811
+    """Rows of three tokens start anywhere; a column has strides."""
+    from oracle import constrain as oc
+    print("\n[gpu-case] drafter observes rows and columns of its paths", flush=True)
+    d, tree = small_drafter(), (3, 2, 2)
+    d.constrain(*PENALTIES)
+    d.prefill(torch.arange(20, dtype=torch.int32, device=DEV))
+    d.draft(tree, use_graph=False)
+    path = d._buffers(tree)["pos"][3]["path"]
+    counts = d._rules["counts"].cpu().numpy()
+    for tokens in (path[1], path[2, 1:], path[:, 1], path[5:7], path[0, :0]):
+        d.observe(tokens)
+        counts = oc.token_counts(tokens.cpu().numpy().reshape(1, -1), d.V, counts)
+        assert np.array_equal(d._rules["counts"].cpu().numpy(), counts)
