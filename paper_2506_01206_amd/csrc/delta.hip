@@ -355,7 +355,8 @@ delta_prepare_kernel(const bf16_t *__restrict__ q, const bf16_t *__restrict__ k,
 #pragma unroll
         for (int i = 0; i < N / 32; ++i) {
             const bf16x8 f = lds_frag(&rows[t * kRow + i * 32 + g4 * 8]);
-            acc = mma(f, f, acc);
+            // (where no lengths are asked for, times zeros: 0, or NaN for a row that is no numbers, however long)
+            acc = mma(f, o.qk_norm ? f : as_frag(make_uint4(0, 0, 0, 0)), acc);
         }
         const float square = (c16 & 2) ? (c16 & 1) ? acc[3] : acc[2] : (c16 & 1) ? acc[1] : acc[0];
         const float inverse = t >= live ? 0.0f : o.qk_norm ? 1.0f / sqrtf(square + o.eps) : 1.0f;

@@ -86,3 +86,23 @@ def test_a_gate_and_a_state_that_are_not_numbers(m, io):  # noqa: F811
     rows[0, 0, 9] = True
     same_but(out, ref, nan)
     same_but(hf, rh, rows)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("io", [synth.BF16, synth.F32])
+def test_keys_that_are_numbers_but_long(m, io):  # noqa: F811
+    """Without a norm a key of 1e19 in every state is a key like others: its square overflows, what it writes does not."""
+    from gpu_util import W, assert_close, to_host, values
+    from oracle import delta
+    from test_gated_delta import TOL, TOL_F32, storage
+    print("\n[gpu-case] gated delta, long keys, io=%s" % io, flush=True)
+    rng = np.random.default_rng(6)
+    c = case(rng, 1, 40, 2, 2, 128, 64, io, False, False)
+    k, beta, dt = W(c["k"]) * 0.1, np.zeros((1, 40, 2)), np.full((1, 40, 2), -1e-3)
+    k[0, 7], beta[0, 7], beta[0, :7] = 1e19, 1e-20, 0.5
+    c["k"], c["beta"], c["dt"], c["dt_bias"], c["A"] = storage(k, io), storage(beta, io), storage(dt, io), None, np.full(2, 1.0, np.float32)
+    options = dict(qk_norm=False, beta_sigmoid=False, dt_softplus=False)
+    out, hf = m.mamba_gated_delta_fwd(**device(c), **options)
+    ro, rh = delta.delta_scan(**{n: W(x) for n, x in c.items()}, **options)
+    assert_close(values(to_host(out)), ro, TOL[io], "out")
+    assert_close(to_host(hf), rh, TOL_F32, "final state")
