@@ -8,7 +8,7 @@ elementary torch operations, with ``own`` true through the library's entry point
              out = x W^T + bias + residual + scale_a (x A_a^T) B_a^T
   sample   the children of draft branches, or the next tokens of requests, drawn without replacement from their logits under temperature,
            top-k, top-p and min-p, with given random numbers; with it, where it is wanted, the distribution that they are drawn from
-             w = exp((x - max x) / T), kept: the top_k largest, of those the fewest that make up top_p, of those w >= min_p
+             w = exp((x - max x) / T), kept: those with w >= min_p, of those the top_k largest, of those the fewest that make up top_p
   verify   which path of a tree of such children a target accepts, and the token behind it
              accepted: u < min(1, p / q); rejected: p = (p - q)_+ / its sum, q = q without the child / its sum; none: drawn from p
 """
@@ -259,10 +259,9 @@ def _plain_sample(s):
     x, order = x.sort(dim=1, descending=True, stable=True)       # equal ones stay in the order of their indices
     at = torch.arange(V, device=x.device)
     w = torch.where(T > 0, torch.exp((x - x[:, :1]) / torch.where(T > 0, T, torch.ones_like(T))), (at == 0).double())
-    w = torch.where((top_k <= 0) | (at < top_k), w, torch.zeros_like(w))
+    w = torch.where((w >= torch.clamp(min_p, max=1.0)) & ((top_k <= 0) | (at < top_k)), w, torch.zeros_like(w))
     c = w.cumsum(1)
     w = torch.where((at == 0) | (top_p >= 1) | (c - w < top_p * c[:, -1:]), w, torch.zeros_like(w))
-    w = torch.where(w >= torch.clamp(min_p, max=1.0), w, torch.zeros_like(w))
     w = torch.zeros_like(w).scatter(1, order, w)
     total = w.sum(1, keepdim=True)
     dist = w / total
@@ -379,10 +378,10 @@ def _exact_sample(case, host, logits):
         if host["top_k"][q] > 0:
             order = order[:host["top_k"][q]]
         w = np.exp((x[order] - x[order[0]]) / (T if T > 0 else 1.0))
-        keep = len(order)
+        w = w[w >= min(min_p, 1.0)]
+        keep = len(w)
         if top_p < 1.0:
-            keep = max(1, int(np.searchsorted(np.cumsum(w), top_p * w.sum(), side="left")) + 1)
-        keep = min(keep, int((w >= min(min_p, 1.0)).sum()))
+            keep = min(keep, int(np.searchsorted(np.cumsum(w), top_p * w.sum(), side="left")) + 1)
         dist[m, order[:keep]] = w[:keep] / w[:keep].sum()
         left = dist[m].copy()
         for j in range(k):
