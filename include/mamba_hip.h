@@ -490,6 +490,83 @@ int mamba_topk_constrained_fwd(const void *logits, const mamba_constraints_t *c,
                                void *workspace, size_t workspace_bytes, int64_t M, int64_t V, int k, mamba_dtype_t io,
                                void *hip_stream);
 
+/*
+ * Children that are drawn (Sec. 4.1: the N_i children of a node are samples of the drafter's distribution q_i), and the next tokens of a
+ * verifier that samples.  mamba_sample_fwd, for every row of logits (M,V) bf16 or float32, with the settings of the row's sequence:
+ *   w_v = exp((x_v - max x) / temperature)          temperature 0: 1 for the first of the largest, 0 for the others
+ *   kept: the tokens with w >= min_p; of those the top_k largest; of those the fewest, largest first, whose w reach top_p times the sum of
+ *   theirs (at least one).  Ties go to the lower index; a NaN logit is as -inf, and -inf is never kept.
+ *   q_v = w_v / (sum of w over what is kept), 0 for what is not
+ *   child j: the first token, in the order of the vocabulary, up to which the w of what is kept and not drawn yet add up to more than
+ *   u[m,j] times the sum of all of those: k draws without replacement, so that the children of a node differ
+ *   u: (M,k) float in [0,1) (what is below counts as 0, what is above as just below 1, NaN as 0); 1 <= k <= 8
+ *   idx: int32 (M,k); prob: float (M,k), q of the token; -1 and 0 where no token is left
+ *   dist: (M,V) float or NULL: q of every token (its address needs four bytes' alignment only)
+ *   path_out: int32 (M k, path_len + 1) or NULL, as mamba_topk_constrained_fwd has it
+ * Sums are formed in float64's precision or better (whole multiples of 2^-42 to 2^-63 of the largest weight), whatever the order: results are the
+ * same bit for bit from call to call.  A weight below float64's range is zero, and so are those of finite logits beside an infinite one; a token of
+ * weight zero is not drawn.
+ *
+ * mamba_sampling_t (a HOST struct of device pointers):
+ *   params (n_seq, 3) float: temperature (>= 0), top_p (1 or more: off; 0 or less: the first token only), min_p (0 or less: off; above 1: as 1)
+ *   top_k (n_seq) int32 or NULL; 0 or less: off
+ *   seq_idx (M): the row's sequence; NULL: sequence 0 where n_seq is 1, row m's own where it is M
+ *   path (M, path_len): the tokens that lead to the row, for path_out only; NULL where path_len is 0
+ * A row whose seq_idx is out of range, or with a negative temperature or a NaN among its settings: no token, NaN in all of dist.
+ * workspace: device scratch of mamba_sample_workspace_bytes(M, V, k) bytes; nothing in it has to be kept or cleared between calls.
+ * V <= 2^21, M (V / 2048 rounded up) < 2^24, M < 2^22, path_len <= 4096.
+ */
+typedef struct {
+    const float *params;
+    const int32_t *top_k;
+    const int32_t *seq_idx;
+    const int32_t *path;
+    int64_t n_seq, path_len;
+} mamba_sampling_t;
+
+size_t mamba_sample_workspace_bytes(int64_t M, int64_t V, int k);
+int mamba_sample_fwd(const void *logits, const mamba_sampling_t *s, const float *u, int32_t *idx, float *prob, float *dist,
+                     int32_t *path_out, void *workspace, size_t workspace_bytes, int64_t M, int64_t V, int k, mamba_dtype_t io,
+                     void *hip_stream);
+
+/*
+ * Verification of drafted trees on the device (appendix, verification algorithm; sd_verify of sd_tree_search.h is the same for one chain on the
+ * host).  A tree (HOST int32[gamma], N_i from 1 to 8) has `nodes` = 1 + B_1 + .. + B_gamma nodes, B_i = N_1 ... N_i, the root first, then
+ * position by position, child j of the position's node r at r N_i + j; the first `inner` = nodes - B_gamma of them have children.
+ *   p: (n_seq, nodes, V) float, the target's distribution behind every node; q: (n_seq, inner, V) float, the drafter's
+ *   tokens: int32 (n_seq, nodes - 1), the children's tokens, drawn without replacement as mamba_sample_fwd draws them; one outside [0,V),
+ *   such as the -1 of a node with fewer children, is passed over
+ *   u_accept: float (n_seq, nodes - 1), one for each child; u_sample: float (n_seq)
+ * From the root on, with P = p and Q = q of the node, its children in turn: child c is accepted where u < min(1, P(c) / Q(c)) (Q(c) = 0: as 1
+ * where P(c) > 0), and the walk goes on at its node; else P becomes (P - Q)_+ divided by its sum (and stays where that is zero) and Q becomes q
+ * without the children so far, divided by its sum.  Where none is accepted, a token is drawn from P and the walk ends; behind the last
+ * position it is drawn from p: the first token, in the order of the vocabulary, up to which the probabilities add up to more than u_sample
+ * times their sum; -1 where the sum is zero or no number.  All of this in float64.  An emitted token is distributed as p, whatever q is.
+ *   out: int32 (n_seq, gamma + 1): the accepted tokens, the drawn one, then -1;  count: int32 (n_seq): how many there are (1 .. gamma + 1)
+ *   node: int32 (n_seq, gamma): of the accepted tokens the row in their position (the row of its cache to go on from), then -1
+ * p, q: four bytes' alignment is enough.  n_seq < 2^22, nodes <= 65535, V <= 2^25.
+ */
+int mamba_tree_verify_fwd(const float *p, const float *q, const int32_t *tokens, const float *u_accept, const float *u_sample,
+                          int32_t *out, int32_t *count, int32_t *node, const int32_t *tree, int gamma, int64_t n_seq, int64_t V,
+                          void *hip_stream);
+
+/*
+ * A projection that the rows of many requests share, with each request's own low-rank adapter beside it (one drafter for requests of several
+ * targets or domains):
+ *   out[m,n] = sum_k x[m,k] w[n,k] (+ bias[n]) (+ residual[m,n]) + scale[a] sum_r (sum_k x[m,k] lora_a[a,r,k]) lora_b[a,n,r],  a = adapter_idx[m]
+ * with mamba_linear_fwd's tensors and rules (bf16; up to three outputs; K a multiple of 8; residual may be out0 itself), but rounded once, residual
+ * included.  lora_a (n_adapters, rank, K), lora_b (n_adapters, N, rank) bf16; scale (n_adapters) float or NULL (ones); adapter_idx
+ * device int32 (M): -1 for a row without an adapter (what it gets is mamba_linear_fwd's to the bit where there is no residual), anything else
+ * outside [0, n_adapters) gives NaN in the row.  Rows of one adapter may stand anywhere; next to one another they cost least.  The rank is a multiple of
+ * 8 up to 128 (adapters of a lower one are padded with zeros).  An infinity or a NaN of an adapter reaches its own rows only.
+ * workspace: device scratch of mamba_linear_adapted_workspace_bytes(M, rank) bytes; nothing in it has to be kept or cleared between calls.
+ */
+size_t mamba_linear_adapted_workspace_bytes(int64_t M, int64_t rank);
+int mamba_linear_adapted_fwd(const void *x, const void *w, const float *bias, const void *residual, const void *lora_a,
+                             const void *lora_b, const float *scale, const int32_t *adapter_idx, void *out0, int64_t n0, void *out1,
+                             int64_t n1, void *out2, int64_t n2, void *workspace, size_t workspace_bytes, int64_t M, int64_t K,
+                             int64_t rank, int64_t n_adapters, mamba_dtype_t io, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

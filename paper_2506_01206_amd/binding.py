@@ -74,6 +74,11 @@ class Constraints(ctypes.Structure):
                 + [(n, ctypes.c_int64) for n in ("n_seq", "n_masks", "path_len")])
 
 
+class Sampling(ctypes.Structure):
+    """mamba_sampling_t of include/mamba_hip.h."""
+    _fields_ = [(n, ctypes.c_void_p) for n in ("params", "top_k", "seq_idx", "path")] + [(n, ctypes.c_int64) for n in ("n_seq", "path_len")]
+
+
 def _declare(lib):
     """Attach the C signatures of include/mamba_hip.h to a loaded library."""
     _bpp = ctypes.POINTER(BlockParams)
@@ -106,6 +111,16 @@ def _declare(lib):
     lib.mamba_topk_constrained_workspace_bytes.restype = _sz
     lib.mamba_topk_constrained_fwd.argtypes = [_vp, _cp] + [_vp] * 4 + [_sz, _i64, _i64, _int, _int, _vp]
     lib.mamba_topk_constrained_fwd.restype = _int
+    lib.mamba_sample_workspace_bytes.argtypes = [_i64, _i64, _int]
+    lib.mamba_sample_workspace_bytes.restype = _sz
+    lib.mamba_sample_fwd.argtypes = [_vp, ctypes.POINTER(Sampling)] + [_vp] * 6 + [_sz, _i64, _i64, _int, _int, _vp]
+    lib.mamba_sample_fwd.restype = _int
+    lib.mamba_tree_verify_fwd.argtypes = [_vp] * 8 + [ctypes.POINTER(ctypes.c_int32), _int, _i64, _i64, _vp]
+    lib.mamba_tree_verify_fwd.restype = _int
+    lib.mamba_linear_adapted_workspace_bytes.argtypes = [_i64, _i64]
+    lib.mamba_linear_adapted_workspace_bytes.restype = _sz
+    lib.mamba_linear_adapted_fwd.argtypes = [_vp] * 8 + [_vp, _i64] * 3 + [_vp, _sz] + [_i64] * 4 + [_int, _vp]
+    lib.mamba_linear_adapted_fwd.restype = _int
     lib.mamba_embedding_fwd.argtypes = [_vp, _vp, _vp, _i64, _i64, _i64, _int, _vp]
     lib.mamba_embedding_fwd.restype = _int
     lib.mamba_topk_fwd.argtypes = [_vp, _vp, _vp, _i64, _i64, _int, _int, _vp]
@@ -152,7 +167,9 @@ EXPORTS = ("mamba_status_string", "mamba_conv1d_fwd", "mamba_scan_workspace_byte
            "mamba_block_workspace_layout", "mamba_block_fwd", "mamba_block_step", "mamba_embedding_fwd", "mamba_topk_fwd",
            "mamba2_ssd_workspace_bytes", "mamba2_ssd_fwd", "mamba2_state_step",
            "mamba_gated_delta_workspace_bytes", "mamba_gated_delta_fwd", "mamba_gated_delta_step",
-           "mamba_token_counts", "mamba_logits_constrain_fwd", "mamba_topk_constrained_workspace_bytes", "mamba_topk_constrained_fwd")
+           "mamba_token_counts", "mamba_logits_constrain_fwd", "mamba_topk_constrained_workspace_bytes", "mamba_topk_constrained_fwd",
+           "mamba_sample_workspace_bytes", "mamba_sample_fwd", "mamba_tree_verify_fwd",
+           "mamba_linear_adapted_workspace_bytes", "mamba_linear_adapted_fwd")
 
 
 class MambaError(RuntimeError):
@@ -171,6 +188,10 @@ _delta = _marshal._delta
 _delta.bind(MambaError, torch.OutOfMemoryError, *[ctypes.cast(getattr(lib, name), _vp).value for name in (
     "mamba_gated_delta_workspace_bytes", "mamba_gated_delta_fwd", "mamba_gated_delta_step", "mamba_token_counts",
     "mamba_logits_constrain_fwd", "mamba_topk_constrained_workspace_bytes", "mamba_topk_constrained_fwd")])
+_sample = _marshal._sample
+_sample.bind(MambaError, torch.OutOfMemoryError, *[ctypes.cast(getattr(lib, name), _vp).value for name in (
+    "mamba_sample_workspace_bytes", "mamba_sample_fwd", "mamba_tree_verify_fwd", "mamba_linear_adapted_workspace_bytes",
+    "mamba_linear_adapted_fwd")])
 
 
 def mamba_status_string(status: int) -> str:
@@ -540,3 +561,44 @@ def mamba_topk_constrained_fwd(logits, k, counts=None, penalties=None, seq_idx=N
             workspace = _scratch(need, logits.device, stream)
     return _delta.topk_constrained_fwd(logits, k, counts, penalties, seq_idx, path, bias, mask, mask_idx, idx, val, path_out, want_path,
                                        workspace, _raw(stream))
+
+
+def mamba_sample_workspace_bytes(M, V, k) -> int:
+    return int(lib.mamba_sample_workspace_bytes(M, V, k))
+
+
+def mamba_sample_fwd(logits, u, params, top_k=None, seq_idx=None, path=None, idx=None, prob=None, dist=None, path_out=None, want_dist=False,
+                     want_path=False, workspace=None, stream=None):
+    """u.shape[1] tokens of every row of logits (M,V) bf16|f32, drawn without replacement by u (M,k) f32 in [0,1) under params (S,3) f32
+    (temperature, top_p, min_p) and top_k int32 (S); seq_idx int32 (M), path int32 (M,T) -> idx int32 (M,k), prob f32 (M,k), dist f32 (M,V)
+    or None: what they are drawn from, path_out int32 (M k, T+1) or None: row m k + j the path of row m with its child j behind it."""
+    if stream is not None and workspace is None:
+        workspace = _scratch(mamba_sample_workspace_bytes(*logits.shape, u.shape[1]), logits.device, stream)
+    return _sample.sample_fwd(logits, u, params, top_k, seq_idx, path, idx, prob, dist, path_out, want_dist, want_path, workspace, _raw(stream))
+
+
+def mamba_tree_verify_fwd(p, q, tokens, u_accept, u_sample, tree, out=None, count=None, node=None, stream=None):
+    """Verification of drafted trees (N_1..N_gamma): p (S,nodes,V), q (S,inner nodes,V) f32, tokens int32 and u_accept f32 (S,nodes-1) position
+    by position, u_sample f32 (S) -> out int32 (S,gamma+1): the accepted tokens and the drawn one, then -1, count int32 (S), node int32
+    (S,gamma): rows of the accepted tokens in their positions, then -1."""
+    return _sample.tree_verify_fwd(p, q, tokens, u_accept, u_sample, tuple(tree), out, count, node, _raw(stream))
+
+
+def mamba_linear_adapted_workspace_bytes(M, rank) -> int:
+    return int(lib.mamba_linear_adapted_workspace_bytes(M, rank))
+
+
+def mamba_linear_adapted_fwd(x, w, lora_a, lora_b, adapter_idx, scale=None, bias=None, residual=None, splits=None, outs=None, workspace=None,
+                             stream=None):
+    """mamba_linear_fwd with the adapter of every row's request beside it: x (M,K), w (N,K), lora_a (n,rank,K), lora_b (n,N,rank) bf16,
+    adapter_idx int32 (M) (-1: none), scale (n) f32 -> x @ w.T + scale[a] (x @ lora_a[a].T) @ lora_b[a].T (+ bias) (+ residual); a tuple."""
+    widths = [w.shape[0]] if splits is None else list(splits)
+    if not 1 <= len(widths) <= 3 or sum(widths) != w.shape[0] or (outs is not None and len(outs) != len(widths)):
+        raise ValueError("splits must be the widths of one to three outputs that share the %d columns" % w.shape[0])
+    if stream is not None and workspace is None:
+        workspace = _scratch(mamba_linear_adapted_workspace_bytes(x.shape[0], lora_a.shape[1]), x.device, stream)
+    used = len(widths)
+    o = ([None] * 3 if outs is None else list(outs) + [None] * 3)[:3]
+    widths += [0] * (3 - used)
+    return _sample.linear_adapted_fwd(x, w, lora_a, lora_b, adapter_idx, scale, bias, residual, o[0], widths[0], o[1], widths[1], o[2], widths[2],
+                                      used, workspace, _raw(stream))

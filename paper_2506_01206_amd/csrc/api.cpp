@@ -435,39 +435,91 @@ int mamba_state_fork(void *conv_dst, const void *conv_src, float *ssm_dst, const
     return (int)launch_fork(a, static_cast<hipStream_t>(hip_stream));
 }
 
-int mamba_linear_fwd(const void *x, const void *w, const float *bias, const void *residual, void *out0,
-                     int64_t n0, void *out1, int64_t n1, void *out2, int64_t n2, int64_t M, int64_t K,
-                     mamba_dtype_t io, void *hip_stream)
+namespace {
+
+// The arguments of a product checked, with or without adapters; *done: there is nothing to compute.
+int linear_checked(const LinearArgs &a, mamba_dtype_t io, bool *done)
 {
+    *done = false;
     if (io != MAMBA_BF16) return MAMBA_ERR_UNSUPPORTED;
+    const int64_t n0 = a.width[0], n1 = a.width[1], n2 = a.width[2], M = a.M, K = a.K;
     if (n0 < 0 || n1 < 0 || n2 < 0 || M < 0 || K < 0) return MAMBA_ERR_BAD_SHAPE;
     int64_t N;
     if (__builtin_add_overflow(n0, n1, &N) || __builtin_add_overflow(N, n2, &N)) return MAMBA_ERR_BAD_SHAPE;
     int64_t xb, wb, ob[3];
-    const int64_t widths[3] = {n0, n1, n2};
-    void *outs[3] = {out0, out1, out2};
     if (!size3(M, K, 1, 2, &xb) || !size3(N, K, 1, 2, &wb)) return MAMBA_ERR_BAD_SHAPE;
     for (int i = 0; i < 3; ++i)
-        if (!size3(M, widths[i], 1, 2, &ob[i])) return MAMBA_ERR_BAD_SHAPE;
+        if (!size3(M, a.width[i], 1, 2, &ob[i])) return MAMBA_ERR_BAD_SHAPE;
     if (K % 8 != 0 || M > kMaxGridYZ * 128) return MAMBA_ERR_UNSUPPORTED;
-    if (residual && (n1 != 0 || n2 != 0)) return MAMBA_ERR_UNSUPPORTED;
-    if (M == 0 || N == 0) return MAMBA_OK;
+    if (a.residual && (n1 != 0 || n2 != 0)) return MAMBA_ERR_UNSUPPORTED;
+    *done = M == 0 || N == 0;
+    if (*done) return MAMBA_OK;
     if (K == 0) return MAMBA_ERR_BAD_SHAPE;
-    if (!x || !w) return MAMBA_ERR_NULL_POINTER;
+    if (!a.x || !a.w) return MAMBA_ERR_NULL_POINTER;
     for (int i = 0; i < 3; ++i)
-        if (widths[i] > 0 && !outs[i]) return MAMBA_ERR_NULL_POINTER;
-    if (!aligned16(x) || !aligned16(w) || !aligned16(bias) || !aligned16(residual) || !aligned16(out0) ||
-        !aligned16(out1) || !aligned16(out2))
+        if (a.width[i] > 0 && !a.out[i]) return MAMBA_ERR_NULL_POINTER;
+    if (!aligned16(a.x) || !aligned16(a.w) || !aligned16(a.bias) || !aligned16(a.residual) || !aligned16(a.out[0]) ||
+        !aligned16(a.out[1]) || !aligned16(a.out[2]))
         return MAMBA_ERR_MISALIGNED;
     for (int i = 0; i < 3; ++i) {
-        if (widths[i] == 0) continue;
-        if (overlap(outs[i], ob[i], x, xb) || overlap(outs[i], ob[i], w, wb)) return MAMBA_ERR_ALIAS;
+        if (a.width[i] == 0) continue;
+        if (overlap(a.out[i], ob[i], a.x, xb) || overlap(a.out[i], ob[i], a.w, wb)) return MAMBA_ERR_ALIAS;
         for (int j = i + 1; j < 3; ++j)
-            if (widths[j] > 0 && overlap(outs[i], ob[i], outs[j], ob[j])) return MAMBA_ERR_ALIAS;
+            if (a.width[j] > 0 && overlap(a.out[i], ob[i], a.out[j], ob[j])) return MAMBA_ERR_ALIAS;
     }
-    if (residual && residual != out0 && overlap(residual, ob[0], out0, ob[0])) return MAMBA_ERR_ALIAS;
-    LinearArgs a{x, w, bias, residual, {out0, out1, out2}, {n0, n1, n2}, M, K};
-    return (int)launch_linear(a, static_cast<hipStream_t>(hip_stream));
+    if (a.residual && a.residual != a.out[0] && overlap(a.residual, ob[0], a.out[0], ob[0])) return MAMBA_ERR_ALIAS;
+    return MAMBA_OK;
+}
+
+}  // namespace
+
+int mamba_linear_fwd(const void *x, const void *w, const float *bias, const void *residual, void *out0,
+                     int64_t n0, void *out1, int64_t n1, void *out2, int64_t n2, int64_t M, int64_t K,
+                     mamba_dtype_t io, void *hip_stream)
+{
+    const LinearArgs a{x, w, bias, residual, {out0, out1, out2}, {n0, n1, n2}, M, K};
+    bool done;
+    if (const int st = linear_checked(a, io, &done)) return st;
+    return done ? MAMBA_OK : (int)launch_linear(a, static_cast<hipStream_t>(hip_stream));
+}
+
+size_t mamba_linear_adapted_workspace_bytes(int64_t M, int64_t rank)
+{
+    int64_t bytes;
+    return M > 0 && rank > 0 && rank % 8 == 0 && rank <= 128 && size3(M, rank, 2, 2, &bytes) ? (size_t)bytes : 0;
+}
+
+int mamba_linear_adapted_fwd(const void *x, const void *w, const float *bias, const void *residual, const void *lora_a,
+                             const void *lora_b, const float *scale, const int32_t *adapter_idx, void *out0, int64_t n0, void *out1,
+                             int64_t n1, void *out2, int64_t n2, void *workspace, size_t workspace_bytes, int64_t M, int64_t K,
+                             int64_t rank, int64_t n_adapters, mamba_dtype_t io, void *hip_stream)
+{
+    const LinearArgs a{x, w, bias, residual, {out0, out1, out2}, {n0, n1, n2}, M, K};
+    bool done;
+    if (const int st = linear_checked(a, io, &done)) return st;
+    if (rank < 0 || n_adapters < 0) return MAMBA_ERR_BAD_SHAPE;
+    const int64_t N = n0 + n1 + n2;
+    int64_t ab, bb, tb;
+    if (!size3(n_adapters, rank, K, 2, &ab) || !size3(n_adapters, N, rank, 2, &bb) || !size3(M, rank, 2, 2, &tb)) return MAMBA_ERR_BAD_SHAPE;
+    if (rank == 0 || rank % 8 != 0 || rank > 128 || n_adapters > 0x7ffffffe || K > 0x7ffffff8 || N > 0x7fffffff) return MAMBA_ERR_UNSUPPORTED;
+    if (done) return MAMBA_OK;
+    if (n_adapters == 0) return MAMBA_ERR_BAD_SHAPE;
+    if (!lora_a || !lora_b || !adapter_idx) return MAMBA_ERR_NULL_POINTER;
+    if (!aligned16(lora_a) || !aligned16(lora_b) || !aligned16(scale) || !aligned16(adapter_idx) || !aligned16(workspace)) return MAMBA_ERR_MISALIGNED;
+    if (!workspace || workspace_bytes < (size_t)tb) return MAMBA_ERR_WORKSPACE;
+    for (int i = 0; i < 4; ++i) {
+        const void *out = i < 3 ? a.out[i] : workspace;
+        const int64_t n = i < 3 ? M * a.width[i] * 2 : tb;
+        if (n == 0) continue;
+        if (overlap(out, n, lora_a, ab) || overlap(out, n, lora_b, bb) || overlap(out, n, scale, n_adapters * 4) || overlap(out, n, adapter_idx, M * 4) ||
+            overlap(out, n, bias, N * 4))
+            return MAMBA_ERR_ALIAS;
+        if (i < 3 && overlap(out, n, workspace, tb)) return MAMBA_ERR_ALIAS;
+    }
+    if (overlap(workspace, tb, x, M * K * 2) || overlap(workspace, tb, w, N * K * 2) || overlap(workspace, tb, residual, residual ? M * N * 2 : 0))
+        return MAMBA_ERR_ALIAS;
+    const AdapterArgs l{lora_a, lora_b, scale, adapter_idx, workspace, rank, n_adapters};
+    return (int)launch_linear_adapted(a, l, static_cast<hipStream_t>(hip_stream));
 }
 
 int mamba_rmsnorm_fwd(const void *x, const float *w, void *y, int64_t M, int64_t C, float eps,
@@ -1078,6 +1130,86 @@ int mamba_topk_constrained_fwd(const void *logits, const mamba_constraints_t *c,
             if (overlap(out[i].p, out[i].n, out[j].p, out[j].n)) return MAMBA_ERR_ALIAS;
     }
     return (int)launch_children(logits, idx, val, path_out, workspace, a, M, k, (int)io, static_cast<hipStream_t>(hip_stream));
+}
+
+size_t mamba_sample_workspace_bytes(int64_t M, int64_t V, int k)
+{
+    if (M <= 0 || V <= 0 || k < 1 || k > 8 || !sample_fits(M, V)) return 0;
+    return sample_workspace_bytes(M, V);
+}
+
+int mamba_sample_fwd(const void *logits, const mamba_sampling_t *s, const float *u, int32_t *idx, float *prob, float *dist,
+                     int32_t *path_out, void *workspace, size_t workspace_bytes, int64_t M, int64_t V, int k, mamba_dtype_t io,
+                     void *hip_stream)
+{
+    const int e = io_size(io);
+    if (e == 0) return MAMBA_ERR_UNSUPPORTED;
+    int64_t lb, db;
+    if (!size3(M, V, 1, e, &lb) || !size3(M, V, 1, 4, &db)) return MAMBA_ERR_BAD_SHAPE;
+    if (k < 1 || k > 8 || !sample_fits(M, V)) return MAMBA_ERR_UNSUPPORTED;
+    if (!s) return MAMBA_ERR_NULL_POINTER;
+    if (s->n_seq < 0 || s->path_len < 0) return MAMBA_ERR_BAD_SHAPE;
+    if (s->path_len > 4096) return MAMBA_ERR_UNSUPPORTED;
+    int64_t params;
+    if (!size3(s->n_seq, 3, 1, 4, &params)) return MAMBA_ERR_BAD_SHAPE;
+    if (M == 0) return MAMBA_OK;
+    if (V == 0 || s->n_seq == 0 || (!s->seq_idx && s->n_seq != 1 && s->n_seq != M)) return MAMBA_ERR_BAD_SHAPE;
+    if (!logits || !s->params || !u || !idx || !prob || (s->path_len > 0 && !s->path && path_out)) return MAMBA_ERR_NULL_POINTER;
+    if (!aligned16(logits) || !aligned16(s->params) || !aligned16(s->top_k) || !aligned16(s->seq_idx) || !aligned16(s->path) || !aligned16(u) ||
+        !aligned16(idx) || !aligned16(prob) || !aligned16(path_out) || !aligned16(workspace) || (reinterpret_cast<uintptr_t>(dist) & 3u))
+        return MAMBA_ERR_MISALIGNED;
+    const size_t need = sample_workspace_bytes(M, V);
+    if (!workspace || workspace_bytes < need) return MAMBA_ERR_WORKSPACE;
+    const Span in[6] = {{logits, lb}, {s->params, params}, {s->top_k, s->n_seq * 4}, {s->seq_idx, M * 4}, {s->path, M * s->path_len * 4}, {u, M * k * 4}};
+    const Span out[5] = {{idx, M * k * 4}, {prob, M * k * 4}, {dist, db}, {path_out, M * k * (s->path_len + 1) * 4}, {workspace, (int64_t)need}};
+    for (int i = 0; i < 5; ++i) {
+        for (const Span &r : in)
+            if (overlap(out[i].p, out[i].n, r.p, r.n)) return MAMBA_ERR_ALIAS;
+        for (int j = 0; j < i; ++j)
+            if (overlap(out[i].p, out[i].n, out[j].p, out[j].n)) return MAMBA_ERR_ALIAS;
+    }
+    const SampleArgs a{s->params, s->top_k, s->seq_idx, s->path, u, idx, prob, dist, path_out, s->n_seq, s->path_len, M, V, k};
+    return (int)launch_sample(logits, workspace, a, (int)io, static_cast<hipStream_t>(hip_stream));
+}
+
+int mamba_tree_verify_fwd(const float *p, const float *q, const int32_t *tokens, const float *u_accept, const float *u_sample,
+                          int32_t *out, int32_t *count, int32_t *node, const int32_t *tree, int gamma, int64_t n_seq, int64_t V,
+                          void *hip_stream)
+{
+    static_assert(kMaxDepth == MAMBA_MAX_DEPTH, "a tree fits");
+    if (!tree) return MAMBA_ERR_NULL_POINTER;
+    if (gamma < 1 || gamma > MAMBA_MAX_DEPTH || n_seq < 0 || V < 0) return MAMBA_ERR_BAD_SHAPE;
+    VerifyArgs a{p, q, tokens, u_accept, u_sample, out, count, node, n_seq, V, 1, 0, gamma, {}};
+    int64_t rows = 1;
+    for (int i = 0; i < gamma; ++i) {
+        if (tree[i] < 1) return MAMBA_ERR_BAD_SHAPE;
+        if (tree[i] > kMaxFan) return MAMBA_ERR_UNSUPPORTED;
+        a.tree[i] = tree[i];
+        a.inner = a.nodes;
+        rows *= tree[i];
+        a.nodes += rows;
+        if (a.nodes > kMaxGridYZ) return MAMBA_ERR_UNSUPPORTED;
+    }
+    int64_t pb, qb, tb, ob;
+    if (!size3(n_seq, a.nodes, V, 4, &pb) || !size3(n_seq, a.inner, V, 4, &qb) || !size3(n_seq, a.nodes - 1, 1, 4, &tb) ||
+        !size3(n_seq, gamma + 1, 1, 4, &ob))
+        return MAMBA_ERR_BAD_SHAPE;
+    if (n_seq >= (1 << 22) || V > kMaxVocabulary) return MAMBA_ERR_UNSUPPORTED;
+    if (n_seq == 0) return MAMBA_OK;
+    if (V == 0) return MAMBA_ERR_BAD_SHAPE;
+    if (!p || !q || !tokens || !u_accept || !u_sample || !out || !count || !node) return MAMBA_ERR_NULL_POINTER;
+    if (!aligned16(tokens) || !aligned16(u_accept) || !aligned16(u_sample) || !aligned16(out) || !aligned16(count) || !aligned16(node) ||
+        (reinterpret_cast<uintptr_t>(p) & 3u) || (reinterpret_cast<uintptr_t>(q) & 3u))
+        return MAMBA_ERR_MISALIGNED;
+    const Span in[5] = {{p, pb}, {q, qb}, {tokens, tb}, {u_accept, tb}, {u_sample, n_seq * 4}};
+    const Span outs[3] = {{out, ob}, {count, n_seq * 4}, {node, n_seq * gamma * 4}};
+    for (int i = 0; i < 3; ++i) {
+        for (const Span &r : in)
+            if (overlap(outs[i].p, outs[i].n, r.p, r.n)) return MAMBA_ERR_ALIAS;
+        for (int j = 0; j < i; ++j)
+            if (overlap(outs[i].p, outs[i].n, outs[j].p, outs[j].n)) return MAMBA_ERR_ALIAS;
+    }
+    return (int)launch_verify(a, static_cast<hipStream_t>(hip_stream));
 }
 
 int mamba_tree_plan(const int32_t *tree, int gamma, int64_t n_layers, int64_t D, int64_t N, int K,

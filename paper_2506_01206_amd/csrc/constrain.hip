@@ -10,6 +10,7 @@
 // Every operation is one float32 operation, rounded: which of two tokens is ahead does not depend on how the compiler contracts.
 #include "device_math.h"
 #include "launch.h"
+#include "logit_rows.h"
 
 #include <type_traits>
 
@@ -22,48 +23,6 @@ constexpr int kThreads = 256;
 // four (4.4 with one since the search is without branches); logits of 19 rows 3.6, 4.2 and 5.8.
 constexpr int kSlice = kThreads * 8;                                 // tokens to a workgroup
 constexpr int32_t kNoKey = INT32_MIN;                                // below every key
-
-typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));      // rows of V elements start anywhere
-typedef int32_t i32x4_any __attribute__((ext_vector_type(4), aligned(4)));
-typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
-
-__device__ __forceinline__ void load8(const float *p, float *x)
-{
-    const f32x4_any a = *reinterpret_cast<const f32x4_any *>(p), b = *reinterpret_cast<const f32x4_any *>(p + 4);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = a[i], x[4 + i] = b[i];
-}
-__device__ __forceinline__ void load8(const bf16_t *p, float *x)
-{
-    const u32x4_any a = *reinterpret_cast<const u32x4_any *>(p);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[2 * i] = bf16_lo(a[i]), x[2 * i + 1] = bf16_hi(a[i]);
-}
-__device__ __forceinline__ void load8(const int32_t *p, int32_t *x)
-{
-    const i32x4_any a = *reinterpret_cast<const i32x4_any *>(p), b = *reinterpret_cast<const i32x4_any *>(p + 4);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = a[i], x[4 + i] = b[i];
-}
-__device__ __forceinline__ void store8(float *p, const float *x)
-{
-    f32x4_any a, b;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) a[i] = x[i], b[i] = x[4 + i];
-    *reinterpret_cast<f32x4_any *>(p) = a;
-    *reinterpret_cast<f32x4_any *>(p + 4) = b;
-}
-__device__ __forceinline__ void store8(bf16_t *p, const float *x)
-{
-    u32x4_any a;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) a[i] = f32x2_to_bf16x2(x[2 * i], x[2 * i + 1]);
-    *reinterpret_cast<u32x4_any *>(p) = a;
-}
-
-// A grid of slices by rows has the rows in two of its dimensions: no number of a workgroup is divided.
-constexpr int64_t kRowsY = 65535;
-__device__ __forceinline__ int64_t row_of_block() { return (int64_t)blockIdx.z * kRowsY + blockIdx.y; }
 
 // What holds for one row of logits.
 struct RowRules {

@@ -214,6 +214,16 @@ struct LinearArgs {
     int xproj_n = 0;
 };
 hipError_t launch_linear(const LinearArgs &a, hipStream_t stream);
+// Low-rank adapters beside a product: row m adds scale[a] (x a[a]^T) b[a]^T, a = idx[m] (-1: none; out of range: NaN).
+struct AdapterArgs {
+    const void *a, *b;       // (adapters, rank, K), (adapters, N, rank) bf16
+    const float *scale;      // (adapters) or nullptr: ones
+    const int32_t *idx;      // (M)
+    void *t;                 // scratch (M, 2 rank) bf16
+    int64_t rank, adapters;  // rank: a multiple of 8 up to 128
+};
+hipError_t launch_adapters_down(const void *x, const AdapterArgs &l, int64_t M, int64_t K, hipStream_t stream);   // t = scale x a^T in two terms
+hipError_t launch_linear_adapted(const LinearArgs &a, const AdapterArgs &l, hipStream_t stream);
 // out[0] = silu(conv1d(x w[:D]^T)), out[1] = x w[D:]^T, D = width[0] = width[1], where linear_conv_tiles (routes.h) has a tile for it
 hipError_t launch_linear_conv(const LinearArgs &a, hipStream_t stream);
 hipError_t launch_draft_in(const LinearArgs &a, hipStream_t stream);   // what launch_linear does with norm_w
@@ -257,5 +267,33 @@ hipError_t launch_children(const void *logits, int32_t *idx, float *val, int32_t
                            hipStream_t stream);
 hipError_t launch_token_counts(const int32_t *tokens, int32_t *counts, int64_t n_seq, int64_t L, int64_t V, int accumulate, int prompt,
                                hipStream_t stream);
+
+// Children and next tokens drawn from logits (M, V): what mamba_sampling_t points to, the random numbers and the outputs.
+struct SampleArgs {
+    const float *params;
+    const int32_t *top_k, *seq_idx, *path;
+    const float *u;
+    int32_t *idx;
+    float *prob, *dist;
+    int32_t *path_out;
+    int64_t n_seq, path_len, M, V;
+    int k;
+};
+bool sample_fits(int64_t M, int64_t V);
+size_t sample_workspace_bytes(int64_t M, int64_t V);
+hipError_t launch_sample(const void *logits, void *ws, const SampleArgs &a, int io, hipStream_t stream);
+
+// Verification of drafted trees: p (n_seq, nodes, V), q (n_seq, inner, V), tokens and u_accept (n_seq, nodes - 1).
+constexpr int kMaxFan = 8, kMaxDepth = 16;
+struct VerifyArgs {
+    const float *p, *q;
+    const int32_t *tokens;
+    const float *u_accept, *u_sample;
+    int32_t *out, *count, *node;
+    int64_t n_seq, V, nodes, inner;
+    int gamma;
+    int32_t tree[kMaxDepth];
+};
+hipError_t launch_verify(const VerifyArgs &a, hipStream_t stream);
 
 }  // namespace mamba

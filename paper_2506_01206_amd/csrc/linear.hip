@@ -60,14 +60,116 @@ __device__ __forceinline__ int locate(const OutSplit &o, int64_t n, int64_t *col
     return s;
 }
 
+// ---------------------------------------------------------------------------------------------------
+// Low-rank adapters beside a product (mamba_linear_adapted_fwd): out[m, n] += sum_r t[m, r] b[a, n, r], a the adapter of row m and t its scaled
+// product with the adapter's first matrix (adapters.hip), which is there as two bfloat16 terms side by side, high and low: 16 bits, so that it is
+// not the rounding of t that the output's rounding is lost in.  The kernels below take an AdapterTail behind their other arguments, or
+// nothing: then they are the plain products, instruction for instruction.
+// A wavefront goes through the adapters that its own rows have, smallest first, and multiplies whole tiles by each; a row takes the sums of its
+// own.  (Sums of the others are dropped, not added as zeros: an adapter's infinities and NaN stay with its rows.)
+struct AdapterTail {
+    const bf16_t *t;                 // (M, 2 rank): high terms, low terms
+    const bf16_t *b;                 // (adapters, N, rank)
+    const int32_t *idx;              // (M); -1: none
+    int32_t rank, adapters;          // rank: a multiple of 8
+};
+
+__device__ __forceinline__ int32_t wave_min(int32_t v)
+{
+#pragma unroll
+    for (int d = 32; d; d >>= 1) v = min(v, __shfl_xor(v, d));
+    return v;
+}
+// the adapter of row m (-1 behind the end), and the smallest one above `last` that any row of the wavefront has (the number of adapters: none)
+__device__ __forceinline__ int32_t adapter_of(const AdapterTail &t, int64_t m, int64_t M) { return m < M ? t.idx[m] : -1; }
+template <int MT> __device__ __forceinline__ int32_t next_adapter(const int32_t (&id)[MT], int32_t last, int32_t adapters)
+{
+    int32_t v = adapters;
+#pragma unroll
+    for (int a = 0; a < MT; ++a) v = id[a] > last ? min(v, id[a]) : v;
+    return wave_min(v);
+}
+
+// 32 x 32 tiles from row m0 and column n0 on.  TURNED: acc[a][b] has its rows in the lanes (w fragments first), else its columns.
+template <bool TURNED, int MT, int NT>
+__device__ __forceinline__ void add_adapters(f32x16 (&acc)[MT][NT], const AdapterTail &t, int64_t m0, int64_t M, int64_t n0, int64_t N)
+{
+    const int lane = threadIdx.x & 63, chunks = t.rank >> 3;
+    int32_t id[MT];
+#pragma unroll
+    for (int a = 0; a < MT; ++a) id[a] = adapter_of(t, m0 + a * 32 + (lane & 31), M);
+    auto row_id = [&](int a, int i) __attribute__((always_inline)) { return TURNED ? id[a] : __shfl(id[a], 8 * (i / 4) + 4 * (lane >> 5) + (i & 3)); };
+    for (int32_t cur = next_adapter(id, -1, t.adapters); cur < t.adapters; cur = next_adapter(id, cur, t.adapters)) {
+        const bf16_t *b[NT];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) b[j] = t.b + ((int64_t)cur * N + min(n0 + j * 32 + (lane & 31), N - 1)) * t.rank;
+#pragma unroll
+        for (int a = 0; a < MT; ++a) {
+            if (!__any(id[a] == cur)) continue;
+            const bf16_t *row = t.t + min(m0 + a * 32 + (lane & 31), M - 1) * (2 * t.rank);
+            f32x16 d[NT];
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) d[j][i] = 0.0f;
+            for (int c = lane >> 5; c < 2 * chunks; c += 2) {
+                const bf16x8 xf = *reinterpret_cast<const bf16x8 *>(row + 8 * c);
+                const int cb = c < chunks ? c : c - chunks;
+#pragma unroll
+                for (int j = 0; j < NT; ++j) {
+                    const bf16x8 wf = *reinterpret_cast<const bf16x8 *>(b[j] + 8 * cb);
+                    d[j] = TURNED ? __builtin_amdgcn_mfma_f32_32x32x16_bf16(wf, xf, d[j], 0, 0, 0) : __builtin_amdgcn_mfma_f32_32x32x16_bf16(xf, wf, d[j], 0, 0, 0);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const bool mine = row_id(a, i) == cur;
+#pragma unroll
+                for (int j = 0; j < NT; ++j) acc[a][j][i] += mine ? d[j][i] : 0.0f;
+            }
+        }
+    }
+    // a row whose index is out of range: NaN
+#pragma unroll
+    for (int a = 0; a < MT; ++a) {
+        if (!__any(id[a] < -1 || id[a] >= t.adapters)) continue;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int32_t r = row_id(a, i);
+#pragma unroll
+            for (int j = 0; j < NT; ++j) acc[a][j][i] = r < -1 || r >= t.adapters ? __int_as_float(0x7fc00000) : acc[a][j][i];
+        }
+    }
+}
+
+// The accumulators of an adapted product start from the residual, so that its outputs are rounded once.  (`dead` leading rows are not read: where
+// the residual is the output itself their owner may be writing them.)
+template <bool TURNED, int MT, int NT>
+__device__ __forceinline__ void start_from(f32x16 (&acc)[MT][NT], const bf16_t *residual, int64_t m0, int64_t first, int64_t M, int64_t n0, int64_t N)
+{
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int a = 0; a < MT; ++a)
+#pragma unroll
+        for (int b = 0; b < NT; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int across = 8 * (i / 4) + 4 * (lane >> 5) + (i & 3);
+                const int64_t m = max(min(m0 + a * 32 + (TURNED ? lane & 31 : across), M - 1), first);
+                const int64_t n = min(n0 + b * 32 + (TURNED ? across : lane & 31), N - 1);
+                acc[a][b][i] = bf16_to_f32(residual[m * N + n]);
+            }
+}
+
 // grid: (ceil(N / BN), ceil(M / BM)).  WSTREAM: w is read once and is large (the LM head on a draft position): its
 // loads are streaming, so that they do not push the blocks' weights, which the next position reads again, out of
 // the last-level cache.
-template <int BM, int BN, int BK, bool WSTREAM = false>
+template <int BM, int BN, int BK, bool WSTREAM = false, typename... Tail>
 __global__ void __launch_bounds__(kThreads)
 linear_kernel(const bf16_t *__restrict__ x, const bf16_t *__restrict__ w, const float *__restrict__ bias,
-              const bf16_t *residual, OutSplit out, int64_t M, int64_t N, int64_t K, int vector_out)
+              const bf16_t *residual, OutSplit out, int64_t M, int64_t N, int64_t K, int vector_out, Tail... tail)
 {
+    constexpr bool kAdapted = sizeof...(Tail) > 0;
     constexpr int MT = BM / 64, NT = BN / 64;                 // 32 x 32 MFMA tiles per wavefront along m, n
     constexpr int kBN = BN, kBK = BK;
     constexpr int kStageCols = BN < 128 ? BN : 128;           // the output tile is staged at most 128 columns at a time
@@ -132,6 +234,8 @@ linear_kernel(const bf16_t *__restrict__ x, const bf16_t *__restrict__ w, const 
 
     const int frag_row = lane & 31, frag_k = (lane >> 5) * 16;    // byte offset of the lane's 8 k values
     fetch(0);
+    if constexpr (kAdapted)
+        if (residual) start_from<false>(acc, residual, m0 + wm * (BM / 2), 0, M, n0 + wn * (BN / 2), N);
     for (int64_t k0 = 0; k0 < K; k0 += kBK) {
         __syncthreads();                                          // everyone is done reading the last slab
         park();
@@ -154,6 +258,7 @@ linear_kernel(const bf16_t *__restrict__ x, const bf16_t *__restrict__ w, const 
         }
     }
 
+    if constexpr (kAdapted) add_adapters<false>(acc, tail..., m0 + wm * (BM / 2), M, n0 + wn * (BN / 2), N);
     // epilogue.  acc[a][b][i] is C[8 * (i / 4) + 4 * (lane / 32) + i % 4][lane % 32] of its 32 x 32 tile.
     // The tile leaves through LDS 128 columns at a time.
 #pragma unroll
@@ -188,7 +293,7 @@ linear_kernel(const bf16_t *__restrict__ x, const bf16_t *__restrict__ w, const 
                 int64_t col;
                 const int s = locate(out, n, &col);
                 const int64_t off = m * out.width[s] + col;
-                if (residual) {
+                if (!kAdapted && residual) {
                     const uint4 r = *reinterpret_cast<const uint4 *>(residual + off);   // single output: same offset
                     v.x = f32x2_to_bf16x2(bf16_lo(v.x) + bf16_lo(r.x), bf16_hi(v.x) + bf16_hi(r.x));
                     v.y = f32x2_to_bf16x2(bf16_lo(v.y) + bf16_lo(r.y), bf16_hi(v.y) + bf16_hi(r.y));
@@ -206,7 +311,7 @@ linear_kernel(const bf16_t *__restrict__ x, const bf16_t *__restrict__ w, const 
                 int64_t col;
                 const int s = locate(out, n, &col);
                 const int64_t off = m * out.width[s] + col;
-                if (residual) v += bf16_to_f32(residual[off]);
+                if (!kAdapted && residual) v += bf16_to_f32(residual[off]);
                 out.ptr[s][off] = (bf16_t)f32_to_bf16(v);
             }
         }
@@ -330,11 +435,12 @@ __device__ __forceinline__ void load_to_lds16(const char *base, uint32_t lane_of
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_addr), "v"(lane_off), "s"(base) : "memory");
 }
 
-template <int BM, int BN, bool CONV = false, int WM = 2, int WN = 2>
+template <int BM, int BN, bool CONV = false, int WM = 2, int WN = 2, typename... Tail>
 __global__ void __launch_bounds__(64 * WM * WN)
 linear_wide_kernel(const bf16_t *x, const bf16_t *w, const float *__restrict__ bias, const bf16_t *residual,
-                   OutSplit out, int64_t M, int64_t N, int64_t K, int tiles_n, int n_tiles, ConvTail conv)
+                   OutSplit out, int64_t M, int64_t N, int64_t K, int tiles_n, int n_tiles, ConvTail conv, Tail... tail)
 {
+    constexpr bool kAdapted = sizeof...(Tail) > 0;
     constexpr int NW = WM * WN, kThr = 64 * NW;
     constexpr int MT = BM / WM / 32, NT = BN / WN / 32;           // 32 x 32 MFMA tiles per wavefront along m and n
     constexpr int kRows = BM + BN;
@@ -469,6 +575,8 @@ linear_wide_kernel(const bf16_t *x, const bf16_t *w, const float *__restrict__ b
     typedef std::integral_constant<int, 0> Even;
     typedef std::integral_constant<int, 1> Odd;
     const int S = (int)(K / kWideBK);
+    if constexpr (kAdapted)
+        if (residual) start_from<true>(acc, residual, m0 + wm * (BM / WM), m0 + dead, M, n0 + wn * (BN / WN), N);
     request(0, 0, L0(), L4());
     request(kWideBK, kStage, L0(), L4());
     // vmcnt(loads of one slab): slab 0 is in, slab 1 may be under way (vmcnt is split over bits 3:0 and 15:14)
@@ -482,12 +590,13 @@ linear_wide_kernel(const bf16_t *x, const bf16_t *w, const float *__restrict__ b
     }
     slab(Even(), 0, std::false_type(), std::true_type());         // S is even: two slabs left, nothing more to request
     slab(Odd(), 0, std::false_type(), std::false_type());
+    if constexpr (kAdapted) add_adapters<true>(acc, tail..., m0 + wm * (BM / WM), M, n0 + wn * (BN / WN), N);
     // Epilogue.  The residual chunks this thread will add are requested first, all at once: with one workgroup per
     // CU nothing else would hide their latency, and fetched four at a time inside the store loop they cost a third
     // of the tile's time.
     constexpr int kCpr = BN / 8, kChunks = BM * kCpr / kThr;
     u32x4 res[kChunks];
-    if (residual) {
+    if (!kAdapted && residual) {
 #pragma unroll
         for (int i = 0; i < kChunks; ++i) {
             const int c = tid + i * kThr, row = c / kCpr, cc = c % kCpr;
@@ -529,7 +638,7 @@ linear_wide_kernel(const bf16_t *x, const bf16_t *w, const float *__restrict__ b
         int64_t col;
         const int sp = locate(out, n0 + cc * 8, &col);
         const int64_t off = (m0 + row) * out.width[sp] + col;
-        if (residual) {
+        if (!kAdapted && residual) {
             const u32x4 r = res[i];
             v.x = f32x2_to_bf16x2(bf16_lo(v.x) + bf16_lo(r.x), bf16_hi(v.x) + bf16_hi(r.x));
             v.y = f32x2_to_bf16x2(bf16_lo(v.y) + bf16_lo(r.y), bf16_hi(v.y) + bf16_hi(r.y));
@@ -576,11 +685,12 @@ __device__ __forceinline__ void wave_sync()
 // Requires M >= BM, N % BN == 0, K % 64 == 0 and output widths that are multiples of 8; the last row block moves back as above.
 // grid: 8 * ceil(tiles / 8) workgroups, each XCD a contiguous range of tiles in groups of group_n columns: a walk over all
 // columns would bring all of w into every XCD's L2.
-template <int BM, int BN, int WM, int WN, int STAGES, int PER_CU, bool CONV = false>
+template <int BM, int BN, int WM, int WN, int STAGES, int PER_CU, bool CONV = false, typename... Tail>
 __global__ void __launch_bounds__(64 * WM * WN, WM * WN * PER_CU / 4)
 linear_ring_kernel(const bf16_t *x, const bf16_t *w, const float *__restrict__ bias, const bf16_t *residual,
-                   int64_t M, int64_t K, int tiles_m, int tiles_n, int group_n, OutSplit out, ConvTail conv)
+                   int64_t M, int64_t K, int tiles_m, int tiles_n, int group_n, OutSplit out, ConvTail conv, Tail... tail)
 {
+    constexpr bool kAdapted = sizeof...(Tail) > 0;
     constexpr int NW = WM * WN;
     constexpr int MT = BM / WM / 32, NT = BN / WN / 32;           // 32 x 32 MFMA tiles per wavefront along m and n
     constexpr int kStage = (BM + BN) * kWideRow;
@@ -677,6 +787,8 @@ linear_ring_kernel(const bf16_t *x, const bf16_t *w, const float *__restrict__ b
         return (m0 + row) * out.width[*sp] + col;
     };
     u32x4 res[MT][NT][2];
+    if constexpr (kAdapted)
+        if (residual) start_from<true>(acc, residual, m0 + wm * (BM / WM), m0 + dead, M, n0 + wn * (BN / WN), (int64_t)tiles_n * BN);
 
 #pragma unroll
     for (int i = 0; i < STAGES - 1; ++i) {
@@ -690,7 +802,7 @@ linear_ring_kernel(const bf16_t *x, const bf16_t *w, const float *__restrict__ b
     const unsigned char *cur = lds;
     load_frags(cur, 0, f0);
     request(L0(), L1());
-    const int fetch_res = residual ? (S > 3 ? S - 3 : 0) : -1;
+    const int fetch_res = !kAdapted && residual ? (S > 3 ? S - 3 : 0) : -1;
 #pragma unroll 1
     for (int s = 0; s < S; ++s) {
         if (s == fetch_res) {
@@ -726,6 +838,7 @@ linear_ring_kernel(const bf16_t *x, const bf16_t *w, const float *__restrict__ b
         multiply(f1);
     }
 
+    if constexpr (kAdapted) add_adapters<true>(acc, tail..., m0 + wm * (BM / WM), M, n0 + wn * (BN / WN), (int64_t)tiles_n * BN);
     if constexpr (CONV) {
         // the whole tile, since windows reach into the rows of other wavefronts; every read of the stages is behind the last barrier
         constexpr int kOutRow = BN * 2 + 16, kCpr = BN / 8;
@@ -775,7 +888,7 @@ linear_ring_kernel(const bf16_t *x, const bf16_t *w, const float *__restrict__ b
             for (int i = 0; i < 2; ++i) {
                 const int pr = 16 * i + (lane >> 2), row = out_row(a, i);
                 uint4 v = *reinterpret_cast<const uint4 *>(patch + pr * 64 + (((lane & 3) ^ ((pr >> 1) & 3)) << 4));
-                if (residual) {
+                if (!kAdapted && residual) {
                     const u32x4 q = res[a][b][i];
                     v.x = f32x2_to_bf16x2(bf16_lo(v.x) + bf16_lo(q.x), bf16_hi(v.x) + bf16_hi(q.x));
                     v.y = f32x2_to_bf16x2(bf16_lo(v.y) + bf16_lo(q.y), bf16_hi(v.y) + bf16_hi(q.y));
@@ -809,14 +922,63 @@ linear_ring_kernel(const bf16_t *x, const bf16_t *w, const float *__restrict__ b
 // 768, K = 1536 6.2 (8.5), 1000 x 768 9.0 (11.8), 512 x 512, K = 1024 3.9 (5.9).
 typedef float f32x4v __attribute__((ext_vector_type(4)));
 
+// Adapters of the rows of a tile: wavefront q multiplies by every NW-th of them, into partial tiles that are added up anyway.
+template <int NW, int MT, int NT>
+__device__ __forceinline__ void add_adapters_few(f32x4v (&acc)[MT][NT], const AdapterTail &t, int wave, int m0, int M, int n0, int N)
+{
+    const int lane = threadIdx.x & 63, li = lane & 15, lg = lane >> 4, chunks = t.rank >> 3;
+    const int32_t id[1] = {lane < 16 * MT ? adapter_of(t, m0 + lane, M) : -1};
+    int turn = 0;
+    for (int32_t cur = next_adapter(id, -1, t.adapters); cur < t.adapters; cur = next_adapter(id, cur, t.adapters), ++turn) {
+        if (turn % NW != wave) continue;
+        const uint64_t rows = __ballot(id[0] == cur);
+        f32x4v d[MT][NT];
+#pragma unroll
+        for (int a = 0; a < MT; ++a)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) d[a][n] = f32x4v(0.0f);
+        for (int c0 = 0; c0 < 2 * chunks; c0 += 4) {
+            const int c = c0 + lg;
+            const bool in = c < 2 * chunks;
+            const int ct = in ? c : 0, cb = ct < chunks ? ct : ct - chunks;
+            bf16x8 wf[NT];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) wf[n] = *reinterpret_cast<const bf16x8 *>(t.b + ((int64_t)cur * N + min(n0 + 16 * n + li, N - 1)) * t.rank + 8 * cb);
+#pragma unroll
+            for (int a = 0; a < MT; ++a) {
+                const u32x4 raw = *reinterpret_cast<const u32x4 *>(t.t + (int64_t)min(m0 + 16 * a + li, M - 1) * (2 * t.rank) + 8 * ct);
+                const bf16x8 xf = __builtin_bit_cast(bf16x8, in ? raw : u32x4(0u));
+#pragma unroll
+                for (int n = 0; n < NT; ++n) d[a][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf, wf[n], d[a][n], 0, 0, 0);
+            }
+        }
+#pragma unroll
+        for (int a = 0; a < MT; ++a)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[a][n][i] += rows >> (16 * a + 4 * lg + i) & 1 ? d[a][n][i] : 0.0f;
+    }
+    const uint64_t bad = __ballot(id[0] < -1 || id[0] >= t.adapters);   // out of range: NaN
+    if (bad && wave == 0) {
+#pragma unroll
+        for (int a = 0; a < MT; ++a)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[a][n][i] = bad >> (16 * a + 4 * lg + i) & 1 ? __int_as_float(0x7fc00000) : acc[a][n][i];
+    }
+}
+
 // EVEN: K = 64 NW G, one trip of every wavefront; otherwise any K that is a multiple of 8.
 // STREAM: w is read once and is large (the LM head on a draft position): its loads are streaming, so that they do not push the
 // blocks' weights, which the next position reads again, out of the last-level cache.
-template <int MT, int CG, int NW, int G, bool EVEN, bool STREAM>
+template <int MT, int CG, int NW, int G, bool EVEN, bool STREAM, typename... Tail>
 __global__ void __launch_bounds__(64 * NW)
 linear_few_kernel(const bf16_t *__restrict__ x, const bf16_t *__restrict__ w, const float *__restrict__ bias,
-                  const bf16_t *residual, int M, int N, int K, OutSplit out)
+                  const bf16_t *residual, int M, int N, int K, OutSplit out, Tail... tail)
 {
+    constexpr bool kAdapted = sizeof...(Tail) > 0;
     constexpr int kThr = NW * 64;
     constexpr int NT = (CG + 1) / 2;                               // column tiles of 16
     constexpr int kStep = (NT + MT) * 2048;                        // fragments of one step: NT column tiles of w, then MT row tiles
@@ -932,6 +1094,7 @@ linear_few_kernel(const bf16_t *__restrict__ x, const bf16_t *__restrict__ w, co
             wave_sync();
         }
     }
+    if constexpr (kAdapted) add_adapters_few<NW>(acc, tail..., wave, m0, M, n0, N);
     // acc[t][n][i] is C[m = 16 t + 4 (lane / 16) + i][16 n + lane % 16]
 #pragma unroll
     for (int t = 0; t < MT; ++t)
@@ -950,8 +1113,9 @@ linear_few_kernel(const bf16_t *__restrict__ x, const bf16_t *__restrict__ w, co
 #pragma unroll
         for (int q = 0; q < NW; ++q) v += reinterpret_cast<const float *>(patch[q])[at];
         if (o6 >= 4 * MT * NT || om[j] >= M || on[j] >= N || li >= 8 * CG) continue;
-        v = bf16_to_f32(f32_to_bf16(v + (bias ? bias_in[j] : 0.0f)));   // same two roundings as the tiled kernel
-        if (residual) {
+        if constexpr (kAdapted) v = v + (bias ? bias_in[j] : 0.0f) + (residual ? bf16_to_f32(res[j]) : 0.0f);
+        else v = bf16_to_f32(f32_to_bf16(v + (bias ? bias_in[j] : 0.0f)));   // same two roundings as the tiled kernel
+        if (!kAdapted && residual) {
             out.ptr[0][(int64_t)om[j] * N + on[j]] = (bf16_t)f32_to_bf16(v + bf16_to_f32(res[j]));
             continue;
         }
@@ -962,12 +1126,12 @@ linear_few_kernel(const bf16_t *__restrict__ x, const bf16_t *__restrict__ w, co
     }
 }
 
-template <int MT, int CG, bool STREAM = false>
+template <int MT, int CG, bool STREAM = false, typename... Tail>
 hipError_t launch_few(const bf16_t *x, const bf16_t *w, const float *bias, const bf16_t *res, const OutSplit &o, int64_t M, int64_t N, int64_t K,
-                      hipStream_t stream)
+                      hipStream_t stream, Tail... tail)
 {
     const dim3 grid((unsigned)((N + 8 * CG - 1) / (8 * CG)), (unsigned)((M + 16 * MT - 1) / (16 * MT)));
-#define MAMBA_FEW_K(NW, G, EVEN) linear_few_kernel<MT, CG, NW, G, EVEN, STREAM><<<grid, 64 * NW, 0, stream>>>(x, w, bias, res, (int)M, (int)N, (int)K, o)
+#define MAMBA_FEW_K(NW, G, EVEN) linear_few_kernel<MT, CG, NW, G, EVEN, STREAM><<<grid, 64 * NW, 0, stream>>>(x, w, bias, res, (int)M, (int)N, (int)K, o, tail...)
     const int64_t per = (K + 511) / 512;
     if (K == 256) MAMBA_FEW_K(4, 1, true);
     else if (K < 256) MAMBA_FEW_K(4, 1, false);
@@ -980,9 +1144,9 @@ hipError_t launch_few(const bf16_t *x, const bf16_t *w, const float *bias, const
     return hipGetLastError();
 }
 
-template <int BM, int BN, int WM, int WN, int STAGES, int PER_CU, bool CONV = false>
+template <int BM, int BN, int WM, int WN, int STAGES, int PER_CU, bool CONV = false, typename... Tail>
 hipError_t launch_ring(const bf16_t *x, const bf16_t *w, const float *bias, const bf16_t *res, const OutSplit &o, int64_t M, int64_t N, int64_t K,
-                       hipStream_t stream, const ConvTail &conv = ConvTail{})
+                       hipStream_t stream, const ConvTail &conv, Tail... tail)
 {
     const int tiles_m = (int)row_blocks(M, BM, CONV), tiles_n = (int)(N / BN);
     // columns of a group: as many as bring about 2 MB of w, half of an XCD's L2, in groups of equal width
@@ -990,24 +1154,27 @@ hipError_t launch_ring(const bf16_t *x, const bf16_t *w, const float *bias, cons
     const int64_t groups = (tiles_n + most - 1) / most;
     const unsigned per_xcd = (unsigned)((tiles_m * tiles_n + 7) / 8);
     linear_ring_kernel<BM, BN, WM, WN, STAGES, PER_CU, CONV><<<8 * per_xcd, 64 * WM * WN, 0, stream>>>(
-        x, w, bias, res, M, K, tiles_m, tiles_n, (int)((tiles_n + groups - 1) / groups), o, conv);
+        x, w, bias, res, M, K, tiles_m, tiles_n, (int)((tiles_n + groups - 1) / groups), o, conv, tail...);
     return hipGetLastError();
 }
 
-template <int BM, int BN, bool CONV = false, int WM = 2, int WN = 2>
+template <int BM, int BN, bool CONV = false, int WM = 2, int WN = 2, typename... Tail>
 hipError_t launch_wide(const bf16_t *x, const bf16_t *w, const float *bias, const bf16_t *res, const OutSplit &o, int64_t M, int64_t N, int64_t K,
-                       hipStream_t stream, ConvTail conv = ConvTail{})
+                       hipStream_t stream, ConvTail conv, Tail... tail)
 {
     const int64_t tiles_n = N / BN, z_blocks = row_blocks(M, BM, false);
     const int64_t n_tiles = z_blocks * tiles_n + (CONV ? (row_blocks(M, BM, true) - z_blocks) * (o.width[0] / BN) : 0);
     conv.z_blocks = (int)z_blocks;
-    linear_wide_kernel<BM, BN, CONV, WM, WN><<<(unsigned)(8 * ((n_tiles + 7) / 8)), 64 * WM * WN, 0, stream>>>(x, w, bias, res, o, M, N, K, (int)tiles_n, (int)n_tiles, conv);
+    linear_wide_kernel<BM, BN, CONV, WM, WN><<<(unsigned)(8 * ((n_tiles + 7) / 8)), 64 * WM * WN, 0, stream>>>(x, w, bias, res, o, M, N, K, (int)tiles_n, (int)n_tiles, conv, tail...);
     return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_linear(const LinearArgs &a, hipStream_t stream)
+namespace {
+
+// the kernel of a product, with or without an AdapterTail
+template <typename... Tail> hipError_t launch_product(const LinearArgs &a, hipStream_t stream, Tail... tail)
 {
     OutSplit o;
     for (int s = 0; s < 3; ++s) {
@@ -1018,19 +1185,19 @@ hipError_t launch_linear(const LinearArgs &a, hipStream_t stream)
     const int vec = linear_vector_out(a.width) ? 1 : 0;
     const bf16_t *x = static_cast<const bf16_t *>(a.x), *w = static_cast<const bf16_t *>(a.w);
     const bf16_t *res = static_cast<const bf16_t *>(a.residual);
-    if (a.norm_w) return launch_draft_in(a, stream);
-#define MAMBA_LINEAR(HOW, ...) return launch_##HOW<__VA_ARGS__>(x, w, a.bias, res, o, a.M, N, a.K, stream)
+#define MAMBA_FEW(...) return launch_few<__VA_ARGS__>(x, w, a.bias, res, o, a.M, N, a.K, stream, tail...)
+#define MAMBA_LINEAR(HOW, ...) return launch_##HOW<__VA_ARGS__>(x, w, a.bias, res, o, a.M, N, a.K, stream, ConvTail{}, tail...)
 #define MAMBA_TILES(BM, BN, ...)                                                                                                      \
     linear_kernel<BM, BN, __VA_ARGS__><<<dim3((unsigned)((N + BN - 1) / BN), (unsigned)((a.M + BM - 1) / BM)), kThreads, 0, stream>>>( \
-        x, w, a.bias, res, o, a.M, N, a.K, vec);                                                                                      \
+        x, w, a.bias, res, o, a.M, N, a.K, vec, tail...);                                                                             \
     return hipGetLastError()
     switch (linear_route(a.M, a.width, a.K)) {
-    case kFew16x16Stream: MAMBA_LINEAR(few, 1, 2, true);
-    case kFew16x8: MAMBA_LINEAR(few, 1, 1);
-    case kFew16x16: MAMBA_LINEAR(few, 1, 2);
-    case kFew32x16: MAMBA_LINEAR(few, 2, 2);
-    case kFew64x32: MAMBA_LINEAR(few, 4, 4);
-    case kFew32x32: MAMBA_LINEAR(few, 2, 4);
+    case kFew16x16Stream: MAMBA_FEW(1, 2, true);
+    case kFew16x8: MAMBA_FEW(1, 1);
+    case kFew16x16: MAMBA_FEW(1, 2);
+    case kFew32x16: MAMBA_FEW(2, 2);
+    case kFew64x32: MAMBA_FEW(4, 4);
+    case kFew32x32: MAMBA_FEW(2, 4);
     case kRing64: MAMBA_LINEAR(ring, 64, 64, 2, 2, 4, 2);
     case kRing64x128: MAMBA_LINEAR(ring, 64, 128, 2, 4, 6, 1);
     case kRing128: MAMBA_LINEAR(ring, 128, 128, 2, 4, 4, 1);
@@ -1049,6 +1216,17 @@ hipError_t launch_linear(const LinearArgs &a, hipStream_t stream)
     return hipErrorInvalidValue;
 #undef MAMBA_TILES
 #undef MAMBA_LINEAR
+#undef MAMBA_FEW
+}
+
+}  // namespace
+
+hipError_t launch_linear(const LinearArgs &a, hipStream_t stream) { return a.norm_w ? launch_draft_in(a, stream) : launch_product(a, stream); }
+
+hipError_t launch_linear_adapted(const LinearArgs &a, const AdapterArgs &l, hipStream_t stream)
+{
+    if (const hipError_t e = launch_adapters_down(a.x, l, a.M, a.K, stream)) return e;
+    return launch_product(a, stream, AdapterTail{static_cast<const bf16_t *>(l.t), static_cast<const bf16_t *>(l.b), l.idx, (int32_t)l.rank, (int32_t)l.adapters});
 }
 
 hipError_t launch_linear_conv(const LinearArgs &a, hipStream_t stream)

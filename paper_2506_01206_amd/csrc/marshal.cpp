@@ -315,17 +315,24 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", "argument marshalling o
 
 }  // namespace
 
-PyObject *marshal_delta_module();   // marshal_delta.cpp
+PyObject *marshal_delta_module();    // marshal_delta.cpp
+PyObject *marshal_sample_module();   // marshal_sample.cpp
 
 PyMODINIT_FUNC PyInit__marshal(void)
 {
     PyObject *m = PyModule_Create(&module);
     if (!m) return nullptr;
-    PyObject *delta = marshal_delta_module();
-    if (!delta || PyModule_AddObject(m, "_delta", delta) < 0) {   // (takes the reference where it succeeds)
-        Py_XDECREF(delta);
-        Py_DECREF(m);
-        return nullptr;
+    const struct {
+        const char *name;
+        PyObject *(*make)();
+    } parts[] = {{"_delta", marshal_delta_module}, {"_sample", marshal_sample_module}};
+    for (const auto &part : parts) {
+        PyObject *made = part.make();
+        if (!made || PyModule_AddObject(m, part.name, made) < 0) {   // (takes the reference where it succeeds)
+            Py_XDECREF(made);
+            Py_DECREF(m);
+            return nullptr;
+        }
     }
     return m;
 }

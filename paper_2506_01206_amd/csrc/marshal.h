@@ -1,4 +1,4 @@
-// What the two halves of the binding's marshalling module (marshal.cpp, marshal_delta.cpp) share: checks of tensors, outputs and
+// What the parts of the binding's marshalling module (marshal.cpp, marshal_delta.cpp, marshal_sample.cpp) share: checks of tensors, outputs and
 // scratch allocated for the caller, the call into the C ABI and its errors.
 #pragma once
 #define PY_SSIZE_T_CLEAN
@@ -107,6 +107,18 @@ void *ptr(PyObject *o, at::ScalarType type, Shape shape, const char *name)
     return pointer(t);
 }
 float *fptr(PyObject *o, Shape shape, const char *name) { return static_cast<float *>(ptr(o, at::kFloat, shape, name)); }
+
+// all of these are tensors or None, and the checks before have seen to it that the tensors are the GPU's
+[[maybe_unused]] void on_current_device(std::initializer_list<PyObject *> objects)
+{
+    const int current = c10::hip::current_device();
+    for (PyObject *o : objects)
+        if (o != Py_None && tensor(o, "tensor").get_device() != current) {
+            PyErr_Format(PyExc_ValueError, "all tensors must live on the current device (%d), one lives on %d", current,
+                         (int)tensor(o, "tensor").get_device());
+            throw PyFailed();
+        }
+}
 
 int io_code(const at::Tensor &t)
 {

@@ -17,18 +17,6 @@ struct Api {
     decltype(&::mamba_topk_constrained_fwd) topk_constrained_fwd;
 } api;
 
-// all of these are tensors or None, and the checks before have seen to it that the tensors are the GPU's
-void on_current_device(std::initializer_list<PyObject *> objects)
-{
-    const int current = c10::hip::current_device();
-    for (PyObject *o : objects)
-        if (o != Py_None && tensor(o, "tensor").get_device() != current) {
-            PyErr_Format(PyExc_ValueError, "all tensors must live on the current device (%d), one lives on %d", current,
-                         (int)tensor(o, "tensor").get_device());
-            throw PyFailed();
-        }
-}
-
 float number(PyObject *o)
 {
     const double v = PyFloat_AsDouble(o);

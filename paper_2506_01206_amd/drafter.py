@@ -4,9 +4,9 @@ The paper's drafter is a Mamba language model (Mamba-130M, Sec. 3.1): embedding,
 blocks, a final RMSNorm and the LM head.  It encodes the prefix once and then drafts a tree
 (N_1..N_gamma) as batch generation (Sec. 4.1): at position i every live branch proposes N_i children,
 the children copy their parent's states and all B_i = N_1 * ... * N_i branches advance together.
-Here the N_i children of a node are its N_i most probable next tokens (greedy candidates instead of
-samples, so that runs are reproducible), under penalties, biases and masks where the verifier decodes by
-some (``constrain``).  States live in one cache per distinct batch size
+Here the N_i children of a node are its N_i most probable next tokens, or N_i samples of its distribution from given random
+numbers (``sample``; ``verify`` accepts a path of them as the target's distributions have it), under penalties, biases and masks where the
+verifier decodes by some (``constrain``), from an LM head that low-rank adapters fit to the request (``adapt``).  States live in one cache per distinct batch size
 (``mamba_tree_plan``); every draft position has fixed shapes, allocates nothing and never touches
 the host, so a whole draft round is captured once per tree in a HIP graph and replayed.
 
@@ -36,6 +36,8 @@ class MambaDrafter:
         self.root_logits = torch.empty((1, self.V), dtype=torch.bfloat16, device=self.dev)
         self._trees = {}
         self._rules = None
+        self._sampling = None
+        self._adapters = None
 
     # ------------------------------------------------------------------ rules that the verifier decodes by
     def constrain(self, repetition=1.0, presence=0.0, frequency=0.0, bias=None, mask=None):
@@ -64,8 +66,7 @@ class MambaDrafter:
                          penalties=penalties.to(self.dev),
                          bias=torch.zeros((self.V,), dtype=torch.float32, device=self.dev),
                          masks=[torch.full((1, words), -1, dtype=torch.int32, device=self.dev) for _ in range(m.MAMBA_MAX_DEPTH)])
-            for bufs in self._trees.values():
-                bufs["constrained_graph"] = None         # (of buffers that were dropped)
+            self._forget("constrained")
             self._rules = rules
         r = self._rules
         r["penalties"].copy_(penalties)
@@ -83,6 +84,65 @@ class MambaDrafter:
             row = row.clone()
         m.mamba_token_counts(row, self.V, counts=self._rules["counts"])
 
+    # ------------------------------------------------------------------ children that are drawn
+    def sample(self, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
+        """Draw the children of every node from its distribution (without replacement) instead of taking the most probable ones; ``draft`` takes
+        the random numbers.  A branch that has fewer tokens left than the tree has children there gets token -1 for the others.  Calling it again
+        changes the settings in place (captured rounds follow); None for ``temperature`` goes back to the most probable ones."""
+        if temperature is None:
+            self._sampling = None
+            return
+        if not temperature >= 0 or top_p != top_p or min_p != min_p:
+            raise ValueError("temperature must be zero or more, top_p and min_p numbers, got %r, %r, %r" % (temperature, top_p, min_p))
+        params, top_k = torch.tensor([[temperature, top_p, min_p]], dtype=torch.float32), torch.tensor([int(top_k)], dtype=torch.int32)
+        if self._sampling is None:
+            self._forget("sampling")
+            self._sampling = dict(params=torch.empty((1, 3), dtype=torch.float32, device=self.dev), top_k=torch.empty((1,), dtype=torch.int32, device=self.dev))
+        self._sampling["params"].copy_(params)
+        self._sampling["top_k"].copy_(top_k)
+
+    # ------------------------------------------------------------------ adapters of the LM head
+    def adapt(self, lora_a, lora_b=None, scale=None, which=0):
+        """Put low-rank adapters beside the LM head: lora_a (n, rank, d_model), lora_b (n, V, rank) bf16, scale (n) f32; ``which`` of them the
+        next ``prefill`` and drafts take (``use_adapter`` changes that).  The tensors are kept, not copied: what is written to them holds for captured
+        rounds too.  None for ``lora_a`` drops them."""
+        if lora_a is None:
+            self._adapters = None
+            return
+        n, rank = lora_a.shape[:2] if lora_a.dim() == 3 else (0, 0)
+        if (lora_b is None or tuple(lora_a.shape) != (n, rank, self.dm) or tuple(lora_b.shape) != (n, self.V, rank)
+                or lora_a.dtype != torch.bfloat16 or lora_b.dtype != torch.bfloat16 or (scale is not None and tuple(scale.shape) != (n,))):
+            raise ValueError("adapters must have shapes (n, rank, %d) and (n, %d, rank) in bfloat16, and scale (n)" % (self.dm, self.V))
+        if rank == 0 or rank % 8 or rank > 128 or not 0 <= which < n:
+            raise ValueError("the rank must be a multiple of 8 up to 128, and the adapter one of the %d" % n)
+        self._forget("adapted")
+        self._adapters = dict(a=lora_a, b=lora_b, scale=scale, which=torch.full((1,), which, dtype=torch.int32, device=self.dev), idx={}, ws={})
+
+    def use_adapter(self, which):
+        """The adapter that the next ``prefill`` and drafts take, -1 for none (captured rounds follow)."""
+        if self._adapters is None:
+            raise RuntimeError("use_adapter() is for a drafter with adapters: call adapt() first")
+        if not -1 <= which < self._adapters["a"].shape[0]:
+            raise ValueError("the adapter must be one of the %d, or -1" % self._adapters["a"].shape[0])
+        for t in (self._adapters["which"], *self._adapters["idx"].values()):
+            t.fill_(which)
+
+    def _head(self, normed, out):
+        if self._adapters is None:
+            m.mamba_linear_fwd(normed, self.lm_head, outs=[out])
+            return
+        l, rows = self._adapters, normed.shape[0]
+        if rows not in l["idx"]:
+            l["idx"][rows] = l["which"].repeat(rows)
+            l["ws"][rows] = torch.empty(max(m.mamba_linear_adapted_workspace_bytes(rows, l["a"].shape[1]), 16), dtype=torch.uint8, device=self.dev)
+        m.mamba_linear_adapted_fwd(normed, self.lm_head, l["a"], l["b"], l["idx"][rows], scale=l["scale"], outs=[out], workspace=l["ws"][rows])
+
+    def _forget(self, what):
+        """Captured rounds with buffers that are about to be dropped."""
+        for bufs in self._trees.values():
+            for kind in [k for k in bufs if k.endswith("graph") and what in k]:
+                bufs[kind] = None
+
     # ------------------------------------------------------------------ prefix encoding
     def prefill(self, tokens, prompt_len=None):
         """Encode a prefix (int32[L]); returns the logits of the next token (1, V) and keeps the
@@ -99,7 +159,7 @@ class MambaDrafter:
             m.mamba_block_fwd(blk, hid, hidden_out=hid, conv_state_out=self.root_conv[l], h_final=self.root_ssm[l],
                               workspace=ws)
         last = m.mamba_rmsnorm_fwd(hid[0, L - 1:L].contiguous(), self.norm_f, self.eps)
-        m.mamba_linear_fwd(last, self.lm_head, outs=[self.root_logits])
+        self._head(last, self.root_logits)
         if self._rules is not None:
             counts = self._rules["counts"]
             counts.zero_()
@@ -135,7 +195,9 @@ class MambaDrafter:
             p, n_i = bufs["pos"][i], tree[i - 1]
             # the N_i most probable tokens of every branch become its children: child j of branch b sits
             # in row b * N_i + j, which is the order parent[row] = row // N_i assumes
-            if self._rules is None:
+            if self._sampling is not None:
+                self._draw(bufs, i, logits)
+            elif self._rules is None:
                 m.mamba_topk_fwd(logits, n_i, idx=p["cand"], val=p["cand_val"])
             else:
                 r = self._rules
@@ -149,20 +211,69 @@ class MambaDrafter:
                                    conv_dst=c.conv[dst][l], ssm_dst=c.ssm[dst][l], hidden_out=p["hid"],
                                    workspace=p["ws"])
             m.mamba_rmsnorm_fwd(p["hid"], self.norm_f, self.eps, y=p["normed"])
-            m.mamba_linear_fwd(p["normed"], self.lm_head, outs=[p["logits"]])
+            self._head(p["normed"], p["logits"])
             logits = p["logits"]
 
-    def draft(self, tree, use_graph=True):
+    def _drawn(self, bufs):
+        """Buffers of a tree whose children are drawn: random numbers, what the children were drawn from, node by node, and scratch."""
+        if "drawn" not in bufs:
+            c, mk = bufs["cache"], lambda shape, dt: torch.empty(shape, dtype=dt, device=self.dev)
+            d = dict(u=[None], ws=[None], prob=[None], q=mk((1, sum(c.batch[i] for i in range(c.gamma)), self.V), torch.float32))
+            for i in range(1, c.gamma + 1):
+                rows, n = c.batch[i - 1], bufs["tree"][i - 1]
+                d["u"].append(mk((rows, n), torch.float32))
+                d["prob"].append(mk((rows, n), torch.float32))
+                d["ws"].append(mk((max(m.mamba_sample_workspace_bytes(rows, self.V, n), 16),), torch.uint8))
+            bufs["drawn"] = d
+        return bufs["drawn"]
+
+    def _draw(self, bufs, i, logits):
+        c, p, d, s = bufs["cache"], bufs["pos"][i], self._drawn(bufs), self._sampling
+        path = bufs["pos"][i - 1]["path"] if i > 1 else None
+        first = sum(c.batch[j] for j in range(i - 1))
+        if self._rules is not None:
+            r = self._rules
+            if "ruled" not in p:
+                p["ruled"] = torch.empty_like(logits)
+            logits = m.mamba_logits_constrain_fwd(logits, counts=r["counts"], penalties=r["penalties"], bias=r["bias"], mask=r["masks"][i - 1],
+                                                  path=path, out=p["ruled"])
+        m.mamba_sample_fwd(logits, d["u"][i], s["params"], top_k=s["top_k"], path=path, idx=p["cand"], prob=d["prob"][i],
+                           dist=d["q"][0, first:first + c.batch[i - 1]], path_out=p["path"], workspace=d["ws"][i])
+
+    def verify(self, tree, p, u_accept=None, u_sample=None):
+        """Which path of the tree drafted last (under ``sample``) a target accepts: p (nodes, V) f32, its distributions behind the nodes, the root
+        first, then position by position; u_accept (nodes - 1), u_sample (1) f32 in [0,1) (None: torch's random numbers).  Returns the emitted
+        tokens int32 (gamma + 1), -1 behind them, their number int32 (1), and the accepted ones' rows in their positions int32 (gamma)."""
+        bufs = self._trees.get(tuple(int(n) for n in tree), {})
+        if "drawn" not in bufs:
+            raise RuntimeError("verify() is for a tree whose children were drawn: call sample() and draft() first")
+        tokens = torch.cat([bufs["pos"][i]["cand"].view(-1) for i in range(1, bufs["cache"].gamma + 1)]).view(1, -1)
+        draws = lambda u, n: torch.rand((1, n), device=self.dev) if u is None else u.reshape(1, n)
+        out, count, node = m.mamba_tree_verify_fwd(p[None], bufs["drawn"]["q"], tokens, draws(u_accept, tokens.shape[1]),
+                                                   draws(u_sample, 1).reshape(1), bufs["tree"])
+        return out[0], count, node[0]
+
+    def draft(self, tree, use_graph=True, u=None):
         """Draft one tree from the current root.  Returns, per position, the draft tokens int32[B_i]
-        (device tensors; parents are j // N_i) and the logits after the last position."""
+        (device tensors; parents are j // N_i) and the logits after the last position.  Under ``sample`` u holds the random
+        numbers of all children, position by position (f32 in [0,1); None: torch's)."""
         bufs = self._buffers(tree)
         c = bufs["cache"]
         c.set_root(self.root_conv, self.root_ssm)
-        kind = "graph" if self._rules is None else "constrained_graph"
+        if self._sampling is not None:
+            at = 0
+            total = sum(c.batch[i] for i in range(1, c.gamma + 1))
+            if u is not None and u.numel() != total:
+                raise ValueError("u must have %d random numbers, got %d" % (total, u.numel()))
+            for buf in self._drawn(bufs)["u"][1:]:
+                buf.uniform_() if u is None else buf.copy_(u.reshape(-1)[at:at + buf.numel()].view_as(buf))
+                at += buf.numel()
+        kind = "".join(("constrained_" if self._rules is not None else "", "sampling_" if self._sampling is not None else "",
+                        "adapted_" if self._adapters is not None else "", "graph"))
         if not use_graph:
             self._round(bufs)
         else:
-            if bufs[kind] is None:
+            if bufs.get(kind) is None:
                 self._round(bufs)                        # loads every kernel before the capture
                 c.set_root(self.root_conv, self.root_ssm)
                 g = torch.cuda.CUDAGraph()

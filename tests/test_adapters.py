@@ -1,0 +1,208 @@
+"""Projections with low-rank adapters of many requests (mamba_linear_adapted_fwd): refusals (no GPU needed), and the kernels against the oracle."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import sampling as oracle
+
+
+def P(i):
+    return (i + 1) << 40
+
+
+@pytest.fixture(scope="module")
+def m():
+    from paper_2506_01206_amd import binding
+    return binding
+
+
+def call(m, x=P(0), w=P(1), bias=None, residual=None, a=P(2), b=P(3), scale=None, idx=P(4), out0=P(5), n0=64, out1=None, n1=0, out2=None, n2=0, ws=P(8),
+         ws_bytes=1 << 39, M=4, K=32, rank=16, n=3, io=1):
+    return m.lib.mamba_linear_adapted_fwd(x, w, bias, residual, a, b, scale, idx, out0, n0, out1, n1, out2, n2, ws, ws_bytes, M, K, rank, n, io, None)
+
+
+def test_refusals(m):
+    S = m.STATUS
+    for name in ("x", "w", "a", "b", "idx", "out0"):
+        assert call(m, **{name: None}) == S["NULL_POINTER"], name
+    for name in ("x", "w", "bias", "residual", "a", "b", "scale", "idx", "out0", "ws"):
+        assert call(m, **{name: P(20) + 8}) == S["MISALIGNED"], name
+    need = m.mamba_linear_adapted_workspace_bytes(4, 16)
+    assert need == 4 * 16 * 4
+    assert call(m, ws=None) == S["WORKSPACE"] and call(m, ws_bytes=need - 1) == S["WORKSPACE"]
+    for bad in (dict(M=-1), dict(K=-8), dict(n0=-1), dict(rank=-8), dict(n=-1), dict(n=0), dict(K=0), dict(n=1 << 30, K=1 << 34), dict(n1=1 << 62, n0=1 << 62)):
+        assert call(m, **bad) == S["BAD_SHAPE"], bad
+    for bad in (dict(io=0), dict(io=2), dict(K=36), dict(rank=0), dict(rank=12), dict(rank=136), dict(M=65535 * 128 + 1), dict(residual=P(9), n1=8, out1=P(10)),
+                dict(n=0x7fffffff, K=8, n0=8, rank=8)):
+        assert call(m, **bad) == S["UNSUPPORTED"], bad
+    assert call(m, M=0) == S["OK"] and call(m, n0=0) == S["OK"] and call(m, M=0, n=0) == S["OK"]
+    for a, b in (("out0", 0), ("out0", 1), ("out0", 2), ("out0", 3), ("out0", 4), ("out0", 8), ("ws", 0), ("ws", 1), ("ws", 2), ("ws", 3), ("ws", 4)):
+        assert call(m, **{a: P(b)}) == S["ALIAS"], (a, b)
+    assert call(m, scale=P(5)) == S["ALIAS"] and call(m, bias=P(8)) == S["ALIAS"] and call(m, residual=P(8)) == S["ALIAS"]
+    assert call(m, out1=P(5) + 256, n1=64) == S["ALIAS"] and call(m, residual=P(5) + 16) == S["ALIAS"]
+    for bad in ((0, 16), (4, 0), (4, 12), (4, 136), (-1, 16), (1 << 62, 16)):
+        assert m.mamba_linear_adapted_workspace_bytes(*bad) == 0, bad
+
+
+def test_binding_refuses_what_does_not_fit(m):
+    x, w, a, b, i = torch.zeros(2, 8), torch.zeros(16, 8), torch.zeros(1, 8, 8), torch.zeros(1, 16, 8), torch.zeros(2, dtype=torch.int32)
+    with pytest.raises(ValueError, match="GPU"):
+        m.mamba_linear_adapted_fwd(x, w, a, b, i)
+    for splits in ((8,), (8, 9), (4, 4, 4, 4), ()):
+        with pytest.raises(ValueError, match="splits"):
+            m.mamba_linear_adapted_fwd(x, w, a, b, i, splits=splits)
+    with pytest.raises(ValueError, match="splits"):
+        m.mamba_linear_adapted_fwd(x, w, a, b, i, splits=(8, 8), outs=[x])
+
+
+# ----------------------------------------------------------------------------------------------------------- the kernels
+gpu = pytest.mark.gpu
+DEV = "cuda:0"
+BF16 = torch.bfloat16
+
+
+def inputs(rng, M, K, N, rank, n, rows="mixed", bias=False, residual=False, scale=True):
+    bf = lambda *s, std=1.0: torch.from_numpy((rng.standard_normal(s) * std).astype(np.float32)).to(DEV, BF16)
+    idx = {"mixed": lambda: rng.integers(-1, n, M), "sorted": lambda: np.sort(rng.integers(-1, n, M)), "one": lambda: np.full(M, n - 1), "none": lambda: np.full(M, -1),
+           "own": lambda: np.arange(M) % n}[rows]()
+    return dict(x=bf(M, K), w=bf(N, K, std=K ** -0.5), lora_a=bf(n, rank, K, std=K ** -0.5), lora_b=bf(n, N, rank, std=rank ** -0.5),
+                adapter_idx=torch.from_numpy(idx.astype(np.int32)).to(DEV),
+                scale=torch.from_numpy(rng.uniform(0.5, 2.0, n).astype(np.float32)).to(DEV) if scale else None,
+                bias=torch.from_numpy(rng.standard_normal(N).astype(np.float32)).to(DEV) if bias else None, residual=bf(M, N, std=3.0) if residual else None)
+
+
+def f64(t):
+    return None if t is None else t.double().cpu().numpy()
+
+
+def check(m, c, splits=None):
+    outs = m.mamba_linear_adapted_fwd(**c, splits=splits)
+    got = torch.cat([o.double() for o in outs], 1).cpu().numpy()
+    idx = c["adapter_idx"].cpu().numpy()
+    ref, size, delta = oracle.adapted(f64(c["x"]), f64(c["w"]), f64(c["lora_a"]), f64(c["lora_b"]), idx, f64(c["scale"]), f64(c["bias"]), f64(c["residual"]))
+    assert np.array_equal(np.isnan(got), np.isnan(ref))
+    # The output's rounding; float32 sums of K products (and of the residual, the bias and twice the rank), each step off by half a step of what
+    # is added up so far; t's two terms, which leave out 2^-16 of it at most; the low terms and the scaling of t in float32.
+    K, rank = c["x"].shape[1], c["lora_a"].shape[1]
+    extra = (0 if c["bias"] is None else np.abs(f64(c["bias"]))) + (0 if c["residual"] is None else np.abs(f64(c["residual"])))
+    steps = (K + 2 * rank + 4) * 2.0 ** -24
+    bound = 2.0 ** -8 * np.abs(ref) + (1 + 2.0 ** -8) * (steps * (size + delta + extra) + (2.0 ** -16 + steps) * delta)
+    err = np.abs(got - ref)
+    ok = np.isnan(ref) | (err <= bound)
+    assert ok.all(), (float(np.nanmax(err - bound)), np.argwhere(~ok)[:4])
+    return outs
+
+
+@gpu
+@pytest.mark.parametrize("rank", [8, 16, 24, 40, 64, 128])
+@pytest.mark.parametrize("M,K,N", [(1, 8, 8), (1, 1536, 768), (3, 40, 17), (17, 768, 80), (40, 256, 130), (64, 512, 2048), (65, 72, 257), (129, 1024, 512), (333, 768, 1536)])
+def test_against_oracle(m, M, K, N, rank):
+    rng = np.random.default_rng(M + K + N + rank)
+    for rows in ("mixed", "sorted", "one", "own"):
+        check(m, inputs(rng, M, K, N, rank, 5, rows, bias=rows == "mixed", residual=rows == "sorted", scale=rows != "one"))
+
+
+@gpu
+@pytest.mark.parametrize("M,K,N,splits", [(700, 768, 1536, (768, 768)), (1030, 1536, 768, None), (2100, 1024, 2048, None), (4111, 1024, 1024, (512, 256, 256)), (8200, 768, 1536, None),
+                                          (5000, 264, 1000, (1, 998, 1)), (600, 2048, 4096, None), (300, 64, 777, (700, 70, 7)), (9000, 1536, 768, None)])
+def test_many_rows(m, M, K, N, splits):
+    """Shapes that take every kind of tile, rows of several adapters in one of them."""
+    rng = np.random.default_rng(M + N)
+    for rows, rank in (("sorted", 32), ("mixed", 8), ("one", 16)):
+        check(m, inputs(rng, M, K, N, rank, 6, rows, bias=rows == "mixed", residual=splits is None and rows != "one"), splits)
+
+
+@gpu
+@pytest.mark.parametrize("M,K,N", [(24, 768, 50280), (2, 2048, 131071), (70, 512, 9000), (16, 2056, 12345)])
+def test_vocabularies(m, M, K, N):
+    rng = np.random.default_rng(N)
+    check(m, inputs(rng, M, K, N, 16, 8))
+
+
+@gpu
+@pytest.mark.parametrize("M,K,N", [(12, 768, 768), (333, 768, 1536), (3000, 768, 1536), (2000, 80, 100)])
+def test_rows_without_an_adapter_are_the_plain_product(m, M, K, N):
+    rng = np.random.default_rng(N)
+    for rows in ("none", "mixed"):
+        c = inputs(rng, M, K, N, 16, 3, rows, bias=True)
+        (got,), (ref,) = m.mamba_linear_adapted_fwd(**c), m.mamba_linear_fwd(c["x"], c["w"], c["bias"])
+        free = c["adapter_idx"] < 0
+        assert torch.equal(got[free], ref[free])
+
+
+@gpu
+@pytest.mark.parametrize("M,K,N", [(20, 256, 96), (700, 768, 768), (3000, 256, 512), (900, 72, 100)])
+def test_indices_out_of_range_and_what_is_no_number(m, M, K, N):
+    """A row whose adapter is out of range is NaN; infinities and NaN of an adapter, of a row, stay where they belong."""
+    rng = np.random.default_rng(M)
+    c = inputs(rng, M, K, N, 16, 4)
+    idx = c["adapter_idx"]
+    idx[::7], idx[3::50], idx[5::90] = 4, -2, 2 ** 31 - 1
+    check(m, c)
+    (clean,) = m.mamba_linear_adapted_fwd(**c)
+    for name, at in (("lora_a", (1, 0, 0)), ("lora_b", (1, 5, 3))):
+        for bad in (float("nan"), float("inf")):
+            kept = c[name][at].clone()
+            c[name][at] = bad
+            (got,) = m.mamba_linear_adapted_fwd(**c)
+            c[name][at] = kept
+            others = idx != 1
+            assert torch.equal(got[others].view(torch.int16), clean[others].view(torch.int16))
+            hit = got[idx == 1] if name == "lora_a" else got[idx == 1][:, 5]
+            assert not bool(torch.isfinite(hit.float()).any())
+    c["x"][2] = float("nan")
+    (got,) = m.mamba_linear_adapted_fwd(**c)
+    assert bool(torch.isnan(got[2].float()).all())
+    keep = torch.arange(M, device=DEV) != 2
+    assert torch.equal(got[keep].view(torch.int16), clean[keep].view(torch.int16))
+
+
+@gpu
+@pytest.mark.parametrize("M,K,N", [(5, 1536, 768), (333, 1536, 768), (2500, 768, 768), (500, 64, 100)])
+def test_residual_in_place_given_outputs_and_repeats(m, M, K, N):
+    rng = np.random.default_rng(K)
+    c = inputs(rng, M, K, N, 16, 3, residual=True)
+    (ref,) = m.mamba_linear_adapted_fwd(**c)
+    ws = torch.full((m.mamba_linear_adapted_workspace_bytes(M, 16),), 255, dtype=torch.uint8, device=DEV)
+    big = torch.full((M + 4, N), 7.0, dtype=BF16, device=DEV)
+    for _ in range(2):
+        big[:M] = c["residual"]
+        (got,) = m.mamba_linear_adapted_fwd(**{**c, "residual": big[:M]}, outs=[big[:M]], workspace=ws)
+        assert got.data_ptr() == big.data_ptr() and torch.equal(got, ref) and bool((big[M:] == 7).all())
+    assert m.mamba_linear_adapted_fwd(**{**c, "x": c["x"][:0], "residual": None, "adapter_idx": c["adapter_idx"][:0]})[0].shape == (0, N)
+
+
+@gpu
+def test_streams_and_graphs(m):
+    rng = np.random.default_rng(1)
+    for M, K, N in ((24, 768, 1536), (1500, 768, 1536)):
+        c = inputs(rng, M, K, N, 16, 8)
+        (ref,) = m.mamba_linear_adapted_fwd(**c)
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        (got,) = m.mamba_linear_adapted_fwd(**c, stream=side)
+        torch.cuda.current_stream().wait_stream(side)
+        assert torch.equal(got, ref)
+        out, ws = torch.empty_like(ref), torch.empty(m.mamba_linear_adapted_workspace_bytes(M, 16), dtype=torch.uint8, device=DEV)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            m.mamba_linear_adapted_fwd(**c, outs=[out], workspace=ws)
+        for _ in range(3):
+            out.zero_()
+            ws.fill_(255)
+            g.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out, m.mamba_linear_adapted_fwd(**c)[0])
+            c["adapter_idx"].copy_(torch.randint(-1, 8, (M,), device=DEV))
+
+
+@gpu
+def test_refusals_of_the_binding(m):
+    c = inputs(np.random.default_rng(2), 4, 32, 64, 16, 3)
+    for bad in (dict(x=c["x"].float()), dict(w=c["w"].t()), dict(lora_a=c["lora_a"][:, :, :16].contiguous()), dict(lora_b=c["lora_b"][:2].contiguous()),
+                dict(adapter_idx=c["adapter_idx"].long()), dict(adapter_idx=c["adapter_idx"][:3]), dict(scale=c["scale"].double()), dict(scale=c["scale"][:2]),
+                dict(bias=torch.zeros(63, device=DEV)), dict(residual=torch.zeros(4, 64, device=DEV)), dict(lora_a=c["lora_a"].cpu())):
+        with pytest.raises((ValueError, TypeError)):
+            m.mamba_linear_adapted_fwd(**{**c, **bad})
+    with pytest.raises(m.MambaError):
+        m.mamba_linear_adapted_fwd(**{**c, "lora_a": c["lora_a"][:, :12].contiguous(), "lora_b": c["lora_b"][..., :12].contiguous()})
