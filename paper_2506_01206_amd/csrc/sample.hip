@@ -29,7 +29,7 @@ namespace {
 typedef unsigned long long u64;
 
 constexpr int kThreads = 256;                                        // of the kernels that have a chunk of a row
-constexpr int kSlice = kThreads * 8;
+constexpr int kSlice = kThreads * 8;                                 // tokens of a chunk
 constexpr int kMaxChunks = 1024;
 constexpr int kBins = 128;                                           // of the weights of a row or chunk
 constexpr int kWide = 1024, kWideWaves = kWide / 64;                 // threads of the kernel that has a row
@@ -226,9 +226,8 @@ struct Chunks {
     float *most;                                                     // (chunks)
 };
 
-template <typename T, int PER>
-__global__ void __launch_bounds__(kThreads)
-bins_kernel(const T *__restrict__ logits, Chunks to, SampleArgs a, int scale)
+template <typename T>
+__global__ void __launch_bounds__(kThreads) bins_kernel(const T *__restrict__ logits, Chunks to, SampleArgs a, int scale)
 {
     const int64_t m = row_of_block(), chunk = m * gridDim.x + blockIdx.x;
     if (m >= a.M) return;
@@ -238,18 +237,14 @@ bins_kernel(const T *__restrict__ logits, Chunks to, SampleArgs a, int scale)
     __shared__ u64 first_mass;
     __shared__ uint32_t first_number;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    Eight e[PER];
-#pragma unroll
-    for (int i = 0; i < PER; ++i) e[i].load(logits + m * a.V, (int32_t)((blockIdx.x * PER + i) * kSlice) + tid * 8, (int32_t)a.V);
+    Eight e;
+    e.load(logits + m * a.V, (int32_t)blockIdx.x * kSlice + tid * 8, (int32_t)a.V);
     const Settings r = settings_of(a, m);
     if (tid < kBins) mass[tid] = 0, number[tid] = 0;
+    e.settle();
     float top = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        e[i].settle();
-#pragma unroll
-        for (int j = 0; j < 8; ++j) top = fmaxf(top, e[i].x[j]);
-    }
+    for (int j = 0; j < 8; ++j) top = fmaxf(top, e.x[j]);
     top = wave_max(top);
     if (lane == 0) part[wave] = top;
     __syncthreads();
@@ -257,21 +252,19 @@ bins_kernel(const T *__restrict__ logits, Chunks to, SampleArgs a, int scale)
     const int top_mark = top_mark_of(top, r.per_bin);
     u64 last_mass = 0;                                               // (of the last bin: it may have most of the tokens)
     uint32_t last_number = 0;
+    u64 w[8];
 #pragma unroll
-    for (int i = 0; i < PER; ++i)
+    for (int j = 0; j < 8; ++j) w[j] = r.weights.units(e.x[j], top, scale);   // (-infinity: none, as its weight is; in the last bin)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float x = e[i].x[j];
-            if (!counts(x)) continue;
-            const int b = bin_of(mark_of(x, r.per_bin), top_mark);
-            const u64 w = r.weights.units(x, top, scale);
-            if (b < kBins - 1) {
-                atomicAdd(&mass[b], w);
-                if (r.top_k > 0) atomicAdd(&number[b], 1u);
-            } else {
-                last_mass += w, ++last_number;
-            }
+    for (int j = 0; j < 8; ++j) {
+        const int b = bin_of(mark_of(e.x[j], r.per_bin), top_mark);
+        if (b < kBins - 1) {
+            atomicAdd(&mass[b], w[j]);
+            if (r.top_k > 0) atomicAdd(&number[b], 1u);
+        } else {
+            last_mass += w[j], last_number += counts(e.x[j]);
         }
+    }
     last_mass = wave_sum(last_mass);
     if (lane == 0) atomicAdd(&mass[kBins - 1], last_mass);
     if (r.top_k > 0) {
@@ -529,15 +522,15 @@ __device__ __forceinline__ u64 wide_prefix(u64 v, u64 *parts, u64 *total)
 
 template <typename T> struct Row {
     const T *x;
-    int32_t V, chunk;                                                // tokens of a chunk
+    int32_t V;
     float top, per_bin;
     int top_mark, scale;
     Weights weights;
     Order<T> order;
     const ChunkScale *chunks;
     // units of a token relative to its chunk's largest logit, and to the row's
-    __device__ __forceinline__ u64 own_units(float v, int32_t token) const { return weights.units(v, chunks[token / chunk].most, scale); }
-    __device__ __forceinline__ u64 units(float v, int32_t token) const { return scaled(own_units(v, token), chunks[token / chunk].factor); }
+    __device__ __forceinline__ u64 own_units(float v, int32_t token) const { return weights.units(v, chunks[token / kSlice].most, scale); }
+    __device__ __forceinline__ u64 units(float v, int32_t token) const { return scaled(own_units(v, token), chunks[token / kSlice].factor); }
     __device__ __forceinline__ int bin(float v) const { return bin_of(mark_of(v, per_bin), top_mark); }
     // f(logit, token) for every token that counts, a thread's share of them
     template <typename F> __device__ __forceinline__ void each(F f) const
@@ -731,7 +724,7 @@ __device__ __forceinline__ void chunk_sums(RowShared &s, const Chunks &from, int
         tokens.each([&](u64 place, u64) {
             const float v = row.order.logit(place);
             const int32_t token = row.order.token(place);
-            if (place >= cut.place && row.bin(v) == cut.bin) atomicAdd(&s.chunk_mass[token / row.chunk], row.own_units(v, token));
+            if (place >= cut.place && row.bin(v) == cut.bin) atomicAdd(&s.chunk_mass[token / kSlice], row.own_units(v, token));
         });
     __syncthreads();
 }
@@ -750,7 +743,7 @@ __device__ __attribute__((noinline)) Cut scan_cut(RowShared &s, const Settings &
 // Where next to nothing is left beside what was drawn, units are too coarse for it: the sums of the chunks with drawn tokens again, relative to the
 // largest that is left there, and all chunks' against the largest that is left anywhere.  (A chunk whose largest has no weight beside the row's has
 // none here.)
-template <int PER, typename T>
+template <typename T>
 __device__ __attribute__((noinline)) void sums_of_the_rest(RowShared &s, const Row<T> &row, u64 cut, int drawn, float top, int chunks)
 {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -764,10 +757,10 @@ __device__ __attribute__((noinline)) void sums_of_the_rest(RowShared &s, const R
 #pragma unroll 1
     for (int d = 0; d < drawn; ++d) {
         if (!s.drawn[d]) continue;
-        const int chunk = row.order.token(s.drawn[d]) / row.chunk, first = chunk * row.chunk + 2 * PER * tid;
-        float v[2 * PER], most = -INFINITY;
+        const int chunk = row.order.token(s.drawn[d]) / kSlice, first = chunk * kSlice + 2 * tid;
+        float v[2], most = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < 2 * PER; ++i) {
+        for (int i = 0; i < 2; ++i) {
             v[i] = ld_io(row.x, min(first + i, row.V - 1));
             const u64 place = row.order.place(v[i], first + i);
             bool open = first + i < row.V && counts(v[i]) && place >= cut;
@@ -778,7 +771,7 @@ __device__ __attribute__((noinline)) void sums_of_the_rest(RowShared &s, const R
         most = most_of_all(most);
         u64 sum = 0, all;
 #pragma unroll
-        for (int i = 0; i < 2 * PER; ++i) sum += counts(v[i]) ? row.weights.units(v[i], most, row.scale) : 0;
+        for (int i = 0; i < 2; ++i) sum += counts(v[i]) ? row.weights.units(v[i], most, row.scale) : 0;
         wide_prefix(sum, s.wave_part, &all);
         if (tid == 0) s.chunk_mass[chunk] = all, s.scale[chunk].most = most;
     }
@@ -789,7 +782,7 @@ __device__ __attribute__((noinline)) void sums_of_the_rest(RowShared &s, const R
     __syncthreads();
 }
 
-template <typename T, int PER>
+template <typename T>
 __global__ void __launch_bounds__(kWide)
 draw_kernel(const T *__restrict__ logits, Chunks from, const RowBins *__restrict__ rows, const ChunkScale *__restrict__ scales, const u64 *__restrict__ list,
             RowCut *__restrict__ cuts, SampleArgs a, int scale, int chunks, Order<T> order)
@@ -805,7 +798,7 @@ draw_kernel(const T *__restrict__ logits, Chunks from, const RowBins *__restrict
     const u64 first_place = tid < (int)n && tid < kList ? list[m * kList + tid] : 0;
     const Settings r = settings_of(a, m);
     __syncthreads();
-    Row<T> row{logits + m * a.V, (int32_t)a.V, PER * kSlice, top, r.per_bin, top_mark_of(top, r.per_bin), scale, r.weights, order, s.scale};
+    Row<T> row{logits + m * a.V, (int32_t)a.V, top, r.per_bin, top_mark_of(top, r.per_bin), scale, r.weights, order, s.scale};
     const bool some = r.known && counts(top);
 
     Cut cut{0, kBins};
@@ -845,7 +838,7 @@ draw_kernel(const T *__restrict__ logits, Chunks from, const RowBins *__restrict
             for (int d = 0, is = 0; out && d < j; ++d) is |= s.drawn[d] == cut.place, out = d + 1 < j || is;
             if (j > 0 && left < (r.top_k > 0 && r.top_k <= 1024 ? (u64)1 << 30 : (u64)1 << 39) && !out) {
                 const Row<T> row_there = row;
-                sums_of_the_rest<PER>(s, row_there, cut.place, j, top, chunks);
+                sums_of_the_rest(s, row_there, cut.place, j, top, chunks);
                 mine = tid < chunks ? scaled(s.chunk_mass[tid], s.scale[tid].factor) : 0;
                 at = wide_prefix(mine, s.wave_part, &left);
             }
@@ -858,28 +851,28 @@ draw_kernel(const T *__restrict__ logits, Chunks from, const RowBins *__restrict
             __syncthreads();
             const int chunk = s.chunk;
             const u64 inside = s.need;
-            const int32_t first = chunk * (PER * kSlice) + 2 * PER * tid;
+            const int32_t first = chunk * kSlice + 2 * tid;
             const float most = s.scale[chunk].most;
-            float v[2 * PER];
-            u64 w[2 * PER], sum = 0, all;
+            float v[2];
+            u64 w[2], sum = 0, all;
 #pragma unroll
-            for (int i = 0; i < 2 * PER; ++i) v[i] = ld_io(row.x, min(first + i, row.V - 1));
+            for (int i = 0; i < 2; ++i) v[i] = ld_io(row.x, min(first + i, row.V - 1));
 #pragma unroll
-            for (int i = 0; i < 2 * PER; ++i) {
+            for (int i = 0; i < 2; ++i) {
                 const u64 p = order.place(v[i], first + i);
                 w[i] = first + i < row.V && counts(v[i]) && p >= cut.place ? row.weights.units(v[i], most, scale) : 0;
             }
             for (int d = 0; d < j; ++d) {
                 const int32_t token = s.drawn[d] ? order.token(s.drawn[d]) : -1;
 #pragma unroll
-                for (int i = 0; i < 2 * PER; ++i) w[i] = first + i == token ? 0 : w[i];
+                for (int i = 0; i < 2; ++i) w[i] = first + i == token ? 0 : w[i];
             }
 #pragma unroll
-            for (int i = 0; i < 2 * PER; ++i) sum += w[i];
+            for (int i = 0; i < 2; ++i) sum += w[i];
             u64 start = wide_prefix(sum, s.wave_part, &all);
             if (start <= inside && inside < start + sum) {           // one thread
 #pragma unroll
-                for (int i = 0; i < 2 * PER; ++i) {
+                for (int i = 0; i < 2; ++i) {
                     if (start <= inside && inside < start + w[i]) s.drawn[j] = order.place(v[i], first + i), s.chunk_mass[chunk] -= w[i];
                     start += w[i];
                 }
@@ -932,20 +925,14 @@ dist_kernel(const T *__restrict__ logits, const RowCut *__restrict__ cuts, float
     }
 }
 
-// Slices of 2048 tokens to a chunk: four where that leaves every CU some workgroups, one to have more of them where it does not.
-int slices_per_chunk(int64_t M, int64_t V) { return M * V >= (int64_t)8 << 20 ? 4 : 1; }
-int64_t chunks_of(int64_t M, int64_t V)
-{
-    const int64_t tokens = (int64_t)slices_per_chunk(M, V) * kSlice;
-    return (V + tokens - 1) / tokens;
-}
+int64_t chunks_of(int64_t V) { return (V + kSlice - 1) / kSlice; }
 
 struct Places {                                                      // of the parts of the workspace, in bytes
     size_t mass, number, rows, scales, cuts, list, most, all;
 };
 Places places_of(int64_t M, int64_t V)
 {
-    const size_t chunks = (size_t)(M * chunks_of(M, V));
+    const size_t chunks = (size_t)(M * chunks_of(V));
     auto up = [](size_t n) { return (n + 15) / 16 * 16; };
     Places p;
     p.mass = 0;
@@ -959,12 +946,12 @@ Places places_of(int64_t M, int64_t V)
     return p;
 }
 
-template <typename T, int PER> hipError_t launch(const T *logits, unsigned char *ws, const SampleArgs &a, hipStream_t stream)
+template <typename T> hipError_t launch(const T *logits, unsigned char *ws, const SampleArgs &a, hipStream_t stream)
 {
     const Places p = places_of(a.M, a.V);
-    const int64_t chunks = chunks_of(a.M, a.V);
+    const int64_t chunks = chunks_of(a.V);
     const unsigned rows_y = (unsigned)(a.M < kRowsY ? a.M : kRowsY), rows_z = (unsigned)((a.M + kRowsY - 1) / kRowsY);
-    const dim3 grid((unsigned)chunks, rows_y, rows_z), slices((unsigned)((a.V + kSlice - 1) / kSlice), rows_y, rows_z);
+    const dim3 grid((unsigned)chunks, rows_y, rows_z);
     const Chunks c{reinterpret_cast<u64 *>(ws + p.mass), reinterpret_cast<uint32_t *>(ws + p.number), reinterpret_cast<float *>(ws + p.most)};
     RowBins *rows = reinterpret_cast<RowBins *>(ws + p.rows);
     ChunkScale *scales = reinterpret_cast<ChunkScale *>(ws + p.scales);
@@ -974,11 +961,11 @@ template <typename T, int PER> hipError_t launch(const T *logits, unsigned char 
     while ((int64_t)1 << bits < a.V) ++bits;
     const int scale = bits < 12 ? 51 : 63 - bits;
     const Order<T> order{bits};
-    bins_kernel<T, PER><<<grid, kThreads, 0, stream>>>(logits, c, a, scale);
+    bins_kernel<T><<<grid, kThreads, 0, stream>>>(logits, c, a, scale);
     plan_kernel<T><<<(unsigned)a.M, kWide, 0, stream>>>(c, rows, scales, a, (int)chunks);
-    gather_kernel<T><<<slices, kThreads, 0, stream>>>(logits, rows, list, a.M, (int32_t)a.V, order);
-    draw_kernel<T, PER><<<(unsigned)a.M, kWide, 0, stream>>>(logits, c, rows, scales, list, cuts, a, scale, (int)chunks, order);
-    if (a.dist) dist_kernel<T><<<slices, kThreads, 0, stream>>>(logits, cuts, a.dist, a);
+    gather_kernel<T><<<grid, kThreads, 0, stream>>>(logits, rows, list, a.M, (int32_t)a.V, order);
+    draw_kernel<T><<<(unsigned)a.M, kWide, 0, stream>>>(logits, c, rows, scales, list, cuts, a, scale, (int)chunks, order);
+    if (a.dist) dist_kernel<T><<<grid, kThreads, 0, stream>>>(logits, cuts, a.dist, a);
     return hipGetLastError();
 }
 
@@ -987,7 +974,7 @@ template <typename T, int PER> hipError_t launch(const T *logits, unsigned char 
 // (a launch has fewer than 2^32 threads, and the kernel of a row a thread for each of its chunks)
 bool sample_fits(int64_t M, int64_t V)
 {
-    return V <= (int64_t)kSlice * kMaxChunks && M <= (0xffffffff / kWide) && M <= (0xffffffff / kThreads) / (V > 0 ? (V + kSlice - 1) / kSlice : 1);
+    return V <= (int64_t)kSlice * kMaxChunks && M <= (0xffffffff / kWide) && M <= (0xffffffff / kThreads) / (V > 0 ? chunks_of(V) : 1);
 }
 
 size_t sample_workspace_bytes(int64_t M, int64_t V) { return places_of(M, V).all; }
@@ -995,13 +982,7 @@ size_t sample_workspace_bytes(int64_t M, int64_t V) { return places_of(M, V).all
 hipError_t launch_sample(const void *logits, void *ws, const SampleArgs &a, int io, hipStream_t stream)
 {
     unsigned char *w = static_cast<unsigned char *>(ws);
-    const bool four = slices_per_chunk(a.M, a.V) == 4;
-    if (io == kIoBf16) {
-        const bf16_t *x = static_cast<const bf16_t *>(logits);
-        return four ? launch<bf16_t, 4>(x, w, a, stream) : launch<bf16_t, 1>(x, w, a, stream);
-    }
-    const float *x = static_cast<const float *>(logits);
-    return four ? launch<float, 4>(x, w, a, stream) : launch<float, 1>(x, w, a, stream);
+    return io == kIoBf16 ? launch(static_cast<const bf16_t *>(logits), w, a, stream) : launch(static_cast<const float *>(logits), w, a, stream);
 }
 
 }  // namespace mamba
