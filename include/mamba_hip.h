@@ -558,7 +558,7 @@ int mamba_tree_verify_fwd(const float *p, const float *q, const int32_t *tokens,
  * included.  lora_a (n_adapters, rank, K), lora_b (n_adapters, N, rank) bf16; scale (n_adapters) float or NULL (ones); adapter_idx
  * device int32 (M): -1 for a row without an adapter (what it gets is mamba_linear_fwd's to the bit where there is no residual), anything else
  * outside [0, n_adapters) gives NaN in the row.  Rows of one adapter may stand anywhere; next to one another they cost least.  The rank is a multiple of
- * 8 up to 128 (adapters of a lower one are padded with zeros).  An infinity or a NaN of an adapter reaches its own rows only.
+ * 8 up to 128 (adapters of a lower one are padded with zeros).  An infinity or a NaN of an adapter reaches its own rows only (an infinity as a NaN, it may be).
  * workspace: device scratch of mamba_linear_adapted_workspace_bytes(M, rank) bytes; nothing in it has to be kept or cleared between calls.
  */
 size_t mamba_linear_adapted_workspace_bytes(int64_t M, int64_t rank);

@@ -12,89 +12,166 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4v __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
+constexpr int kThreads = 256, kWaves = 4;
+constexpr int kLine = 128;                                           // 64 k of a row in LDS
+
 __device__ __forceinline__ int32_t wave_min(int32_t v)
 {
 #pragma unroll
     for (int d = 32; d; d >>= 1) v = min(v, __shfl_xor(v, d));
     return v;
 }
-
-// One workgroup per 16 rows and all ranks (RT tiles of 16), its NW wavefronts share the k range in steps of 32, every NW-th each.  Rows of several
-// adapters are multiplied by each of them, and a row takes the sums of its own.
-template <int RT, int NW>
-__global__ void __launch_bounds__(64 * NW)
-down_kernel(const bf16_t *__restrict__ x, const bf16_t *__restrict__ a, const float *__restrict__ scale, const int32_t *__restrict__ idx,
-            bf16_t *__restrict__ t, int64_t M, int K, int rank, int adapters)
+// 16 bytes a lane from an address of its own into LDS at lds_addr + 16 lane (see linear.hip: the waits for them are explicit)
+__device__ __forceinline__ void load_to_lds16(const void *from, uint32_t lds_addr)
 {
-    __shared__ float part[NW][RT * 256];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, li = lane & 15, lg = lane >> 4;
-    const int64_t m0 = (int64_t)blockIdx.x * 16;
-    const int32_t id = lane < 16 && m0 + lane < M ? idx[m0 + lane] : -1;
-    const bf16_t *row = x + min(m0 + li, M - 1) * K;
-    f32x4v sum[RT];
-#pragma unroll
-    for (int r = 0; r < RT; ++r) sum[r] = f32x4v(0.0f);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_addr), "v"(from) : "memory");
+}
+__device__ __forceinline__ void lds_barrier()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// A workgroup has 16 G rows and all ranks (RT tiles of 16) of one adapter: of those that its rows have, smallest first, every gridDim.y-th from the
+// blockIdx.y-th on, so that rows of many adapters are not multiplied by one after the other.  A row's sums are written by who has its adapter.
+// G of the wavefronts' four quarters go by rows, the others by k: slabs of 64 k (128 where all four go by k), four stages of them in LDS, straight from
+// memory, a row's 16-byte slot c at c ^ (row / 2 & 7).
+// Bound by x from memory where there are many rows, by trips to memory where there are few.
+template <int RT, int G>
+__global__ void __launch_bounds__(kThreads)
+down_kernel(const bf16_t *__restrict__ x, const bf16_t *__restrict__ a, const float *__restrict__ scale, const int32_t *__restrict__ idx,
+            bf16_t *__restrict__ t, uint32_t *__restrict__ zeros, int64_t M, int K, int rank, int adapters)
+{
+    constexpr int BM = 16 * G, BN = 16 * RT, S = kWaves / G, kBlocks = S == 4 ? 2 : 1, kStep = 64 * kBlocks;   // blocks of 64 k to a slab
+    constexpr int kStages = 4, kStage = (BM + BN) * kLine * kBlocks;
+    constexpr int kGroups = (BM + BN) / 8 * kBlocks, NL = (kGroups + kWaves - 1) / kWaves;   // loads of 8 rows, and of a wavefront
+    constexpr int kPart = S * BM * BN * 4;
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[kStages * kStage > kPart ? kStages * kStage : kPart];
+    const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, lg = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), group = wave % G, split = wave / G;
+    const int64_t m0 = (int64_t)blockIdx.x * BM;
+    if (blockIdx.x == 0 && blockIdx.y == 0 && tid < 32) zeros[tid] = 0;
+    const int32_t id = lane < BM && m0 + lane < M ? idx[m0 + lane] : -1;
     auto next = [&](int32_t last) { return wave_min(id > last && id < adapters ? id : adapters); };
-    bool any = false;
-    for (int32_t cur = next(-1); cur < adapters; cur = next(cur)) {
-        any = true;
-        const uint64_t rows = __ballot(id == cur);
-        const bf16_t *w = a + (int64_t)cur * rank * K;
+    const uint32_t lds0 = (uint32_t)(size_t)(__attribute__((address_space(3))) unsigned char *)lds;
+    const int slabs = (K + kStep - 1) / kStep, chunks = K / 8;
+    int turn = 0;
+    for (int32_t cur = next(-1); cur < adapters; cur = next(cur), ++turn) {
+        if (turn % (int)gridDim.y != (int)blockIdx.y) continue;
+        // what this lane brings: of load i rows 8 g .. 8 g + 7 of a block, x's first
+        const bf16_t *row[NL];
+        int chunk[NL];
+        uint32_t to[NL];
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+            const int g = min(i * kWaves + wave, kGroups - 1), block = g / ((BM + BN) / 8), r = g % ((BM + BN) / 8) * 8 + (lane >> 3);
+            row[i] = r < BM ? x + min(m0 + r, M - 1) * K : a + ((int64_t)cur * rank + min(r - BM, rank - 1)) * K;
+            chunk[i] = 8 * block + ((lane & 7) ^ (r >> 1 & 7));
+            to[i] = (uint32_t)g * 1024;
+        }
+        auto request = [&](int slab, int stage) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < NL; ++i) {
+                const int c = slab * (kStep / 8) + chunk[i];
+                load_to_lds16(row[i] + (c < chunks ? c : 0) * 8, lds0 + stage * kStage + to[i]);   // (behind K: something, see below)
+            }
+        };
+        // until no more than the loads of `slabs_under_way` slabs are under way (vmcnt is split over bits 3:0 and 15:14)
+        auto wait_for = [&](int slabs_under_way) __attribute__((always_inline)) {
+            static_assert(2 * NL < 64, "fits the counter");
+            if (slabs_under_way >= 2) __builtin_amdgcn_s_waitcnt(0x0F70 | ((2 * NL) & 15) | (((2 * NL) >> 4) << 14));
+            else if (slabs_under_way == 1) __builtin_amdgcn_s_waitcnt(0x0F70 | (NL & 15) | ((NL >> 4) << 14));
+            else __builtin_amdgcn_s_waitcnt(0x0F70);
+        };
         f32x4v d[RT];
 #pragma unroll
         for (int r = 0; r < RT; ++r) d[r] = f32x4v(0.0f);
-        for (int k = wave * 32 + lg * 8; k < (K + 31) / 32 * 32; k += NW * 32) {
-            const bool in = k < K;                                   // (K is a multiple of 8)
-            const u32x4 raw = *reinterpret_cast<const u32x4 *>(row + (in ? k : 0));
-            const bf16x8 xf = __builtin_bit_cast(bf16x8, in ? raw : u32x4(0u));
+        lds_barrier();                                               // (the last adapter's sums are read)
 #pragma unroll
-            for (int r = 0; r < RT; ++r) {
-                const u32x4 wr = *reinterpret_cast<const u32x4 *>(w + (int64_t)min(16 * r + li, rank - 1) * K + (in ? k : 0));
-                d[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf, __builtin_bit_cast(bf16x8, in ? wr : u32x4(0u)), d[r], 0, 0, 0);
+        for (int i = 0; i < kStages - 1; ++i)
+            if (i < slabs) request(i, i);
+        int stage = 0;
+#pragma unroll 1
+        for (int s = 0; s < slabs; ++s) {
+            wait_for(min(slabs - 1 - s, kStages - 2));
+            lds_barrier();                                           // slab s is there, slab s - 1 is read
+            if (s + kStages - 1 < slabs) request(s + kStages - 1, (stage + kStages - 1) % kStages);
+            const unsigned char *from = lds + stage * kStage;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {                            // steps of 32 k
+                const int step = S == 1 ? h : S == 2 ? split : split & 1, block = S == 4 ? split >> 1 : 0;
+                if (S > 1 && h > 0) break;
+                const int c = 4 * step + lg;
+                const bool in = s * (kStep / 8) + 8 * block + c < chunks;
+                auto fragment = [&](int r) __attribute__((always_inline)) {
+                    const u32x4 v = *reinterpret_cast<const u32x4 *>(from + (block * (BM + BN) + r) * kLine + ((c ^ (r >> 1 & 7)) << 4));
+                    return __builtin_bit_cast(bf16x8, in ? v : u32x4(0u));
+                };
+                const bf16x8 xf = fragment(16 * group + li);
+#pragma unroll
+                for (int r = 0; r < RT; ++r) d[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf, fragment(BM + 16 * r + li), d[r], 0, 0, 0);
             }
+            stage = stage + 1 == kStages ? 0 : stage + 1;
         }
+        lds_barrier();
+        // d[r][i] is t[4 (lane / 16) + i][16 r + lane % 16] of the group's rows
+        float *part = reinterpret_cast<float *>(lds) + split * (BM * BN);
 #pragma unroll
         for (int r = 0; r < RT; ++r)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) sum[r][i] = rows >> (4 * lg + i) & 1 ? d[r][i] : sum[r][i];
-    }
-    if (!any) return;                                                // (the same in all wavefronts)
-    // sum[r][i] is t[4 (lane / 16) + i][16 r + lane % 16]
+            for (int i = 0; i < 4; ++i) part[(16 * group + 4 * lg + i) * BN + 16 * r + li] = d[r][i];
+        lds_barrier();
+        const float by = scale ? scale[cur] : 1.0f;
+        for (int e = tid; e < BM * BN / 2; e += kThreads) {          // two ranks of a row
+            const int mr = e / (BN / 2), r = 2 * (e % (BN / 2));
+            const int64_t m = m0 + mr;
+            if (m >= M || r >= rank || idx[m] != cur) continue;
+            float v[2] = {0.0f, 0.0f};
 #pragma unroll
-    for (int r = 0; r < RT; ++r)
+            for (int q = 0; q < S; ++q) {
+                const float2 p = *reinterpret_cast<const float2 *>(reinterpret_cast<const float *>(lds) + q * (BM * BN) + mr * BN + r);
+                v[0] += p.x, v[1] += p.y;
+            }
+            float low[2];
+            uint32_t high[2];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) part[wave][(r * 4 + i) * 64 + lane] = sum[r][i];
-    __syncthreads();
-    for (int e = tid; e < RT * 256; e += 64 * NW) {
-        float v = 0.0f;
-#pragma unroll
-        for (int q = 0; q < NW; ++q) v += part[q][e];
-        const int l = e & 63, r = (e >> 8) * 16 + (l & 15), mr = 4 * (l >> 4) + (e >> 6 & 3);
-        const int64_t m = m0 + mr;
-        const int32_t of = m < M ? idx[m] : -1;
-        if (of < 0 || of >= adapters || r >= rank) continue;
-        if (scale) v *= scale[of];
-        const uint32_t high = f32_to_bf16(v);
-        const float low = v - bf16_to_f32(high);
-        t[m * (2 * rank) + r] = (bf16_t)high;
-        t[m * (2 * rank) + rank + r] = (bf16_t)f32_to_bf16(low == low ? low : 0.0f);   // (an infinity has no low term)
+            for (int i = 0; i < 2; ++i) {
+                v[i] *= by;
+                high[i] = f32_to_bf16(v[i]);
+                const float rest = v[i] - bf16_to_f32(high[i]);
+                low[i] = rest == rest ? rest : 0.0f;                 // (an infinity has no low term)
+            }
+            *reinterpret_cast<uint32_t *>(t + m * (2 * rank) + r) = high[0] | high[1] << 16;
+            *reinterpret_cast<uint32_t *>(t + m * (2 * rank) + rank + r) = f32x2_to_bf16x2(low[0], low[1]);
+        }
     }
 }
 
-}  // namespace
-
-hipError_t launch_adapters_down(const void *x, const AdapterArgs &l, int64_t M, int64_t K, hipStream_t stream)
+template <int G> hipError_t launch(const bf16_t *x, const AdapterArgs &l, int64_t M, int64_t K, hipStream_t stream)
 {
-    const bf16_t *xp = static_cast<const bf16_t *>(x), *a = static_cast<const bf16_t *>(l.a);
-    const unsigned grid = (unsigned)((M + 15) / 16);
-#define MAMBA_DOWN(RT) \
-    down_kernel<RT, 8><<<grid, 512, 0, stream>>>(xp, a, l.scale, l.idx, static_cast<bf16_t *>(l.t), M, (int)K, (int)l.rank, (int)l.adapters)
+    const bf16_t *a = static_cast<const bf16_t *>(l.a);
+    const int64_t most = M <= 64 ? 16 : 4;                           // adapters of a workgroup's rows at once
+    const dim3 grid((unsigned)((M + 16 * G - 1) / (16 * G)), (unsigned)(l.adapters < most ? l.adapters : most));
+#define MAMBA_DOWN(RT)                                                                                                            \
+    down_kernel<RT, G><<<grid, kThreads, 0, stream>>>(x, a, l.scale, l.idx, static_cast<bf16_t *>(l.t), static_cast<uint32_t *>(l.zeros), M, (int)K, \
+                                                      (int)l.rank, (int)l.adapters)
     if (l.rank <= 16) MAMBA_DOWN(1);
     else if (l.rank <= 32) MAMBA_DOWN(2);
     else if (l.rank <= 64) MAMBA_DOWN(4);
     else MAMBA_DOWN(8);
 #undef MAMBA_DOWN
     return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_adapters_down(const void *x, const AdapterArgs &l, int64_t M, int64_t K, hipStream_t stream)
+{
+    const bf16_t *xp = static_cast<const bf16_t *>(x);
+    if (M >= 12288) return launch<4>(xp, l, M, K, stream);
+    if (M >= 6144) return launch<2>(xp, l, M, K, stream);
+    return launch<1>(xp, l, M, K, stream);
 }
 
 }  // namespace mamba

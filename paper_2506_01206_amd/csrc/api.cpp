@@ -483,10 +483,12 @@ int mamba_linear_fwd(const void *x, const void *w, const float *bias, const void
     return done ? MAMBA_OK : (int)launch_linear(a, static_cast<hipStream_t>(hip_stream));
 }
 
+static constexpr int64_t kAdapterZeros = 128;   // ahead of the rows' sums
+
 size_t mamba_linear_adapted_workspace_bytes(int64_t M, int64_t rank)
 {
     int64_t bytes;
-    return M > 0 && rank > 0 && rank % 8 == 0 && rank <= 128 && size3(M, rank, 2, 2, &bytes) ? (size_t)bytes : 0;
+    return M > 0 && rank > 0 && rank % 8 == 0 && rank <= 128 && size3(M, rank, 2, 2, &bytes) ? (size_t)bytes + kAdapterZeros : 0;
 }
 
 int mamba_linear_adapted_fwd(const void *x, const void *w, const float *bias, const void *residual, const void *lora_a,
@@ -501,6 +503,7 @@ int mamba_linear_adapted_fwd(const void *x, const void *w, const float *bias, co
     const int64_t N = n0 + n1 + n2;
     int64_t ab, bb, tb;
     if (!size3(n_adapters, rank, K, 2, &ab) || !size3(n_adapters, N, rank, 2, &bb) || !size3(M, rank, 2, 2, &tb)) return MAMBA_ERR_BAD_SHAPE;
+    tb += kAdapterZeros;
     if (rank == 0 || rank % 8 != 0 || rank > 128 || n_adapters > 0x7ffffffe || K > 0x7ffffff8 || N > 0x7fffffff) return MAMBA_ERR_UNSUPPORTED;
     if (done) return MAMBA_OK;
     if (n_adapters == 0) return MAMBA_ERR_BAD_SHAPE;
@@ -518,7 +521,7 @@ int mamba_linear_adapted_fwd(const void *x, const void *w, const float *bias, co
     }
     if (overlap(workspace, tb, x, M * K * 2) || overlap(workspace, tb, w, N * K * 2) || overlap(workspace, tb, residual, residual ? M * N * 2 : 0))
         return MAMBA_ERR_ALIAS;
-    const AdapterArgs l{lora_a, lora_b, scale, adapter_idx, workspace, rank, n_adapters};
+    const AdapterArgs l{lora_a, lora_b, scale, adapter_idx, static_cast<char *>(workspace) + kAdapterZeros, workspace, rank, n_adapters};
     return (int)launch_linear_adapted(a, l, static_cast<hipStream_t>(hip_stream));
 }
 

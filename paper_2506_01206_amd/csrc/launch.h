@@ -220,6 +220,7 @@ struct AdapterArgs {
     const float *scale;      // (adapters) or nullptr: ones
     const int32_t *idx;      // (M)
     void *t;                 // scratch (M, 2 rank) bf16
+    void *zeros;             // scratch of 128 bytes, which launch_adapters_down clears
     int64_t rank, adapters;  // rank: a multiple of 8 up to 128
 };
 hipError_t launch_adapters_down(const void *x, const AdapterArgs &l, int64_t M, int64_t K, hipStream_t stream);   // t = scale x a^T in two terms

@@ -65,12 +65,13 @@ __device__ __forceinline__ int locate(const OutSplit &o, int64_t n, int64_t *col
 // product with the adapter's first matrix (adapters.hip), which is there as two bfloat16 terms side by side, high and low: 16 bits, so that it is
 // not the rounding of t that the output's rounding is lost in.  The kernels below take an AdapterTail behind their other arguments, or
 // nothing: then they are the plain products, instruction for instruction.
-// A wavefront goes through the adapters that its own rows have, smallest first, and multiplies whole tiles by each; a row takes the sums of its
-// own.  (Sums of the others are dropped, not added as zeros: an adapter's infinities and NaN stay with its rows.)
+// The adapters of a tile's rows are gone through, smallest first; a row takes the sums of its own.  (Sums of the others are dropped, or added as zeros
+// where that is what they are: an adapter's infinities and NaN stay with its rows.)
 struct AdapterTail {
     const bf16_t *t;                 // (M, 2 rank): high terms, low terms
     const bf16_t *b;                 // (adapters, N, rank)
     const int32_t *idx;              // (M); -1: none
+    const bf16_t *zeros;             // 128 bytes of them
     int32_t rank, adapters;          // rank: a multiple of 8
 };
 
@@ -90,15 +91,15 @@ template <int MT> __device__ __forceinline__ int32_t next_adapter(const int32_t 
     return wave_min(v);
 }
 
-// 32 x 32 tiles from row m0 and column n0 on.  TURNED: acc[a][b] has its rows in the lanes (w fragments first), else its columns.
-template <bool TURNED, int MT, int NT>
+// 32 x 32 tiles from row m0 and column n0 on, acc[a][b] with its columns in the lanes (linear_kernel), fragments straight from memory.
+template <int MT, int NT>
 __device__ __forceinline__ void add_adapters(f32x16 (&acc)[MT][NT], const AdapterTail &t, int64_t m0, int64_t M, int64_t n0, int64_t N)
 {
     const int lane = threadIdx.x & 63, chunks = t.rank >> 3;
     int32_t id[MT];
 #pragma unroll
     for (int a = 0; a < MT; ++a) id[a] = adapter_of(t, m0 + a * 32 + (lane & 31), M);
-    auto row_id = [&](int a, int i) __attribute__((always_inline)) { return TURNED ? id[a] : __shfl(id[a], 8 * (i / 4) + 4 * (lane >> 5) + (i & 3)); };
+    auto row_id = [&](int a, int i) __attribute__((always_inline)) { return __shfl(id[a], 8 * (i / 4) + 4 * (lane >> 5) + (i & 3)); };
     for (int32_t cur = next_adapter(id, -1, t.adapters); cur < t.adapters; cur = next_adapter(id, cur, t.adapters)) {
         const bf16_t *b[NT];
 #pragma unroll
@@ -116,10 +117,8 @@ __device__ __forceinline__ void add_adapters(f32x16 (&acc)[MT][NT], const Adapte
                 const bf16x8 xf = *reinterpret_cast<const bf16x8 *>(row + 8 * c);
                 const int cb = c < chunks ? c : c - chunks;
 #pragma unroll
-                for (int j = 0; j < NT; ++j) {
-                    const bf16x8 wf = *reinterpret_cast<const bf16x8 *>(b[j] + 8 * cb);
-                    d[j] = TURNED ? __builtin_amdgcn_mfma_f32_32x32x16_bf16(wf, xf, d[j], 0, 0, 0) : __builtin_amdgcn_mfma_f32_32x32x16_bf16(xf, wf, d[j], 0, 0, 0);
-                }
+                for (int j = 0; j < NT; ++j)
+                    d[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xf, *reinterpret_cast<const bf16x8 *>(b[j] + 8 * cb), d[j], 0, 0, 0);
             }
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
@@ -142,10 +141,9 @@ __device__ __forceinline__ void add_adapters(f32x16 (&acc)[MT][NT], const Adapte
     }
 }
 
-// The accumulators of an adapted product start from the residual, so that its outputs are rounded once.  (`dead` leading rows are not read: where
-// the residual is the output itself their owner may be writing them.)
-template <bool TURNED, int MT, int NT>
-__device__ __forceinline__ void start_from(f32x16 (&acc)[MT][NT], const bf16_t *residual, int64_t m0, int64_t first, int64_t M, int64_t n0, int64_t N)
+// Its accumulators start from the residual, so that outputs are rounded once.
+template <int MT, int NT>
+__device__ __forceinline__ void start_from(f32x16 (&acc)[MT][NT], const bf16_t *residual, int64_t m0, int64_t M, int64_t n0, int64_t N)
 {
     const int lane = threadIdx.x & 63;
 #pragma unroll
@@ -154,9 +152,7 @@ __device__ __forceinline__ void start_from(f32x16 (&acc)[MT][NT], const bf16_t *
         for (int b = 0; b < NT; ++b)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                const int across = 8 * (i / 4) + 4 * (lane >> 5) + (i & 3);
-                const int64_t m = max(min(m0 + a * 32 + (TURNED ? lane & 31 : across), M - 1), first);
-                const int64_t n = min(n0 + b * 32 + (TURNED ? across : lane & 31), N - 1);
+                const int64_t m = min(m0 + a * 32 + 8 * (i / 4) + 4 * (lane >> 5) + (i & 3), M - 1), n = min(n0 + b * 32 + (lane & 31), N - 1);
                 acc[a][b][i] = bf16_to_f32(residual[m * N + n]);
             }
 }
@@ -235,7 +231,7 @@ linear_kernel(const bf16_t *__restrict__ x, const bf16_t *__restrict__ w, const 
     const int frag_row = lane & 31, frag_k = (lane >> 5) * 16;    // byte offset of the lane's 8 k values
     fetch(0);
     if constexpr (kAdapted)
-        if (residual) start_from<false>(acc, residual, m0 + wm * (BM / 2), 0, M, n0 + wn * (BN / 2), N);
+        if (residual) start_from(acc, residual, m0 + wm * (BM / 2), M, n0 + wn * (BN / 2), N);
     for (int64_t k0 = 0; k0 < K; k0 += kBK) {
         __syncthreads();                                          // everyone is done reading the last slab
         park();
@@ -258,7 +254,7 @@ linear_kernel(const bf16_t *__restrict__ x, const bf16_t *__restrict__ w, const 
         }
     }
 
-    if constexpr (kAdapted) add_adapters<false>(acc, tail..., m0 + wm * (BM / 2), M, n0 + wn * (BN / 2), N);
+    if constexpr (kAdapted) add_adapters(acc, tail..., m0 + wm * (BM / 2), M, n0 + wn * (BN / 2), N);
     // epilogue.  acc[a][b][i] is C[8 * (i / 4) + 4 * (lane / 32) + i % 4][lane % 32] of its 32 x 32 tile.
     // The tile leaves through LDS 128 columns at a time.
 #pragma unroll
@@ -435,6 +431,126 @@ __device__ __forceinline__ void load_to_lds16(const char *base, uint32_t lane_of
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_addr), "v"(lane_off), "s"(base) : "memory");
 }
 
+// the same from an address of each lane's own
+__device__ __forceinline__ void load_to_lds16(const void *from, uint32_t lds_addr)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_addr), "v"(from) : "memory");
+}
+
+// Eight bfloat16 with zeros for what is no finite number; whether there was any.
+__device__ __forceinline__ bool only_finite(bf16x8 &v)
+{
+    u32x4 u = __builtin_bit_cast(u32x4, v);
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const bool low = (u[i] & 0x7f80u) == 0x7f80u, high = (u[i] & 0x7f800000u) == 0x7f800000u;
+        odd |= low || high;
+        u[i] &= (low ? 0u : 0xffffu) | (high ? 0u : 0xffff0000u);
+    }
+    v = __builtin_bit_cast(bf16x8, u);
+    return odd;
+}
+
+// Adapters of the tiles of linear_wide_kernel and linear_ring_kernel: more slabs of 64 k behind the product's own, an adapter's two terms of t against
+// its B twice.  Rows that are not the adapter's read a line of zeros, and so does what is behind the rank.  Zero times an infinity is no zero: where
+// B has what is no finite number, zeros stand in for it, and two more products, of the largest number by itself and by its negative, make the outputs of
+// its column NaN in the adapter's own rows.  Two stages in turn, the next slab's loads under way while one is multiplied.  Uses the first two stages
+// and leaves them free; all wavefronts come and go together.
+template <int BM, int BN, int WM, int WN, int kRow, int MT, int NT>
+__device__ __forceinline__ void add_adapter_slabs(f32x16 (&acc)[MT][NT], const AdapterTail &t, unsigned char *lds, int64_t m0, int64_t n0, int64_t N,
+                                                  const int (&frag_x)[4], const int (&frag_w)[4])
+{
+    constexpr int NW = WM * WN, kStage = (BM + BN) * kRow, NLX = BM / 8 / NW;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wm = wave / WN;
+    const uint32_t lds0 = (uint32_t)(size_t)(__attribute__((address_space(3))) unsigned char *)lds;
+    const int chunks = t.rank >> 3, slabs = (2 * chunks + 7) / 8;
+    int32_t mine[(BM + 63) / 64], row_id[NLX];                        // of all rows, 64 to a register; of those that this lane brings
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < (BM + 63) / 64; ++i) {
+        mine[i] = i * 64 + lane < BM ? t.idx[m0 + i * 64 + lane] : -1;
+        bad |= mine[i] < -1 || mine[i] >= t.adapters;
+    }
+#pragma unroll
+    for (int i = 0; i < NLX; ++i) row_id[i] = t.idx[m0 + 8 * (NW * i + wave) + (lane >> 3)];
+    lds_barrier_linear();                                             // the stages are free
+    auto request = [&](int32_t cur, int slab, int stage) __attribute__((always_inline)) {
+        // a wavefront's rows 8 (NW i + wave) + lane / 8, the 16-byte slot lane % 8 of which is chunk (lane % 8) ^ (4 (wave & 1) + lane / 16) & 7
+        const int c = 8 * slab + ((lane & 7) ^ ((4 * (wave & 1) + (lane >> 4)) & 7)), cb = c < chunks ? c : c - chunks;
+        const bool in = c < 2 * chunks;
+#pragma unroll
+        for (int i = 0; i < NLX; ++i) {
+            const int row = 8 * (NW * i + wave) + (lane >> 3);
+            const bf16_t *from = in && row_id[i] == cur ? t.t + (m0 + row) * (2 * t.rank) + 8 * c : t.zeros + 8 * (lane & 7);
+            load_to_lds16(from, lds0 + stage * kStage + wave * 1024 + i * (1024 * NW));
+        }
+#pragma unroll
+        for (int i = 0; i < BN / 8 / NW; ++i) {
+            const int row = 8 * (NW * i + wave) + (lane >> 3);
+            const bf16_t *from = in ? t.b + ((int64_t)cur * N + n0 + row) * t.rank + 8 * cb : t.zeros + 8 * (lane & 7);
+            load_to_lds16(from, lds0 + stage * kStage + BM * kRow + wave * 1024 + i * (1024 * NW));
+        }
+    };
+    int32_t cur = next_adapter(mine, -1, t.adapters);
+    int slab = 0, stage = 0;
+    if (cur < t.adapters) request(cur, 0, 0);
+    while (cur < t.adapters) {
+        const int32_t next = slab + 1 < slabs ? cur : next_adapter(mine, cur, t.adapters);
+        const int next_slab = slab + 1 < slabs ? slab + 1 : 0;
+        __builtin_amdgcn_s_waitcnt(0x0070);                           // this slab has landed (this wavefront's part), and the last one's reads are over
+        lds_barrier_linear();
+        if (next < t.adapters) request(next, next_slab, 1 - stage);
+        const unsigned char *from = lds + stage * kStage;
+        uint32_t odd = 0;                                             // columns (of block b in bit b) with what is no finite number
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) {
+            bf16x8 xf[MT], wf[NT];
+#pragma unroll
+            for (int a = 0; a < MT; ++a) xf[a] = *reinterpret_cast<const bf16x8 *>(from + frag_x[ks] + a * 32 * kRow);
+#pragma unroll
+            for (int b = 0; b < NT; ++b) {
+                wf[b] = *reinterpret_cast<const bf16x8 *>(from + frag_w[ks] + b * 32 * kRow);
+                odd |= (uint32_t)only_finite(wf[b]) << b;
+            }
+#pragma unroll
+            for (int a = 0; a < MT; ++a)
+#pragma unroll
+                for (int b = 0; b < NT; ++b) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wf[b], xf[a], acc[a][b], 0, 0, 0);
+        }
+        if (__any(odd != 0)) {
+            odd |= __shfl_xor(odd, 32);
+            // (one k, in the lower half of the lanes)
+#pragma unroll
+            for (int a = 0; a < MT; ++a) {
+                const bool own = lane < 32 && t.idx[m0 + wm * (BM / WM) + a * 32 + (lane & 31)] == cur;
+                const bf16x8 xf = __builtin_bit_cast(bf16x8, u32x4{own ? 0x7f7fu : 0u, 0u, 0u, 0u});
+#pragma unroll
+                for (int b = 0; b < NT; ++b) {
+                    const bool column = lane < 32 && (odd >> b & 1);
+                    const bf16x8 plus = __builtin_bit_cast(bf16x8, u32x4{column ? 0x7f7fu : 0u, 0u, 0u, 0u});
+                    const bf16x8 minus = __builtin_bit_cast(bf16x8, u32x4{column ? 0xff7fu : 0u, 0u, 0u, 0u});
+                    acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(plus, xf, acc[a][b], 0, 0, 0);
+                    acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(minus, xf, acc[a][b], 0, 0, 0);
+                }
+            }
+        }
+        cur = next, slab = next_slab, stage = 1 - stage;
+    }
+    if (__any(bad)) {                                                 // a row whose index is out of range: NaN
+#pragma unroll
+        for (int a = 0; a < MT; ++a) {
+            const int32_t id = t.idx[m0 + wm * (BM / WM) + a * 32 + (lane & 31)];
+            const bool out = id < -1 || id >= t.adapters;
+#pragma unroll
+            for (int b = 0; b < NT; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[a][b][i] = out ? __int_as_float(0x7fc00000) : acc[a][b][i];
+        }
+    }
+}
+
 template <int BM, int BN, bool CONV = false, int WM = 2, int WN = 2, typename... Tail>
 __global__ void __launch_bounds__(64 * WM * WN)
 linear_wide_kernel(const bf16_t *x, const bf16_t *w, const float *__restrict__ bias, const bf16_t *residual,
@@ -575,8 +691,6 @@ linear_wide_kernel(const bf16_t *x, const bf16_t *w, const float *__restrict__ b
     typedef std::integral_constant<int, 0> Even;
     typedef std::integral_constant<int, 1> Odd;
     const int S = (int)(K / kWideBK);
-    if constexpr (kAdapted)
-        if (residual) start_from<true>(acc, residual, m0 + wm * (BM / WM), m0 + dead, M, n0 + wn * (BN / WN), N);
     request(0, 0, L0(), L4());
     request(kWideBK, kStage, L0(), L4());
     // vmcnt(loads of one slab): slab 0 is in, slab 1 may be under way (vmcnt is split over bits 3:0 and 15:14)
@@ -590,13 +704,15 @@ linear_wide_kernel(const bf16_t *x, const bf16_t *w, const float *__restrict__ b
     }
     slab(Even(), 0, std::false_type(), std::true_type());         // S is even: two slabs left, nothing more to request
     slab(Odd(), 0, std::false_type(), std::false_type());
-    if constexpr (kAdapted) add_adapters<true>(acc, tail..., m0 + wm * (BM / WM), M, n0 + wn * (BN / WN), N);
+    if constexpr (kAdapted) {
+        add_adapter_slabs<BM, BN, WM, WN, kWideRow>(acc, tail..., lds, m0, n0, N, frag_x, frag_w);
+    }
     // Epilogue.  The residual chunks this thread will add are requested first, all at once: with one workgroup per
     // CU nothing else would hide their latency, and fetched four at a time inside the store loop they cost a third
     // of the tile's time.
     constexpr int kCpr = BN / 8, kChunks = BM * kCpr / kThr;
     u32x4 res[kChunks];
-    if (!kAdapted && residual) {
+    if (residual) {
 #pragma unroll
         for (int i = 0; i < kChunks; ++i) {
             const int c = tid + i * kThr, row = c / kCpr, cc = c % kCpr;
@@ -607,6 +723,17 @@ linear_wide_kernel(const bf16_t *x, const bf16_t *w, const float *__restrict__ b
         }
     }
     lds_barrier_linear();                                         // the stages are free for the output tile (the requests stay in flight)
+    if constexpr (kAdapted) {
+        // outputs that are rounded once, residual included: it stands where they will, until they take it along
+        if (residual) {
+#pragma unroll
+            for (int i = 0; i < kChunks; ++i) {
+                const int c = tid + i * kThr;
+                *reinterpret_cast<u32x4 *>(lds + (c / kCpr) * kOutRow + (c % kCpr) * 16) = res[i];
+            }
+            lds_barrier_linear();
+        }
+    }
 
     // acc[a][b][4 g + j] is C[m = 32 a + lane % 32][n = 32 b + 8 g + 4 (lane / 32) + j] of the wavefront's part
 #pragma unroll
@@ -619,9 +746,16 @@ linear_wide_kernel(const bf16_t *x, const bf16_t *w, const float *__restrict__ b
 #pragma unroll
             for (int a = 0; a < MT; ++a) {
                 const int ml = wm * (BM / WM) + a * 32 + (lane & 31);
+                float4 add = bv;
+                if constexpr (kAdapted) {
+                    if (residual) {
+                        const uint2 q = *reinterpret_cast<const uint2 *>(lds + ml * kOutRow + nl * 2);
+                        add = make_float4(bv.x + bf16_lo(q.x), bv.y + bf16_hi(q.x), bv.z + bf16_lo(q.y), bv.w + bf16_hi(q.y));
+                    }
+                }
                 uint2 v;
-                v.x = f32x2_to_bf16x2(acc[a][b][4 * g + 0] + bv.x, acc[a][b][4 * g + 1] + bv.y);
-                v.y = f32x2_to_bf16x2(acc[a][b][4 * g + 2] + bv.z, acc[a][b][4 * g + 3] + bv.w);
+                v.x = f32x2_to_bf16x2(acc[a][b][4 * g + 0] + add.x, acc[a][b][4 * g + 1] + add.y);
+                v.y = f32x2_to_bf16x2(acc[a][b][4 * g + 2] + add.z, acc[a][b][4 * g + 3] + add.w);
                 *reinterpret_cast<uint2 *>(lds + ml * kOutRow + nl * 2) = v;
             }
             __builtin_amdgcn_sched_barrier(0);                    // one group at a time: the accumulators stay where they are until used
@@ -787,8 +921,6 @@ linear_ring_kernel(const bf16_t *x, const bf16_t *w, const float *__restrict__ b
         return (m0 + row) * out.width[*sp] + col;
     };
     u32x4 res[MT][NT][2];
-    if constexpr (kAdapted)
-        if (residual) start_from<true>(acc, residual, m0 + wm * (BM / WM), m0 + dead, M, n0 + wn * (BN / WN), (int64_t)tiles_n * BN);
 
 #pragma unroll
     for (int i = 0; i < STAGES - 1; ++i) {
@@ -802,7 +934,7 @@ linear_ring_kernel(const bf16_t *x, const bf16_t *w, const float *__restrict__ b
     const unsigned char *cur = lds;
     load_frags(cur, 0, f0);
     request(L0(), L1());
-    const int fetch_res = !kAdapted && residual ? (S > 3 ? S - 3 : 0) : -1;
+    const int fetch_res = residual ? (S > 3 ? S - 3 : 0) : -1;
 #pragma unroll 1
     for (int s = 0; s < S; ++s) {
         if (s == fetch_res) {
@@ -838,7 +970,9 @@ linear_ring_kernel(const bf16_t *x, const bf16_t *w, const float *__restrict__ b
         multiply(f1);
     }
 
-    if constexpr (kAdapted) add_adapters<true>(acc, tail..., m0 + wm * (BM / WM), M, n0 + wn * (BN / WN), (int64_t)tiles_n * BN);
+    if constexpr (kAdapted) {
+        add_adapter_slabs<BM, BN, WM, WN, kWideRow>(acc, tail..., lds, m0, n0, (int64_t)tiles_n * BN, frag_x, frag_w);
+    }
     if constexpr (CONV) {
         // the whole tile, since windows reach into the rows of other wavefronts; every read of the stages is behind the last barrier
         constexpr int kOutRow = BN * 2 + 16, kCpr = BN / 8;
@@ -874,10 +1008,26 @@ linear_ring_kernel(const bf16_t *x, const bf16_t *w, const float *__restrict__ b
 #pragma unroll
         for (int b = 0; b < NT; ++b) {
             const int r = lane & 31;
+            if constexpr (kAdapted) {                             // (as in linear_wide_kernel: the residual where the outputs will be)
+                if (residual) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int pr = 16 * i + (lane >> 2);
+                        *reinterpret_cast<u32x4 *>(patch + pr * 64 + (((lane & 3) ^ ((pr >> 1) & 3)) << 4)) = res[a][b][i];
+                    }
+                    wave_sync();
+                }
+            }
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 float4 bv = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
                 if (bias) bv = *reinterpret_cast<const float4 *>(bias + n0 + wn * (BN / WN) + b * 32 + 8 * g + 4 * (lane >> 5));
+                if constexpr (kAdapted) {
+                    if (residual) {
+                        const uint2 q = *reinterpret_cast<const uint2 *>(patch + r * 64 + ((g ^ ((r >> 1) & 3)) << 4) + 8 * (lane >> 5));
+                        bv = make_float4(bv.x + bf16_lo(q.x), bv.y + bf16_hi(q.x), bv.z + bf16_lo(q.y), bv.w + bf16_hi(q.y));
+                    }
+                }
                 uint2 v;
                 v.x = f32x2_to_bf16x2(acc[a][b][4 * g + 0] + bv.x, acc[a][b][4 * g + 1] + bv.y);
                 v.y = f32x2_to_bf16x2(acc[a][b][4 * g + 2] + bv.z, acc[a][b][4 * g + 3] + bv.w);
@@ -1226,7 +1376,7 @@ hipError_t launch_linear(const LinearArgs &a, hipStream_t stream) { return a.nor
 hipError_t launch_linear_adapted(const LinearArgs &a, const AdapterArgs &l, hipStream_t stream)
 {
     if (const hipError_t e = launch_adapters_down(a.x, l, a.M, a.K, stream)) return e;
-    return launch_product(a, stream, AdapterTail{static_cast<const bf16_t *>(l.t), static_cast<const bf16_t *>(l.b), l.idx, (int32_t)l.rank, (int32_t)l.adapters});
+    return launch_product(a, stream, AdapterTail{static_cast<const bf16_t *>(l.t), static_cast<const bf16_t *>(l.b), l.idx, static_cast<const bf16_t *>(l.zeros), (int32_t)l.rank, (int32_t)l.adapters});
 }
 
 hipError_t launch_linear_conv(const LinearArgs &a, hipStream_t stream)
