@@ -16,37 +16,25 @@ namespace mamba {
 namespace {
 
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
-constexpr int kTile = kThreads * 4;                                  // tokens that the workgroup adds up together
-constexpr int kMaxTiles = (1 << 25) / kTile;
+constexpr int kTrip = 64 * 4;                                        // tokens that a wavefront has at once
 
-struct Shared {
-    double tile[kMaxTiles];                                          // sums of P by tiles
-    double part[2][kWaves];
-    double sum[2];
-    int32_t token, where;
-};
-
-// The children of one node that were rejected so far, and what P and Q became by them.
+// The children of a node that were rejected so far, and what P and Q became by them.
 struct Rejections {
-    int n = 0;
     int32_t token[kMaxFan];
     double of_gap[kMaxFan], of_rest[kMaxFan];                        // 1 / sums; 0: the sum was zero
+};
+struct Shared {
+    double part[2][2][kWaves];                                       // sums of the wavefronts' ranges, in turn: the others may still be being read
+    Rejections rejected;
+};
 
-    // P - Q ahead of the division, P and Q of a token with probabilities p and q; `left`: q of the token while it is not rejected
-    __device__ __forceinline__ void at(double p, double q, int32_t v, double *P, double *Q, double *left) const
-    {
-        double Pv = p, Qv = q;
-#pragma unroll
-        for (int i = 0; i < kMaxFan; ++i) {
-            if (i < n) {
-                const double gap = fmax(Pv - Qv, 0.0);
-                Pv = of_gap[i] > 0.0 ? gap * of_gap[i] : Pv;
-                q = v == token[i] ? 0.0 : q;
-                Qv = q * of_rest[i];
-            }
-        }
-        *P = Pv, *Q = Qv, *left = q;
-    }
+// What is added up over the tokens of a row: P after the first `levels` rejections, or where `gap` says so what P is ahead of Q there (then of q too what
+// is left beside the rejected children and `token`).  (One function for all passes, not inlined: its instructions are fetched once.)
+struct Weighing {
+    const float *p, *q;                                              // q: nullptr: zeros
+    int levels;
+    bool gap;
+    int32_t token;
 };
 
 __device__ __forceinline__ double wave_sum(double v)
@@ -56,177 +44,203 @@ __device__ __forceinline__ double wave_sum(double v)
     return v;
 }
 
-// four tokens of a row from v0 on, zeros behind its end
-__device__ __forceinline__ void load4(const float *row, int32_t v0, int32_t V, float *x)
+// P and Q of four tokens with probabilities p and q; `left`: q while the token is not rejected
+__device__ __forceinline__ void after_rejections(const Rejections &r, int levels, int32_t v0, double (&P)[4], double (&Q)[4], double (&left)[4])
 {
-    if (v0 + 4 <= V) {
-        const f32x4_any a = *reinterpret_cast<const f32x4_any *>(row + v0);
+#pragma unroll 1
+    for (int l = 0; l < levels; ++l) {
+        const int32_t token = r.token[l];
+        const double of_gap = r.of_gap[l], of_rest = r.of_rest[l];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = a[i];
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = v0 + i < V ? row[v0 + i] : 0.0f;
+        for (int i = 0; i < 4; ++i) {
+            const double gap = fmax(P[i] - Q[i], 0.0);
+            P[i] = of_gap > 0.0 ? gap * of_gap : P[i];
+            left[i] = v0 + i == token ? 0.0 : left[i];
+            Q[i] = left[i] * of_rest;
+        }
     }
 }
+// x: what is added up of four tokens, y: of q
+__device__ __forceinline__ void weigh(const Rejections &r, const Weighing &w, const f32x4_any &pv, const f32x4_any &qv, int32_t v0, double (&x)[4], double (&y)[4])
+{
+    double P[4], Q[4], left[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) P[i] = pv[i], left[i] = Q[i] = qv[i];
+    after_rejections(r, w.levels, v0, P, Q, left);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = w.gap ? fmax(P[i] - Q[i], 0.0) : P[i], y[i] = v0 + i == w.token ? 0.0 : left[i];
+}
+// four tokens of a row from v on, zeros from `end` on
+__device__ __forceinline__ f32x4_any load4(const float *row, int32_t v, int32_t end)
+{
+    if (v + 4 <= end) return *reinterpret_cast<const f32x4_any *>(row + v);
+    f32x4_any x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = v + i < end ? row[v + i] : 0.0f;
+    return x;
+}
 
-// One workgroup to a sequence.
+// Tokens from .. from + length - 1 added up: by wavefronts, which have `per_of(length)` each in one piece, and all together, in an order that depends on
+// the numbers alone.
+struct Sums {
+    const double *by_wave;                                           // of the first
+    double first, second;
+};
+__device__ __forceinline__ int32_t per_of(int32_t length) { return ((length + kWaves - 1) / kWaves + 3) / 4 * 4; }
+__device__ __attribute__((noinline)) Sums sums_of(Shared &s, int turn, Weighing w, int32_t from, int32_t length)
+{
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int32_t per = per_of(length), begin = from + min(wave * per, length), end = from + min((wave + 1) * per, length);
+    constexpr int kAhead = 4;
+    double x = 0.0, y = 0.0;
+#pragma unroll 1
+    for (int32_t v0 = begin; v0 < end; v0 += kAhead * kTrip) {
+        f32x4_any pv[kAhead], qv[kAhead];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            const int32_t v = v0 + j * kTrip + lane * 4;
+            pv[j] = load4(w.p, v, end);
+            qv[j] = w.q ? load4(w.q, v, end) : f32x4_any(0.0f);
+        }
+#pragma unroll 1
+        for (int j = 0; j < kAhead; ++j) {
+            double xs[4], ys[4];
+            weigh(s.rejected, w, pv[0], qv[0], v0 + j * kTrip + lane * 4, xs, ys);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x += xs[i], y += ys[i];
+#pragma unroll
+            for (int i = 0; i + 1 < kAhead; ++i) pv[i] = pv[i + 1], qv[i] = qv[i + 1];
+        }
+    }
+    x = wave_sum(x), y = wave_sum(y);
+    double(*part)[kWaves] = s.part[turn];
+    if (lane == 0) part[0][wave] = x, part[1][wave] = y;
+    __syncthreads();
+    Sums r{part[0], 0.0, 0.0};
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) r.first += part[0][i], r.second += part[1][i];
+    return r;
+}
+
+// One workgroup to a sequence.  A pass over a row of p and q is what a rejection takes: every wavefront has a sixteenth of it, in one piece, so that
+// its sum is also where the search for a drawn token begins, which goes on in sixteenths of a sixteenth.  Bound by what one CU brings in: a pass
+// over 50280 tokens reads 400 KB.
 __global__ void __launch_bounds__(kThreads) verify_kernel(VerifyArgs a)
 {
     __shared__ Shared s;
     const int64_t b = blockIdx.x;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63;
     const int32_t V = (int32_t)a.V;
     const float *p_rows = a.p + b * a.nodes * a.V, *q_rows = a.q + b * a.inner * a.V;
     const int32_t *tokens = a.tokens + b * (a.nodes - 1);
     const float *u_accept = a.u_accept + b * (a.nodes - 1);
     int32_t *out = a.out + b * (a.gamma + 1), *node = a.node + b * a.gamma;
-
-    // sums over the row of what f gives for a token, in an order that depends on V alone; the first of the two by tiles too
-    auto sums = [&](const float *p, const float *q, auto f) {
-        double total[2] = {0.0, 0.0};
-        for (int t = 0; t * kTile < V; ++t) {
-            const int32_t v0 = t * kTile + tid * 4;
-            float pv[4] = {}, qv[4] = {};
-            load4(p, v0, V, pv);
-            if (q) load4(q, v0, V, qv);
-            double x[2] = {0.0, 0.0};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                double y[2] = {0.0, 0.0};
-                f((double)pv[i], (double)qv[i], v0 + i, y);
-                x[0] += y[0], x[1] += y[1];
-            }
-            __syncthreads();
-            x[0] = wave_sum(x[0]), x[1] = wave_sum(x[1]);
-            if (lane == 0) s.part[0][wave] = x[0], s.part[1][wave] = x[1];
-            __syncthreads();
-            double y[2] = {0.0, 0.0};
-            for (int w = 0; w < kWaves; ++w) y[0] += s.part[0][w], y[1] += s.part[1][w];
-            if (tid == 0) s.tile[t] = y[0];
-            total[0] += y[0], total[1] += y[1];
-        }
-        s.sum[0] = total[0], s.sum[1] = total[1];                    // (the same from all threads)
-        __syncthreads();
-    };
-    // the token at which the sums of f pass u times `total`, the tiles' sums of f in s.tile
-    auto drawn = [&](const float *p, const float *q, double total, float u, auto f) -> int32_t {
-        if (!(total > 0.0)) return -1;
-        const double bound = (double)u * total;
-        const int tiles = (V + kTile - 1) / kTile;
-        int t = 0;
-        double before = 0.0;
-        for (; t < tiles - 1 && !(before + s.tile[t] > bound); ++t) before += s.tile[t];
-        int32_t last = -1;                                           // of those with any weight
-        for (; t < tiles; ++t) {
-            const int32_t v0 = t * kTile + tid * 4;
-            float pv[4] = {}, qv[4] = {};
-            load4(p, v0, V, pv);
-            if (q) load4(q, v0, V, qv);
-            double x[4], mine = 0.0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                double y[2] = {0.0, 0.0};
-                f((double)pv[i], (double)qv[i], v0 + i, y);
-                x[i] = y[0];
-                mine += y[0];
-            }
-            double to = mine;
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const double o = __shfl_up(to, d);
-                to += lane >= d ? o : 0.0;
-            }
-            __syncthreads();
-            if (lane == 63) s.part[0][wave] = to;
-            if (tid == 0) s.token = V, s.where = -1;
-            __syncthreads();
-            double from = before;
-            for (int w = 0; w < wave; ++w) from += s.part[0][w];
-            double at = from + (to - mine);
-            int32_t first = V, some = -1;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                at += x[i];
-                if (x[i] > 0.0) {
-                    some = v0 + i;
-                    if (at > bound && first == V) first = v0 + i;
-                }
-            }
-            if (first < V) atomicMin(&s.token, first);
-            if (some >= 0) atomicMax(&s.where, some);
-            __syncthreads();
-            if (s.where >= 0) last = s.where;
-            if (s.token < V) return s.token;
-            before += s.tile[t];
-            __syncthreads();
-        }
-        return last;                                                 // (the last bits of the sums)
-    };
+    int turn = 0;
+    auto sums = [&](const Weighing &w, int32_t from, int32_t length) { return sums_of(s, turn ^= 1, w, from, length); };
 
     int64_t row = 0, rows = 1, nodes = 0, children = 0;              // of the node, of its position, ahead of that
     int depth = 0;
-    int32_t token = -1;
+    Weighing w{};                                                    // of the token that is drawn
+    Sums all{};                                                      // and its sums over the row, where there are some
+    bool known = false;
+#pragma unroll 1
     for (; depth < a.gamma; ++depth) {
         const int fan = a.tree[depth];
         const float *p = p_rows + (nodes + row) * a.V, *q = q_rows + (nodes + row) * a.V;
         const int64_t first = children + row * fan;
-        Rejections r;
-        double sum = 1.0;
-        bool fresh = false;                                          // s.tile has the sums of the last gap
-        int taken = -1;
+        int n = 0, taken = -1;                                       // rejections; the child that was accepted
         int32_t c = -1;
+        known = false;
+#pragma unroll 1
         for (int j = 0; j < fan; ++j) {
             c = tokens[first + j];
+            const float u = u_accept[first + j];
             if (c < 0 || c >= V) continue;
-            double P, Q, left;
-            r.at((double)p[c], (double)q[c], c, &P, &Q, &left);
-            const double ratio = Q > 0.0 ? P / Q : P > 0.0 ? 1.0 : 0.0;
-            if ((double)u_accept[first + j] < (ratio < 1.0 ? ratio : 1.0)) {
+            double P[4] = {p[c], 0.0, 0.0, 0.0}, Q[4] = {q[c], 0.0, 0.0, 0.0}, left[4] = {Q[0], 0.0, 0.0, 0.0};
+            after_rejections(s.rejected, n, c, P, Q, left);
+            const double ratio = Q[0] > 0.0 ? P[0] / Q[0] : P[0] > 0.0 ? 1.0 : 0.0;
+            if ((double)u < (ratio < 1.0 ? ratio : 1.0)) {
                 taken = j;
                 break;
             }
-            sums(p, q, [&](double pv, double qv, int32_t v, double (&y)[2]) {
-                double Pv, Qv, rest;
-                r.at(pv, qv, v, &Pv, &Qv, &rest);
-                y[0] = fmax(Pv - Qv, 0.0), y[1] = v == c ? 0.0 : rest;
-            });
-            sum = s.sum[0];
-            const double rest = s.sum[1];
-#pragma unroll
-            for (int i = 0; i < kMaxFan; ++i)
-                if (i == r.n) r.token[i] = c, r.of_gap[i] = sum > 0.0 ? 1.0 / sum : 0.0, r.of_rest[i] = rest > 0.0 ? 1.0 / rest : 0.0;
-            ++r.n;
-            fresh = sum > 0.0;
-        }
-        if (taken >= 0) {
-            if (tid == 0) out[depth] = c, node[depth] = (int32_t)(row * fan + taken);
-            nodes += rows, children += rows * fan, row = row * fan + taken, rows *= fan;
-            continue;
-        }
-        auto residual = [&](double pv, double qv, int32_t v, double (&y)[2]) {
-            double Pv, Qv, rest;
-            if (fresh) {                                             // ahead of its division: what the tiles hold
-                --r.n;
-                r.at(pv, qv, v, &Pv, &Qv, &rest);
-                ++r.n;
-                y[0] = fmax(Pv - Qv, 0.0);
-            } else {
-                r.at(pv, qv, v, &Pv, &Qv, &rest);
-                y[0] = Pv;
+            w = Weighing{p, q, n, true, c};
+            all = sums(w, 0, V);
+            known = all.first > 0.0;
+            if (tid == 0) {
+                s.rejected.token[n] = c;
+                s.rejected.of_gap[n] = known ? 1.0 / all.first : 0.0;
+                s.rejected.of_rest[n] = all.second > 0.0 ? 1.0 / all.second : 0.0;
             }
-        };
-        if (!fresh) {
-            sums(p, q, residual);
-            sum = s.sum[0];
+            ++n;
+            __syncthreads();
         }
-        token = drawn(p, q, sum, a.u_sample[b], residual);
-        break;
+        if (taken < 0) {
+            // from what P is ahead of Q at the last rejection, undivided, or where that was nothing from P
+            if (!known) w = Weighing{p, q, n, false, -1};
+            break;
+        }
+        if (tid == 0) out[depth] = c, node[depth] = (int32_t)(row * fan + taken);
+        __syncthreads();                                             // (what the rejections are read by is over)
+        nodes += rows, children += rows * fan, row = row * fan + taken, rows *= fan;
     }
-    if (depth == a.gamma) {
-        const float *p = p_rows + (nodes + row) * a.V;
-        auto itself = [](double pv, double, int32_t, double (&y)[2]) { y[0] = pv; };
-        sums(p, nullptr, itself);
-        token = drawn(p, nullptr, s.sum[0], a.u_sample[b], itself);
+    if (depth == a.gamma) w = Weighing{p_rows + (nodes + row) * a.V, nullptr, 0, false, -1}, known = false;
+
+    // ---- the token at which the sums pass u times their total
+    int32_t token = -1, from = 0, length = V;
+    double before = 0.0, bound = 0.0;
+#pragma unroll 1
+    for (bool whole = true;; whole = false) {                        // the range in which they do; the last that has any (the last bits of the sums)
+        if (!known) all = sums(w, from, length);
+        known = false;
+        if (whole) bound = (double)a.u_sample[b] * all.first;
+        if (whole && !(all.first > 0.0)) {
+            length = 0;
+            break;
+        }
+        const int32_t per = per_of(length);
+        int at = -1;
+        double at_before = before;
+#pragma unroll 1
+        for (int i = 0; i < kWaves; ++i) {
+            const double x = all.by_wave[i];
+            if (x > 0.0) {
+                at = i, at_before = before;
+                if (before + x > bound) break;
+            }
+            before += x;
+        }
+        if (at < 0) {
+            length = 0;
+            break;
+        }
+        before = at_before;
+        from += min(at * per, length), length = min(per, length - min(at * per, length));
+        if (length <= kTrip) break;
+    }
+    if (length > 0) {                                                // (every wavefront looks through the same tokens)
+        const int32_t v0 = from + lane * 4, end = from + length;
+        double x[4], y[4], mine = 0.0;
+        weigh(s.rejected, w, load4(w.p, v0, end), w.q ? load4(w.q, v0, end) : f32x4_any(0.0f), v0, x, y);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = v0 + i < end ? x[i] : 0.0, mine += x[i];
+        double to = mine;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const double o = __shfl_up(to, d);
+            to += lane >= d ? o : 0.0;
+        }
+        double at = before + (to - mine);
+        int32_t there = -1, some = -1;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            at += x[i];
+            if (x[i] > 0.0) {
+                some = v0 + i;
+                if (at > bound && there < 0) there = v0 + i;
+            }
+        }
+        const uint64_t is = __ballot(there >= 0), any = __ballot(some >= 0);
+        token = is ? __builtin_amdgcn_readlane(there, __builtin_ctzll(is)) : any ? __builtin_amdgcn_readlane(some, 63 - __builtin_clzll(any)) : -1;
     }
     if (tid == 0) {
         out[depth] = token;
