@@ -544,11 +544,13 @@ int mamba_sample_fwd(const void *logits, const mamba_sampling_t *s, const float 
  * times their sum; -1 where the sum is zero or no number.  All of this in float64.  An emitted token is distributed as p, whatever q is.
  *   out: int32 (n_seq, gamma + 1): the accepted tokens, the drawn one, then -1;  count: int32 (n_seq): how many there are (1 .. gamma + 1)
  *   node: int32 (n_seq, gamma): of the accepted tokens the row in their position (the row of its cache to go on from), then -1
- * p, q: four bytes' alignment is enough.  n_seq < 2^22, nodes <= 65535, V <= 2^25.
+ * p, q: four bytes' alignment is enough.  workspace: device scratch of mamba_tree_verify_workspace_bytes(n_seq) bytes; nothing in it has to be kept or
+ * cleared between calls.  n_seq (V / 2048 rounded up, 256 at most) < 2^24, nodes <= 65535, V <= 2^25.
  */
+size_t mamba_tree_verify_workspace_bytes(int64_t n_seq);
 int mamba_tree_verify_fwd(const float *p, const float *q, const int32_t *tokens, const float *u_accept, const float *u_sample,
-                          int32_t *out, int32_t *count, int32_t *node, const int32_t *tree, int gamma, int64_t n_seq, int64_t V,
-                          void *hip_stream);
+                          int32_t *out, int32_t *count, int32_t *node, void *workspace, size_t workspace_bytes, const int32_t *tree,
+                          int gamma, int64_t n_seq, int64_t V, void *hip_stream);
 
 /*
  * A projection that the rows of many requests share, with each request's own low-rank adapter beside it (one drafter for requests of several

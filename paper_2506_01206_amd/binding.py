@@ -115,7 +115,9 @@ def _declare(lib):
     lib.mamba_sample_workspace_bytes.restype = _sz
     lib.mamba_sample_fwd.argtypes = [_vp, ctypes.POINTER(Sampling)] + [_vp] * 6 + [_sz, _i64, _i64, _int, _int, _vp]
     lib.mamba_sample_fwd.restype = _int
-    lib.mamba_tree_verify_fwd.argtypes = [_vp] * 8 + [ctypes.POINTER(ctypes.c_int32), _int, _i64, _i64, _vp]
+    lib.mamba_tree_verify_workspace_bytes.argtypes = [_i64]
+    lib.mamba_tree_verify_workspace_bytes.restype = _sz
+    lib.mamba_tree_verify_fwd.argtypes = [_vp] * 9 + [_sz, ctypes.POINTER(ctypes.c_int32), _int, _i64, _i64, _vp]
     lib.mamba_tree_verify_fwd.restype = _int
     lib.mamba_linear_adapted_workspace_bytes.argtypes = [_i64, _i64]
     lib.mamba_linear_adapted_workspace_bytes.restype = _sz
@@ -168,7 +170,7 @@ EXPORTS = ("mamba_status_string", "mamba_conv1d_fwd", "mamba_scan_workspace_byte
            "mamba2_ssd_workspace_bytes", "mamba2_ssd_fwd", "mamba2_state_step",
            "mamba_gated_delta_workspace_bytes", "mamba_gated_delta_fwd", "mamba_gated_delta_step",
            "mamba_token_counts", "mamba_logits_constrain_fwd", "mamba_topk_constrained_workspace_bytes", "mamba_topk_constrained_fwd",
-           "mamba_sample_workspace_bytes", "mamba_sample_fwd", "mamba_tree_verify_fwd",
+           "mamba_sample_workspace_bytes", "mamba_sample_fwd", "mamba_tree_verify_workspace_bytes", "mamba_tree_verify_fwd",
            "mamba_linear_adapted_workspace_bytes", "mamba_linear_adapted_fwd")
 
 
@@ -190,7 +192,7 @@ _delta.bind(MambaError, torch.OutOfMemoryError, *[ctypes.cast(getattr(lib, name)
     "mamba_logits_constrain_fwd", "mamba_topk_constrained_workspace_bytes", "mamba_topk_constrained_fwd")])
 _sample = _marshal._sample
 _sample.bind(MambaError, torch.OutOfMemoryError, *[ctypes.cast(getattr(lib, name), _vp).value for name in (
-    "mamba_sample_workspace_bytes", "mamba_sample_fwd", "mamba_tree_verify_fwd", "mamba_linear_adapted_workspace_bytes",
+    "mamba_sample_workspace_bytes", "mamba_sample_fwd", "mamba_tree_verify_workspace_bytes", "mamba_tree_verify_fwd", "mamba_linear_adapted_workspace_bytes",
     "mamba_linear_adapted_fwd")])
 
 
@@ -577,11 +579,17 @@ def mamba_sample_fwd(logits, u, params, top_k=None, seq_idx=None, path=None, idx
     return _sample.sample_fwd(logits, u, params, top_k, seq_idx, path, idx, prob, dist, path_out, want_dist, want_path, workspace, _raw(stream))
 
 
-def mamba_tree_verify_fwd(p, q, tokens, u_accept, u_sample, tree, out=None, count=None, node=None, stream=None):
+def mamba_tree_verify_workspace_bytes(n_seq) -> int:
+    return int(lib.mamba_tree_verify_workspace_bytes(n_seq))
+
+
+def mamba_tree_verify_fwd(p, q, tokens, u_accept, u_sample, tree, out=None, count=None, node=None, workspace=None, stream=None):
     """Verification of drafted trees (N_1..N_gamma): p (S,nodes,V), q (S,inner nodes,V) f32, tokens int32 and u_accept f32 (S,nodes-1) position
     by position, u_sample f32 (S) -> out int32 (S,gamma+1): the accepted tokens and the drawn one, then -1, count int32 (S), node int32
     (S,gamma): rows of the accepted tokens in their positions, then -1."""
-    return _sample.tree_verify_fwd(p, q, tokens, u_accept, u_sample, tuple(tree), out, count, node, _raw(stream))
+    if stream is not None and workspace is None:
+        workspace = _scratch(mamba_tree_verify_workspace_bytes(p.shape[0]), p.device, stream)
+    return _sample.tree_verify_fwd(p, q, tokens, u_accept, u_sample, tuple(tree), out, count, node, workspace, _raw(stream))
 
 
 def mamba_linear_adapted_workspace_bytes(M, rank) -> int:

@@ -1175,9 +1175,14 @@ int mamba_sample_fwd(const void *logits, const mamba_sampling_t *s, const float 
     return (int)launch_sample(logits, workspace, a, (int)io, static_cast<hipStream_t>(hip_stream));
 }
 
+size_t mamba_tree_verify_workspace_bytes(int64_t n_seq)
+{
+    return n_seq > 0 && verify_fits(n_seq, 1) ? verify_workspace_bytes(n_seq) : 0;
+}
+
 int mamba_tree_verify_fwd(const float *p, const float *q, const int32_t *tokens, const float *u_accept, const float *u_sample,
-                          int32_t *out, int32_t *count, int32_t *node, const int32_t *tree, int gamma, int64_t n_seq, int64_t V,
-                          void *hip_stream)
+                          int32_t *out, int32_t *count, int32_t *node, void *workspace, size_t workspace_bytes, const int32_t *tree,
+                          int gamma, int64_t n_seq, int64_t V, void *hip_stream)
 {
     static_assert(kMaxDepth == MAMBA_MAX_DEPTH, "a tree fits");
     if (!tree) return MAMBA_ERR_NULL_POINTER;
@@ -1197,22 +1202,24 @@ int mamba_tree_verify_fwd(const float *p, const float *q, const int32_t *tokens,
     if (!size3(n_seq, a.nodes, V, 4, &pb) || !size3(n_seq, a.inner, V, 4, &qb) || !size3(n_seq, a.nodes - 1, 1, 4, &tb) ||
         !size3(n_seq, gamma + 1, 1, 4, &ob))
         return MAMBA_ERR_BAD_SHAPE;
-    if (n_seq >= (1 << 22) || V > kMaxVocabulary) return MAMBA_ERR_UNSUPPORTED;
+    if (V > kMaxVocabulary || (V > 0 && !verify_fits(n_seq, V))) return MAMBA_ERR_UNSUPPORTED;
     if (n_seq == 0) return MAMBA_OK;
     if (V == 0) return MAMBA_ERR_BAD_SHAPE;
     if (!p || !q || !tokens || !u_accept || !u_sample || !out || !count || !node) return MAMBA_ERR_NULL_POINTER;
     if (!aligned16(tokens) || !aligned16(u_accept) || !aligned16(u_sample) || !aligned16(out) || !aligned16(count) || !aligned16(node) ||
-        (reinterpret_cast<uintptr_t>(p) & 3u) || (reinterpret_cast<uintptr_t>(q) & 3u))
+        !aligned16(workspace) || (reinterpret_cast<uintptr_t>(p) & 3u) || (reinterpret_cast<uintptr_t>(q) & 3u))
         return MAMBA_ERR_MISALIGNED;
+    const size_t need = verify_workspace_bytes(n_seq);
+    if (!workspace || workspace_bytes < need) return MAMBA_ERR_WORKSPACE;
     const Span in[5] = {{p, pb}, {q, qb}, {tokens, tb}, {u_accept, tb}, {u_sample, n_seq * 4}};
-    const Span outs[3] = {{out, ob}, {count, n_seq * 4}, {node, n_seq * gamma * 4}};
-    for (int i = 0; i < 3; ++i) {
+    const Span outs[4] = {{out, ob}, {count, n_seq * 4}, {node, n_seq * gamma * 4}, {workspace, (int64_t)need}};
+    for (int i = 0; i < 4; ++i) {
         for (const Span &r : in)
             if (overlap(outs[i].p, outs[i].n, r.p, r.n)) return MAMBA_ERR_ALIAS;
         for (int j = 0; j < i; ++j)
             if (overlap(outs[i].p, outs[i].n, outs[j].p, outs[j].n)) return MAMBA_ERR_ALIAS;
     }
-    return (int)launch_verify(a, static_cast<hipStream_t>(hip_stream));
+    return (int)launch_verify(a, workspace, static_cast<hipStream_t>(hip_stream));
 }
 
 int mamba_tree_plan(const int32_t *tree, int gamma, int64_t n_layers, int64_t D, int64_t N, int K,

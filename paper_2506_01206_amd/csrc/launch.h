@@ -295,6 +295,8 @@ struct VerifyArgs {
     int gamma;
     int32_t tree[kMaxDepth];
 };
-hipError_t launch_verify(const VerifyArgs &a, hipStream_t stream);
+bool verify_fits(int64_t n_seq, int64_t V);   // V > 0
+size_t verify_workspace_bytes(int64_t n_seq);
+hipError_t launch_verify(const VerifyArgs &a, void *ws, hipStream_t stream);
 
 }  // namespace mamba

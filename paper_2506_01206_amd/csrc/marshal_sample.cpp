@@ -8,6 +8,7 @@ namespace {
 struct Api {
     decltype(&::mamba_sample_workspace_bytes) sample_workspace_bytes;
     decltype(&::mamba_sample_fwd) sample_fwd;
+    decltype(&::mamba_tree_verify_workspace_bytes) tree_verify_workspace_bytes;
     decltype(&::mamba_tree_verify_fwd) tree_verify_fwd;
     decltype(&::mamba_linear_adapted_workspace_bytes) linear_adapted_workspace_bytes;
     decltype(&::mamba_linear_adapted_fwd) linear_adapted_fwd;
@@ -80,9 +81,10 @@ PyObject *tree_verify_fwd(Args a)
     const float *ua = fptr(u_accept, {S, nodes - 1}, "u_accept"), *us = fptr(u_sample, {S}, "u_sample");
     int32_t *op = const_cast<int32_t *>(ints(out.object, {S, gamma + 1}, "out")), *cp = const_cast<int32_t *>(ints(count.object, {S}, "count")),
             *np = const_cast<int32_t *>(ints(node.object, {S, gamma}, "node"));
-    on_current_device({p, q, tokens, u_accept, u_sample, out.object, count.object, node.object});
-    Call{"mamba_tree_verify_fwd", api.tree_verify_fwd, pp, qp, tp, ua, us, op, cp, np, static_cast<const int32_t *>(fan), (int)gamma, S, V,
-         stream_of(a[9])};
+    const Workspace ws(a[9], api.tree_verify_workspace_bytes(S), pt);
+    on_current_device({p, q, tokens, u_accept, u_sample, out.object, count.object, node.object, a[9]});
+    Call{"mamba_tree_verify_fwd", api.tree_verify_fwd, pp, qp, tp, ua, us, op, cp, np, ws.data, ws.bytes, static_cast<const int32_t *>(fan), (int)gamma, S, V,
+         stream_of(a[10])};
     return result({out.object, count.object, node.object});
 }
 
@@ -119,7 +121,7 @@ PyObject *bind(PyObject *, Args args, Py_ssize_t n) { return bind_to<Api, &api>(
 
 PyMethodDef methods[] = {
     {"bind", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&bind)), METH_FASTCALL, nullptr},
-    MAMBA_ENTRY(sample_fwd, 14), MAMBA_ENTRY(tree_verify_fwd, 10), MAMBA_ENTRY(linear_adapted_fwd, 17), {nullptr, nullptr, 0, nullptr}};
+    MAMBA_ENTRY(sample_fwd, 14), MAMBA_ENTRY(tree_verify_fwd, 11), MAMBA_ENTRY(linear_adapted_fwd, 17), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal._sample", "argument marshalling of drawn children, verification and adapted projections", -1,
                       methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -174,13 +174,14 @@ def test_rounds_of_several_requests_with_the_operators_themselves():
     idx, prob = torch.empty(S, n, dtype=torch.int32, device=DEV), torch.empty(S, n, device=DEV)
     ws1 = torch.empty(m.mamba_linear_adapted_workspace_bytes(S, R), dtype=torch.uint8, device=DEV)
     ws2 = torch.empty(m.mamba_sample_workspace_bytes(S, V, n), dtype=torch.uint8, device=DEV)
+    ws3 = torch.empty(m.mamba_tree_verify_workspace_bytes(S), dtype=torch.uint8, device=DEV)
     outs = [torch.empty(S, 2, dtype=torch.int32, device=DEV), torch.empty(S, dtype=torch.int32, device=DEV), torch.empty(S, 1, dtype=torch.int32, device=DEV)]
 
     def chain():
         m.mamba_linear_adapted_fwd(hidden, head, a, b, adapter, outs=[logits], workspace=ws1)
         m.mamba_logits_constrain_fwd(logits, counts=counts, penalties=pen, out=logits)
         m.mamba_sample_fwd(logits, u, par, top_k=top_k, idx=idx, prob=prob, dist=q.view(S, V), workspace=ws2)
-        m.mamba_tree_verify_fwd(target, q, idx, ua, us, (n,), out=outs[0], count=outs[1], node=outs[2])
+        m.mamba_tree_verify_fwd(target, q, idx, ua, us, (n,), out=outs[0], count=outs[1], node=outs[2], workspace=ws3)
     chain()
     g = torch.cuda.CUDAGraph()
     with torch.cuda.graph(g):

@@ -71,9 +71,9 @@ def m():
     return binding
 
 
-def call(m, p=P(0), q=P(1), tokens=P(2), ua=P(3), us=P(4), out=P(5), count=P(6), node=P(7), tree=(3, 2), gamma=None, S=4, V=100):
+def call(m, p=P(0), q=P(1), tokens=P(2), ua=P(3), us=P(4), out=P(5), count=P(6), node=P(7), ws=P(8), ws_bytes=1 << 39, tree=(3, 2), gamma=None, S=4, V=100):
     arr = None if tree is None else (ctypes.c_int32 * max(len(tree), 1))(*tree)
-    return m.lib.mamba_tree_verify_fwd(p, q, tokens, ua, us, out, count, node, arr, (len(tree) if tree else 1) if gamma is None else gamma, S, V, None)
+    return m.lib.mamba_tree_verify_fwd(p, q, tokens, ua, us, out, count, node, ws, ws_bytes, arr, (len(tree) if tree else 1) if gamma is None else gamma, S, V, None)
 
 
 def test_refusals(m):
@@ -82,12 +82,15 @@ def test_refusals(m):
         assert call(m, **{name: None}) == S["NULL_POINTER"], name
         assert call(m, **{name: P(9) + 2}) == S["MISALIGNED"], name
     assert call(m, tree=None) == S["NULL_POINTER"]
+    assert call(m, ws=P(9) + 8) == S["MISALIGNED"] and call(m, ws=None) == S["WORKSPACE"]
+    assert call(m, ws_bytes=m.mamba_tree_verify_workspace_bytes(4) - 1) == S["WORKSPACE"]
+    assert m.mamba_tree_verify_workspace_bytes(0) == 0 and m.mamba_tree_verify_workspace_bytes(-1) == 0 and m.mamba_tree_verify_workspace_bytes(1 << 40) == 0
     for bad in (dict(gamma=0), dict(tree=(1,) * 17), dict(tree=(3, 0)), dict(tree=(-1,)), dict(S=-1), dict(V=-1), dict(V=0), dict(S=1 << 21, V=1 << 40)):
         assert call(m, **bad) == S["BAD_SHAPE"], bad
-    for bad in (dict(tree=(9,)), dict(tree=(8,) * 6), dict(S=1 << 22), dict(V=(1 << 25) + 1)):
+    for bad in (dict(tree=(9,)), dict(tree=(8,) * 6), dict(S=1 << 24), dict(S=1 << 20, V=50000), dict(V=(1 << 25) + 1)):
         assert call(m, **bad) == S["UNSUPPORTED"], bad
     assert call(m, S=0) == S["OK"]
-    for a, b in (("out", 2), ("count", 0), ("node", 4), ("count", 5), ("node", 6)):
+    for a, b in (("out", 2), ("count", 0), ("node", 4), ("count", 5), ("node", 6), ("ws", 0), ("ws", 5), ("node", 8)):
         assert call(m, **{a: P(b)}) == S["ALIAS"], (a, b)
 
 
@@ -132,6 +135,23 @@ def test_large_vocabularies(m):
     rng = np.random.default_rng(9)
     check(m, some_trees(rng, 2, 50280, (3, 2), 2.0))
     check(m, some_trees(rng, 3, 131071, (1, 1), 0.7))
+    check(m, some_trees(rng, 1, 700001, (2,), 1.0))              # pieces of more than one trip
+
+
+@gpu
+def test_more_rejections_than_rounds(m):
+    """Children that the target does not want, fifteen of them on one way."""
+    rng = np.random.default_rng(15)
+    for tree in ((8, 8, 2), (5, 5, 5)):
+        c = some_trees(rng, 4, 400, tree, 0.5)
+        rows = oracle.tree_rows(tree)
+        u = np.ones(c["u_accept"].shape, np.float32) - np.float32(2.0 ** -24)
+        first = 0
+        for r, n in zip(rows, tree):                             # the last child of every node is taken, where its ratio is above zero
+            u[:, first + n - 1:first + r * n:n] = 0.0
+            first += r * n
+        check(m, {**c, "u_accept": u})
+        check(m, {**c, "u_accept": np.full_like(u, 1 - 2.0 ** -24)})
 
 
 @gpu
@@ -188,7 +208,8 @@ def test_streams_graphs_and_given_outputs(m):
     got = m.mamba_tree_verify_fwd(**c, stream=side)
     torch.cuda.current_stream().wait_stream(side)
     outs = [torch.full((t.shape[0] + 1,) + t.shape[1:], -9, dtype=torch.int32, device=DEV) for t in ref]
-    one = lambda: m.mamba_tree_verify_fwd(**c, out=outs[0][:7], count=outs[1][:7], node=outs[2][:7])
+    ws = torch.empty(m.mamba_tree_verify_workspace_bytes(7), dtype=torch.uint8, device=DEV)
+    one = lambda: m.mamba_tree_verify_fwd(**c, out=outs[0][:7], count=outs[1][:7], node=outs[2][:7], workspace=ws)
     one()
     g = torch.cuda.CUDAGraph()
     with torch.cuda.graph(g):
@@ -196,6 +217,7 @@ def test_streams_graphs_and_given_outputs(m):
     for _ in range(3):
         for t in outs:
             t.fill_(-9)
+        ws.fill_(255)
         g.replay()
         torch.cuda.synchronize()
         for a, b, o in zip(ref, got, outs):
