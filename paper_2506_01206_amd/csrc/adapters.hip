@@ -12,15 +12,8 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4v __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kThreads = 256, kWaves = 4;
 constexpr int kLine = 128;                                           // 64 k of a row in LDS
 
-__device__ __forceinline__ int32_t wave_min(int32_t v)
-{
-#pragma unroll
-    for (int d = 32; d; d >>= 1) v = min(v, __shfl_xor(v, d));
-    return v;
-}
 // 16 bytes a lane from an address of its own into LDS at lds_addr + 16 lane (see linear.hip: the waits for them are explicit)
 __device__ __forceinline__ void load_to_lds16(const void *from, uint32_t lds_addr)
 {
@@ -33,18 +26,19 @@ __device__ __forceinline__ void lds_barrier()
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
-// A workgroup has 16 G rows and all ranks (RT tiles of 16) of one adapter: of those that its rows have, smallest first, every gridDim.y-th from the
+// A workgroup has 16 G rows and all ranks (RT tiles of 16) of one adapter: of those that its rows have, in the rows' order, every gridDim.y-th from the
 // blockIdx.y-th on, so that rows of many adapters are not multiplied by one after the other.  A row's sums are written by who has its adapter.
-// G of the wavefronts' four quarters go by rows, the others by k: slabs of 64 k (128 where all four go by k), four stages of them in LDS, straight from
-// memory, a row's 16-byte slot c at c ^ (row / 2 & 7).
+// Of the W wavefronts G go by rows, W / G by k: slabs of 64 or 128 k, or as many as give each of those 32, four of them in LDS, straight from memory, a
+// row's 16-byte slot c at c ^ (row / 2 & 7).
 // Bound by x from memory where there are many rows, by trips to memory where there are few.
-template <int RT, int G>
-__global__ void __launch_bounds__(kThreads)
+template <int RT, int G, int W>
+__global__ void __launch_bounds__(64 * W)
 down_kernel(const bf16_t *__restrict__ x, const bf16_t *__restrict__ a, const float *__restrict__ scale, const int32_t *__restrict__ idx,
             bf16_t *__restrict__ t, uint32_t *__restrict__ zeros, int64_t M, int K, int rank, int adapters)
 {
-    constexpr int BM = 16 * G, BN = 16 * RT, S = kWaves / G, kBlocks = S == 4 ? 2 : 1, kStep = 64 * kBlocks;   // blocks of 64 k to a slab
-    constexpr int kStages = 4, kStage = (BM + BN) * kLine * kBlocks;
+    constexpr int kWaves = W, kThreads = 64 * W, kStages = 4;
+    constexpr int BM = 16 * G, BN = 16 * RT, S = W / G, kBlocks = S > 4 ? S / 2 : RT < 8 || S > 2 ? 2 : 1, kStep = 64 * kBlocks;   // blocks of 64 k to a slab
+    constexpr int kStage = (BM + BN) * kLine * kBlocks;
     constexpr int kGroups = (BM + BN) / 8 * kBlocks, NL = (kGroups + kWaves - 1) / kWaves;   // loads of 8 rows, and of a wavefront
     constexpr int kPart = S * BM * BN * 4;
     __shared__ __attribute__((aligned(1024))) unsigned char lds[kStages * kStage > kPart ? kStages * kStage : kPart];
@@ -53,11 +47,12 @@ down_kernel(const bf16_t *__restrict__ x, const bf16_t *__restrict__ a, const fl
     const int64_t m0 = (int64_t)blockIdx.x * BM;
     if (blockIdx.x == 0 && blockIdx.y == 0 && tid < 32) zeros[tid] = 0;
     const int32_t id = lane < BM && m0 + lane < M ? idx[m0 + lane] : -1;
-    auto next = [&](int32_t last) { return wave_min(id > last && id < adapters ? id : adapters); };
     const uint32_t lds0 = (uint32_t)(size_t)(__attribute__((address_space(3))) unsigned char *)lds;
     const int slabs = (K + kStep - 1) / kStep, chunks = K / 8;
     int turn = 0;
-    for (int32_t cur = next(-1); cur < adapters; cur = next(cur), ++turn) {
+    for (uint64_t left = __ballot(id >= 0 && id < adapters); left; ++turn) {
+        const int32_t cur = __builtin_amdgcn_readlane(id, __builtin_ctzll(left));
+        left &= ~__ballot(id == cur);
         if (turn % (int)gridDim.y != (int)blockIdx.y) continue;
         // what this lane brings: of load i rows 8 g .. 8 g + 7 of a block, x's first
         const bf16_t *row[NL];
@@ -79,9 +74,9 @@ down_kernel(const bf16_t *__restrict__ x, const bf16_t *__restrict__ a, const fl
         };
         // until no more than the loads of `slabs_under_way` slabs are under way (vmcnt is split over bits 3:0 and 15:14)
         auto wait_for = [&](int slabs_under_way) __attribute__((always_inline)) {
-            static_assert(2 * NL < 64, "fits the counter");
+            static_assert((kStages - 2) * NL < 64 && kStages == 4, "fits the counter");
             if (slabs_under_way >= 2) __builtin_amdgcn_s_waitcnt(0x0F70 | ((2 * NL) & 15) | (((2 * NL) >> 4) << 14));
-            else if (slabs_under_way == 1) __builtin_amdgcn_s_waitcnt(0x0F70 | (NL & 15) | ((NL >> 4) << 14));
+            else if (slabs_under_way >= 1) __builtin_amdgcn_s_waitcnt(0x0F70 | (NL & 15) | ((NL >> 4) << 14));
             else __builtin_amdgcn_s_waitcnt(0x0F70);
         };
         f32x4v d[RT];
@@ -99,10 +94,8 @@ down_kernel(const bf16_t *__restrict__ x, const bf16_t *__restrict__ a, const fl
             if (s + kStages - 1 < slabs) request(s + kStages - 1, (stage + kStages - 1) % kStages);
             const unsigned char *from = lds + stage * kStage;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {                            // steps of 32 k
-                const int step = S == 1 ? h : S == 2 ? split : split & 1, block = S == 4 ? split >> 1 : 0;
-                if (S > 1 && h > 0) break;
-                const int c = 4 * step + lg;
+            for (int h = 0; h < 2 * kBlocks / S; ++h) {              // steps of 32 k
+                const int block = (split + S * h) >> 1, c = 4 * ((split + S * h) & 1) + lg;
                 const bool in = s * (kStep / 8) + 8 * block + c < chunks;
                 auto fragment = [&](int r) __attribute__((always_inline)) {
                     const u32x4 v = *reinterpret_cast<const u32x4 *>(from + (block * (BM + BN) + r) * kLine + ((c ^ (r >> 1 & 7)) << 4));
@@ -148,19 +141,12 @@ down_kernel(const bf16_t *__restrict__ x, const bf16_t *__restrict__ a, const fl
     }
 }
 
-template <int G> hipError_t launch(const bf16_t *x, const AdapterArgs &l, int64_t M, int64_t K, hipStream_t stream)
+template <int RT, int G, int W> hipError_t launch(const bf16_t *x, const AdapterArgs &l, int64_t M, int64_t K, hipStream_t stream)
 {
-    const bf16_t *a = static_cast<const bf16_t *>(l.a);
     const int64_t most = M <= 64 ? 16 : 4;                           // adapters of a workgroup's rows at once
     const dim3 grid((unsigned)((M + 16 * G - 1) / (16 * G)), (unsigned)(l.adapters < most ? l.adapters : most));
-#define MAMBA_DOWN(RT)                                                                                                            \
-    down_kernel<RT, G><<<grid, kThreads, 0, stream>>>(x, a, l.scale, l.idx, static_cast<bf16_t *>(l.t), static_cast<uint32_t *>(l.zeros), M, (int)K, \
-                                                      (int)l.rank, (int)l.adapters)
-    if (l.rank <= 16) MAMBA_DOWN(1);
-    else if (l.rank <= 32) MAMBA_DOWN(2);
-    else if (l.rank <= 64) MAMBA_DOWN(4);
-    else MAMBA_DOWN(8);
-#undef MAMBA_DOWN
+    down_kernel<RT, G, W><<<grid, 64 * W, 0, stream>>>(x, static_cast<const bf16_t *>(l.a), l.scale, l.idx, static_cast<bf16_t *>(l.t),
+                                                       static_cast<uint32_t *>(l.zeros), M, (int)K, (int)l.rank, (int)l.adapters);
     return hipGetLastError();
 }
 
@@ -169,9 +155,18 @@ template <int G> hipError_t launch(const bf16_t *x, const AdapterArgs &l, int64_
 hipError_t launch_adapters_down(const void *x, const AdapterArgs &l, int64_t M, int64_t K, hipStream_t stream)
 {
     const bf16_t *xp = static_cast<const bf16_t *>(x);
-    if (M >= 12288) return launch<4>(xp, l, M, K, stream);
-    if (M >= 6144) return launch<2>(xp, l, M, K, stream);
-    return launch<1>(xp, l, M, K, stream);
+#define MAMBA_DOWN(G, W)                                                \
+    do {                                                                \
+        if (l.rank <= 16) return launch<1, G, W>(xp, l, M, K, stream);  \
+        if (l.rank <= 32) return launch<2, G, W>(xp, l, M, K, stream);  \
+        if (l.rank <= 64) return launch<4, G, W>(xp, l, M, K, stream);  \
+        return launch<8, G, 4>(xp, l, M, K, stream);                    \
+    } while (0)
+    if (M >= 12288) MAMBA_DOWN(4, 4);
+    if (M >= 6144) MAMBA_DOWN(2, 4);
+    if (M > 64) MAMBA_DOWN(1, 4);
+    MAMBA_DOWN(1, 8);
+#undef MAMBA_DOWN
 }
 
 }  // namespace mamba

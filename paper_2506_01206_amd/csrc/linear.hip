@@ -65,7 +65,7 @@ __device__ __forceinline__ int locate(const OutSplit &o, int64_t n, int64_t *col
 // product with the adapter's first matrix (adapters.hip), which is there as two bfloat16 terms side by side, high and low: 16 bits, so that it is
 // not the rounding of t that the output's rounding is lost in.  The kernels below take an AdapterTail behind their other arguments, or
 // nothing: then they are the plain products, instruction for instruction.
-// The adapters of a tile's rows are gone through, smallest first; a row takes the sums of its own.  (Sums of the others are dropped, or added as zeros
+// The adapters of a tile's rows are gone through, in the rows' order; a row takes the sums of its own.  (Sums of the others are dropped, or added as zeros
 // where that is what they are: an adapter's infinities and NaN stay with its rows.)
 struct AdapterTail {
     const bf16_t *t;                 // (M, 2 rank): high terms, low terms
@@ -75,23 +75,46 @@ struct AdapterTail {
     int32_t rank, adapters;          // rank: a multiple of 8
 };
 
-__device__ __forceinline__ int32_t wave_min(int32_t v)
-{
-#pragma unroll
-    for (int d = 32; d; d >>= 1) v = min(v, __shfl_xor(v, d));
-    return v;
-}
-// the adapter of row m (-1 behind the end), and the smallest one above `last` that any row of the wavefront has (the number of adapters: none)
+// the adapter of row m (-1 behind the end)
 __device__ __forceinline__ int32_t adapter_of(const AdapterTail &t, int64_t m, int64_t M) { return m < M ? t.idx[m] : -1; }
-template <int MT> __device__ __forceinline__ int32_t next_adapter(const int32_t (&id)[MT], int32_t last, int32_t adapters)
-{
-    int32_t v = adapters;
+// The adapters that a wavefront's rows have, 64 of them to a register, in the order in which they first come; behind the last: `adapters`.
+template <int R> struct InTurn {
+    uint64_t left[R];
+    __device__ __forceinline__ void begin(const int32_t (&id)[R], int32_t adapters)
+    {
 #pragma unroll
-    for (int a = 0; a < MT; ++a) v = id[a] > last ? min(v, id[a]) : v;
-    return wave_min(v);
+        for (int i = 0; i < R; ++i) left[i] = __ballot(id[i] >= 0 && id[i] < adapters);
+    }
+    __device__ __forceinline__ int32_t next(const int32_t (&id)[R], int32_t adapters)
+    {
+        int32_t cur = adapters;
+#pragma unroll
+        for (int i = R - 1; i >= 0; --i) cur = left[i] ? __builtin_amdgcn_readlane(id[i], __builtin_ctzll(left[i])) : cur;
+#pragma unroll
+        for (int i = 0; i < R; ++i) left[i] &= ~__ballot(id[i] == cur);
+        return cur;
+    }
+};
+
+// Eight bfloat16 with zeros for what is no finite number; whether there was any.
+__device__ __forceinline__ bool only_finite(bf16x8 &v)
+{
+    u32x4 u = __builtin_bit_cast(u32x4, v);
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const bool low = (u[i] & 0x7f80u) == 0x7f80u, high = (u[i] & 0x7f800000u) == 0x7f800000u;
+        odd |= low || high;
+        u[i] &= (low ? 0u : 0xffffu) | (high ? 0u : 0xffff0000u);
+    }
+    v = __builtin_bit_cast(bf16x8, u);
+    return odd;
 }
 
-// 32 x 32 tiles from row m0 and column n0 on, acc[a][b] with its columns in the lanes (linear_kernel), fragments straight from memory.
+// 32 x 32 tiles from row m0 and column n0 on, acc[a][b] with its columns in the lanes (linear_kernel), fragments straight from memory: four steps of
+// 16 k, of whichever adapters, on their way at a time.  A row's terms are zeros in another adapter's steps.  Zero times an infinity is no zero: where B
+// has what is no finite number, zeros stand in for it, and two more products, of the largest number by itself and by its negative, make the outputs of its
+// column NaN in the adapter's own rows.
 template <int MT, int NT>
 __device__ __forceinline__ void add_adapters(f32x16 (&acc)[MT][NT], const AdapterTail &t, int64_t m0, int64_t M, int64_t n0, int64_t N)
 {
@@ -99,45 +122,77 @@ __device__ __forceinline__ void add_adapters(f32x16 (&acc)[MT][NT], const Adapte
     int32_t id[MT];
 #pragma unroll
     for (int a = 0; a < MT; ++a) id[a] = adapter_of(t, m0 + a * 32 + (lane & 31), M);
-    auto row_id = [&](int a, int i) __attribute__((always_inline)) { return __shfl(id[a], 8 * (i / 4) + 4 * (lane >> 5) + (i & 3)); };
-    for (int32_t cur = next_adapter(id, -1, t.adapters); cur < t.adapters; cur = next_adapter(id, cur, t.adapters)) {
-        const bf16_t *b[NT];
+    const bf16_t *row[MT];
 #pragma unroll
-        for (int j = 0; j < NT; ++j) b[j] = t.b + ((int64_t)cur * N + min(n0 + j * 32 + (lane & 31), N - 1)) * t.rank;
+    for (int a = 0; a < MT; ++a) row[a] = t.t + min(m0 + a * 32 + (lane & 31), M - 1) * (2 * t.rank) + 8 * (lane >> 5);
+    int64_t column[NT];
 #pragma unroll
-        for (int a = 0; a < MT; ++a) {
-            if (!__any(id[a] == cur)) continue;
-            const bf16_t *row = t.t + min(m0 + a * 32 + (lane & 31), M - 1) * (2 * t.rank);
-            f32x16 d[NT];
+    for (int j = 0; j < NT; ++j) column[j] = min(n0 + j * 32 + (lane & 31), N - 1) * t.rank;
+    struct Step {
+        int32_t of;
+        bf16x8 xf[MT], wf[NT];
+    } step[4];
+    InTurn<MT> turn;
+    turn.begin(id, t.adapters);
+    int32_t ahead = turn.next(id, t.adapters);
+    int c = 0;
+    auto request = [&](Step &f) __attribute__((always_inline)) {
+        f.of = ahead;
+        const int32_t of = ahead < t.adapters ? ahead : 0;            // (behind the last adapter: something, of no row)
+        const int mine = c + (lane >> 5), cb = mine < chunks ? mine : mine - chunks;
 #pragma unroll
-            for (int j = 0; j < NT; ++j)
+        for (int a = 0; a < MT; ++a) f.xf[a] = *reinterpret_cast<const bf16x8 *>(row[a] + 8 * c);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) d[j][i] = 0.0f;
-            for (int c = lane >> 5; c < 2 * chunks; c += 2) {
-                const bf16x8 xf = *reinterpret_cast<const bf16x8 *>(row + 8 * c);
-                const int cb = c < chunks ? c : c - chunks;
+        for (int j = 0; j < NT; ++j) f.wf[j] = *reinterpret_cast<const bf16x8 *>(t.b + (int64_t)of * N * t.rank + column[j] + 8 * cb);
+        c += 2;
+        if (c >= 2 * chunks) c = 0, ahead = turn.next(id, t.adapters);
+    };
+    if (ahead < t.adapters) {
 #pragma unroll
-                for (int j = 0; j < NT; ++j)
-                    d[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xf, *reinterpret_cast<const bf16x8 *>(b[j] + 8 * cb), d[j], 0, 0, 0);
-            }
+        for (int q = 0; q < 4; ++q) request(step[q]);
+#pragma unroll 1
+        while (step[0].of < t.adapters) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const bool mine = row_id(a, i) == cur;
+            for (int q = 0; q < 4; ++q) {
+                Step &f = step[q];
+                bool odd[NT];
 #pragma unroll
-                for (int j = 0; j < NT; ++j) acc[a][j][i] += mine ? d[j][i] : 0.0f;
+                for (int j = 0; j < NT; ++j) odd[j] = only_finite(f.wf[j]);
+#pragma unroll
+                for (int a = 0; a < MT; ++a) {
+                    const u32x4 raw = __builtin_bit_cast(u32x4, f.xf[a]);
+                    f.xf[a] = __builtin_bit_cast(bf16x8, id[a] == f.of ? raw : u32x4(0u));
+#pragma unroll
+                    for (int j = 0; j < NT; ++j) acc[a][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.xf[a], f.wf[j], acc[a][j], 0, 0, 0);
+                }
+#pragma unroll
+                for (int j = 0; j < NT; ++j) {
+                    if (!__any(odd[j])) continue;
+                    const uint64_t columns = __ballot(odd[j]);        // (one k, in the lower half of the lanes)
+                    const bool column = lane < 32 && ((columns | columns >> 32) >> lane & 1);
+                    const bf16x8 plus = __builtin_bit_cast(bf16x8, u32x4{column ? 0x7f7fu : 0u, 0u, 0u, 0u});
+                    const bf16x8 minus = __builtin_bit_cast(bf16x8, u32x4{column ? 0xff7fu : 0u, 0u, 0u, 0u});
+#pragma unroll
+                    for (int a = 0; a < MT; ++a) {
+                        const bf16x8 own = __builtin_bit_cast(bf16x8, u32x4{lane < 32 && id[a] == f.of ? 0x7f7fu : 0u, 0u, 0u, 0u});
+                        acc[a][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(own, plus, acc[a][j], 0, 0, 0);
+                        acc[a][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(own, minus, acc[a][j], 0, 0, 0);
+                    }
+                }
+                request(f);
             }
         }
     }
+    auto bit = [&](uint64_t rows, int i) __attribute__((always_inline)) { return rows >> (8 * (i / 4) + 4 * (lane >> 5) + (i & 3)) & 1; };
     // a row whose index is out of range: NaN
 #pragma unroll
     for (int a = 0; a < MT; ++a) {
-        if (!__any(id[a] < -1 || id[a] >= t.adapters)) continue;
+        const uint64_t rows = __ballot(id[a] < -1 || id[a] >= t.adapters);
+        if (!rows) continue;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int32_t r = row_id(a, i);
+        for (int i = 0; i < 16; ++i)
 #pragma unroll
-            for (int j = 0; j < NT; ++j) acc[a][j][i] = r < -1 || r >= t.adapters ? __int_as_float(0x7fc00000) : acc[a][j][i];
-        }
+            for (int j = 0; j < NT; ++j) acc[a][j][i] = bit(rows, i) ? __int_as_float(0x7fc00000) : acc[a][j][i];
     }
 }
 
@@ -431,125 +486,135 @@ __device__ __forceinline__ void load_to_lds16(const char *base, uint32_t lane_of
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_addr), "v"(lane_off), "s"(base) : "memory");
 }
 
+constexpr int kSlabRow = kWideRow;
+
 // the same from an address of each lane's own
 __device__ __forceinline__ void load_to_lds16(const void *from, uint32_t lds_addr)
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_addr), "v"(from) : "memory");
 }
 
-// Eight bfloat16 with zeros for what is no finite number; whether there was any.
-__device__ __forceinline__ bool only_finite(bf16x8 &v)
-{
-    u32x4 u = __builtin_bit_cast(u32x4, v);
-    bool odd = false;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const bool low = (u[i] & 0x7f80u) == 0x7f80u, high = (u[i] & 0x7f800000u) == 0x7f800000u;
-        odd |= low || high;
-        u[i] &= (low ? 0u : 0xffffu) | (high ? 0u : 0xffff0000u);
-    }
-    v = __builtin_bit_cast(bf16x8, u);
-    return odd;
-}
-
 // Adapters of the tiles of linear_wide_kernel and linear_ring_kernel: more slabs of 64 k behind the product's own, an adapter's two terms of t against
 // its B twice.  Rows that are not the adapter's read a line of zeros, and so does what is behind the rank.  Zero times an infinity is no zero: where
 // B has what is no finite number, zeros stand in for it, and two more products, of the largest number by itself and by its negative, make the outputs of
-// its column NaN in the adapter's own rows.  Two stages in turn, the next slab's loads under way while one is multiplied.  Uses the first two stages
-// and leaves them free; all wavefronts come and go together.
-template <int BM, int BN, int WM, int WN, int kRow, int MT, int NT>
-__device__ __forceinline__ void add_adapter_slabs(f32x16 (&acc)[MT][NT], const AdapterTail &t, unsigned char *lds, int64_t m0, int64_t n0, int64_t N,
-                                                  const int (&frag_x)[4], const int (&frag_w)[4])
-{
-    constexpr int NW = WM * WN, kStage = (BM + BN) * kRow, NLX = BM / 8 / NW;
-    const int lane = threadIdx.x & 63;
-    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wm = wave / WN;
-    const uint32_t lds0 = (uint32_t)(size_t)(__attribute__((address_space(3))) unsigned char *)lds;
-    const int chunks = t.rank >> 3, slabs = (2 * chunks + 7) / 8;
-    int32_t mine[(BM + 63) / 64], row_id[NLX];                        // of all rows, 64 to a register; of those that this lane brings
-    bool bad = false;
+// its column NaN in the adapter's own rows.  The stages are the product's first two, in turn; a slab is requested two ahead of its products.
+template <int BM, int BN, int WM, int WN> struct AdapterSlabs {
+    static constexpr int NW = WM * WN, kStage = (BM + BN) * kSlabRow, NLX = BM / 8 / NW, NLW = BN / 8 / NW, kIds = (BM + 63) / 64;
+    AdapterTail t;
+    int64_t m0, n0, N;
+    int32_t ids[kIds], row_id[NLX];                                   // the adapters of all rows, 64 to a register; of those that this lane brings
+    InTurn<kIds> turn;
+    int32_t now, next, ahead;                                         // adapters of the slab to be multiplied, the one behind it, the one to be requested
+    int slab;                                                         // which of its slabs that is
+
+    // (every wavefront has all rows' adapters, and so the same order of slabs)
+    __device__ __forceinline__ void begin(const AdapterTail &tail, int64_t row0, int64_t column0, int64_t columns)
+    {
+        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+        t = tail, m0 = row0, n0 = column0, N = columns;
 #pragma unroll
-    for (int i = 0; i < (BM + 63) / 64; ++i) {
-        mine[i] = i * 64 + lane < BM ? t.idx[m0 + i * 64 + lane] : -1;
-        bad |= mine[i] < -1 || mine[i] >= t.adapters;
+        for (int i = 0; i < kIds; ++i) ids[i] = i * 64 + lane < BM ? t.idx[m0 + i * 64 + lane] : -1;
+#pragma unroll
+        for (int i = 0; i < NLX; ++i) row_id[i] = t.idx[m0 + 8 * (NW * i + wave) + (lane >> 3)];
     }
-#pragma unroll
-    for (int i = 0; i < NLX; ++i) row_id[i] = t.idx[m0 + 8 * (NW * i + wave) + (lane >> 3)];
-    lds_barrier_linear();                                             // the stages are free
-    auto request = [&](int32_t cur, int slab, int stage) __attribute__((always_inline)) {
+    // (apart, so that the product's own first requests do not wait for the rows' adapters)
+    __device__ __forceinline__ void find_first()
+    {
+        turn.begin(ids, t.adapters);
+        now = next = t.adapters;
+        ahead = turn.next(ids, t.adapters);
+        slab = 0;
+    }
+    __device__ __forceinline__ void request(uint32_t lds0, int stage)
+    {
+        now = next, next = ahead;
+        if (ahead >= t.adapters) return;
+        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), chunks = t.rank >> 3;
         // a wavefront's rows 8 (NW i + wave) + lane / 8, the 16-byte slot lane % 8 of which is chunk (lane % 8) ^ (4 (wave & 1) + lane / 16) & 7
         const int c = 8 * slab + ((lane & 7) ^ ((4 * (wave & 1) + (lane >> 4)) & 7)), cb = c < chunks ? c : c - chunks;
         const bool in = c < 2 * chunks;
+        const bf16_t *zeros = t.zeros + 8 * (lane & 7);
 #pragma unroll
         for (int i = 0; i < NLX; ++i) {
             const int row = 8 * (NW * i + wave) + (lane >> 3);
-            const bf16_t *from = in && row_id[i] == cur ? t.t + (m0 + row) * (2 * t.rank) + 8 * c : t.zeros + 8 * (lane & 7);
-            load_to_lds16(from, lds0 + stage * kStage + wave * 1024 + i * (1024 * NW));
+            load_to_lds16(in && row_id[i] == ahead ? t.t + (m0 + row) * (2 * t.rank) + 8 * c : zeros, lds0 + stage * kStage + wave * 1024 + i * (1024 * NW));
         }
+        const bf16_t *b = t.b + ((int64_t)ahead * N + n0 + 8 * wave + (lane >> 3)) * t.rank + 8 * cb;
 #pragma unroll
-        for (int i = 0; i < BN / 8 / NW; ++i) {
-            const int row = 8 * (NW * i + wave) + (lane >> 3);
-            const bf16_t *from = in ? t.b + ((int64_t)cur * N + n0 + row) * t.rank + 8 * cb : t.zeros + 8 * (lane & 7);
-            load_to_lds16(from, lds0 + stage * kStage + BM * kRow + wave * 1024 + i * (1024 * NW));
-        }
-    };
-    int32_t cur = next_adapter(mine, -1, t.adapters);
-    int slab = 0, stage = 0;
-    if (cur < t.adapters) request(cur, 0, 0);
-    while (cur < t.adapters) {
-        const int32_t next = slab + 1 < slabs ? cur : next_adapter(mine, cur, t.adapters);
-        const int next_slab = slab + 1 < slabs ? slab + 1 : 0;
-        __builtin_amdgcn_s_waitcnt(0x0070);                           // this slab has landed (this wavefront's part), and the last one's reads are over
-        lds_barrier_linear();
-        if (next < t.adapters) request(next, next_slab, 1 - stage);
-        const unsigned char *from = lds + stage * kStage;
-        uint32_t odd = 0;                                             // columns (of block b in bit b) with what is no finite number
+        for (int i = 0; i < NLW; ++i)
+            load_to_lds16(in ? b + (int64_t)(8 * NW * i) * t.rank : zeros, lds0 + stage * kStage + BM * kSlabRow + wave * 1024 + i * (1024 * NW));
+        if (8 * ++slab >= 2 * chunks) slab = 0, ahead = turn.next(ids, t.adapters);
+    }
+    // All slabs, of which the first two have been requested, and what they overwrite been read.
+    template <int MT, int NT>
+    __device__ __forceinline__ void multiply(f32x16 (&acc)[MT][NT], const unsigned char *lds, uint32_t lds0, const int (&frag_x)[4], const int (&frag_w)[4])
+    {
+        const int lane = threadIdx.x & 63, wm = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) / WN;
+        int stage = 0;
+        bool bad = false;
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks) {
-            bf16x8 xf[MT], wf[NT];
+        for (int i = 0; i < kIds; ++i) bad |= ids[i] < -1 || ids[i] >= t.adapters;
+#pragma unroll 1
+        while (now < t.adapters) {
+            // until this slab has landed: no more under way than the next one's loads (vmcnt is split over bits 3:0 and 15:14)
+            constexpr int NL = NLX + NLW;
+            if (next < t.adapters) __builtin_amdgcn_s_waitcnt(0x0F70 | (NL & 15) | ((NL >> 4) << 14));
+            else __builtin_amdgcn_s_waitcnt(0x0F70);
+            lds_barrier_linear();
+            const unsigned char *from = lds + stage * kStage;
+            uint32_t odd = 0;                                         // columns (of block b in bit b) with what is no finite number
 #pragma unroll
-            for (int a = 0; a < MT; ++a) xf[a] = *reinterpret_cast<const bf16x8 *>(from + frag_x[ks] + a * 32 * kRow);
+            for (int ks = 0; ks < 4; ++ks) {
+                bf16x8 xf[MT], wf[NT];
 #pragma unroll
-            for (int b = 0; b < NT; ++b) {
-                wf[b] = *reinterpret_cast<const bf16x8 *>(from + frag_w[ks] + b * 32 * kRow);
-                odd |= (uint32_t)only_finite(wf[b]) << b;
-            }
-#pragma unroll
-            for (int a = 0; a < MT; ++a)
-#pragma unroll
-                for (int b = 0; b < NT; ++b) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wf[b], xf[a], acc[a][b], 0, 0, 0);
-        }
-        if (__any(odd != 0)) {
-            odd |= __shfl_xor(odd, 32);
-            // (one k, in the lower half of the lanes)
-#pragma unroll
-            for (int a = 0; a < MT; ++a) {
-                const bool own = lane < 32 && t.idx[m0 + wm * (BM / WM) + a * 32 + (lane & 31)] == cur;
-                const bf16x8 xf = __builtin_bit_cast(bf16x8, u32x4{own ? 0x7f7fu : 0u, 0u, 0u, 0u});
+                for (int a = 0; a < MT; ++a) xf[a] = *reinterpret_cast<const bf16x8 *>(from + frag_x[ks] + a * 32 * kSlabRow);
 #pragma unroll
                 for (int b = 0; b < NT; ++b) {
-                    const bool column = lane < 32 && (odd >> b & 1);
-                    const bf16x8 plus = __builtin_bit_cast(bf16x8, u32x4{column ? 0x7f7fu : 0u, 0u, 0u, 0u});
-                    const bf16x8 minus = __builtin_bit_cast(bf16x8, u32x4{column ? 0xff7fu : 0u, 0u, 0u, 0u});
-                    acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(plus, xf, acc[a][b], 0, 0, 0);
-                    acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(minus, xf, acc[a][b], 0, 0, 0);
+                    wf[b] = *reinterpret_cast<const bf16x8 *>(from + frag_w[ks] + b * 32 * kSlabRow);
+                    odd |= (uint32_t)only_finite(wf[b]) << b;
+                }
+#pragma unroll
+                for (int a = 0; a < MT; ++a)
+#pragma unroll
+                    for (int b = 0; b < NT; ++b) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wf[b], xf[a], acc[a][b], 0, 0, 0);
+            }
+            if (__any(odd != 0)) {
+                odd |= __shfl_xor(odd, 32);
+                // (one k, in the lower half of the lanes)
+#pragma unroll
+                for (int a = 0; a < MT; ++a) {
+                    const bool own = lane < 32 && t.idx[m0 + wm * (BM / WM) + a * 32 + (lane & 31)] == now;
+                    const bf16x8 xf = __builtin_bit_cast(bf16x8, u32x4{own ? 0x7f7fu : 0u, 0u, 0u, 0u});
+#pragma unroll
+                    for (int b = 0; b < NT; ++b) {
+                        const bool column = lane < 32 && (odd >> b & 1);
+                        const bf16x8 plus = __builtin_bit_cast(bf16x8, u32x4{column ? 0x7f7fu : 0u, 0u, 0u, 0u});
+                        const bf16x8 minus = __builtin_bit_cast(bf16x8, u32x4{column ? 0xff7fu : 0u, 0u, 0u, 0u});
+                        acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(plus, xf, acc[a][b], 0, 0, 0);
+                        acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(minus, xf, acc[a][b], 0, 0, 0);
+                    }
                 }
             }
+            if (ahead < t.adapters) lds_barrier_linear();             // (the stage has been read)
+            request(lds0, stage);
+            stage = 1 - stage;
         }
-        cur = next, slab = next_slab, stage = 1 - stage;
-    }
-    if (__any(bad)) {                                                 // a row whose index is out of range: NaN
+        if (__any(bad)) {                                             // a row whose index is out of range: NaN
 #pragma unroll
-        for (int a = 0; a < MT; ++a) {
-            const int32_t id = t.idx[m0 + wm * (BM / WM) + a * 32 + (lane & 31)];
-            const bool out = id < -1 || id >= t.adapters;
+            for (int a = 0; a < MT; ++a) {
+                const int32_t id = t.idx[m0 + wm * (BM / WM) + a * 32 + (lane & 31)];
+                const bool out = id < -1 || id >= t.adapters;
 #pragma unroll
-            for (int b = 0; b < NT; ++b)
+                for (int b = 0; b < NT; ++b)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) acc[a][b][i] = out ? __int_as_float(0x7fc00000) : acc[a][b][i];
+                    for (int i = 0; i < 16; ++i) acc[a][b][i] = out ? __int_as_float(0x7fc00000) : acc[a][b][i];
+            }
         }
     }
-}
+};
+struct NoSlabs {
+    __device__ void request(uint32_t, int) {}
+};
 
 template <int BM, int BN, bool CONV = false, int WM = 2, int WN = 2, typename... Tail>
 __global__ void __launch_bounds__(64 * WM * WN)
@@ -651,6 +716,8 @@ linear_wide_kernel(const bf16_t *x, const bf16_t *w, const float *__restrict__ b
     // free, and the last quarter requests slab s + 2 into it (REQUEST) and reads the first fragments of slab s + 1
     // (NEXT) between its multiplications.
     Frags f0, f1;
+    std::conditional_t<kAdapted, AdapterSlabs<BM, BN, WM, WN>, NoSlabs> more;
+    if constexpr (kAdapted) more.begin(tail..., m0, n0, N);
     auto slab = [&](auto parity, int64_t k_next, auto do_request, auto do_next) __attribute__((always_inline)) {
         constexpr int P = decltype(parity)::value;
         constexpr bool REQUEST = decltype(do_request)::value, NEXT = decltype(do_next)::value;
@@ -674,6 +741,7 @@ linear_wide_kernel(const bf16_t *x, const bf16_t *w, const float *__restrict__ b
         // vmcnt(0) lgkmcnt(0): this wavefront's part of slab s + 1 is in LDS, its fragments of slab s are in registers
         __builtin_amdgcn_s_waitcnt(0x0070);
         lds_barrier_linear();
+        if constexpr (kAdapted && !REQUEST) more.request(lds0, P);    // (the last two of the product's own: the adapters' first come behind them)
 #define MAMBA_WIDE_LAST(A, FROM, TO)                                                                                  \
         if constexpr (REQUEST) request(k_next, P * kStage, FROM(), TO());                                             \
         if constexpr (NEXT) {                                                                                         \
@@ -702,11 +770,10 @@ linear_wide_kernel(const bf16_t *x, const bf16_t *w, const float *__restrict__ b
         slab(Even(), (int64_t)(s + 2) * kWideBK, std::true_type(), std::true_type());
         slab(Odd(), (int64_t)(s + 3) * kWideBK, std::true_type(), std::true_type());
     }
+    if constexpr (kAdapted) more.find_first();
     slab(Even(), 0, std::false_type(), std::true_type());         // S is even: two slabs left, nothing more to request
     slab(Odd(), 0, std::false_type(), std::false_type());
-    if constexpr (kAdapted) {
-        add_adapter_slabs<BM, BN, WM, WN, kWideRow>(acc, tail..., lds, m0, n0, N, frag_x, frag_w);
-    }
+    if constexpr (kAdapted) more.multiply(acc, lds, lds0, frag_x, frag_w);
     // Epilogue.  The residual chunks this thread will add are requested first, all at once: with one workgroup per
     // CU nothing else would hide their latency, and fetched four at a time inside the store loop they cost a third
     // of the tile's time.
@@ -971,7 +1038,12 @@ linear_ring_kernel(const bf16_t *x, const bf16_t *w, const float *__restrict__ b
     }
 
     if constexpr (kAdapted) {
-        add_adapter_slabs<BM, BN, WM, WN, kWideRow>(acc, tail..., lds, m0, n0, (int64_t)tiles_n * BN, frag_x, frag_w);
+        AdapterSlabs<BM, BN, WM, WN> more;
+        more.begin(tail..., m0, n0, (int64_t)tiles_n * BN);
+        more.find_first();
+        more.request(lds0, 0);                                    // (every read of the stages is behind the last barrier)
+        more.request(lds0, 1);
+        more.multiply(acc, lds, lds0, frag_x, frag_w);
     }
     if constexpr (CONV) {
         // the whole tile, since windows reach into the rows of other wavefronts; every read of the stages is behind the last barrier
@@ -1079,7 +1151,9 @@ __device__ __forceinline__ void add_adapters_few(f32x4v (&acc)[MT][NT], const Ad
     const int lane = threadIdx.x & 63, li = lane & 15, lg = lane >> 4, chunks = t.rank >> 3;
     const int32_t id[1] = {lane < 16 * MT ? adapter_of(t, m0 + lane, M) : -1};
     int turn = 0;
-    for (int32_t cur = next_adapter(id, -1, t.adapters); cur < t.adapters; cur = next_adapter(id, cur, t.adapters), ++turn) {
+    InTurn<1> in_turn;
+    in_turn.begin(id, t.adapters);
+    for (int32_t cur = in_turn.next(id, t.adapters); cur < t.adapters; cur = in_turn.next(id, t.adapters), ++turn) {
         if (turn % NW != wave) continue;
         const uint64_t rows = __ballot(id[0] == cur);
         f32x4v d[MT][NT];
