@@ -28,7 +28,7 @@ __device__ __forceinline__ void lds_barrier()
 
 // A workgroup has 16 G rows and all ranks (RT tiles of 16) of one adapter: of those that its rows have, in the rows' order, every gridDim.y-th from the
 // blockIdx.y-th on, so that rows of many adapters are not multiplied by one after the other.  A row's sums are written by who has its adapter.
-// Of the W wavefronts G go by rows, W / G by k: slabs of 64 or 128 k, or as many as give each of those 32, four of them in LDS, straight from memory, a
+// Of the W wavefronts G go by rows, W / G by k: slabs of as many k as give each of those 32, four of them in LDS, straight from memory, a
 // row's 16-byte slot c at c ^ (row / 2 & 7).
 // Bound by x from memory where there are many rows, by trips to memory where there are few.
 template <int RT, int G, int W>
@@ -37,7 +37,7 @@ down_kernel(const bf16_t *__restrict__ x, const bf16_t *__restrict__ a, const fl
             bf16_t *__restrict__ t, uint32_t *__restrict__ zeros, int64_t M, int K, int rank, int adapters)
 {
     constexpr int kWaves = W, kThreads = 64 * W, kStages = 4;
-    constexpr int BM = 16 * G, BN = 16 * RT, S = W / G, kBlocks = S > 4 ? S / 2 : RT < 8 || S > 2 ? 2 : 1, kStep = 64 * kBlocks;   // blocks of 64 k to a slab
+    constexpr int BM = 16 * G, BN = 16 * RT, S = W / G, kBlocks = S > 2 ? S / 2 : 1, kStep = 64 * kBlocks;   // blocks of 64 k to a slab
     constexpr int kStage = (BM + BN) * kLine * kBlocks;
     constexpr int kGroups = (BM + BN) / 8 * kBlocks, NL = (kGroups + kWaves - 1) / kWaves;   // loads of 8 rows, and of a wavefront
     constexpr int kPart = S * BM * BN * 4;
@@ -162,7 +162,6 @@ hipError_t launch_adapters_down(const void *x, const AdapterArgs &l, int64_t M, 
         if (l.rank <= 64) return launch<4, G, W>(xp, l, M, K, stream);  \
         return launch<8, G, 4>(xp, l, M, K, stream);                    \
     } while (0)
-    if (M >= 12288) MAMBA_DOWN(4, 4);
     if (M >= 6144) MAMBA_DOWN(2, 4);
     if (M > 64) MAMBA_DOWN(1, 4);
     MAMBA_DOWN(1, 8);
