@@ -12,6 +12,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4v __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
+constexpr int64_t kEnough = 256;                                      // workgroups, one to a compute unit
 constexpr int kLine = 128;                                           // 64 k of a row in LDS
 
 // 16 bytes a lane from an address of its own into LDS at lds_addr + 16 lane (see linear.hip: the waits for them are explicit)
@@ -26,7 +27,7 @@ __device__ __forceinline__ void lds_barrier()
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
-// A workgroup has 16 G rows and all ranks (RT tiles of 16) of one adapter: of those that its rows have, in the rows' order, every gridDim.y-th from the
+// A workgroup has 16 G rows and RT tiles of 16 ranks of one adapter: of those that its rows have, in the rows' order, every gridDim.y-th from the
 // blockIdx.y-th on, so that rows of many adapters are not multiplied by one after the other.  A row's sums are written by who has its adapter.
 // Of the W wavefronts G go by rows, W / G by k: slabs of as many k as give each of those 32, four of them in LDS, straight from memory, a
 // row's 16-byte slot c at c ^ (row / 2 & 7).
@@ -45,7 +46,8 @@ down_kernel(const bf16_t *__restrict__ x, const bf16_t *__restrict__ a, const fl
     const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, lg = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), group = wave % G, split = wave / G;
     const int64_t m0 = (int64_t)blockIdx.x * BM;
-    if (blockIdx.x == 0 && blockIdx.y == 0 && tid < 32) zeros[tid] = 0;
+    const int rank0 = (int)blockIdx.z * BN, ranks = min(rank - rank0, BN);
+    if (blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0 && tid < 32) zeros[tid] = 0;
     const int32_t id = lane < BM && m0 + lane < M ? idx[m0 + lane] : -1;
     const uint32_t lds0 = (uint32_t)(size_t)(__attribute__((address_space(3))) unsigned char *)lds;
     const int slabs = (K + kStep - 1) / kStep, chunks = K / 8;
@@ -61,7 +63,7 @@ down_kernel(const bf16_t *__restrict__ x, const bf16_t *__restrict__ a, const fl
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
             const int g = min(i * kWaves + wave, kGroups - 1), block = g / ((BM + BN) / 8), r = g % ((BM + BN) / 8) * 8 + (lane >> 3);
-            row[i] = r < BM ? x + min(m0 + r, M - 1) * K : a + ((int64_t)cur * rank + min(r - BM, rank - 1)) * K;
+            row[i] = r < BM ? x + min(m0 + r, M - 1) * K : a + ((int64_t)cur * rank + rank0 + min(r - BM, ranks - 1)) * K;
             chunk[i] = 8 * block + ((lane & 7) ^ (r >> 1 & 7));
             to[i] = (uint32_t)g * 1024;
         }
@@ -119,7 +121,7 @@ down_kernel(const bf16_t *__restrict__ x, const bf16_t *__restrict__ a, const fl
         for (int e = tid; e < BM * BN / 2; e += kThreads) {          // two ranks of a row
             const int mr = e / (BN / 2), r = 2 * (e % (BN / 2));
             const int64_t m = m0 + mr;
-            if (m >= M || r >= rank || idx[m] != cur) continue;
+            if (m >= M || r >= ranks || idx[m] != cur) continue;
             float v[2] = {0.0f, 0.0f};
 #pragma unroll
             for (int q = 0; q < S; ++q) {
@@ -135,16 +137,17 @@ down_kernel(const bf16_t *__restrict__ x, const bf16_t *__restrict__ a, const fl
                 const float rest = v[i] - bf16_to_f32(high[i]);
                 low[i] = rest == rest ? rest : 0.0f;                 // (an infinity has no low term)
             }
-            *reinterpret_cast<uint32_t *>(t + m * (2 * rank) + r) = high[0] | high[1] << 16;
-            *reinterpret_cast<uint32_t *>(t + m * (2 * rank) + rank + r) = f32x2_to_bf16x2(low[0], low[1]);
+            *reinterpret_cast<uint32_t *>(t + m * (2 * rank) + rank0 + r) = high[0] | high[1] << 16;
+            *reinterpret_cast<uint32_t *>(t + m * (2 * rank) + rank + rank0 + r) = f32x2_to_bf16x2(low[0], low[1]);
         }
     }
 }
 
 template <int RT, int G, int W> hipError_t launch(const bf16_t *x, const AdapterArgs &l, int64_t M, int64_t K, hipStream_t stream)
 {
-    const int64_t most = M <= 64 ? 16 : 4;                           // adapters of a workgroup's rows at once
-    const dim3 grid((unsigned)((M + 16 * G - 1) / (16 * G)), (unsigned)(l.adapters < most ? l.adapters : most));
+    const int64_t tiles = (M + 16 * G - 1) / (16 * G), parts = (l.rank + 16 * RT - 1) / (16 * RT);
+    const int64_t turns = tiles * parts >= kEnough / 4 ? 4 : 16;     // adapters of a workgroup's rows at once
+    const dim3 grid((unsigned)tiles, (unsigned)(l.adapters < turns ? l.adapters : turns), (unsigned)parts);
     down_kernel<RT, G, W><<<grid, 64 * W, 0, stream>>>(x, static_cast<const bf16_t *>(l.a), l.scale, l.idx, static_cast<bf16_t *>(l.t),
                                                        static_cast<uint32_t *>(l.zeros), M, (int)K, (int)l.rank, (int)l.adapters);
     return hipGetLastError();
@@ -152,20 +155,22 @@ template <int RT, int G, int W> hipError_t launch(const bf16_t *x, const Adapter
 
 }  // namespace
 
+// Ranks are split over workgroups, 16 of them or more to one, while there are not enough of those: x is read again from the second-level cache then.
 hipError_t launch_adapters_down(const void *x, const AdapterArgs &l, int64_t M, int64_t K, hipStream_t stream)
 {
     const bf16_t *xp = static_cast<const bf16_t *>(x);
-#define MAMBA_DOWN(G, W)                                                \
-    do {                                                                \
-        if (l.rank <= 16) return launch<1, G, W>(xp, l, M, K, stream);  \
-        if (l.rank <= 32) return launch<2, G, W>(xp, l, M, K, stream);  \
-        if (l.rank <= 64) return launch<4, G, W>(xp, l, M, K, stream);  \
-        return launch<8, G, 4>(xp, l, M, K, stream);                    \
-    } while (0)
-    if (M >= 6144) MAMBA_DOWN(2, 4);
-    if (M > 64) MAMBA_DOWN(1, 4);
-    MAMBA_DOWN(1, 8);
-#undef MAMBA_DOWN
+    if (M <= 64) return launch<1, 1, 8>(xp, l, M, K, stream);
+    if (M >= 6144) {
+        if (l.rank <= 16) return launch<1, 2, 4>(xp, l, M, K, stream);
+        if (l.rank <= 32) return launch<2, 2, 4>(xp, l, M, K, stream);
+        if (l.rank <= 64) return launch<4, 2, 4>(xp, l, M, K, stream);
+        return launch<8, 2, 4>(xp, l, M, K, stream);
+    }
+    const int64_t tiles = (M + 15) / 16, parts = (kEnough + tiles - 1) / tiles;   // (of the ranks)
+    if (l.rank <= 16 || l.rank <= 16 * parts) return launch<1, 1, 4>(xp, l, M, K, stream);
+    if (l.rank <= 32 || l.rank <= 32 * parts) return launch<2, 1, 4>(xp, l, M, K, stream);
+    if (l.rank <= 64 || l.rank <= 64 * parts) return launch<4, 1, 4>(xp, l, M, K, stream);
+    return launch<8, 1, 4>(xp, l, M, K, stream);
 }
 
 }  // namespace mamba
