@@ -337,7 +337,9 @@ template <typename T> __device__ __forceinline__ CutBins cut_bins(const RowBins 
     CutBins c{-1, kBins - 1, 0.0f, -1, -1, -1};
     const int top_mark = top_mark_of(top, r.per_bin);
     if (r.min_p > 0.0f) {
-        const float away = r.T * (log2_hw(r.min_p) * kLn2), border = top + away, around = fmaxf(fmaxf(fabsf(border), fabsf(top)), fabsf(away)) * 0x1p-18f;
+        const float away = r.T * (log2_hw(r.min_p) * kLn2), border = top + away;
+        // (roundings of these, and the logarithm's: near one, where a weight's own rounding counts too, not relative to it)
+        const float around = fmaxf(fmaxf(fabsf(border), fabsf(top)), fabsf(away)) * 0x1p-18f + r.T * 0x1p-20f;
         float above = border + around;
         // (a logit of the row's type, so that what is above it has a larger key)
         if (Order<T>::kShort) above = above >= 0.0f ? __uint_as_float((__float_as_uint(above) + 0xffffu) & 0xffff0000u) : __uint_as_float(__float_as_uint(above) & 0xffff0000u);

@@ -150,6 +150,16 @@ def test_rows_whose_settings_are_not_known(m):
 
 
 @gpu
+@pytest.mark.parametrize("T", [1e-45, 1e-30, 1e-4, 1e6, 1e30, np.inf])
+def test_temperatures_at_their_ends(m, T):
+    """From rows of one token left to rows whose tokens all weigh the same, under every kind of cut."""
+    rng = np.random.default_rng(12)
+    x = np.concatenate([rows(rng, 3, 3001), rows(rng, 1, 3001) * 1e37, np.round(rows(rng, 2, 3001))])
+    for top_p, min_p, top_k in ((1.0, 0.0, 0), (0.625, 0.0, 0), (1e-45, 0.0, 0), (1.0, 1e-45, 0), (1.0, 1.0, 0), (1.0, 0.0, 2 ** 31 - 1), (0.75, 0.5, 700)):
+        check(m, x, rng.uniform(size=(6, 4)), [[T, top_p, min_p]], [top_k])
+
+
+@gpu
 def test_infinities_nan_and_empty_rows(m):
     rng = np.random.default_rng(5)
     x = rows(rng, 12, 5003)
