@@ -245,7 +245,7 @@ class MambaDrafter:
         first, then position by position; u_accept (nodes - 1), u_sample (1) f32 in [0,1) (None: torch's random numbers).  Returns the emitted
         tokens int32 (gamma + 1), -1 behind them, their number int32 (1), and the accepted ones' rows in their positions int32 (gamma)."""
         bufs = self._trees.get(tuple(int(n) for n in tree), {})
-        if "drawn" not in bufs:
+        if not bufs.get("sampled"):
             raise RuntimeError("verify() is for a tree whose children were drawn: call sample() and draft() first")
         tokens = torch.cat([bufs["pos"][i]["cand"].view(-1) for i in range(1, bufs["cache"].gamma + 1)]).view(1, -1)
         draws = lambda u, n: torch.rand((1, n), device=self.dev) if u is None else u.reshape(1, n)
@@ -260,6 +260,7 @@ class MambaDrafter:
         bufs = self._buffers(tree)
         c = bufs["cache"]
         c.set_root(self.root_conv, self.root_ssm)
+        bufs["sampled"] = self._sampling is not None     # of the tree that the buffers hold
         if self._sampling is not None:
             at = 0
             total = sum(c.batch[i] for i in range(1, c.gamma + 1))

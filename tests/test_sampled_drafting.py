@@ -201,3 +201,21 @@ def test_rounds_of_several_requests_with_the_operators_themselves():
         assert np.array_equal(idx.cpu().numpy(), ri)
         ro, rc, rn = oracle.verify(target.cpu().numpy(), q.cpu().numpy(), idx.cpu().numpy(), ua.cpu().numpy(), us.cpu().numpy(), (n,))
         assert all(np.array_equal(t.cpu().numpy(), r) for t, r in zip(outs, (ro, rc, rn)))
+
+
+@pytest.mark.gpu
+def test_a_tree_that_was_not_drawn_is_not_verified():
+    """What an earlier round drew is not what a greedy round's children came from."""
+    d, tree = small_drafter(layers=1), (2, 1)
+    d.prefill(torch.arange(20, dtype=torch.int32, device=DEV))
+    p = torch.full((5, d.V), 1.0 / d.V, device=DEV)
+    for use_graph in (False, True):
+        d.sample(0.8)
+        d.draft(tree, use_graph)
+        d.verify(tree, p)
+        d.sample(None)
+        d.draft(tree, use_graph)
+        with pytest.raises(RuntimeError, match="drawn"):
+            d.verify(tree, p)
+        with pytest.raises(RuntimeError, match="drawn"):
+            d.verify((3,), p)
