@@ -185,6 +185,15 @@ struct Eight {
     }
 };
 
+// What the workgroup wrote to LDS is there for all of it.  (Its stores to memory and loads from there stay under way: nothing but LDS goes from thread to
+// thread in these kernels, and a barrier that waits for stores costs a microsecond each time.)
+__device__ __forceinline__ void lds_barrier()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
 // lanes of a wavefront by DPP: what comes from `CTRL`'s lane, where ROWS has the row, else what `other` says
 template <int CTRL, int ROWS = 0xf> __device__ __forceinline__ uint32_t from_lane(uint32_t other, uint32_t v)
 {
@@ -247,7 +256,7 @@ __global__ void __launch_bounds__(kThreads) bins_kernel(const T *__restrict__ lo
     for (int j = 0; j < 8; ++j) top = fmaxf(top, e.x[j]);
     top = wave_max(top);
     if (lane == 0) part[wave] = top;
-    __syncthreads();
+    lds_barrier();
     top = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
     const int top_mark = top_mark_of(top, r.per_bin);
     u64 last_mass = 0;                                               // (of the last bin: it may have most of the tokens)
@@ -271,14 +280,14 @@ __global__ void __launch_bounds__(kThreads) bins_kernel(const T *__restrict__ lo
         last_number = (uint32_t)wave_sum((u64)last_number);
         if (lane == 0) atomicAdd(&number[kBins - 1], last_number);
     }
-    __syncthreads();
+    lds_barrier();
     u64 v = 0, n = 0;
     if (wave < 2) {
         v = wave_prefix(mass[tid]);
         n = r.top_k > 0 ? wave_prefix((u64)number[tid]) : 0;
         if (tid == 63) first_mass = v, first_number = (uint32_t)n;
     }
-    __syncthreads();
+    lds_barrier();
     if (wave == 1) v += first_mass, n += first_number;
     if (tid < kBins) {
         to.mass[chunk * kBins + tid] = v;
@@ -379,7 +388,7 @@ __global__ void __launch_bounds__(kWide) plan_kernel(Chunks from, RowBins *__res
     const Settings r = settings_of(a, m);
     float top = wave_max(own);
     if (lane == 0) part[wave] = top;
-    __syncthreads();
+    lds_barrier();
     top = wave_max(part[lane & (kWideWaves - 1)]);
     const int top_mark = top_mark_of(top, r.per_bin);
     if (tid < chunks) {
@@ -388,7 +397,7 @@ __global__ void __launch_bounds__(kWide) plan_kernel(Chunks from, RowBins *__res
         scale[tid] = mine;
         scales[m * chunks + tid] = mine;
     }
-    __syncthreads();
+    lds_barrier();
     u64 v = 0;
     uint32_t n = 0;
 #pragma unroll 1
@@ -408,14 +417,14 @@ __global__ void __launch_bounds__(kWide) plan_kernel(Chunks from, RowBins *__res
     }
     mass_part[tid] = v;
     number_part[tid] = n;
-    __syncthreads();
+    lds_barrier();
     if (tid < kBins) {
 #pragma unroll
         for (int g = 1; g < kGroups; ++g) v += mass_part[g * kBins + tid], n += number_part[g * kBins + tid];
         s.mass[tid] = v, s.number[tid] = n;
         rows[m].mass[tid] = v, rows[m].number[tid] = n;
     }
-    __syncthreads();
+    lds_barrier();
     if (wave == 0) {
         CutBins c{-1, kBins - 1, 0.0f, -1, -1, -1};
         if (r.known && counts(top)) c = cut_bins<T>(s, r, top, lane);
@@ -438,7 +447,7 @@ gather_kernel(const T *__restrict__ logits, RowBins *__restrict__ rows, u64 *__r
     e.load(logits + m * V, (int32_t)blockIdx.x * kSlice + tid * 8, V);
     if (tid == 0) found = 0;
     if (!c.any()) return;
-    __syncthreads();
+    lds_barrier();
     // the bins as ranges of the scale that marks are on, the upper ends not among them
     const int top_mark = top_mark_of(top, per_bin);
     auto from_of = [&](int last_bin) { return last_bin >= kBins - 1 ? -INFINITY : (float)(top_mark - start_of(last_bin + 1) + 1); };
@@ -462,9 +471,9 @@ gather_kernel(const T *__restrict__ logits, RowBins *__restrict__ rows, u64 *__r
         for (int j = 0; j < 8; ++j) hits &= counts(e.x[j]) ? ~0u : ~(1u << j);
         at = atomicAdd(&found, (uint32_t)__popc(hits));
     }
-    __syncthreads();
+    lds_barrier();
     if (tid == 0) base = found ? atomicAdd(&rows[m].listed, found) : 0;
-    __syncthreads();
+    lds_barrier();
     at += base;
     if (hits) {
 #pragma unroll
@@ -502,20 +511,21 @@ struct RowShared {
     u64 wave_part[kWideWaves];
     float part[kWideWaves];
     u64 drawn[8];
+    float u[8];
     u64 few[kFew], few_mass[kFew];
     u64 lo, hi, need, before, cut, found, sum;
     uint32_t n_few, n;
     int32_t chunk;
 };
 
-// prefix sums over the workgroup, without the thread's own; the whole sum in *total
-__device__ __forceinline__ u64 wide_prefix(u64 v, u64 *parts, u64 *total)
+// prefix sums over the workgroup, without the thread's own; the whole sum in *total.  FREE: nobody reads parts any more.
+template <bool FREE> __device__ __forceinline__ u64 wide_prefix(u64 v, u64 *parts, u64 *total)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const u64 mine = wave_prefix(v);
-    __syncthreads();                                                 // (the last use of parts is over)
+    if (!FREE) lds_barrier();
     if (lane == 63) parts[wave] = mine;
-    __syncthreads();
+    lds_barrier();
     const u64 waves = wave_prefix(lane < kWideWaves ? parts[lane] : 0);
     *total = lane_of(waves, kWideWaves - 1);
     const int before = __builtin_amdgcn_readfirstlane(wave - 1);
@@ -594,20 +604,20 @@ __device__ __forceinline__ u64 reach(RowShared &s, const Row<T> &row, const Toke
         const int b = row.bin(row.order.logit(place));
         return b >= first && b <= last;
     };
-    __syncthreads();
+    lds_barrier();
     if (tid == 0) s.need = need, s.before = 0, s.cut = 0, s.found = 0, s.n_few = 0;
 #pragma unroll 1
     for (int turn = 0; n > kFew && turn < 8; ++turn) {               // (lo < hi: places differ)
         const int width = 64 - __clzll(hi - lo), shift = width > 10 ? width - 10 : 0;
         s.fine_mass[padded(tid)] = 0, s.fine_number[padded(tid)] = 0;
-        __syncthreads();
+        lds_barrier();
         tokens.each([&](u64 place, u64 w) {
             if (place < lo || place > hi || !in_bins(place)) return;
             const int at = padded((int)((hi - place) >> shift));
             atomicAdd(&s.fine_mass[at], w);
             atomicAdd(&s.fine_number[at], 1u);
         });
-        __syncthreads();
+        lds_barrier();
         if (wave == 0) {
             // the lane whose 16 parts reach what is needed, then of those the part
             const u64 wanted = s.need;
@@ -635,16 +645,16 @@ __device__ __forceinline__ u64 reach(RowShared &s, const Row<T> &row, const Toke
                 s.n = s.fine_number[padded(first + at)];
             }
         }
-        __syncthreads();
+        lds_barrier();
         lo = s.lo, hi = s.hi, n = s.n;
     }
-    __syncthreads();
+    lds_barrier();
     tokens.each([&](u64 place, u64 w) {
         if (place < lo || place > hi || !in_bins(place)) return;
         const uint32_t at = atomicAdd(&s.n_few, 1u);
         if (at < kFew) s.few[at] = place, s.few_mass[at] = w;
     });
-    __syncthreads();
+    lds_barrier();
     if (wave == 0) {
         const int few = (int)min(s.n_few, (uint32_t)kFew);
         const u64 place = lane < few ? s.few[lane] : 0, mine = lane < few ? s.few_mass[lane] : 0;
@@ -661,7 +671,7 @@ __device__ __forceinline__ u64 reach(RowShared &s, const Row<T> &row, const Toke
             s.found = s.before + mass_before + mine;
         }
     }
-    __syncthreads();
+    lds_barrier();
     *units = s.found;
     return s.cut;
 }
@@ -680,9 +690,9 @@ template <typename T, typename Tokens> __device__ __forceinline__ Cut cut_of(Row
     Cut cut{0, kBins};
     u64 sum = s.bins.mass[kBins - 1], number = s.bins.number[kBins - 1];
     if (c.min_first >= 0) {
-        __syncthreads();
+        lds_barrier();
         if (tid == 0) s.lo = ~(u64)0, s.sum = 0, s.n = 0;
-        __syncthreads();
+        lds_barrier();
         u64 lowest = ~(u64)0, mass = 0;
         uint32_t n = 0;
         tokens.each([&](u64 place, u64 w) {
@@ -691,7 +701,7 @@ template <typename T, typename Tokens> __device__ __forceinline__ Cut cut_of(Row
             lowest = min(lowest, place), mass += w, ++n;
         });
         if (n) atomicMin(&s.lo, lowest), atomicAdd(&s.sum, mass), atomicAdd(&s.n, n);
-        __syncthreads();
+        lds_barrier();
         sum = ahead_of(s.bins.mass, c.min_first) + s.sum, number = ahead_of(s.bins.number, c.min_first) + s.n;
         cut.place = s.lo, cut.bin = bin_of_place(s.lo);
         if (s.n == 0) cut.place = ((u64)row.order.key(row.order.place(c.min_above, 0)) + 1) << row.order.bits, cut.bin = c.min_first;   // all of the bins before, nothing of these
@@ -716,19 +726,19 @@ template <typename T, typename Tokens> __device__ __forceinline__ Cut cut_of(Row
 template <typename T, typename Tokens>
 __device__ __forceinline__ void chunk_sums(RowShared &s, const Chunks &from, int64_t m, int chunks, const Cut &cut, const Row<T> &row, const Tokens &tokens)
 {
-    __syncthreads();
+    lds_barrier();
     for (int i = threadIdx.x; i < chunks; i += kWide) {
         const int shift = s.scale[i].shift, b = cut.bin == kBins ? kBins - 1 : chunk_bin(start_of(cut.bin), shift);
         s.chunk_mass[i] = shift < kNoChunk && b >= 0 ? from.mass[(m * chunks + i) * kBins + b] : 0;
     }
-    __syncthreads();
+    lds_barrier();
     if (cut.bin < kBins)
         tokens.each([&](u64 place, u64) {
             const float v = row.order.logit(place);
             const int32_t token = row.order.token(place);
             if (place >= cut.place && row.bin(v) == cut.bin) atomicAdd(&s.chunk_mass[token / kSlice], row.own_units(v, token));
         });
-    __syncthreads();
+    lds_barrier();
 }
 
 // Where the bins with cuts have more tokens than a workgroup's registers: the same by reading the row for every step.  (Not inlined: a row seldom
@@ -751,9 +761,9 @@ __device__ __attribute__((noinline)) void sums_of_the_rest(RowShared &s, const R
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     auto most_of_all = [&](float v) {
         v = wave_max(v);
-        __syncthreads();
+        lds_barrier();
         if (lane == 0) s.part[wave] = v;
-        __syncthreads();
+        lds_barrier();
         return wave_max(s.part[lane & (kWideWaves - 1)]);
     };
 #pragma unroll 1
@@ -774,14 +784,14 @@ __device__ __attribute__((noinline)) void sums_of_the_rest(RowShared &s, const R
         u64 sum = 0, all;
 #pragma unroll
         for (int i = 0; i < 2; ++i) sum += counts(v[i]) ? row.weights.units(v[i], most, row.scale) : 0;
-        wide_prefix(sum, s.wave_part, &all);
+        wide_prefix<false>(sum, s.wave_part, &all);
         if (tid == 0) s.chunk_mass[chunk] = all, s.scale[chunk].most = most;
     }
-    __syncthreads();
+    lds_barrier();
     const float mine = tid < chunks && s.chunk_mass[tid] > 0 && row.weights.of(s.scale[tid].most, top) > 0.0 ? s.scale[tid].most : -INFINITY;
     const float most = most_of_all(mine);
     if (tid < chunks) s.scale[tid].factor = counts(mine) ? row.weights.of(mine, most) : 0.0;
-    __syncthreads();
+    lds_barrier();
 }
 
 template <typename T>
@@ -797,9 +807,10 @@ draw_kernel(const T *__restrict__ logits, Chunks from, const RowBins *__restrict
     const CutBins c = rows[m].cuts;
     if (tid < kBins) s.bins.mass[tid] = rows[m].mass[tid], s.bins.number[tid] = rows[m].number[tid];
     if (tid < chunks) s.scale[tid] = scales[m * chunks + tid];
+    if (tid < 8) s.drawn[tid] = 0, s.u[tid] = tid < a.k ? a.u[m * a.k + tid] : 0.0f;
     const u64 first_place = tid < (int)n && tid < kList ? list[m * kList + tid] : 0;
     const Settings r = settings_of(a, m);
-    __syncthreads();
+    lds_barrier();
     Row<T> row{logits + m * a.V, (int32_t)a.V, top, r.per_bin, top_mark_of(top, r.per_bin), scale, r.weights, order, s.scale};
     const bool some = r.known && counts(top);
 
@@ -825,72 +836,80 @@ draw_kernel(const T *__restrict__ logits, Chunks from, const RowBins *__restrict
         if (n <= kList || cut.bin == kBins) chunk_sums(s, from, m, chunks, cut, row, held);
     }
 
-    // ---- the draws
+    // ---- the draws: the chunk by every wavefront for itself, the token by all of them
     double inv_sum = 0.0;
+    const int per = (chunks + 63) / 64, lane = tid & 63;             // chunks to a lane
+    auto mass_of = [&](int i) { return i < chunks ? scaled(s.chunk_mass[i], s.scale[i].factor) : 0; };
+    auto prefix_of_chunks = [&](u64 *mine) {
+        u64 sum = 0;
 #pragma unroll 1
-    for (int j = 0; j < a.k; ++j) {
-        const float u = a.u[m * a.k + j];
-        u64 mine = 0, left = 0, at = 0;
-        if (some) {
-            mine = tid < chunks ? scaled(s.chunk_mass[tid], s.scale[tid].factor) : 0;
-            at = wide_prefix(mine, s.wave_part, &left);
-            if (j == 0) inv_sum = 1.0 / __builtin_ldexp((double)left, -scale);
-            // (that the last of what is kept was drawn, with nothing left, says that all of it was)
-            bool out = left == 0 && cut.place != 0;
-            for (int d = 0, is = 0; out && d < j; ++d) is |= s.drawn[d] == cut.place, out = d + 1 < j || is;
-            if (j > 0 && left < (r.top_k > 0 && r.top_k <= 1024 ? (u64)1 << 30 : (u64)1 << 39) && !out) {
-                const Row<T> row_there = row;
-                sums_of_the_rest(s, row_there, cut.place, j, top, chunks);
-                mine = tid < chunks ? scaled(s.chunk_mass[tid], s.scale[tid].factor) : 0;
-                at = wide_prefix(mine, s.wave_part, &left);
-            }
+        for (int i = 0; i < per; ++i) sum += mass_of(lane * per + i);
+        *mine = sum;
+        return wave_prefix(sum);
+    };
+#pragma unroll 1
+    for (int j = 0; some && j < a.k; ++j) {
+        const float u = s.u[j];
+        u64 mine, to = prefix_of_chunks(&mine), left = lane_of(to, 63);
+        if (j == 0) inv_sum = 1.0 / __builtin_ldexp((double)left, -scale);
+        // (that the last of what is kept was drawn, with nothing left, says that all of it was)
+        bool out = left == 0 && cut.place != 0;
+        for (int d = 0, is = 0; out && d < j; ++d) is |= s.drawn[d] == cut.place, out = d + 1 < j || is;
+        if (j > 0 && left < (r.top_k > 0 && r.top_k <= 1024 ? (u64)1 << 30 : (u64)1 << 39) && !out) {
+            const Row<T> row_there = row;
+            sums_of_the_rest(s, row_there, cut.place, j, top, chunks);
+            to = prefix_of_chunks(&mine), left = lane_of(to, 63);
         }
-        if (tid == 0) s.drawn[j] = 0;
-        if (left > 0) {                                              // (the same for all threads)
-            const u64 f = !(u > 0.0f) ? 0 : u >= 1.0f ? ~(u64)0 : (u64)((double)u * 18446744073709551616.0);
-            const u64 bound = __umul64hi(left, f);                   // the sum that is to be passed
-            if (at <= bound && bound < at + mine) s.chunk = tid, s.need = min((u64)((double)(bound - at) / s.scale[tid].factor), s.chunk_mass[tid] - 1);
-            __syncthreads();
-            const int chunk = s.chunk;
-            const u64 inside = s.need;
-            const int32_t first = chunk * kSlice + 2 * tid;
-            const float most = s.scale[chunk].most;
-            float v[2];
-            u64 w[2], sum = 0, all;
+        if (left == 0) break;                                        // (the same for all threads, and for good: nothing is left)
+        const u64 f = !(u > 0.0f) ? 0 : u >= 1.0f ? ~(u64)0 : (u64)((double)u * 18446744073709551616.0);
+        const u64 bound = __umul64hi(left, f);                       // the sum that is to be passed
+        int chunk = __builtin_ctzll(__ballot(to > bound));
+        u64 ahead = lane_of(to - mine, chunk);
+        if (per > 1) {
+            const u64 one = lane < per ? mass_of(chunk * per + lane) : 0, to_one = ahead + wave_prefix(one);
+            const int at = __builtin_ctzll(__ballot(to_one > bound));
+            chunk = chunk * per + at, ahead = lane_of(to_one - one, at);
+        }
+        const u64 inside = min((u64)((double)(bound - ahead) / s.scale[chunk].factor), s.chunk_mass[chunk] - 1);
+        const int32_t first = chunk * kSlice + 2 * tid;
+        const float most = s.scale[chunk].most;
+        float v[2];
+        u64 w[2], sum = 0, all;
 #pragma unroll
-            for (int i = 0; i < 2; ++i) v[i] = ld_io(row.x, min(first + i, row.V - 1));
+        for (int i = 0; i < 2; ++i) v[i] = ld_io(row.x, min(first + i, row.V - 1));
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const u64 p = order.place(v[i], first + i);
+            w[i] = first + i < row.V && counts(v[i]) && p >= cut.place ? row.weights.units(v[i], most, scale) : 0;
+        }
+        for (int d = 0; d < j; ++d) {
+            const int32_t token = s.drawn[d] ? order.token(s.drawn[d]) : -1;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) w[i] = first + i == token ? 0 : w[i];
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) sum += w[i];
+        u64 start = wide_prefix<true>(sum, s.wave_part, &all);       // (every read of the chunks' sums is behind its barrier)
+        if (start <= inside && inside < start + sum) {               // one thread
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const u64 p = order.place(v[i], first + i);
-                w[i] = first + i < row.V && counts(v[i]) && p >= cut.place ? row.weights.units(v[i], most, scale) : 0;
-            }
-            for (int d = 0; d < j; ++d) {
-                const int32_t token = s.drawn[d] ? order.token(s.drawn[d]) : -1;
-#pragma unroll
-                for (int i = 0; i < 2; ++i) w[i] = first + i == token ? 0 : w[i];
-            }
-#pragma unroll
-            for (int i = 0; i < 2; ++i) sum += w[i];
-            u64 start = wide_prefix(sum, s.wave_part, &all);
-            if (start <= inside && inside < start + sum) {           // one thread
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    if (start <= inside && inside < start + w[i]) s.drawn[j] = order.place(v[i], first + i), s.chunk_mass[chunk] -= w[i];
-                    start += w[i];
-                }
+                if (start <= inside && inside < start + w[i]) s.drawn[j] = order.place(v[i], first + i), s.chunk_mass[chunk] -= w[i];
+                start += w[i];
             }
         }
-        __syncthreads();
+        lds_barrier();
+    }
+    // a wavefront to a child
+    if (const int j = __builtin_amdgcn_readfirstlane(tid >> 6); j < a.k) {
         const u64 place = s.drawn[j];
         const int64_t out = m * a.k + j;
         const int32_t token = place ? order.token(place) : -1;
-        if (tid == 0) {
+        if (lane == 0) {
             a.idx[out] = token;
             a.prob[out] = place ? (float)(row.weights.of(order.logit(place), top) * inv_sum) : 0.0f;
         }
         if (a.path_out)
-            for (int64_t t = tid; t <= a.path_len; t += kWide)
-                a.path_out[out * (a.path_len + 1) + t] = t < a.path_len ? a.path[m * a.path_len + t] : token;
+            for (int64_t t = lane; t <= a.path_len; t += 64) a.path_out[out * (a.path_len + 1) + t] = t < a.path_len ? a.path[m * a.path_len + t] : token;
     }
     if (tid == 0 && a.dist) {
         const bool all = cut.place == 0;
