@@ -1,5 +1,5 @@
-// Rows of a vocabulary as the kernels over logits read and write them: eight tokens of a lane at a time, rows that start anywhere, and a
-// grid of slices by rows.
+// Rows of a vocabulary as the kernels over logits read and write them: eight tokens of a lane at a time, rows that start anywhere, a grid of
+// slices by rows; a workgroup's barrier and a wavefront's lanes by DPP.
 #pragma once
 #include "device_math.h"
 
@@ -44,6 +44,20 @@ __device__ __forceinline__ void store8(bf16_t *p, const float *x)
     *reinterpret_cast<u32x4_any *>(p) = a;
 }
 
+// What the workgroup wrote to LDS is there for all of it.  (Its stores to memory and loads from there stay under way: nothing but LDS goes from thread to
+// thread in these kernels, and a barrier that waits for stores costs a microsecond each time.)
+__device__ __forceinline__ void lds_barrier()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// lanes of a wavefront by DPP: what comes from `CTRL`'s lane, where ROWS has the row, else what `other` says
+template <int CTRL, int ROWS = 0xf> __device__ __forceinline__ uint32_t from_lane(uint32_t other, uint32_t v)
+{
+    return (uint32_t)__builtin_amdgcn_update_dpp((int)other, (int)v, CTRL, ROWS, 0xf, false);
+}
 // A grid of slices by rows has the rows in two of its dimensions: no number of a workgroup is divided.
 constexpr int64_t kRowsY = 65535;
 __device__ __forceinline__ int64_t row_of_block() { return (int64_t)blockIdx.z * kRowsY + blockIdx.y; }

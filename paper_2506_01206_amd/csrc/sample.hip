@@ -185,20 +185,6 @@ struct Eight {
     }
 };
 
-// What the workgroup wrote to LDS is there for all of it.  (Its stores to memory and loads from there stay under way: nothing but LDS goes from thread to
-// thread in these kernels, and a barrier that waits for stores costs a microsecond each time.)
-__device__ __forceinline__ void lds_barrier()
-{
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
-    __builtin_amdgcn_s_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
-}
-
-// lanes of a wavefront by DPP: what comes from `CTRL`'s lane, where ROWS has the row, else what `other` says
-template <int CTRL, int ROWS = 0xf> __device__ __forceinline__ uint32_t from_lane(uint32_t other, uint32_t v)
-{
-    return (uint32_t)__builtin_amdgcn_update_dpp((int)other, (int)v, CTRL, ROWS, 0xf, false);
-}
 template <int CTRL, int ROWS = 0xf> __device__ __forceinline__ u64 plus_lane(u64 v)
 {
     return v + ((u64)from_lane<CTRL, ROWS>(0, (uint32_t)(v >> 32)) << 32 | from_lane<CTRL, ROWS>(0, (uint32_t)v));

@@ -25,6 +25,8 @@ constexpr int kThreads = 256, kWaves = kThreads / 64, kTrip = kThreads * 8;   //
 constexpr int kMostPieces = 256;
 constexpr int kMostRounds = 8;
 
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
 // What is added up over the tokens of a row: P after the first `levels` rejections, or where `gap` says so what P is ahead of Q there (then of q too what
 // is left beside the rejected children and `token`).
 struct Weighing {
@@ -49,12 +51,23 @@ struct Sums {
     double first, second;
 };
 
-__device__ __forceinline__ double wave_sum(double v)
+// (by DPP: six trips through LDS for a sum were a sixth of a launch of few sequences)
+template <int CTRL, int ROWS = 0xf> __device__ __forceinline__ double plus_lane(double v)
 {
-#pragma unroll
-    for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
-    return v;
+    const u32x2 u = __builtin_bit_cast(u32x2, v);
+    return v + __builtin_bit_cast(double, u32x2{from_lane<CTRL, ROWS>(0, u.x), from_lane<CTRL, ROWS>(0, u.y)});
 }
+// prefix sums with the lane's own: row_shr 1, 2, 4, 8, row_bcast 15, 31
+__device__ __forceinline__ double wave_prefix(double v)
+{
+    return plus_lane<0x143, 0xc>(plus_lane<0x142, 0xa>(plus_lane<0x118>(plus_lane<0x114>(plus_lane<0x112>(plus_lane<0x111>(v))))));
+}
+__device__ __forceinline__ double lane_of(double v, int lane)
+{
+    const u32x2 u = __builtin_bit_cast(u32x2, v);
+    return __builtin_bit_cast(double, u32x2{(uint32_t)__builtin_amdgcn_readlane((int)u.x, lane), (uint32_t)__builtin_amdgcn_readlane((int)u.y, lane)});
+}
+__device__ __forceinline__ double wave_sum(double v) { return lane_of(wave_prefix(v), 63); }
 
 // P and Q of N tokens, from v0 on, with probabilities p and q; `left`: q while the token is not rejected
 template <int N> __device__ __forceinline__ void after_rejections(const Walk &s, int levels, int32_t v0, double (&P)[N], double (&Q)[N], double (&left)[N])
@@ -131,7 +144,7 @@ __device__ __forceinline__ Sums add_up(const Walk &s, const Sequence &in, int32_
     }
     x = wave_sum(x), y = wave_sum(y);
     if ((tid & 63) == 0) part[tid >> 6] = x, part[kWaves + (tid >> 6)] = y;
-    __syncthreads();
+    lds_barrier();
     Sums r{0.0, 0.0};
 #pragma unroll
     for (int i = 0; i < kWaves; ++i) r.first += part[i], r.second += part[kWaves + i];
@@ -158,11 +171,11 @@ __device__ __forceinline__ void go_on(Walk &s, const VerifyArgs &a, const Sequen
 {
     const int lane = threadIdx.x & 63;
     const bool writes = threadIdx.x == 0;                            // (the walk; accepted tokens, which the others come to as well, one workgroup)
-    __syncthreads();
+    lds_barrier();
     int32_t n = s.n, next = s.next, depth = s.depth, known = s.known;
     int64_t row = s.row, rows = s.rows, nodes = s.nodes, children = s.children;
     const bool waited = s.phase == kWaiting;
-    __syncthreads();
+    lds_barrier();
     if (waited) {
         if (writes) {
             s.token[n] = s.w.token;
@@ -171,7 +184,7 @@ __device__ __forceinline__ void go_on(Walk &s, const VerifyArgs &a, const Sequen
         }
         known = got.first > 0.0;
         ++n, ++next;
-        __syncthreads();
+        lds_barrier();
     }
     int phase = kWalking;
     Weighing w = s.w;
@@ -215,12 +228,12 @@ __device__ __forceinline__ void go_on(Walk &s, const VerifyArgs &a, const Sequen
         nodes += rows, children += rows * fan, row = row * fan + taken, rows *= fan;
         ++depth, n = 0, next = 0, known = 0;
     }
-    __syncthreads();
+    lds_barrier();
     if (writes) {
         s.row = row, s.rows = rows, s.nodes = nodes, s.children = children;
         s.depth = depth, s.phase = phase, s.n = n, s.next = next, s.known = known, s.w = w;
     }
-    __syncthreads();
+    lds_barrier();
 }
 
 __device__ __forceinline__ void begin(Walk &s, const Walk *from)
@@ -233,7 +246,7 @@ __device__ __forceinline__ void begin(Walk &s, const Walk *from)
             s.depth = 0, s.phase = kWalking, s.n = 0, s.next = 0, s.known = 0, s.turn = 0;
         }
     }
-    __syncthreads();
+    lds_barrier();
 }
 
 // pieces: (2, n_seq, kMostPieces), walks: (2, n_seq), in turn: the other launch's are being read
@@ -269,7 +282,7 @@ __global__ void __launch_bounds__(kThreads) round_kernel(VerifyArgs a, Between b
         }
     }
     if (blockIdx.x == 0) {
-        __syncthreads();
+        lds_barrier();
         if (threadIdx.x == 0) *to = s;
     }
 }
@@ -295,7 +308,7 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(VerifyArgs a, Between be
             const Sums v = add_up(s, in, i * per, min((i + 1) * per, in.V), part[i & 1]);
             if (tid == 0) own[i] = v;
         }
-        __syncthreads();
+        lds_barrier();
     };
     if (s.phase == kWaiting) {
         Sums got = total_of(between.pieces + (s.turn * a.n_seq + b) * kMostPieces, pieces);
@@ -306,16 +319,16 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(VerifyArgs a, Between be
             got = total_of(own, pieces);
             go_on(s, a, in, got, out, node, blockIdx.x);
             if (tid == 0 && s.phase == kDecided && s.known) s.turn = -1;
-            __syncthreads();
+            lds_barrier();
         }
     }
     if (!s.known) {
         add_all();
         if (tid == 0) s.turn = -1;
-        __syncthreads();
+        lds_barrier();
     }
     for (int i = tid; i < pieces && s.turn >= 0; i += kThreads) own[i] = between.pieces[(s.turn * a.n_seq + b) * kMostPieces + i];
-    __syncthreads();
+    lds_barrier();
 
     // ---- the piece in which the sums pass u times their total; the last that has any (the last bits of the sums)
     const double total = total_of(own, pieces).first, bound = (double)u * total;
@@ -324,20 +337,15 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(VerifyArgs a, Between be
         int at = -1;
         for (int i0 = 0; i0 < pieces && (at < 0 || !(at_before + own[at].first > bound)); i0 += 64) {
             const double x = i0 + lane < pieces ? own[i0 + lane].first : 0.0;
-            double to = x;
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const double o = __shfl_up(to, d);
-                to += lane >= d ? o : 0.0;
-            }
+            const double to = wave_prefix(x);
             const uint64_t some = __ballot(x > 0.0), there = __ballot(x > 0.0 && before + (to - x) + x > bound);
             const int l = there ? __builtin_ctzll(there) : some ? 63 - __builtin_clzll(some) : -1;
-            if (l >= 0) at = i0 + l, at_before = before + __shfl(to - x, l);
-            before += __shfl(to, 63);
+            if (l >= 0) at = i0 + l, at_before = before + lane_of(to - x, l);
+            before += lane_of(to, 63);
         }
         if (lane == 0) piece = total > 0.0 ? at : -1, before_piece = at_before;
     }
-    __syncthreads();
+    lds_barrier();
     int32_t token = -1;
     if (piece >= 0) {
         const float *p = in.p_of(s.w), *q = in.q_of(s.w);
@@ -354,16 +362,11 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(VerifyArgs a, Between be
 #pragma unroll
                 for (int i = 0; i < 4; ++i) x[4 * j + i] = v + 4 * j + i < end ? xs[i] : 0.0, mine += x[4 * j + i];
             }
-            double to = mine;
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const double o = __shfl_up(to, d);
-                to += lane >= d ? o : 0.0;
-            }
-            __syncthreads();
+            const double to = wave_prefix(mine);
+            lds_barrier();
             if (lane == 63) part[0][wave] = to;
             if (tid == 0) found = INT32_MAX, last = -1;
-            __syncthreads();
+            lds_barrier();
             double at = before + (to - mine);
 #pragma unroll
             for (int w = 0; w < kWaves; ++w) at += w < wave ? part[0][w] : 0.0, before += part[0][w];
@@ -378,7 +381,7 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(VerifyArgs a, Between be
             }
             if (there < INT32_MAX) atomicMin(&found, there);
             if (some >= 0) atomicMax(&last, some);
-            __syncthreads();
+            lds_barrier();
             if (found < INT32_MAX) token = found;
             else if (last >= 0) token = last;
             if (found < INT32_MAX) break;
