@@ -1,5 +1,5 @@
 // The way into low-rank adapters of many requests (mamba_linear_adapted_fwd): t[m, r] = scale[a] sum_k x[m, k] A[a, r, k], a = idx[m] the
-// adapter of row m.  The way out, t B^T, is part of the shared product's own kernel (linear.hip).
+// adapter of row m.  The way out, t B^T, is part of the shared product's own kernel (linear.hip; for one row both are).
 //
 // t leaves as two bfloat16 terms, high and low, side by side: the product with B has its 16 bits then, more than the output keeps.
 #include "device_math.h"
@@ -31,7 +31,7 @@ __device__ __forceinline__ void lds_barrier()
 // blockIdx.y-th on, so that rows of many adapters are not multiplied by one after the other.  A row's sums are written by who has its adapter.
 // Of the W wavefronts G go by rows, W / G by k: slabs of as many k as give each of those 32, four of them in LDS, straight from memory, a
 // row's 16-byte slot c at c ^ (row / 2 & 7).
-// Bound by x from memory where there are many rows, by trips to memory where there are few.  us: one row, K = 1536, rank 8 3.9; 333 rows, K = 768, rank 16
+// Bound by x from memory where there are many rows, by trips to memory where there are few.  us: 24 rows, K = 768, 8 adapters of rank 16 4.3; 333 rows, K = 768, rank 16
 // 4.3; 4097 rows, K = 1024, 16 adapters of rank 64 in runs 9.2; 16384 rows, K = 2048, 32 of rank 32 32 (2.1 TB/s; 64 rows to a workgroup 37, slabs of
 // twice the k 34, workgroups that begin at different k, for the sake of the memory's channels, the same).
 template <int RT, int G, int W>

@@ -21,6 +21,7 @@
 // chunks (+ residual), so that stores are coalesced; output splits that are not multiples of 8
 // columns take an element-wise path.
 #include <algorithm>
+#include <tuple>
 #include <type_traits>
 
 #include "conv_lane.h"
@@ -1147,7 +1148,7 @@ linear_ring_kernel(const bf16_t *x, const bf16_t *w, const float *__restrict__ b
 typedef float f32x4v __attribute__((ext_vector_type(4)));
 
 // Adapters of the rows of a tile: wavefront q multiplies by every NW-th of them, into partial tiles that are added up anyway.
-// us, with an adapter and without: 1 x 768, K = 1536, rank 8 3.6 and 3.1, 333 x 1536, K = 768, rank 16 7.8 and 6.3: one more trip to memory.
+// us, with an adapter and without: 333 x 1536, K = 768, rank 16 7.8 and 6.3: one more trip to memory.
 template <int NW, int MT, int NT>
 __device__ __forceinline__ void add_adapters_few(f32x4v (&acc)[MT][NT], const AdapterTail &t, int wave, int m0, int M, int n0, int N)
 {
@@ -1200,6 +1201,22 @@ __device__ __forceinline__ void add_adapters_few(f32x4v (&acc)[MT][NT], const Ad
 // EVEN: K = 64 NW G, one trip of every wavefront; otherwise any K that is a multiple of 8.
 // STREAM: w is read once and is large (the LM head on a draft position): its loads are streaming, so that they do not push the
 // blocks' weights, which the next position reads again, out of the last-level cache.
+// One row with its adapter in one launch: A's ranks are RT more column tiles of the product, the sums of which every workgroup has for itself, and the outputs
+// take t B^T on their way, t in float32.  1 x 768, K = 1536, rank 8: 4.3 us under the profiler, 3.1 without an adapter.
+template <int R> struct OneRowTail {
+    static constexpr int RT = R;
+    const bf16_t *a, *b;
+    const float *scale;
+    const int32_t *idx;
+    int32_t rank, adapters;
+};
+template <typename... Tail> struct RankTiles {
+    static constexpr int n = 0;
+};
+template <int R> struct RankTiles<OneRowTail<R>> {
+    static constexpr int n = R;
+};
+
 template <int MT, int CG, int NW, int G, bool EVEN, bool STREAM, typename... Tail>
 __global__ void __launch_bounds__(64 * NW)
 linear_few_kernel(const bf16_t *__restrict__ x, const bf16_t *__restrict__ w, const float *__restrict__ bias,
@@ -1208,11 +1225,12 @@ linear_few_kernel(const bf16_t *__restrict__ x, const bf16_t *__restrict__ w, co
     constexpr bool kAdapted = sizeof...(Tail) > 0;
     constexpr int kThr = NW * 64;
     constexpr int NT = (CG + 1) / 2;                               // column tiles of 16
-    constexpr int kStep = (NT + MT) * 2048;                        // fragments of one step: NT column tiles of w, then MT row tiles
+    constexpr int RT = RankTiles<Tail...>::n, NA = NT + RT, CA = CG + 2 * RT;   // column tiles of w and A, groups of 8 rows of them
+    constexpr int kStep = (NA + MT) * 2048;                        // fragments of one step: NT column tiles of w, RT of A, then MT row tiles
     constexpr int PB = G * NW * kStep <= 32 * 1024 ? G : 1;        // patches in turn: several workgroups to a CU
     constexpr int OPT = (MT * NT * 256 + kThr - 1) / kThr;         // outputs per thread
     // a wavefront's patches, and its partial tiles once it is done with those
-    constexpr int kWave = PB * kStep > MT * NT * 1024 ? PB * kStep : MT * NT * 1024;
+    constexpr int kWave = PB * kStep > MT * NA * 1024 ? PB * kStep : MT * NA * 1024;
     __shared__ __attribute__((aligned(16))) unsigned char patch[NW][kWave];
     const unsigned tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -1235,6 +1253,23 @@ linear_few_kernel(const bf16_t *__restrict__ x, const bf16_t *__restrict__ w, co
         bias_in[j] = (bias ? bias : reinterpret_cast<const float *>(x))[bias ? col : 0u];
         res[j] = (residual ? residual : x)[residual ? (int64_t)min(om[j], M - 1) * N + col : 0];   // single output tensor
     }
+    // the row's adapter (0 stands in for none) and its B for this thread's outputs, asked for behind the first of w and x
+    static_assert(RT == 0 || (MT == 1 && OPT == 1), "one row");
+    int32_t id = 0, of = 0, rank = 0;
+    u32x4 b_in[RT > 0 ? 2 * RT : 1];
+    float scale = 1.0f;
+    const char *ab = nullptr;
+    auto look_up = [&](const auto &t) __attribute__((always_inline)) {
+        id = __builtin_amdgcn_readfirstlane(t.idx[0]);
+        of = id >= 0 && id < t.adapters ? id : 0;
+        if (t.scale) scale = t.scale[of];
+        ab = reinterpret_cast<const char *>(t.a + (int64_t)of * rank * K);
+        const bf16_t *b = t.b + ((int64_t)of * N + min(on[0], N - 1)) * rank;
+#pragma unroll
+        for (int c = 0; c < 2 * RT; ++c) b_in[c] = *reinterpret_cast<const u32x4 *>(b + 8 * min(c, rank / 8 - 1));
+        id = id >= t.adapters ? -2 : id;
+    };
+    if constexpr (RT > 0) rank = std::get<0>(std::tie(tail...)).rank;
     __builtin_amdgcn_sched_barrier(0);
 
     // ---- the wavefront's share of k: steps [s_first, s_end)
@@ -1242,13 +1277,19 @@ linear_few_kernel(const bf16_t *__restrict__ x, const bf16_t *__restrict__ w, co
     const int s_first = wave * per, s_end = EVEN || s_first + per < steps ? s_first + per : steps;
     const unsigned kchunks = (unsigned)K >> 3;                     // K % 8 == 0
     const char *wb = reinterpret_cast<const char *>(w + (int64_t)n0 * K), *xb = reinterpret_cast<const char *>(x + (int64_t)m0 * K);
-    unsigned wo[CG], xo[2 * MT];
-    int64_t wfar[CG], xfar[2 * MT];
+    unsigned wo[CA], xo[2 * MT];
+    int64_t wfar[CA], xfar[2 * MT];
 #pragma unroll
     for (unsigned t = 0; t < CG; ++t) {
         const unsigned r = min(8 * t + lrow, (unsigned)(N - 1 - n0));
         wo[t] = r * (2u * (unsigned)K) + 16 * lch;
         wfar[t] = (int64_t)r * 2 * K + 16 * lch;
+    }
+#pragma unroll
+    for (unsigned t = 0; t < 2 * RT; ++t) {
+        const unsigned r = min(8 * t + lrow, (unsigned)(rank - 1));
+        wo[CG + t] = r * (2u * (unsigned)K) + 16 * lch;
+        wfar[CG + t] = (int64_t)r * 2 * K + 16 * lch;
     }
 #pragma unroll
     for (unsigned t = 0; t < 2 * MT; ++t) {
@@ -1259,15 +1300,15 @@ linear_few_kernel(const bf16_t *__restrict__ x, const bf16_t *__restrict__ w, co
     const unsigned put = (lrow * 8 + (lch ^ lrow)) * 16;           // + 1024 t: chunks xor-swizzled by the row, no bank conflicts either way
     const unsigned get0 = (li * 8 + (lg ^ (li & 7))) * 16, get1 = (li * 8 + ((lg + 4) ^ (li & 7))) * 16;
 
-    f32x4v acc[MT][NT];
+    f32x4v acc[MT][NA];
 #pragma unroll
     for (int t = 0; t < MT; ++t)
 #pragma unroll
-        for (int n = 0; n < NT; ++n) acc[t][n] = f32x4v(0.0f);
+        for (int n = 0; n < NA; ++n) acc[t][n] = f32x4v(0.0f);
     bool first = true;
     for (int s0 = s_first; EVEN ? first : s0 < s_end; s0 += G) {
         first = false;
-        u32x4 wf[G][CG], xf[G][2 * MT];
+        u32x4 wf[G][CA], xf[G][2 * MT];
 #pragma unroll
         for (int g = 0; g < G; ++g) {
             const int s = EVEN || s0 + g < s_end ? s0 + g : 0;
@@ -1281,6 +1322,17 @@ linear_few_kernel(const bf16_t *__restrict__ x, const bf16_t *__restrict__ w, co
 #pragma unroll
             for (int t = 0; t < 2 * MT; ++t) xf[g][t] = *reinterpret_cast<const u32x4 *>(EVEN ? xs + xo[t] : xs + (xfar[t] - back));
         }
+        if constexpr (RT > 0) {
+            __builtin_amdgcn_sched_barrier(0);
+            if (s0 == s_first) look_up(tail...);
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                const int s = EVEN || s0 + g < s_end ? s0 + g : 0;
+                const unsigned back = EVEN || 8u * (unsigned)s + lch < kchunks ? 0u : 16 * lch;
+#pragma unroll
+                for (int t = CG; t < CA; ++t) wf[g][t] = *reinterpret_cast<const u32x4 *>(ab + (int64_t)s * 128 + (EVEN ? (int64_t)wo[t] : wfar[t] - back));
+            }
+        }
         __builtin_amdgcn_sched_barrier(0);                         // all of it in flight before any of it is used
         if (s0 == s_first) args_here(out.ptr[0], out.ptr[1], out.ptr[2], out.width[0], out.width[1], out.width[2]);
         auto fill = [&](int g) __attribute__((always_inline)) {
@@ -1289,21 +1341,23 @@ linear_few_kernel(const bf16_t *__restrict__ x, const bf16_t *__restrict__ w, co
 #pragma unroll
             for (int t = 0; t < CG; ++t) *reinterpret_cast<u32x4 *>(p + 1024 * t + put) = ok ? wf[g][t] : u32x4(0u);
 #pragma unroll
-            for (int t = 0; t < 2 * MT; ++t) *reinterpret_cast<u32x4 *>(p + 2048 * NT + 1024 * t + put) = ok ? xf[g][t] : u32x4(0u);
+            for (int t = CG; t < CA; ++t) *reinterpret_cast<u32x4 *>(p + 2048 * NT + 1024 * (t - CG) + put) = ok ? wf[g][t] : u32x4(0u);
+#pragma unroll
+            for (int t = 0; t < 2 * MT; ++t) *reinterpret_cast<u32x4 *>(p + 2048 * NA + 1024 * t + put) = ok ? xf[g][t] : u32x4(0u);
         };
         auto product = [&](int g) __attribute__((always_inline)) {
             const unsigned char *p = patch[wave] + g % PB * kStep;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const unsigned get = h ? get1 : get0;
-                bf16x8 wv[NT];
+                bf16x8 wv[NA];
 #pragma unroll
-                for (int n = 0; n < NT; ++n) wv[n] = *reinterpret_cast<const bf16x8 *>(p + 2048 * n + get);
+                for (int n = 0; n < NA; ++n) wv[n] = *reinterpret_cast<const bf16x8 *>(p + 2048 * n + get);
 #pragma unroll
                 for (int t = 0; t < MT; ++t) {
-                    const bf16x8 xv = *reinterpret_cast<const bf16x8 *>(p + 2048 * (NT + t) + get);
+                    const bf16x8 xv = *reinterpret_cast<const bf16x8 *>(p + 2048 * (NA + t) + get);
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) acc[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xv, wv[n], acc[t][n], 0, 0, 0);
+                    for (int n = 0; n < NA; ++n) acc[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xv, wv[n], acc[t][n], 0, 0, 0);
                 }
             }
         };
@@ -1321,17 +1375,37 @@ linear_few_kernel(const bf16_t *__restrict__ x, const bf16_t *__restrict__ w, co
             wave_sync();
         }
     }
-    if constexpr (kAdapted) add_adapters_few<NW>(acc, tail..., wave, m0, M, n0, N);
+    if constexpr (RT > 0 && !EVEN) {
+        if (s_first >= s_end) look_up(tail...);                    // (a wavefront without a share of k has outputs all the same)
+    }
+    if constexpr (kAdapted && RT == 0) add_adapters_few<NW>(acc, tail..., wave, m0, M, n0, N);
     // acc[t][n][i] is C[m = 16 t + 4 (lane / 16) + i][16 n + lane % 16]
 #pragma unroll
     for (int t = 0; t < MT; ++t)
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int n = 0; n < NA; ++n)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) reinterpret_cast<float *>(patch[wave])[(4 * (t * NT + n) + i) * 64 + lane] = acc[t][n][i];
+            for (int i = 0; i < 4; ++i) reinterpret_cast<float *>(patch[wave])[(4 * (t * NA + n) + i) * 64 + lane] = acc[t][n][i];
 #pragma unroll
     for (int j = 0; j < OPT; ++j) values_here(bias_in[j]);
     lds_barrier_linear();
+    float plus = 0.0f;
+    if constexpr (RT > 0) {
+        // t: row 0 of A's tiles
+        __shared__ float t_row[16 * RT];
+        if (tid < 16 * RT) {
+            float v = 0.0f;
+#pragma unroll
+            for (int q = 0; q < NW; ++q) v += reinterpret_cast<const float *>(patch[q])[4 * (NT + (tid >> 4)) * 64 + (tid & 15)];
+            t_row[tid] = (int)tid < rank ? v * scale : 0.0f;
+        }
+        lds_barrier_linear();
+#pragma unroll
+        for (int c = 0; c < 2 * RT; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) plus += t_row[8 * c + 2 * i] * bf16_lo(b_in[c][i]), plus += t_row[8 * c + 2 * i + 1] * bf16_hi(b_in[c][i]);
+        plus = id >= 0 ? plus : id == -1 ? 0.0f : __int_as_float(0x7fc00000);
+    }
 
 #pragma unroll
     for (int j = 0; j < OPT; ++j) {
@@ -1340,6 +1414,7 @@ linear_few_kernel(const bf16_t *__restrict__ x, const bf16_t *__restrict__ w, co
 #pragma unroll
         for (int q = 0; q < NW; ++q) v += reinterpret_cast<const float *>(patch[q])[at];
         if (o6 >= 4 * MT * NT || om[j] >= M || on[j] >= N || li >= 8 * CG) continue;
+        if constexpr (RT > 0) v += plus;
         if constexpr (kAdapted) v = v + (bias ? bias_in[j] : 0.0f) + (residual ? bf16_to_f32(res[j]) : 0.0f);
         else v = bf16_to_f32(f32_to_bf16(v + (bias ? bias_in[j] : 0.0f)));   // same two roundings as the tiled kernel
         if (!kAdapted && residual) {
@@ -1450,8 +1525,41 @@ template <typename... Tail> hipError_t launch_product(const LinearArgs &a, hipSt
 
 hipError_t launch_linear(const LinearArgs &a, hipStream_t stream) { return a.norm_w ? launch_draft_in(a, stream) : launch_product(a, stream); }
 
+namespace {
+
+// One row in one launch; *fits: it does, and costs less than two.  Every workgroup reads all of the adapter's A.  us, in a chain of graph replays, by the
+// rank (two launches): 768 columns, K = 1536: 8 3.6 (7.0), 32 4.5 (7.2); 2304, 768: 8 2.9 (5.9), 32 3.5 (6.1); 4096, 4096: 16 9.9 (14.0), 32 11.6 (14.1);
+// 8192, 2048: 16 9.6 (12.5), but 32 13.5 (12.4); 50280, 768: 16 18.0 (17.7), 32 27.2 (18.2).
+template <int RT> hipError_t launch_one_row(const LinearArgs &a, const AdapterArgs &l, hipStream_t stream, bool *fits)
+{
+    OutSplit o;
+    for (int s = 0; s < 3; ++s) {
+        o.ptr[s] = static_cast<bf16_t *>(a.out[s]);
+        o.width[s] = a.width[s];
+    }
+    const int64_t N = a.width[0] + a.width[1] + a.width[2];
+    const bf16_t *x = static_cast<const bf16_t *>(a.x), *w = static_cast<const bf16_t *>(a.w), *res = static_cast<const bf16_t *>(a.residual);
+    const OneRowTail<RT> tail{static_cast<const bf16_t *>(l.a), static_cast<const bf16_t *>(l.b), l.scale, l.idx, (int32_t)l.rank, (int32_t)l.adapters};
+    const LinearKernel kernel = linear_route(a.M, a.width, a.K);
+    *fits = (kernel == kFew16x8 ? (N + 7) / 8 : (N + 15) / 16) * RT <= 768;   // (workgroups and tiles of 16 ranks)
+    if (!*fits) return hipSuccess;
+    switch (kernel) {
+    case kFew16x16Stream: return launch_few<1, 2, true>(x, w, a.bias, res, o, a.M, N, a.K, stream, tail);
+    case kFew16x8: return launch_few<1, 1>(x, w, a.bias, res, o, a.M, N, a.K, stream, tail);
+    case kFew16x16: return launch_few<1, 2>(x, w, a.bias, res, o, a.M, N, a.K, stream, tail);
+    default: *fits = false; return hipSuccess;
+    }
+}
+
+}  // namespace
+
 hipError_t launch_linear_adapted(const LinearArgs &a, const AdapterArgs &l, hipStream_t stream)
 {
+    if (a.M == 1 && l.rank <= 32) {
+        bool fits;
+        const hipError_t e = l.rank <= 16 ? launch_one_row<1>(a, l, stream, &fits) : launch_one_row<2>(a, l, stream, &fits);
+        if (fits) return e;
+    }
     if (const hipError_t e = launch_adapters_down(a.x, l, a.M, a.K, stream)) return e;
     return launch_product(a, stream, AdapterTail{static_cast<const bf16_t *>(l.t), static_cast<const bf16_t *>(l.b), l.idx, static_cast<const bf16_t *>(l.zeros), (int32_t)l.rank, (int32_t)l.adapters});
 }

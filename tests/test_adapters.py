@@ -131,6 +131,28 @@ def test_rows_without_an_adapter_are_the_plain_product(m, M, K, N):
 
 
 @gpu
+@pytest.mark.parametrize("rank", [8, 16, 24, 32, 40])
+@pytest.mark.parametrize("K,N,splits", [(8, 3, None), (64, 40, None), (72, 33, (1, 31, 1)), (256, 2050, None), (512, 768, None), (768, 2304, (768, 768, 768)), (1000, 96, None), (2056, 12345, None),
+                                        (768, 50280, None), (4096, 1024, None)])
+def test_one_row(m, K, N, splits, rank):
+    """A single request's row: its adapter, another one, none, one that is not there; what is no number in an adapter of its own and of another."""
+    rng = np.random.default_rng(K + N + rank)
+    c = inputs(rng, 1, K, N, rank, 3, bias=True, residual=splits is None)
+    for at in (0, 2, -1, 3, -2):
+        c["adapter_idx"].fill_(at)
+        check(m, c, splits)
+    c["adapter_idx"].fill_(1)
+    clean = m.mamba_linear_adapted_fwd(**c, splits=splits)
+    c["lora_a"][2, rank - 1, K - 1], c["lora_b"][0] = float("nan"), float("inf")
+    assert all(torch.equal(x, y) for x, y in zip(clean, m.mamba_linear_adapted_fwd(**c, splits=splits)))
+    c["lora_b"][1, N - 1, rank - 1] = float("nan")
+    got = torch.cat(m.mamba_linear_adapted_fwd(**c, splits=splits), 1)
+    assert bool(torch.isnan(got[0, N - 1])) and torch.equal(got[:, :N - 1], torch.cat(clean, 1)[:, :N - 1])
+    c["adapter_idx"].fill_(2)
+    assert bool(torch.isnan(torch.cat(m.mamba_linear_adapted_fwd(**c, splits=splits), 1).float()).all())
+
+
+@gpu
 @pytest.mark.parametrize("M,K,N", [(20, 256, 96), (700, 768, 768), (3000, 256, 512), (900, 72, 100)])
 def test_indices_out_of_range_and_what_is_no_number(m, M, K, N):
     """A row whose adapter is out of range is NaN; infinities and NaN of an adapter, of a row, stay where they belong."""
