@@ -488,9 +488,9 @@ struct RowCut {
 };
 
 // ---- the cut, and the draws: one workgroup to a row
-// Bound by what follows one another.  One row of 50280, top-p, one child, 12 us: the row's sums 2.1, units of the tokens 0.7, the cut 3.8, sums of the chunks
-// 1.8, the child 3.1.  A further child costs 2.6 (its chunk 0.2, the chunk's tokens 0.5, their weights and sums 1.2, the next one's sums 0.9), a cut of
-// another kind 2.2.  96 rows of three children 19, 128 rows of 131071 20.  (A part of a range found by all 16 wavefronts in place of one: 0.7 us
+// Bound by what follows one another.  One row of 50280, top-p, one child, 11 us: the row's sums 2.1, units of the tokens 0.7, the cut 3.6, sums of the chunks
+// 1.8, the child 2.3.  A further child costs 2.2 (its chunk 0.8, the chunk's tokens 0.5, their weights and sums 0.6, the rest 0.3), a cut of
+// another kind 2.2.  96 rows of three children 18, 128 rows of 131071 18.  (A part of a range found by all 16 wavefronts in place of one: 0.7 us
 // slower; prefix sums of four wavefronts share a SIMD's issue.)
 constexpr int kFew = 64;                                             // places that a wavefront looks through
 constexpr int kFine = 1024;                                          // parts that a range of places is cut into
@@ -512,7 +512,8 @@ struct RowShared {
     u64 few[kFew], few_mass[kFew];
     u64 lo, hi, need, before, cut, found, sum;
     uint32_t n_few, n;
-    int32_t chunk;
+    int32_t chunk;                                                   // of the next child (-1: nothing is left, -2: the rest is to be weighed anew)
+    double inv_sum;
 };
 
 // prefix sums over the workgroup, without the thread's own; the whole sum in *total.  FREE: nobody reads parts any more.
@@ -811,6 +812,7 @@ draw_kernel(const T *__restrict__ logits, Chunks from, const RowBins *__restrict
     const CutBins c = rows[m].cuts;
     if (tid < kBins) s.bins.mass[tid] = rows[m].mass[tid], s.bins.number[tid] = rows[m].number[tid];
     if (tid < chunks) s.scale[tid] = scales[m * chunks + tid];
+    if (tid == 0) s.inv_sum = 0.0;
     if (tid < 8) s.drawn[tid] = 0, s.u[tid] = tid < a.k ? a.u[m * a.k + tid] : 0.0f;
     const u64 first_place = tid < (int)n && tid < kList ? list[m * kList + tid] : 0;
     const Settings r = settings_of(a, m);
@@ -840,31 +842,27 @@ draw_kernel(const T *__restrict__ logits, Chunks from, const RowBins *__restrict
         if (n <= kList || cut.bin == kBins) chunk_sums(s, from, m, chunks, cut, row, held);
     }
 
-    // ---- the draws: the chunk by every wavefront for itself, the token by all of them
-    double inv_sum = 0.0;
-    const int per = (chunks + 63) / 64, lane = tid & 63;             // chunks to a lane
-    auto mass_of = [&](int i) { return i < chunks ? scaled(s.chunk_mass[i], s.scale[i].factor) : 0; };
-    auto prefix_of_chunks = [&](u64 *mine) {
-        u64 sum = 0;
+    // ---- the draws: the chunk by one wavefront (by all of them, alike, it took 0.3 us longer: they share the SIMDs' issue), the token by all
+    const int per = (chunks + 63) / 64, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);   // chunks to a lane
+    auto choose = [&](int j, bool weighed_anew) {
+        auto mass_of = [&](int i) { return i < chunks ? scaled(s.chunk_mass[i], s.scale[i].factor) : 0; };
+        u64 mine = 0;
 #pragma unroll 1
-        for (int i = 0; i < per; ++i) sum += mass_of(lane * per + i);
-        *mine = sum;
-        return wave_prefix(sum);
-    };
-#pragma unroll 1
-    for (int j = 0; some && j < a.k; ++j) {
-        const float u = s.u[j];
-        u64 mine, to = prefix_of_chunks(&mine), left = lane_of(to, 63);
-        if (j == 0) inv_sum = 1.0 / __builtin_ldexp((double)left, -scale);
+        for (int i = 0; i < per; ++i) mine += mass_of(lane * per + i);
+        const u64 to = wave_prefix(mine), left = lane_of(to, 63);
+        if (j == 0) s.inv_sum = 1.0 / __builtin_ldexp((double)left, -scale);
         // (that the last of what is kept was drawn, with nothing left, says that all of it was)
         bool out = left == 0 && cut.place != 0;
         for (int d = 0, is = 0; out && d < j; ++d) is |= s.drawn[d] == cut.place, out = d + 1 < j || is;
-        if (j > 0 && left < (r.top_k > 0 && r.top_k <= 1024 ? (u64)1 << 30 : (u64)1 << 39) && !out) {
-            const Row<T> row_there = row;
-            sums_of_the_rest(s, row_there, cut.place, j, top, chunks);
-            to = prefix_of_chunks(&mine), left = lane_of(to, 63);
+        if (j > 0 && !weighed_anew && left < (r.top_k > 0 && r.top_k <= 1024 ? (u64)1 << 30 : (u64)1 << 39) && !out) {
+            s.chunk = -2;
+            return;
         }
-        if (left == 0) break;                                        // (the same for all threads, and for good: nothing is left)
+        if (left == 0) {
+            s.chunk = -1;
+            return;
+        }
+        const float u = s.u[j];
         const u64 f = !(u > 0.0f) ? 0 : u >= 1.0f ? ~(u64)0 : (u64)((double)u * 18446744073709551616.0);
         const u64 bound = __umul64hi(left, f);                       // the sum that is to be passed
         int chunk = __builtin_ctzll(__ballot(to > bound));
@@ -874,7 +872,22 @@ draw_kernel(const T *__restrict__ logits, Chunks from, const RowBins *__restrict
             const int at = __builtin_ctzll(__ballot(to_one > bound));
             chunk = chunk * per + at, ahead = lane_of(to_one - one, at);
         }
-        const u64 inside = min((u64)((double)(bound - ahead) / s.scale[chunk].factor), s.chunk_mass[chunk] - 1);
+        s.chunk = chunk;
+        s.need = min((u64)((double)(bound - ahead) / s.scale[chunk].factor), s.chunk_mass[chunk] - 1);
+    };
+#pragma unroll 1
+    for (int j = 0; some && j < a.k; ++j) {
+        if (wave == 0) choose(j, false);
+        lds_barrier();
+        if (s.chunk == -2) {
+            const Row<T> row_there = row;
+            sums_of_the_rest(s, row_there, cut.place, j, top, chunks);
+            if (wave == 0) choose(j, true);
+            lds_barrier();
+        }
+        const int chunk = s.chunk;
+        if (chunk < 0) break;                                        // (for good)
+        const u64 inside = s.need;
         const int32_t first = chunk * kSlice + 2 * tid;
         const float most = s.scale[chunk].most;
         float v[2];
@@ -893,7 +906,7 @@ draw_kernel(const T *__restrict__ logits, Chunks from, const RowBins *__restrict
         }
 #pragma unroll
         for (int i = 0; i < 2; ++i) sum += w[i];
-        u64 start = wide_prefix<true>(sum, s.wave_part, &all);       // (every read of the chunks' sums is behind its barrier)
+        u64 start = wide_prefix<true>(sum, s.wave_part, &all);       // (of the chunks' sums nothing is read by then)
         if (start <= inside && inside < start + sum) {               // one thread
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
@@ -904,20 +917,20 @@ draw_kernel(const T *__restrict__ logits, Chunks from, const RowBins *__restrict
         lds_barrier();
     }
     // a wavefront to a child
-    if (const int j = __builtin_amdgcn_readfirstlane(tid >> 6); j < a.k) {
+    if (const int j = wave; j < a.k) {
         const u64 place = s.drawn[j];
         const int64_t out = m * a.k + j;
         const int32_t token = place ? order.token(place) : -1;
         if (lane == 0) {
             a.idx[out] = token;
-            a.prob[out] = place ? (float)(row.weights.of(order.logit(place), top) * inv_sum) : 0.0f;
+            a.prob[out] = place ? (float)(row.weights.of(order.logit(place), top) * s.inv_sum) : 0.0f;
         }
         if (a.path_out)
             for (int64_t t = lane; t <= a.path_len; t += 64) a.path_out[out * (a.path_len + 1) + t] = t < a.path_len ? a.path[m * a.path_len + t] : token;
     }
     if (tid == 0 && a.dist) {
         const bool all = cut.place == 0;
-        cuts[m] = RowCut{inv_sum, all ? -INFINITY : order.logit(cut.place), all ? -1 : order.token(cut.place), top, !r.known ? -1 : some ? 1 : 0};
+        cuts[m] = RowCut{s.inv_sum, all ? -INFINITY : order.logit(cut.place), all ? -1 : order.token(cut.place), top, !r.known ? -1 : some ? 1 : 0};
     }
 }
 
