@@ -113,6 +113,16 @@ def test_many_rows(m, M, K, N, splits):
 
 
 @gpu
+@pytest.mark.parametrize("M,K,N,n,rank", [(16, 512, 768, 16, 16), (40, 256, 130, 37, 24), (64, 512, 9000, 64, 8), (333, 768, 1536, 333, 8), (700, 768, 1536, 300, 16), (2100, 1024, 2048, 150, 8),
+                                          (4100, 1536, 768, 40, 40), (9000, 512, 512, 1000, 8), (1500, 72, 100, 90, 16)])
+def test_rows_of_many_adapters(m, M, K, N, n, rank):
+    """Every row of a tile with an adapter of its own, and rows in no order."""
+    rng = np.random.default_rng(M + n)
+    for rows in ("own", "mixed"):
+        check(m, inputs(rng, M, K, N, rank, n, rows))
+
+
+@gpu
 @pytest.mark.parametrize("M,K,N", [(24, 768, 50280), (2, 2048, 131071), (70, 512, 9000), (16, 2056, 12345)])
 def test_vocabularies(m, M, K, N):
     rng = np.random.default_rng(N)
@@ -216,6 +226,27 @@ def test_streams_and_graphs(m):
             torch.cuda.synchronize()
             assert torch.equal(out, m.mamba_linear_adapted_fwd(**c)[0])
             c["adapter_idx"].copy_(torch.randint(-1, 8, (M,), device=DEV))
+
+
+@gpu
+@pytest.mark.parametrize("M,K,N,n,rank", [(1, 64, 12288, 12000, 16), (3, 64, 1000003, 40, 64), (300, 128, 1000064, 40, 64)])
+def test_long_offsets(m, M, K, N, n, rank):
+    """Adapters whose offsets pass 32 bits: as the same ones by themselves."""
+    if torch.cuda.mem_get_info()[0] < 30 << 30:
+        pytest.skip("needs 30 GB")
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(n)
+    normal = lambda *s, std=1.0: torch.empty(*s, dtype=BF16, device=DEV).normal_(0.0, std, generator=gen)
+    x, w, a, b = normal(M, K), normal(N, K, std=K ** -0.5), normal(n, rank, K, std=K ** -0.5), normal(n, N, rank, std=rank ** -0.5)
+    used = torch.tensor([n - 1, 0, n - 2], device=DEV)
+    which = torch.arange(M, device=DEV) % 3
+    (got,) = m.mamba_linear_adapted_fwd(x, w, a, b, used[which].int())
+    (ref,) = m.mamba_linear_adapted_fwd(x, w, a[used].contiguous(), b[used].contiguous(), which.int())
+    assert torch.equal(got, ref)
+    del b
+    ends = torch.tensor([0, 1, N // 2, N - 1], device=DEV)
+    plain = x.double() @ w[ends].double().t()
+    assert not bool((got[:, ends].double() - plain).abs().max() < 0.1)                # (they add something everywhere that counts)
 
 
 @gpu

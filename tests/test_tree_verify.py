@@ -139,6 +139,25 @@ def test_large_vocabularies(m):
 
 
 @gpu
+def test_long_offsets(m):
+    """Sequences whose offsets pass 32 bits: as each by itself."""
+    S, V, tree = 1100, (1 << 20) + 3, (1, 1)
+    if torch.cuda.mem_get_info()[0] < 30 << 30:
+        pytest.skip("needs 30 GB")
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(2)
+    p, q = torch.rand(S, 3, V, device=DEV, generator=gen), torch.rand(S, 2, V, device=DEV, generator=gen)
+    tokens = torch.randint(0, V, (S, 2), device=DEV, generator=gen, dtype=torch.int32)
+    ua, us = torch.rand(S, 2, device=DEV, generator=gen), torch.rand(S, device=DEV, generator=gen)
+    got = m.mamba_tree_verify_fwd(p, q, tokens, ua, us, tree)
+    for b in (0, 682, 1023, S - 1):
+        at = slice(b, b + 1)
+        one = m.mamba_tree_verify_fwd(p[at].clone(), q[at].clone(), tokens[at].clone(), ua[at].clone(), us[at].clone(), tree)
+        assert all(torch.equal(x[at], y) for x, y in zip(got, one)), b
+    assert bool(((got[0] >= 0).sum(1) == got[1]).all()) and len(got[1].unique()) > 1
+
+
+@gpu
 def test_more_rejections_than_rounds(m):
     """Children that the target does not want, fifteen of them on one way."""
     rng = np.random.default_rng(15)
