@@ -424,7 +424,7 @@ __global__ void __launch_bounds__(kWide) plan_kernel(Chunks from, RowBins *__res
 }
 
 // ---- the tokens of those bins: a workgroup to a chunk
-// The row once more, against a range of logits for every cut.  128 rows of 131071 float32 logits 13 us (5.1 TB/s, from the last-level cache in part), one
+// The row once more, against a range of marks for every cut.  128 rows of 131071 float32 logits 13 us (5.1 TB/s, from the last-level cache in part), one
 // row 3 to 4: the launch and three trips to memory.
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
@@ -441,17 +441,15 @@ gather_kernel(const T *__restrict__ logits, RowBins *__restrict__ rows, u64 *__r
     if (tid == 0) found = 0;
     if (!c.any()) return;
     lds_barrier();
-    // the bins as ranges of the scale that marks are on, the upper ends not among them
+    // the bins as ranges of marks, both ends among them (integers, as the bins were made from: from 2^24 on float32 has no odd ones)
     const int top_mark = top_mark_of(top, per_bin);
-    auto from_of = [&](int last_bin) { return last_bin >= kBins - 1 ? -INFINITY : (float)(top_mark - start_of(last_bin + 1) + 1); };
-    auto to_of = [&](int first_bin) { return first_bin == 0 ? INFINITY : (float)(top_mark - start_of(first_bin) + 1); };
     uint32_t hits = 0;
     auto mark_hits = [&](int first_bin, int last_bin) {
-        const float from = from_of(last_bin), to = to_of(first_bin);
+        const int from = last_bin >= kBins - 1 ? INT32_MIN : top_mark - start_of(last_bin + 1) + 1, to = first_bin == 0 ? INT32_MAX : top_mark - start_of(first_bin);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const float y = scale_of(e.x[j], per_bin);
-            hits |= (uint32_t)(y >= from && y < to) << j;
+            const int mark = mark_of(e.x[j], per_bin);
+            hits |= (uint32_t)(mark >= from && mark <= to) << j;
         }
     };
     e.settle();
@@ -714,9 +712,8 @@ template <typename T, typename Tokens> __device__ __forceinline__ Cut cut_of(Row
     u64 inside;
     if (r.top_k > 0 && (u64)r.top_k < number) {
         const bool alone = c.min_first < 0 && c.p_first < 0;
-        cut.place = reach<true>(s, row, tokens, c.k_bin, c.k_bin, alone ? tokens.number() : kFew + 1, (u64)r.top_k - ahead_of(s.bins.number, c.k_bin), &inside);
-        cut.bin = c.k_bin;
-        sum = ahead_of(s.bins.mass, c.k_bin) + inside;
+        const u64 place = reach<true>(s, row, tokens, c.k_bin, c.k_bin, alone ? tokens.number() : kFew + 1, (u64)r.top_k - ahead_of(s.bins.number, c.k_bin), &inside);
+        if (place > cut.place) cut.place = place, cut.bin = c.k_bin, sum = ahead_of(s.bins.mass, c.k_bin) + inside;   // (a cut is one of the list's places)
     }
     if (r.top_p < 1.0f) {
         const u64 need = share_of(sum, r.top_p), before = ahead_of(s.bins.mass, c.p_first);
