@@ -139,7 +139,7 @@ __device__ __forceinline__ Settings settings_of(const SampleArgs &a, int64_t m)
 // mark each for ten octaves, two for nine, eight for twelve, so that a bin of one largest is made up of whole bins of any smaller one; the last has all
 // below.  (The flatter a row, the more of its tokens are in an octave, and the fewer octaves it takes down to where top-p cuts it: 131071 normally
 // distributed logits, divided by T, with a deviation of 1.3 have 3400 tokens in the bin of the cut, with 2 4500, with 4 1200.)
-constexpr float kEndMark = 0x1p30f;
+constexpr float kEndMark = 0x1p29f;                              // (marks of a row are 2^30 apart at most: their differences are integers too)
 __device__ __forceinline__ float scale_of(float x, float per_bin) { return __builtin_amdgcn_fmed3f(x * per_bin, -kEndMark, kEndMark); }
 __device__ __forceinline__ int mark_of(float x, float per_bin) { return (int)floorf(scale_of(x, per_bin)); }
 __device__ __forceinline__ int top_mark_of(float x, float per_bin) { return (mark_of(x, per_bin) + 7) & ~7; }

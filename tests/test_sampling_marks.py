@@ -1,15 +1,26 @@
 """Drawn children where a unit of logits is millions of bins (low temperatures, large logits): cuts between neighbouring numbers."""
+import os
+import re
+
 import numpy as np
 import pytest
-import torch
 
 from test_sampling import check
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 @pytest.fixture(scope="module")
 def m():
     from paper_2506_01206_amd import binding
     return binding
+
+
+def test_differences_of_marks_are_integers():
+    """A row's first mark, rounded up to a whole octave of eight, and its last one are as far apart as an int holds, and the bins behind them."""
+    with open(os.path.join(ROOT, "paper_2506_01206_amd", "csrc", "sample.hip")) as f:
+        (end,) = re.findall(r"constexpr float kEndMark = 0x1p(\d+)f;", f.read())
+    assert 2 * 2 ** int(end) + 8 + 8 * 128 <= 2 ** 31 - 1
 
 
 # top_p, min_p, top_k: each filter alone, and together
@@ -63,3 +74,25 @@ def test_large_logits(m, top):
         for top_p, min_p, top_k in FILTERS:
             check(m, x, rng.uniform(size=(2, 4)), [[T, top_p, min_p]], [top_k])
             check(m, ties, rng.uniform(size=(2, 2)), [[T, top_p, min_p]], [top_k])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [1.0, 1e-20, 1e-38])
+def test_rows_from_one_end_of_the_marks_to_the_other(m, T):
+    rng = np.random.default_rng(17)
+    x = rng.standard_normal((6, 5003))
+    x[0, [3, 5000]] = np.inf
+    x[0, 7::50] = -3e38
+    x[1, 4] = 3e38
+    x[1, 5::3] = -3e38
+    x[2] = -np.abs(x[2])                                             # all of them at the lower end, beside what does not count
+    x[2, ::2] = -np.inf
+    x[3, 1::2] = -np.inf
+    x[3, ::2] = -3e38
+    x[4] = 3e38
+    x[4, 100:] = -np.inf
+    x[5, :4000] = np.nan
+    x[5, 4000:] = -4.65e7
+    x = x.astype(np.float32)
+    for top_p, min_p, top_k in FILTERS + [(1.0, 0.0, 4999), (1.0, 0.0, 2501), (1.0, 0.0, 2502), (1.0, 1.0, 3000)]:
+        check(m, x, rng.uniform(size=(6, 3)), [[T, top_p, min_p]], [top_k])
