@@ -538,10 +538,11 @@ int mamba_sample_fwd(const void *logits, const mamba_sampling_t *s, const float 
  *   such as the -1 of a node with fewer children, is passed over
  *   u_accept: float (n_seq, nodes - 1), one for each child; u_sample: float (n_seq)
  * From the root on, with P = p and Q = q of the node, its children in turn: child c is accepted where u < min(1, P(c) / Q(c)) (Q(c) = 0: as 1
- * where P(c) > 0), and the walk goes on at its node; else P becomes (P - Q)_+ divided by its sum (and stays where that is zero) and Q becomes q
- * without the children so far, divided by its sum.  Where none is accepted, a token is drawn from P and the walk ends; behind the last
+ * where P(c) > 0; where one of them, or u, is NaN it is rejected), and the walk goes on at its node; else P becomes (P - Q)_+ divided by its sum
+ * (and stays where that is zero; zero for a token whose P or Q is NaN) and Q becomes q without the children so far, divided by its sum.
+ * Where none is accepted, a token is drawn from P and the walk ends; behind the last
  * position it is drawn from p: the first token, in the order of the vocabulary, up to which the probabilities add up to more than u_sample
- * times their sum; -1 where the sum is zero or no number.  All of this in float64.  An emitted token is distributed as p, whatever q is.
+ * (in [0,1)) times their sum; -1 where the sum is zero or NaN.  All of this in float64.  An emitted token is distributed as p, whatever q is.
  *   out: int32 (n_seq, gamma + 1): the accepted tokens, the drawn one, then -1;  count: int32 (n_seq): how many there are (1 .. gamma + 1)
  *   node: int32 (n_seq, gamma): of the accepted tokens the row in their position (the row of its cache to go on from), then -1
  * p, q: four bytes' alignment is enough.  workspace: device scratch of mamba_tree_verify_workspace_bytes(n_seq) bytes; nothing in it has to be kept or

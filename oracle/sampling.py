@@ -89,14 +89,15 @@ def verify(p, q, tokens, u_accept, u_sample, tree):
                 c = tokens[s, at]
                 if not 0 <= c < V:
                     continue
-                ratio = P[c] / Q[c] if Q[c] > 0 else float(P[c] > 0)
-                if float(u_accept[s, at]) < min(1.0, ratio):
+                ratio = P[c] / Q[c] if Q[c] > 0 else float(Q[c] <= 0 and P[c] > 0)
+                u = float(u_accept[s, at])
+                if u < 1.0 and u < ratio:                        # (a NaN accepts nothing)
                     taken = row * n + j
                     break
-                gap = np.maximum(P - Q, 0.0)
+                gap = np.fmax(P - Q, 0.0)                        # (zero where it is NaN)
                 P = gap / gap.sum() if gap.sum() > 0 else P
                 rest[c] = 0.0
-                Q = rest / rest.sum() if rest.sum() > 0 else np.zeros(V)
+                Q = rest / rest.sum() if rest.sum() > 0 else rest * 0.0
             if taken < 0:
                 behind = P
                 break

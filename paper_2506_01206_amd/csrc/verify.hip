@@ -211,9 +211,10 @@ __device__ __forceinline__ void go_on(Walk &s, const VerifyArgs &a, const Sequen
             double P[1] = {__builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, p_mine), next))};
             double Q[1] = {__builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, q_mine), next))}, left[1] = {Q[0]};
             after_rejections(s, n, c, P, Q, left);
-            const double ratio = Q[0] > 0.0 ? P[0] / Q[0] : P[0] > 0.0 ? 1.0 : 0.0;
+            // (what is no number accepts nothing: no comparison with it is true)
+            const double ratio = Q[0] > 0.0 ? P[0] / Q[0] : Q[0] <= 0.0 && P[0] > 0.0 ? 1.0 : 0.0;
             const float u = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, u_mine), next));
-            if ((double)u < (ratio < 1.0 ? ratio : 1.0)) {
+            if (u < 1.0f && (double)u < ratio) {
                 taken = next;
                 if (writes && blockIdx.x == first_block) out[depth] = c, node[depth] = (int32_t)(row * fan + taken);
                 break;
