@@ -54,7 +54,7 @@ int sd_bandit_update(sd_bandit_t *b, int32_t arm, int64_t n_accept, int32_t gamm
  * Verification of one draft sequence.
  *   p: (gamma + 1, V) target probabilities, row t for position t (row gamma = the extra token);
  *   q: (gamma, V) drafter probabilities; draft: int32[gamma] draft tokens;
- *   u_accept: float[gamma] uniforms of the acceptance tests;
+ *   u_accept: float[gamma] uniforms of the acceptance tests; a token with p, q or u NaN is rejected;
  *   u_sample: one uniform used for the token drawn at a rejection or as the extra token
  *             (inverse-CDF over the vocabulary in index order; unused when greedy);
  *   greedy: nonzero = the target is taken one-hot at its argmax (lowest index on ties).

@@ -61,14 +61,14 @@ def verify(p, q, draft, u_accept, u_sample, greedy):
         top = max(range(len(pr)), key=lambda v: (pr[v], -v))
         pt = (1.0 if top == tok else 0.0) if greedy else pr[tok]
         qt = qr[tok]
-        ratio = pt / qt if qt > 0.0 else (1.0 if pt > 0.0 else 0.0)
-        if float(u_accept[t]) < min(1.0, ratio):
+        ratio = pt / qt if qt > 0.0 else (1.0 if qt <= 0.0 and pt > 0.0 else 0.0)
+        if float(u_accept[t]) < 1.0 and float(u_accept[t]) < ratio:   # (a NaN accepts nothing)
             out.append(tok)
             continue
         if greedy:
             out.append(top)
         else:
-            resid = [max(a - b, 0.0) for a, b in zip(pr, qr)]
+            resid = [a - b if a - b > 0.0 else 0.0 for a, b in zip(pr, qr)]
             out.append(_draw(resid if sum(resid) > 0.0 else pr, float(u_sample)))
         return out
     last = list(map(float, p[gamma]))

@@ -110,9 +110,9 @@ int sd_verify(const float *p, const float *q, const int32_t *draft, const float 
         const int64_t tok = draft[t];
         const double pt = greedy ? (argmax_row(pr, V) == tok ? 1.0 : 0.0) : (double)pr[tok];
         const double qt = (double)qr[tok];
-        // u < min(1, p_t / q_t); a token the drafter gave zero probability cannot have been drafted
-        const double ratio = qt > 0.0 ? pt / qt : (pt > 0.0 ? 1.0 : 0.0);
-        if ((double)u_accept[t] < (ratio < 1.0 ? ratio : 1.0)) {
+        // u < min(1, p_t / q_t); a token the drafter gave zero probability cannot have been drafted; NaN accepts nothing
+        const double ratio = qt > 0.0 ? pt / qt : (qt <= 0.0 && pt > 0.0 ? 1.0 : 0.0);
+        if (u_accept[t] < 1.0f && (double)u_accept[t] < ratio) {
             out_tokens[n++] = (int32_t)tok;
             continue;
         }
