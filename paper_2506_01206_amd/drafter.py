@@ -259,16 +259,16 @@ class MambaDrafter:
         numbers of all children, position by position (f32 in [0,1); None: torch's)."""
         bufs = self._buffers(tree)
         c = bufs["cache"]
-        c.set_root(self.root_conv, self.root_ssm)
-        bufs["sampled"] = self._sampling is not None     # of the tree that the buffers hold
+        total = sum(c.batch[i] for i in range(1, c.gamma + 1))
+        if self._sampling is not None and u is not None and u.numel() != total:
+            raise ValueError("u must have %d random numbers, got %d" % (total, u.numel()))
+        bufs["sampled"] = False                          # of the tree that the buffers hold: until the round is under way
         if self._sampling is not None:
             at = 0
-            total = sum(c.batch[i] for i in range(1, c.gamma + 1))
-            if u is not None and u.numel() != total:
-                raise ValueError("u must have %d random numbers, got %d" % (total, u.numel()))
             for buf in self._drawn(bufs)["u"][1:]:
                 buf.uniform_() if u is None else buf.copy_(u.reshape(-1)[at:at + buf.numel()].view_as(buf))
                 at += buf.numel()
+        c.set_root(self.root_conv, self.root_ssm)
         kind = "".join(("constrained_" if self._rules is not None else "", "sampling_" if self._sampling is not None else "",
                         "adapted_" if self._adapters is not None else "", "graph"))
         if not use_graph:
@@ -286,5 +286,6 @@ class MambaDrafter:
                 torch.cuda.current_stream().wait_stream(side)
                 bufs[kind] = g
             bufs[kind].replay()
+        bufs["sampled"] = self._sampling is not None
         tokens = [bufs["pos"][i]["cand"].view(-1) for i in range(1, c.gamma + 1)]
         return tokens, bufs["pos"][c.gamma]["logits"]
