@@ -598,7 +598,10 @@ template <int BM, int BN, int WM, int WN> struct AdapterSlabs {
                     }
                 }
             }
-            if (ahead < t.adapters) lds_barrier_linear();             // (the stage has been read)
+            if (ahead < t.adapters) {                                 // the stage has been read
+                __builtin_amdgcn_s_waitcnt(0xC07F);                   // lgkmcnt(0)
+                lds_barrier_linear();
+            }
             request(lds0, stage);
             stage = 1 - stage;
         }
