@@ -76,17 +76,19 @@ down_kernel(const bf16_t *__restrict__ x, const bf16_t *__restrict__ a, const fl
                 load_to_lds16(row[i] + (c < chunks ? c : 0) * 8, lds0 + stage * kStage + to[i]);   // (behind K: something, see below)
             }
         };
-        // until no more than the loads of `slabs_under_way` slabs are under way (vmcnt is split over bits 3:0 and 15:14)
+        // until no more than the loads of `slabs_under_way` slabs are under way (vmcnt is split over bits 3:0 and 15:14), and no LDS read (lgkmcnt(0)):
+        // behind the barrier other wavefronts' loads overwrite a stage, and keep no order with one
         auto wait_for = [&](int slabs_under_way) __attribute__((always_inline)) {
             static_assert((kStages - 2) * NL < 64 && kStages == 4, "fits the counter");
-            if (slabs_under_way >= 2) __builtin_amdgcn_s_waitcnt(0x0F70 | ((2 * NL) & 15) | (((2 * NL) >> 4) << 14));
-            else if (slabs_under_way >= 1) __builtin_amdgcn_s_waitcnt(0x0F70 | (NL & 15) | ((NL >> 4) << 14));
-            else __builtin_amdgcn_s_waitcnt(0x0F70);
+            if (slabs_under_way >= 2) __builtin_amdgcn_s_waitcnt(0x0070 | ((2 * NL) & 15) | (((2 * NL) >> 4) << 14));
+            else if (slabs_under_way >= 1) __builtin_amdgcn_s_waitcnt(0x0070 | (NL & 15) | ((NL >> 4) << 14));
+            else __builtin_amdgcn_s_waitcnt(0x0070);
         };
         f32x4v d[RT];
 #pragma unroll
         for (int r = 0; r < RT; ++r) d[r] = f32x4v(0.0f);
-        lds_barrier();                                               // (the last adapter's sums are read)
+        __builtin_amdgcn_s_waitcnt(0xC07F);                          // lgkmcnt(0): the last adapter's sums are read
+        lds_barrier();
 #pragma unroll
         for (int i = 0; i < kStages - 1; ++i)
             if (i < slabs) request(i, i);

@@ -33,3 +33,17 @@ def test_slabs_beside_a_product(tmp_path):
     for name, l in multiply.items():
         assert [x for x in l if x == "barrier"] == ["barrier"] * 2 and l[-1] == "barrier", (name, l)
         assert l[-2] != "barrier" and counters(l[-2])[1] == 0, (name, l)
+
+
+def test_the_way_into_the_adapters(tmp_path):
+    """Stages are requested behind the first barrier of an adapter, where the last one's sums have been read, and behind a slab's."""
+    found = functions("adapters.hip", tmp_path)
+    kernels = {n: l for n, l in found.items() if "down_kernel" in n and n.startswith("_ZN")}
+    assert len(kernels) >= 5
+    for name, l in kernels.items():
+        assert l[1] == "barrier" and l[0] != "barrier" and counters(l[0])[1] == 0, (name, l)
+        assert l[2:4] == ["wait", "barrier"] and l.count("wait") == 1, (name, l)
+    waits = {n: [x for x in l if x != "barrier"] for n, l in found.items() if "down_kernel" in n and n.endswith("UliE_clEi")}
+    assert len(waits) == len(kernels)
+    for name, l in waits.items():
+        assert len(l) == 3 and all(counters(x)[1] == 0 for x in l), (name, l)
