@@ -113,6 +113,12 @@ class MambaDrafter:
         if (lora_b is None or tuple(lora_a.shape) != (n, rank, self.dm) or tuple(lora_b.shape) != (n, self.V, rank)
                 or lora_a.dtype != torch.bfloat16 or lora_b.dtype != torch.bfloat16 or (scale is not None and tuple(scale.shape) != (n,))):
             raise ValueError("adapters must have shapes (n, rank, %d) and (n, %d, rank) in bfloat16, and scale (n)" % (self.dm, self.V))
+        # (what the product would refuse: prefill() would find it when the root's states are another prefix's already)
+        for t in (lora_a, lora_b) + (() if scale is None else (scale,)):
+            if t.device != self.dev or not t.is_contiguous() or t.data_ptr() % 16:
+                raise ValueError("adapters and scale must be contiguous, on %s and aligned to 16 bytes" % (self.dev,))
+        if scale is not None and scale.dtype != torch.float32:
+            raise ValueError("scale must be float32")
         if rank == 0 or rank % 8 or rank > 128 or not 0 <= which < n:
             raise ValueError("the rank must be a multiple of 8 up to 128, and the adapter one of the %d" % n)
         self._forget("adapted")
