@@ -1547,7 +1547,10 @@ template <int RT> hipError_t launch_one_row(const LinearArgs &a, const AdapterAr
     *fits = (kernel == kFew16x8 ? (N + 7) / 8 : (N + 15) / 16) * RT <= 768;   // (workgroups and tiles of 16 ranks)
     if (!*fits) return hipSuccess;
     switch (kernel) {
-    case kFew16x16Stream: return launch_few<1, 2, true>(x, w, a.bias, res, o, a.M, N, a.K, stream, tail);
+    case kFew16x16Stream:
+        if constexpr (RT == 1) return launch_few<1, 2, true>(x, w, a.bias, res, o, a.M, N, a.K, stream, tail);
+        *fits = false;                                            // (8192 columns and more: never with two tiles of ranks)
+        return hipSuccess;
     case kFew16x8: return launch_few<1, 1>(x, w, a.bias, res, o, a.M, N, a.K, stream, tail);
     case kFew16x16: return launch_few<1, 2>(x, w, a.bias, res, o, a.M, N, a.K, stream, tail);
     default: *fits = false; return hipSuccess;
