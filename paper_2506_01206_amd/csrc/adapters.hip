@@ -171,9 +171,9 @@ hipError_t launch_adapters_down(const void *x, const AdapterArgs &l, int64_t M, 
         return launch<8, 2, 4>(xp, l, M, K, stream);
     }
     const int64_t tiles = (M + 15) / 16, parts = (kEnough + tiles - 1) / tiles;   // (of the ranks)
-    if (l.rank <= 16 || l.rank <= 16 * parts) return launch<1, 1, 4>(xp, l, M, K, stream);
-    if (l.rank <= 32 || l.rank <= 32 * parts) return launch<2, 1, 4>(xp, l, M, K, stream);
-    if (l.rank <= 64 || l.rank <= 64 * parts) return launch<4, 1, 4>(xp, l, M, K, stream);
+    if (l.rank <= 16 * parts) return launch<1, 1, 4>(xp, l, M, K, stream);
+    if (l.rank <= 32 * parts) return launch<2, 1, 4>(xp, l, M, K, stream);
+    if (l.rank <= 64 * parts) return launch<4, 1, 4>(xp, l, M, K, stream);
     return launch<8, 1, 4>(xp, l, M, K, stream);
 }
 
