@@ -147,6 +147,13 @@ down_kernel(const bf16_t *__restrict__ x, const bf16_t *__restrict__ a, const fl
     }
 }
 
+// Adapters of a workgroup's rows at once: up to 16 while workgroups are fewer than a quarter of the CUs, and rows of many adapters would be one product
+// after the other; up to 4 beyond, where a workgroup without a turn is one more to be run through.  us, up to 4 | 16, K = 1024, 64 adapters:
+//   rows                 64          333         512         1024        2048        4097        16384
+//   rank 16, no order    9.3| 4.7    10.6| 5.7   10.6| 5.8   10.8| 7.7   13.4|12.6   25.2|28.9   101|98
+//   rank 16, runs        9.4| 4.7     4.2| 4.2    4.1| 4.1    4.1| 4.0    4.0| 4.0    5.3| 7.4   10.0|12.7
+//   rank 64, no order    9.4| 4.8    14.2|10.8   14.4|13.3   19.1|22.9   33.2|32.2   62.6|70.0   267|251
+//   rank 64, runs        9.5| 5.0     5.1| 6.0    5.0| 6.0    6.1| 7.2    6.3| 8.3   12.7|19.4   17.9|24.1
 template <int RT, int G, int W> hipError_t launch(const bf16_t *x, const AdapterArgs &l, int64_t M, int64_t K, hipStream_t stream)
 {
     const int64_t tiles = (M + 16 * G - 1) / (16 * G), parts = (l.rank + 16 * RT - 1) / (16 * RT);
@@ -160,6 +167,13 @@ template <int RT, int G, int W> hipError_t launch(const bf16_t *x, const Adapter
 }  // namespace
 
 // Ranks are split over workgroups, 16 of them or more to one, while there are not enough of those: x is read again from the second-level cache then.
+// Up to 64 rows eight wavefronts share k, four beyond.  us, eight | four: K = 2048, rank 16 1 row 4.5|5.3, 64 4.7|5.6, 256 4.8|5.6; eight adapters of rank
+// 64 24 rows 5.1|5.7, 128 5.4|5.9, 256 7.5|7.5; K = 768 the same to 0.1, but 256 rows of those 5.4|4.7.
+// From 6144 rows a workgroup has 32 of them, 16 below, so that A comes half as often.  us, 16 | 32 rows, K = 2048, runs of 8 to 32 adapters (no order):
+//   rows       4097                    6144                  8192                   16384
+//   rank 16     7.8| 9.5 (44|69)        8.6| 9.4 (47|65)      9.8| 9.7 (65|91)      17.8|13.7 (157|207)
+//   rank 64    15.4|15.3 (67|69)       14.5|15.3 (90|73)     17.6|15.4 (124|124)    29.5|19.5 (227|232)
+//   rank 128   30.2|21.0               28.1|21.0             36.6|20.9              71.6|27.6
 hipError_t launch_adapters_down(const void *x, const AdapterArgs &l, int64_t M, int64_t K, hipStream_t stream)
 {
     const bf16_t *xp = static_cast<const bf16_t *>(x);
