@@ -503,11 +503,11 @@ int mamba_topk_constrained_fwd(const void *logits, const mamba_constraints_t *c,
  *   idx: int32 (M,k); prob: float (M,k), q of the token; -1 and 0 where no token is left
  *   dist: (M,V) float or NULL: q of every token (its address needs four bytes' alignment only)
  *   path_out: int32 (M k, path_len + 1) or NULL, as mamba_topk_constrained_fwd has it
- * Weights are formed in float64 and added up as whole multiples of 2^-(63 - ceil(log2 V)) of the largest one (2^-51 up to 4096 tokens, 2^-47 for
- * 50280, 2^-42 at most), each rounded once, so that sums do not depend on their order and results are the same bit for bit from call to call.  A
- * further child is drawn by the same multiples while 2^39 of them (2^30 under a top_k up to 1024) are left beside the children before it: its sums have
- * those bits then; with fewer left, what is left is weighed anew, relative to its own largest.  A weight below float64's range is zero, and so are those of finite logits beside an infinite one; a token of
- * weight zero is not drawn.
+ * Weights are formed in float64 and added up as whole multiples of 2^-51 of the largest one (of more than 4096 tokens 2^-(63 - ceil(log2 V)): 2^-47 for
+ * 50280, 2^-42 for 2^21), so that sums do not depend on their order and results are the same bit for bit from call to call.  A further
+ * child is drawn by the same multiples while 2^39 of them (2^30 under a top_k up to 1024) are left beside the children before it, which are the bits that
+ * its sums have then; with fewer left, what is left is weighed anew, relative to its own largest.  A weight below float64's range is zero, and so
+ * are those of finite logits beside an infinite one; a token of weight zero is not drawn.
  *
  * mamba_sampling_t (a HOST struct of device pointers):
  *   params (n_seq, 3) float: temperature (>= 0), top_p (1 or more: off; 0 or less: the first token only), min_p (0 or less: off; above 1: as 1)
@@ -563,8 +563,9 @@ int mamba_tree_verify_fwd(const float *p, const float *q, const int32_t *tokens,
  * included.  lora_a (n_adapters, rank, K), lora_b (n_adapters, N, rank) bf16; scale (n_adapters) float or NULL (ones); adapter_idx
  * device int32 (M): -1 for a row without an adapter (what it gets is mamba_linear_fwd's to the bit where there is no residual), anything else
  * outside [0, n_adapters) gives NaN in the row.  Rows of one adapter may stand anywhere; next to one another they cost least.  The rank is a multiple of
- * 8 up to 128 (adapters of a lower one are padded with zeros).  The sums over k of the adapter, scaled, are held in 16 bits (two bfloat16 terms) for
- * several rows, in float32 for one row of a rank up to 32, so that a row's last bits may depend on how many come with it.  An infinity or a NaN of an adapter reaches its own rows only (an infinity as a NaN, it may be).
+ * 8 up to 128 (adapters of a lower one are padded with zeros).  The adapter's sums over k, scaled, are held in 16 bits (two bfloat16 terms), in float32
+ * in most calls of one row: a row's last bits may depend on how many come with it.  An infinity or a NaN of an adapter reaches its own rows only
+ * (an infinity as a NaN, it may be).
  * workspace: device scratch of mamba_linear_adapted_workspace_bytes(M, rank) bytes; nothing in it has to be kept or cleared between calls.
  */
 size_t mamba_linear_adapted_workspace_bytes(int64_t M, int64_t rank);
